@@ -190,6 +190,51 @@ pdy_status attn_merge(const void* o_a, const float* lse_a, const void* o_b, cons
                       int32_t total_tokens, int32_t num_heads_q, int32_t head_dim,
                       void* o, float* lse, void* stream);
 
+/* ---- Keys of another length, and keys shared by the batch ----
+ * A batch of num_seqs sequences; sequence i has the queries cu_seqlens_q[i] ..
+ * cu_seqlens_q[i+1]-1 and the keys cu_seqlens_k[i] .. cu_seqlens_k[i+1]-1 (int32
+ * device arrays of num_seqs + 1).  Either may be empty.
+ *   - seqlens_k (int32 device array of num_seqs, or NULL): only the first
+ *     seqlens_k[i] of a sequence's keys are in use -- a cache with room left, or a
+ *     padded batch (cu_seqlens_k then are multiples of the padded length).  Other
+ *     keys are never read as numbers, whatever they hold.
+ *   - Query rows from cu_seqlens_q[num_seqs] on and key rows from
+ *     cu_seqlens_k[num_seqs] on belong to no sequence: their outputs and gradients
+ *     are left as they were.
+ *   - causal = 1 aligns the sequences' ends: with nq queries and nk keys in use,
+ *     key j is visible to query i iff j <= i + nk - nq (the last query sees all).
+ *   - attn_prefix_*: every row of the batch also sees the prefix_len keys k_prefix,
+ *     v_prefix, bf16 [prefix_len, Hkv, d] (causal or not), which are read once for
+ *     all rows where these are few a sequence.  prefix_len = 0 is attn_cross_*.
+ *   - A row that sees no key gets o = 0, lse = -inf, and no gradient.
+ *   - max_seqlen_q, max_seqlen_k: upper bounds of the sequences' queries and keys;
+ *     rows beyond max_seqlen_q may stay unwritten.  Offsets are trusted as above,
+ *     but clamped to the tensors: wrong ones give wrong results, no stray access.
+ * q, o bf16 [total_q, Hq, d]; k, v bf16 [total_k, Hkv, d] (NULL if total_k = 0); lse
+ * fp32 [Hq, total_q].  Launch shapes and the parts of rows with few keys follow from
+ * the sizes and the offsets' values: results of a sequence depend on its batch in
+ * rounding only.  Other rules as above. */
+size_t attn_cross_fwd_workspace_size(int32_t total_q, int32_t total_k, int32_t num_seqs,
+                                     int32_t max_seqlen_q, int32_t max_seqlen_k,
+                                     int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim);
+pdy_status attn_cross_fwd(const void* q, const void* k, const void* v, const int32_t* cu_seqlens_q,
+                          const int32_t* cu_seqlens_k, const int32_t* seqlens_k, int32_t num_seqs,
+                          int32_t total_q, int32_t total_k, int32_t max_seqlen_q,
+                          int32_t max_seqlen_k, int32_t num_heads_q, int32_t num_heads_kv,
+                          int32_t head_dim, int32_t causal, float scale, void* o, float* lse,
+                          void* workspace, size_t workspace_bytes, void* stream);
+size_t attn_prefix_fwd_workspace_size(int32_t prefix_len, int32_t total_q, int32_t total_k,
+                                      int32_t num_seqs, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                                      int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim);
+pdy_status attn_prefix_fwd(const void* q, const void* k, const void* v, const void* k_prefix,
+                           const void* v_prefix, const int32_t* cu_seqlens_q,
+                           const int32_t* cu_seqlens_k, const int32_t* seqlens_k,
+                           int32_t prefix_len, int32_t num_seqs, int32_t total_q, int32_t total_k,
+                           int32_t max_seqlen_q, int32_t max_seqlen_k, int32_t num_heads_q,
+                           int32_t num_heads_kv, int32_t head_dim, int32_t causal, float scale,
+                           void* o, float* lse, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
 /* Debug helper: copies cu_seqlens to the host (synchronising `stream`) and
  * checks cu[0] = 0, monotonicity and cu[num_seqs] = total_tokens.  On success
  * writes the longest segment length to *max_seqlen_out (may be NULL). */

@@ -5,18 +5,20 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpdyattn.so")
-SOURCES = [os.path.join(CSRC, "pdyattn.hip")]
-HEADERS = [os.path.join(CSRC, f) for f in ("common.hpp", "plan.hpp", "fwd.hpp", "bwd.hpp")] + [
+SOURCES = [os.path.join(CSRC, f) for f in ("pdyattn.hip", "cross.hip")]
+HEADERS = [os.path.join(CSRC, f) for f in ("common.hpp", "host.hpp", "plan.hpp", "fwd.hpp",
+                                           "bwd.hpp", "cross.hpp", "cross_fwd.hpp")] + [
     os.path.join(ROOT, "include", "pdyattn.h")]
 
 ARCH = "gfx950"
 FLAGS = [
-    f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-shared", "-fPIC",
+    f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
     # no packed-fp32 VALU instructions anywhere in device code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-command-line-argument",
@@ -31,19 +33,34 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = False, extra_flags=None, out: str = LIB) -> str:
+    """Every source compiled on its own, at the same time, then linked."""
+    flags = [*FLAGS, *(extra_flags or []), "-I", os.path.join(ROOT, "include")]
     tmp = out + ".tmp"
-    cmd = [hipcc(), *FLAGS, *(extra_flags or []), "-I", os.path.join(ROOT, "include"),
-           "-o", tmp, *SOURCES]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError(f"hipcc failed ({res.returncode})")
-    if verbose and res.stderr.strip():
-        sys.stderr.write(res.stderr)
+    with tempfile.TemporaryDirectory() as work:
+        objs, runs = [], []
+        for src in SOURCES:
+            objs.append(os.path.join(work, os.path.basename(src) + ".o"))
+            runs.append(_start([hipcc(), *flags, "-c", "-o", objs[-1], src], verbose))
+        for run in runs:
+            _finish(run, verbose)
+        _finish(_start([hipcc(), *flags, "-shared", "-o", tmp, *objs], verbose), verbose)
     os.replace(tmp, out)
     return out
+
+
+def _start(cmd, verbose: bool) -> subprocess.Popen:
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def _finish(run: subprocess.Popen, verbose: bool):
+    text, _ = run.communicate()
+    if run.returncode != 0:
+        sys.stderr.write(text)
+        raise RuntimeError(f"hipcc failed ({run.returncode})")
+    if verbose and text.strip():
+        sys.stderr.write(text)
 
 
 if __name__ == "__main__":

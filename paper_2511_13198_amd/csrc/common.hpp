@@ -64,6 +64,13 @@ __device__ __forceinline__ f32x16 zero16() {
   return z;
 }
 
+// The running maximum of an online softmax (base 2) is raised only when a new
+// tile's exceeds it by more than this.
+constexpr float kRescaleSlack = 8.0f;
+
+// key offset within a 32-key block held in accumulator register r (lane half 0)
+__device__ __forceinline__ constexpr int acc_row_off(int r) { return (r >> 2) * 8 + (r & 3); }
+
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Value of x held by lane (l ^ 32), via v_permlane32_swap.

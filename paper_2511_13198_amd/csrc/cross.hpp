@@ -1,0 +1,232 @@
+// What the cross-attention kernels share: the packed batch they work on, the
+// placement of their workgroups, and the output tiles of packed rows.
+//
+// A batch has n sequences.  Sequence i has the queries cu_q[i] .. cu_q[i + 1] and
+// the keys cu_k[i] .. cu_k[i + 1], of which the first len_k[i] are in use (all
+// where len_k is NULL); every row also sees the `prefix` keys that the batch
+// shares.  causal: the last query of a sequence sees all its keys in use, the one
+// before all but the last, ...
+//
+// Packed rows.  The g query heads of a key/value head read the same keys, so a
+// tile's rows are (token, head of the group) pairs: packed row R of kv head hk is
+// head hk g + R % g of token R / g.  A tile of 32 NW rows then holds 32 NW / g
+// tokens, each K/V tile is read once for the whole group, and one token of a
+// sequence still fills g rows of the matrix product.
+//
+// Offsets read from cu_q, cu_k and len_k are clamped to the tensors, so that no
+// value in them makes a kernel leave its tensors.
+#pragma once
+#include "common.hpp"
+
+namespace pdy {
+
+struct CrossBatch {
+  const int32_t* cu_q;   // [n + 1]
+  const int32_t* cu_k;   // [n + 1]
+  const int32_t* len_k;  // [n] or NULL
+  int n;
+  int tq;      // rows of q
+  int tk;      // rows of k, v
+  int prefix;  // shared keys
+  int hq, hkv;
+  int causal;
+};
+
+// One sequence: rows of q and k, keys in use.
+struct CrossSeq {
+  int q_lo, nq, k_lo, nk;
+};
+
+__device__ __forceinline__ CrossSeq cross_seq(const CrossBatch& b, int i) {
+  CrossSeq s;
+  s.q_lo = min(max(b.cu_q[i], 0), b.tq);
+  s.nq = min(max(b.cu_q[i + 1], s.q_lo), b.tq) - s.q_lo;
+  s.k_lo = min(max(b.cu_k[i], 0), b.tk);
+  s.nk = min(max(b.cu_k[i + 1], s.k_lo), b.tk) - s.k_lo;
+  if (b.len_k) s.nk = min(max(b.len_k[i], 0), s.nk);
+  return s;
+}
+
+// Which rows and keys a launch covers.
+enum CrossKeys : int {
+  CROSS_OWN = 0,     // a sequence's rows over its own keys
+  CROSS_FUSED = 1,   // over the shared keys, then its own
+  CROSS_SHARED = 2,  // all rows of the batch, as one sequence, over the shared keys
+};
+
+// How a launch's rows and keys are cut.  An item is a tile of `rows` packed rows of
+// a sequence and kv head; its key tiles are cut into parts, one workgroup each,
+// whose partial results another kernel combines:
+//   units = sum over the sequences of row tiles x key tiles,
+//   a part has at most C = max(least, units * hkv / target) key tiles, so that the
+//   parts are alike whatever the lengths, there are about `target` of them, and
+//   a launch with that many items is not cut (C is then above their key tiles).
+// Every workgroup computes C from the offsets, so that nothing waits for the host.
+struct CrossCut {
+  int keys;         // CrossKeys
+  int rows;         // packed rows per tile
+  int key_tile;     // keys per tile
+  int max_parts;    // 1: not cut
+  int least;        // fewest key tiles of a part
+  float per_head;   // parts wanted per kv head (target / hkv)
+  int slice;        // first slice of the partial results
+  int always_part;  // partial results also of items in one part
+};
+
+struct CrossPlace {
+  CrossSeq s;
+  int tile;  // row tile of the sequence
+  int part, nparts;
+};
+
+__device__ __forceinline__ int cross_tiles(int x, int tile) { return (x + tile - 1) / tile; }
+
+// The sequence that lane l's place in the list stands for (CROSS_SHARED: sequence
+// 0 is the whole batch), and its row tiles and key tiles.
+__device__ __forceinline__ CrossSeq cross_lane_seq(const CrossBatch& b, const CrossCut& c, int i,
+                                                   int g, int& row_tiles, int& key_tiles) {
+  CrossSeq s = {0, 0, 0, 0};
+  row_tiles = key_tiles = 0;
+  if (i < (c.keys == CROSS_SHARED ? 1 : b.n)) {
+    if (c.keys == CROSS_SHARED) s.nq = min(max(b.cu_q[b.n], 0), b.tq);
+    else s = cross_seq(b, i);
+    row_tiles = cross_tiles(s.nq * g, c.rows);
+    key_tiles = cross_tiles(s.nk, c.key_tile) +
+                (c.keys == CROSS_OWN ? 0 : cross_tiles(b.prefix, c.key_tile));
+  }
+  return s;
+}
+
+// Sequence, row tile and part of entry `entry` of a kv head's list; false past its
+// end.  One pass over the sequences, 64 at a time (two where the launch is cut);
+// the results are wave-uniform.
+__device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut& c, int entry,
+                                            CrossPlace& out) {
+  const int l = __lane_id(), g = b.hq / b.hkv;
+  const int n = c.keys == CROSS_SHARED ? 1 : b.n;
+  int cap = 1 << 30;
+  if (c.max_parts > 1) {
+    float units = 0.f;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+      int rt, kt;
+      cross_lane_seq(b, c, i0 + l, g, rt, kt);
+      units += (float)rt * (float)kt;
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) units += __shfl_xor(units, off);
+    cap = max(c.least, (int)fminf(units / c.per_head + 1.f, 1e9f));
+  }
+  int base = 0;
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    int rt, kt;
+    const CrossSeq s = cross_lane_seq(b, c, i0 + l, g, rt, kt);
+    const int parts = max(1, min(c.max_parts, cross_tiles(kt, cap)));
+    const int mine = rt * parts;
+    int incl = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int t = __shfl_up(incl, off);
+      if (l >= off) incl += t;
+    }
+    const int rel = entry - base;
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(rel >= incl - mine && rel < incl);
+    if (hit) {
+      const int src = __builtin_ctzll(hit);
+      auto get = [&](int v) __attribute__((always_inline)) {
+        return __builtin_amdgcn_readlane(v, src);
+      };
+      out.s = CrossSeq{get(s.q_lo), get(s.nq), get(s.k_lo), get(s.nk)};
+      out.nparts = get(parts);
+      const int at = rel - get(incl - mine);
+      out.tile = __builtin_amdgcn_readfirstlane(at / out.nparts);
+      out.part = __builtin_amdgcn_readfirstlane(at % out.nparts);
+      return true;
+    }
+    base += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
+}
+
+// ---------------------------------------------------------------------------
+// Output tiles of packed rows: as store_rows_bf16 and store_rows_f32, with the
+// address of a row (0 .. 31 of the wave's tile) from `at`.
+// ---------------------------------------------------------------------------
+template <int D, class At>
+__device__ __forceinline__ void cross_store_bf16(const f32x16 (&acc)[D / 32], float mul, int nrows,
+                                                 uint16_t* lds, At&& at) {
+  constexpr int P = kBf16Pitch<D>, LANES = D / 8, ROWS = 64 / LANES;
+  if (nrows <= 0) return;  // wave-uniform
+  const int l = __lane_id();
+  const int wr = (l & 31) * P + (l >> 5) * 4;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x16& x = acc[db];
+      const f32x2 v01 = {x[g * 4] * mul, x[g * 4 + 1] * mul};
+      const f32x2 v23 = {x[g * 4 + 2] * mul, x[g * 4 + 3] * mul};
+      *reinterpret_cast<u32x2*>(lds + wr + db * 32 + g * 8) =
+          u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(v01, bf16x2)),
+                __builtin_bit_cast(uint32_t, __builtin_convertvector(v23, bf16x2))};
+    }
+  wave_lds_fence();
+  const int rr = l / LANES, c = (l % LANES) * 8;
+  const uint32_t rd = lds_addr(lds) + (rr * P + c) * 2;
+  static_for<32 / ROWS / 4>([&](auto I) {
+    constexpr int i0 = decltype(I)::value * 4;
+    u32x4 v[4];
+    constexpr int o = i0 * ROWS * P * 2, st = ROWS * P * 2;
+    lds_read4<o, o + st, o + 2 * st, o + 3 * st>(rd, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = (i0 + i) * ROWS + rr;
+      if (r < nrows) *reinterpret_cast<u32x4*>((uint16_t*)at(r) + c) = v[i];
+    }
+  });
+  wave_lds_fence();
+}
+
+template <int D, int PASS, class At>
+__device__ __forceinline__ void cross_store_f32(const f32x16 (&acc)[D / 32], float mul, int nrows,
+                                                float* lds, At&& at) {
+  static_assert((D / 32) % PASS == 0, "whole passes");
+  if (nrows <= 0) return;  // wave-uniform
+  const int l = __lane_id();
+  const int wr = acc_slot_lane(l);
+  const int rr = l >> 3, c = (l & 7) * 4;  // read: 8 lanes a row
+  const uint32_t rd = lds_addr(lds) + (rr * kF32Pitch + c) * 4;
+  static_for<D / 32 / PASS>([&](auto Pass) {
+    constexpr int p = decltype(Pass)::value * PASS;
+#pragma unroll
+    for (int b = 0; b < PASS; ++b) acc_to_lds(acc[p + b], mul, lds + b * kF32Block, wr);
+    wave_lds_fence();
+    static_for<PASS>([&](auto B) {
+      constexpr int b = decltype(B)::value;
+      u32x4 raw[4];
+      constexpr int o = b * kF32Block * 4, st = 8 * kF32Pitch * 4;
+      lds_read4<o, o + st, o + 2 * st, o + 3 * st>(rd, raw);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i * 8 + rr < nrows)
+          *reinterpret_cast<f32x4*>((float*)at(i * 8 + rr) + (p + b) * 32 + c) =
+              __builtin_bit_cast(f32x4, raw[i]);
+    });
+    wave_lds_fence();
+  });
+}
+
+// 8 floats to consecutive bf16 (rounded to nearest even) or to float.
+__device__ __forceinline__ void cross_put8(const float (&x)[8], uint16_t* to) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    v[i] = __builtin_bit_cast(uint32_t,
+                              __builtin_convertvector(f32x2{x[2 * i], x[2 * i + 1]}, bf16x2));
+  *reinterpret_cast<u32x4*>(to) = v;
+}
+__device__ __forceinline__ void cross_put8(const float (&x)[8], float* to) {
+  *reinterpret_cast<f32x4*>(to) = f32x4{x[0], x[1], x[2], x[3]};
+  *reinterpret_cast<f32x4*>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+
+}  // namespace pdy

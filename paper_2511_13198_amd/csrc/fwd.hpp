@@ -31,8 +31,6 @@
 
 namespace pdy {
 
-constexpr float kRescaleSlack = 8.0f;
-
 #ifndef PDY_FWD_BK
 #define PDY_FWD_BK 128
 #endif
@@ -100,9 +98,6 @@ struct FwdArgs {
   float* part_o;
   float* part_lse;
 };
-
-// key offset within a 32-key block held in accumulator register r (lane half 0)
-__device__ __forceinline__ constexpr int acc_row_off(int r) { return (r >> 2) * 8 + (r & 3); }
 
 // Epilogue of a forward workgroup's wave: normalise its 32 rows (wrow0 ..) and
 // write O (bf16) and LSE (natural log), or, for a split-K part, the part's fp32

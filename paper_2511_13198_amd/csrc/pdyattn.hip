@@ -14,30 +14,17 @@
 
 #include "bwd.hpp"
 #include "fwd.hpp"
+#include "host.hpp"
 #include "plan.hpp"
 
+using namespace pdy_host;
+
 namespace {
-
-thread_local char g_err[512] = "";
-
-pdy_status fail(pdy_status st, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof(g_err), fmt, ap);
-  va_end(ap);
-  return st;
-}
-
-pdy_status hip_fail(hipError_t e, const char* what) {
-  return fail(PDY_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
 
 // Smallest tile of a launch that can be large, which bounds the work items (the
 // 64-row tiles of four key groups are only for launches of under kManyItems
 // workgroups of larger ones).
 constexpr int kTile = 128;
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 struct Sizes {
   int64_t T, N, maxlen, hq, hkv, d;
@@ -101,55 +88,6 @@ pdy_status check_sizes(int32_t T, int32_t N, int32_t maxlen, int32_t hq, int32_t
   out->hkv = hkv;
   out->d = d;
   return PDY_OK;
-}
-
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-// ---------------------------------------------------------------------------
-// Optional per-thread kernel timing: while enabled, every launch is bracketed
-// by two events on its own stream; pdy_profile_stop reduces them per kernel.
-// ---------------------------------------------------------------------------
-enum KernelId { K_PLAN = 0, K_FWD, K_DKDV, K_DQ, K_SPLIT_MERGE, K_SPLIT_SUM, K_COUNT };
-const char* const kKernelNames[K_COUNT] = {"plan_kernel",     "fwd_kernel",
-                                           "bwd_dkdv_kernel", "bwd_dq_kernel",
-                                           "split_merge_kernel", "split_sum_kernel"};
-struct ProfRec {
-  int kid;
-  hipEvent_t a, b;
-};
-thread_local bool g_prof_on = false;
-thread_local std::vector<ProfRec> g_prof_recs;
-thread_local std::vector<hipEvent_t> g_prof_pool;
-
-hipError_t prof_event(hipEvent_t* ev) {
-  if (!g_prof_pool.empty()) {
-    *ev = g_prof_pool.back();
-    g_prof_pool.pop_back();
-    return hipSuccess;
-  }
-  return hipEventCreate(ev);
-}
-
-// Launch through `fn` (which enqueues exactly one kernel on `st`), timing it
-// when profiling is on.  Returns the launch error, if any.
-template <typename F>
-hipError_t launch_timed(int kid, hipStream_t st, F fn) {
-  if (!g_prof_on) {
-    fn();
-    return hipGetLastError();
-  }
-  ProfRec r;
-  r.kid = kid;
-  hipError_t e = prof_event(&r.a);
-  if (e == hipSuccess) e = prof_event(&r.b);
-  if (e == hipSuccess) e = hipEventRecord(r.a, st);
-  if (e != hipSuccess) return e;
-  fn();
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  e = hipEventRecord(r.b, st);
-  if (e == hipSuccess) g_prof_recs.push_back(r);
-  return e;
 }
 
 size_t plan_bytes(const Sizes& s, int tile) {
@@ -701,12 +639,6 @@ pdy::Plan make_plan(const int32_t* cu, int32_t* ws, const Sizes& s, int tile, in
   return p;
 }
 
-template <typename K>
-hipError_t set_lds(K kernel, int bytes) {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                             hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-}
-
 template <int D, int NW, int KG>
 hipError_t launch_fwd(const pdy::FwdArgs* a, dim3 grid, hipStream_t st) {
   using C = pdy::FwdCfg<D, NW, KG>;
@@ -772,19 +704,6 @@ hipError_t init_kernels() {
     return hipSuccess;
   }();
   return status;
-}
-
-pdy_status check_scale(float scale, int32_t causal) {
-  if (causal != 0 && causal != 1) return fail(PDY_ERR_INVALID_ARG, "causal must be 0 or 1");
-  if (!std::isfinite(scale) || !(scale > 0.f))
-    return fail(PDY_ERR_INVALID_ARG, "scale must be finite and > 0");
-  return PDY_OK;
-}
-
-pdy_status check_ptr(const void* p, const char* name) {
-  if (p == nullptr) return fail(PDY_ERR_INVALID_ARG, "%s is NULL", name);
-  if (!aligned16(p)) return fail(PDY_ERR_INVALID_ARG, "%s is not 16-byte aligned", name);
-  return PDY_OK;
 }
 
 // The schedule of s's segments in tiles of `tile` (cu == nullptr: one segment

@@ -7,6 +7,7 @@ fallback: if the library is missing or a call fails, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -25,7 +26,8 @@ PDY_ERR_HIP = -4
 SYMBOLS = ("attn_fwd_workspace_size", "attn_bwd_workspace_size", "attn_fwd", "attn_bwd",
            "attn_fwd_chunk_workspace_size", "attn_bwd_chunk_workspace_size", "attn_fwd_chunk",
            "attn_bwd_chunk", "attn_fwd_chunk_shared", "attn_bwd_chunk_shared", "attn_merge",
-           "attn_validate_cu_seqlens", "attn_bwd_noalloc", "pdy_launch_shapes",
+           "attn_cross_fwd_workspace_size", "attn_cross_fwd", "attn_prefix_fwd_workspace_size",
+           "attn_prefix_fwd", "attn_validate_cu_seqlens", "attn_bwd_noalloc", "pdy_launch_shapes",
            "pdy_chunk_launch_shapes", "pdy_status_string", "pdy_last_error",
            "pdy_kernel_count", "pdy_kernel_name", "pdy_profile_start", "pdy_profile_stop")
 
@@ -75,6 +77,14 @@ def lib() -> ctypes.CDLL:
     L.attn_bwd_chunk_shared.restype = i32
     L.attn_merge.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp]
     L.attn_merge.restype = i32
+    L.attn_cross_fwd_workspace_size.argtypes = [i32] * 8
+    L.attn_cross_fwd_workspace_size.restype = sz
+    L.attn_cross_fwd.argtypes = [vp] * 6 + [i32] * 9 + [f32, vp, vp, vp, sz, vp]
+    L.attn_cross_fwd.restype = i32
+    L.attn_prefix_fwd_workspace_size.argtypes = [i32] * 9
+    L.attn_prefix_fwd_workspace_size.restype = sz
+    L.attn_prefix_fwd.argtypes = [vp] * 8 + [i32] * 10 + [f32, vp, vp, vp, sz, vp]
+    L.attn_prefix_fwd.restype = i32
     L.attn_validate_cu_seqlens.argtypes = [vp, i32, i32, ctypes.POINTER(i32), vp]
     L.attn_validate_cu_seqlens.restype = i32
     L.attn_bwd_noalloc.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
@@ -400,3 +410,133 @@ def attn_merge(o_a, lse_a, o_b, lse_b, out=None, lse=None):
                           hq, d, out.data_ptr(), lse.data_ptr(), _stream_handle(o_a.device))
     _check(st, "attn_merge")
     return out, lse
+
+
+# ---------------------------------------------------------------------------
+# Keys of another length, and keys shared by the batch
+# ---------------------------------------------------------------------------
+def cross_fwd_workspace_size(total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k, hq, hkv,
+                             d) -> int:
+    return int(lib().attn_cross_fwd_workspace_size(total_q, total_k, num_seqs, max_seqlen_q,
+                                                   max_seqlen_k, hq, hkv, d))
+
+
+def prefix_fwd_workspace_size(prefix_len, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k,
+                              hq, hkv, d) -> int:
+    return int(lib().attn_prefix_fwd_workspace_size(prefix_len, total_q, total_k, num_seqs,
+                                                    max_seqlen_q, max_seqlen_k, hq, hkv, d))
+
+
+def _on_device(device):
+    """The library launches on the current device: make it the tensors'."""
+    import torch
+    if device.index is None or torch.cuda.current_device() == device.index:
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, q on {device}")
+
+
+def _longest(cu, name: str, total: int) -> int:
+    """The longest sequence of cu (checked on the host, synchronising)."""
+    c = cu.tolist()
+    if c[0] != 0 or any(a > b for a, b in zip(c, c[1:])) or c[-1] > total:
+        raise ValueError(f"{name} must rise from 0 to at most {total}")
+    return max(b - a for a, b in zip(c, c[1:]))
+
+
+def _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k, scale, seqlens_k):
+    """Checked arguments of a call: the pointers and numbers of its inputs."""
+    import torch
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        _check_tensor(t, name, torch.bfloat16, 3)
+    for t, name in ((cu_q, "cu_seqlens_q"), (cu_k, "cu_seqlens_k")):
+        _check_tensor(t, name, torch.int32, 1)
+    T, hq, d = q.shape
+    tk, hkv = k.shape[0], k.shape[1]
+    if k.shape[2] != d or v.shape != k.shape:
+        raise ValueError("k and v must be [Tk, Hkv, d] with q's d")
+    n = cu_q.numel() - 1
+    if n < 1 or cu_k.numel() != n + 1:
+        raise ValueError("cu_seqlens_q and cu_seqlens_k must have num_seqs + 1 >= 2 offsets each")
+    if seqlens_k is not None:
+        _check_tensor(seqlens_k, "seqlens_k", torch.int32, 1)
+        if seqlens_k.numel() != n:
+            raise ValueError("seqlens_k must have num_seqs lengths")
+    dev = q.device
+    _same_device(dev, k=k, v=v, cu_seqlens_q=cu_q, cu_seqlens_k=cu_k, seqlens_k=seqlens_k)
+    pre = ()
+    if kp is not None:
+        _check_tensor(kp, "k_prefix", torch.bfloat16, 3)
+        _check_tensor(vp, "v_prefix", torch.bfloat16, 3)
+        if kp.shape[1:] != (hkv, d) or vp.shape != kp.shape:
+            raise ValueError("k_prefix and v_prefix must be [P, Hkv, d]")
+        _same_device(dev, k_prefix=kp, v_prefix=vp)
+        pre = (kp.shape[0],)
+    max_q = _longest(cu_q, "cu_seqlens_q", T) if max_q is None else int(max_q)
+    max_k = _longest(cu_k, "cu_seqlens_k", tk) if max_k is None else int(max_k)
+    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    ptrs = (q.data_ptr(), k.data_ptr(), v.data_ptr())
+    if pre:
+        ptrs += (kp.data_ptr(), vp.data_ptr())
+    offsets = (cu_q.data_ptr(), cu_k.data_ptr(), _ptr(seqlens_k), *pre)
+    return ptrs, offsets, pre, (n, T, tk, max_q, max_k, hq, hkv, d), scale
+
+
+def _cross_fwd(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k, causal, scale, seqlens_k, out, lse,
+               workspace):
+    import torch
+    ptrs, offsets, pre, sizes, scale = _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k,
+                                                   scale, seqlens_k)
+    n, T, tk, max_q, max_k, hq, hkv, d = sizes
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _check_tensor(out, "out", torch.bfloat16, 3)
+    if lse is None:
+        lse = torch.empty((hq, T), dtype=torch.float32, device=q.device)
+    else:
+        _check_tensor(lse, "lse", torch.float32, 2)
+    if out.shape != q.shape or lse.shape != (hq, T):
+        raise ValueError("out must be q's shape, lse [Hq, T]")
+    if workspace is None:
+        size = prefix_fwd_workspace_size if pre else cross_fwd_workspace_size
+        workspace = _ws(size(*pre, T, tk, n, max_q, max_k, hq, hkv, d), q.device)
+    _same_device(q.device, out=out, lse=lse, workspace=workspace)
+    name = "attn_prefix_fwd" if pre else "attn_cross_fwd"
+    with _on_device(q.device):
+        st = getattr(lib(), name)(*ptrs, *offsets, *sizes, int(bool(causal)), scale,
+                                  out.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
+                                  workspace.numel() * workspace.element_size(),
+                                  _stream_handle(q.device))
+    _check(st, name)
+    return out, lse
+
+
+def attn_cross_fwd(q, k, v, cu_seqlens_q, cu_seqlens_k, max_seqlen_q: Optional[int] = None,
+                   max_seqlen_k: Optional[int] = None, causal: bool = False,
+                   scale: Optional[float] = None, seqlens_k=None, out=None, lse=None,
+                   workspace=None):
+    """O [Tq, Hq, d] bf16 and LSE [Hq, Tq] fp32 of every sequence's queries over
+    its own keys: q [Tq, Hq, d] cut by cu_seqlens_q, k, v [Tk, Hkv, d] by
+    cu_seqlens_k (int32 [N + 1]).  seqlens_k (int32 [N]): only the first so many
+    keys of each are in use.  causal aligns the ends: the last query sees every
+    key.  Rows without a key get O = 0, LSE = -inf; rows of no sequence are left."""
+    return _cross_fwd(q, k, v, None, None, cu_seqlens_q, cu_seqlens_k, max_seqlen_q,
+                      max_seqlen_k, causal, scale, seqlens_k, out, lse, workspace)
+
+
+def attn_prefix_fwd(q, k, v, k_prefix, v_prefix, cu_seqlens_q, cu_seqlens_k,
+                    max_seqlen_q: Optional[int] = None, max_seqlen_k: Optional[int] = None,
+                    causal: bool = True, scale: Optional[float] = None, seqlens_k=None, out=None,
+                    lse=None, workspace=None):
+    """attn_cross_fwd of rows that also see the keys k_prefix, v_prefix [P, Hkv, d],
+    which the whole batch shares."""
+    if k_prefix is None or v_prefix is None:
+        raise ValueError("attn_prefix_fwd needs k_prefix and v_prefix")
+    return _cross_fwd(q, k, v, k_prefix, v_prefix, cu_seqlens_q, cu_seqlens_k, max_seqlen_q,
+                      max_seqlen_k, causal, scale, seqlens_k, out, lse, workspace)
