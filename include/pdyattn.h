@@ -210,6 +210,9 @@ pdy_status attn_merge(const void* o_a, const float* lse_a, const void* o_b, cons
  *   - max_seqlen_q, max_seqlen_k: upper bounds of the sequences' queries and keys;
  *     rows beyond max_seqlen_q may stay unwritten.  Offsets are trusted as above,
  *     but clamped to the tensors: wrong ones give wrong results, no stray access.
+ *   - Gradients of sum(dout * o), given o and lse as the forward wrote them; with
+ *     grad_bf16 = 0 fp32, with 1 bf16 (rounded once, from 32-bit sums).  dk and dv of
+ *     keys not in use are 0; dk_prefix and dv_prefix sum the rows of all sequences.
  * q, o bf16 [total_q, Hq, d]; k, v bf16 [total_k, Hkv, d] (NULL if total_k = 0); lse
  * fp32 [Hq, total_q].  Launch shapes and the parts of rows with few keys follow from
  * the sizes and the offsets' values: results of a sequence depend on its batch in
@@ -234,6 +237,29 @@ pdy_status attn_prefix_fwd(const void* q, const void* k, const void* v, const vo
                            int32_t num_heads_kv, int32_t head_dim, int32_t causal, float scale,
                            void* o, float* lse, void* workspace, size_t workspace_bytes,
                            void* stream);
+size_t attn_cross_bwd_workspace_size(int32_t total_q, int32_t total_k, int32_t num_seqs,
+                                     int32_t max_seqlen_q, int32_t max_seqlen_k,
+                                     int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim);
+pdy_status attn_cross_bwd(const void* q, const void* k, const void* v, const void* o,
+                          const float* lse, const void* dout, const int32_t* cu_seqlens_q,
+                          const int32_t* cu_seqlens_k, const int32_t* seqlens_k, int32_t num_seqs,
+                          int32_t total_q, int32_t total_k, int32_t max_seqlen_q,
+                          int32_t max_seqlen_k, int32_t num_heads_q, int32_t num_heads_kv,
+                          int32_t head_dim, int32_t causal, float scale, int32_t grad_bf16,
+                          void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes,
+                          void* stream);
+size_t attn_prefix_bwd_workspace_size(int32_t prefix_len, int32_t total_q, int32_t total_k,
+                                      int32_t num_seqs, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                                      int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim);
+pdy_status attn_prefix_bwd(const void* q, const void* k, const void* v, const void* k_prefix,
+                           const void* v_prefix, const void* o, const float* lse, const void* dout,
+                           const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k,
+                           const int32_t* seqlens_k, int32_t prefix_len, int32_t num_seqs,
+                           int32_t total_q, int32_t total_k, int32_t max_seqlen_q,
+                           int32_t max_seqlen_k, int32_t num_heads_q, int32_t num_heads_kv,
+                           int32_t head_dim, int32_t causal, float scale, int32_t grad_bf16,
+                           void* dq, void* dk, void* dv, void* dk_prefix, void* dv_prefix,
+                           void* workspace, size_t workspace_bytes, void* stream);
 
 /* Debug helper: copies cu_seqlens to the host (synchronising `stream`) and
  * checks cu[0] = 0, monotonicity and cu[num_seqs] = total_tokens.  On success

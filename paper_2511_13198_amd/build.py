@@ -13,7 +13,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpdyattn.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("pdyattn.hip", "cross.hip")]
 HEADERS = [os.path.join(CSRC, f) for f in ("common.hpp", "host.hpp", "plan.hpp", "fwd.hpp",
-                                           "bwd.hpp", "cross.hpp", "cross_fwd.hpp")] + [
+                                           "bwd.hpp", "cross.hpp", "cross_fwd.hpp", "cross_bwd.hpp")] + [
     os.path.join(ROOT, "include", "pdyattn.h")]
 
 ARCH = "gfx950"

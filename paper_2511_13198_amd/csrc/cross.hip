@@ -7,6 +7,7 @@
 
 #include <algorithm>
 
+#include "cross_bwd.hpp"
 #include "cross_fwd.hpp"
 #include "host.hpp"
 
@@ -63,11 +64,11 @@ int64_t most_items(const CrossSizes& s, int64_t n, int64_t max_q, int rows) {
   return std::min(s.tq * s.g() / rows + n, n * ceil_div(max_q * s.g(), rows));
 }
 
-// ---- forward ----
+// ---- tiles of rows: forward and dQ ----
 
 // Rows of a sequence decide the workgroups' shape: the smallest tile that holds
 // them; few rows leave the waves to key groups.
-CrossShape fwd_shape(int64_t rows) {
+CrossShape row_shape(int64_t rows) {
   if (rows <= 32) return {4, 4};
   if (rows <= 64) return {8, 4};
   if (rows <= 128) return {8, 2};
@@ -77,9 +78,10 @@ CrossShape fwd_shape(int64_t rows) {
 int fwd_key_tile(const CrossSizes& s, const CrossShape& sh) {
   return sh.groups > 1 || s.d == 128 ? 128 : 64;
 }
+int dq_key_tile(const CrossSizes&, const CrossShape&) { return 128; }
 
-// One launch of the forward kernel.
-struct CrossFwd {
+// One launch over tiles of rows.
+struct CrossRows {
   CrossShape sh;
   pdy::CrossCut cut;
   int64_t wgs;  // per kv head
@@ -88,15 +90,16 @@ struct CrossFwd {
 constexpr int kMaxParts = 64;
 constexpr int64_t kPartBytes = (int64_t)256 << 20;  // partial results at most
 
-CrossFwd fwd_launch(const CrossSizes& s, pdy::CrossKeys keys, int max_parts_of = kMaxParts) {
+template <class KeyTile>
+CrossRows rows_launch(const CrossSizes& s, pdy::CrossKeys keys, KeyTile key_tile) {
   const bool shared = keys == pdy::CROSS_SHARED;
   const int64_t n = shared ? 1 : s.n, max_q = shared ? s.tq : s.max_q;
-  CrossFwd f;
-  f.sh = fwd_shape(max_q * s.g());
+  CrossRows f;
+  f.sh = row_shape(max_q * s.g());
   pdy::CrossCut& c = f.cut;
   c.keys = keys;
   c.rows = f.sh.rows();
-  c.key_tile = fwd_key_tile(s, f.sh);
+  c.key_tile = key_tile(s, f.sh);
   c.least = 2;
   c.slice = 0;
   c.always_part = 0;
@@ -106,36 +109,37 @@ CrossFwd fwd_launch(const CrossSizes& s, pdy::CrossKeys keys, int max_parts_of =
   const int64_t tiles = (shared ? 0 : ceil_div(s.max_k, c.key_tile)) +
                         (keys == pdy::CROSS_OWN ? 0 : ceil_div(s.prefix, c.key_tile));
   const int64_t slice = s.tq * s.hq * (s.d + 1) * 4;
-  int64_t parts = std::min<int64_t>({max_parts_of, tiles / c.least, kPartBytes / slice});
+  int64_t parts = std::min<int64_t>({kMaxParts, tiles / c.least, kPartBytes / slice});
   if (items * s.hkv >= target) parts = 1;
   c.max_parts = (int)std::max<int64_t>(1, parts);
   f.wgs = items + (c.max_parts > 1 ? ceil_div(target, s.hkv) + 2 : 0);
   return f;
 }
 
-// The launches of a forward: own keys, or shared and own keys in one, or one each.
-struct CrossFwdPlan {
+// The launches over all rows: own keys, or shared and own keys in one, or one each.
+struct CrossRowsPlan {
   int launches;
-  CrossFwd l[2];
+  CrossRows l[2];
   bool merge() const { return launches > 1 || l[0].cut.max_parts > 1; }
   int slices() const {
     return merge() ? l[0].cut.max_parts + (launches > 1 ? l[1].cut.max_parts : 0) : 0;
   }
 };
 
-CrossFwdPlan fwd_plan(const CrossSizes& s) {
-  CrossFwdPlan p;
+template <class KeyTile>
+CrossRowsPlan rows_plan(const CrossSizes& s, KeyTile key_tile) {
+  CrossRowsPlan p;
   if (s.prefix == 0) {
     p.launches = 1;
-    p.l[0] = fwd_launch(s, pdy::CROSS_OWN);
+    p.l[0] = rows_launch(s, pdy::CROSS_OWN, key_tile);
   } else if (s.seq_rows() > 64) {
     p.launches = 1;
-    p.l[0] = fwd_launch(s, pdy::CROSS_FUSED);
+    p.l[0] = rows_launch(s, pdy::CROSS_FUSED, key_tile);
   } else {
     // few rows a sequence: the shared keys once for the rows of all of them
     p.launches = 2;
-    p.l[0] = fwd_launch(s, pdy::CROSS_SHARED);
-    p.l[1] = fwd_launch(s, pdy::CROSS_OWN);
+    p.l[0] = rows_launch(s, pdy::CROSS_SHARED, key_tile);
+    p.l[1] = rows_launch(s, pdy::CROSS_OWN, key_tile);
     p.l[0].cut.always_part = p.l[1].cut.always_part = 1;
     p.l[1].cut.slice = p.l[0].cut.max_parts;
   }
@@ -150,11 +154,66 @@ size_t part_lse_bytes(const CrossSizes& s, int slices) {
   return align256((size_t)slices * s.tq * s.hq * 4);
 }
 
-size_t fwd_bytes(const CrossSizes& s, const CrossFwdPlan& p) {
+size_t fwd_bytes(const CrossSizes& s, const CrossRowsPlan& p) {
   if (!p.merge()) return 256;
   return 2 * part_n_bytes(s) + part_o_bytes(s, p.slices()) + part_lse_bytes(s, p.slices());
 }
 
+// ---- tiles of keys: dK, dV ----
+struct CrossKv {
+  CrossShape sh;  // groups: query groups; 32 * nw / groups keys
+  pdy::CrossCut cut;
+  int64_t wgs;    // per kv head
+};
+
+int pack_log2(const CrossSizes& s) {
+  int n = 0;
+  while (n < 5 && s.g() % (2 << n) == 0) ++n;
+  return n;
+}
+
+CrossKv kv_launch(const CrossSizes& s) {
+  CrossKv k;
+  auto items = [&](int tile) {
+    return std::min(s.tk / tile + s.n, s.n * ceil_div(s.max_k, tile)) + ceil_div(s.prefix, tile);
+  };
+  k.sh = {8, items(256) * s.hkv >= kCUs ? 1 : 2};
+  pdy::CrossCut& c = k.cut;
+  c.keys = pdy::CROSS_FUSED;
+  c.rows = c.key_tile = k.sh.rows();
+  c.least = 4;
+  c.slice = 0;
+  c.always_part = 0;
+  const int64_t n = items(c.rows), target = 2 * kCUs;
+  c.per_head = (float)((double)target / s.hkv);
+  const int64_t slice = (s.prefix + s.tk) * s.hkv * s.d * 8;
+  int64_t parts = std::min<int64_t>(16, slice ? kPartBytes / slice : 1);
+  // items alike in their rows need no cut once they fill the chip; a shared tile has
+  // the rows of all sequences
+  if (n * s.hkv >= target && (s.prefix == 0 || s.n == 1)) parts = 1;
+  c.max_parts = (int)std::max<int64_t>(1, parts);
+  k.wgs = n + (c.max_parts > 1 ? ceil_div(target, s.hkv) + 2 : 0);
+  return k;
+}
+
+// Workspace of a backward: D, the counts of parts, the partial dQ, and dK and dV.
+struct CrossBwdSpace {
+  size_t dd, counts_q, counts_k, part_q, part_kv, total;
+};
+CrossBwdSpace bwd_space(const CrossSizes& s, const CrossRowsPlan& q, const CrossKv& kv) {
+  CrossBwdSpace x;
+  x.dd = align256((size_t)s.hq * s.tq * 4);
+  x.counts_q = q.merge() ? 2 * part_n_bytes(s) : 0;
+  x.counts_k = kv.cut.max_parts > 1 ? align256((size_t)(s.prefix + s.tk) * 4) : 0;
+  x.part_q = part_o_bytes(s, q.slices());
+  x.part_kv = kv.cut.max_parts > 1 ? align256((size_t)kv.cut.max_parts * (s.prefix + s.tk) *
+                                              s.hkv * s.d * 4)
+                                   : 0;
+  x.total = std::max<size_t>(256, x.dd + x.counts_q + x.counts_k + x.part_q + 2 * x.part_kv);
+  return x;
+}
+
+// ---- kernels by shape; called without arguments they set their attributes ----
 template <int D, int NW, int KG>
 hipError_t launch_fwd(const pdy::CrossFwdArgs* a, dim3 grid, hipStream_t st) {
   using C = pdy::CrossFwdCfg<D, NW, KG>;
@@ -162,14 +221,36 @@ hipError_t launch_fwd(const pdy::CrossFwdArgs* a, dim3 grid, hipStream_t st) {
   hipLaunchKernelGGL((pdy::cross_fwd_kernel<D, NW, KG>), grid, dim3(C::NT), C::LDS_BYTES, st, *a);
   return hipSuccess;
 }
+template <int D, int NW, int KG>
+hipError_t launch_dq(const pdy::CrossBwdArgs* a, dim3 grid, hipStream_t st) {
+  using C = pdy::CrossDqCfg<D, NW, KG>;
+  if (a == nullptr) return set_lds(pdy::cross_dq_kernel<D, NW, KG>, C::LDS_BYTES);
+  hipLaunchKernelGGL((pdy::cross_dq_kernel<D, NW, KG>), grid, dim3(C::NT), C::LDS_BYTES, st, *a);
+  return hipSuccess;
+}
+template <int D, int NW, int QG>
+hipError_t launch_dkdv(const pdy::CrossBwdArgs* a, dim3 grid, hipStream_t st) {
+  using C = pdy::CrossDkdvCfg<D, QG, NW>;
+  if (a == nullptr) return set_lds(pdy::cross_dkdv_kernel<D, QG, NW>, C::LDS_BYTES);
+  hipLaunchKernelGGL((pdy::cross_dkdv_kernel<D, QG, NW>), grid, dim3(C::NT), C::LDS_BYTES, st, *a);
+  return hipSuccess;
+}
 
 struct CrossKernels {
   int nw, groups;
   hipError_t (*fwd[2])(const pdy::CrossFwdArgs*, dim3, hipStream_t);  // d = 64, 128
+  hipError_t (*dq[2])(const pdy::CrossBwdArgs*, dim3, hipStream_t);
+  hipError_t (*dkdv[2])(const pdy::CrossBwdArgs*, dim3, hipStream_t);
 };
 template <int NW, int G>
 constexpr CrossKernels cross_kernels_of() {
-  return CrossKernels{NW, G, {launch_fwd<64, NW, G>, launch_fwd<128, NW, G>}};
+  CrossKernels k{NW, G, {launch_fwd<64, NW, G>, launch_fwd<128, NW, G>},
+                 {launch_dq<64, NW, G>, launch_dq<128, NW, G>}, {nullptr, nullptr}};
+  if constexpr (G <= 2) {
+    k.dkdv[0] = launch_dkdv<64, NW, G>;
+    k.dkdv[1] = launch_dkdv<128, NW, G>;
+  }
+  return k;
 }
 constexpr CrossKernels kCrossKernels[] = {cross_kernels_of<8, 1>(), cross_kernels_of<8, 2>(),
                                           cross_kernels_of<8, 4>(), cross_kernels_of<4, 4>()};
@@ -184,6 +265,8 @@ hipError_t init_cross_kernels() {
     for (const CrossKernels& k : kCrossKernels)
       for (int d = 0; d < 2; ++d) {
         hipError_t e = k.fwd[d](nullptr, dim3(), nullptr);
+        if (e == hipSuccess) e = k.dq[d](nullptr, dim3(), nullptr);
+        if (e == hipSuccess && k.dkdv[d]) e = k.dkdv[d](nullptr, dim3(), nullptr);
         if (e != hipSuccess) return e;
       }
     return hipSuccess;
@@ -205,9 +288,9 @@ struct CrossIn {
 
 pdy_status check_cross_in(const CrossIn& x, const CrossSizes& s) {
   pdy_status st;
-  if ((st = check_ptr(x.q, "q")) || (st = check_offsets(x.cu_q, "cu_seqlens_q")) ||
-      (st = check_offsets(x.cu_k, "cu_seqlens_k")))
+  if ((st = check_offsets(x.cu_q, "cu_seqlens_q")) || (st = check_offsets(x.cu_k, "cu_seqlens_k")))
     return st;
+  if (s.tq > 0 && (st = check_ptr(x.q, "q"))) return st;
   if (s.tk > 0 && ((st = check_ptr(x.k, "k")) || (st = check_ptr(x.v, "v")))) return st;
   if (s.prefix > 0 && ((st = check_ptr(x.kp, "k_prefix")) || (st = check_ptr(x.vp, "v_prefix"))))
     return st;
@@ -230,7 +313,7 @@ pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal,
   if ((st = check_cross_in(x, s)) || (st = check_ptr(o, "o")) || (st = check_ptr(lse, "lse")) ||
       (st = check_ptr(workspace, "workspace")))
     return st;
-  const CrossFwdPlan p = fwd_plan(s);
+  const CrossRowsPlan p = rows_plan(s, fwd_key_tile);
   const size_t need = fwd_bytes(s, p);
   if (workspace_bytes < need)
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, %s needs %zu", workspace_bytes, who,
@@ -258,7 +341,7 @@ pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal,
     a.part_lse = reinterpret_cast<float*>(w + part_o_bytes(s, p.slices()));
   }
   for (int i = 0; i < p.launches; ++i) {
-    const CrossFwd& f = p.l[i];
+    const CrossRows& f = p.l[i];
     a.cut = f.cut;
     if (p.merge()) a.part_n = counts + i * (part_n_bytes(s) / 4);
     const dim3 grid((unsigned)(f.wgs * s.hkv));
@@ -290,6 +373,134 @@ pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal,
   return PDY_OK;
 }
 
+struct CrossGrads {
+  void *dq, *dk, *dv, *dkp, *dvp;
+};
+
+pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, const void* dout,
+                          const CrossSizes& s, int32_t causal, float scale, int32_t grad_bf16,
+                          const CrossGrads& g, void* workspace, size_t workspace_bytes,
+                          void* stream, const char* who) {
+  pdy_status st;
+  if ((st = check_scale(scale, causal)) != PDY_OK) return st;
+  if (grad_bf16 != 0 && grad_bf16 != 1)
+    return fail(PDY_ERR_INVALID_ARG, "grad_bf16 must be 0 or 1 (got %d)", grad_bf16);
+  if (s.tq == 0 && s.tk == 0 && s.prefix == 0) return PDY_OK;
+  if ((st = check_cross_in(x, s)) != PDY_OK) return st;
+  if (s.tq > 0 && ((st = check_ptr(o, "o")) || (st = check_ptr(lse, "lse")) ||
+                   (st = check_ptr(dout, "dout")) || (st = check_ptr(g.dq, "dq"))))
+    return st;
+  if (s.tk > 0 && ((st = check_ptr(g.dk, "dk")) || (st = check_ptr(g.dv, "dv")))) return st;
+  if (s.prefix > 0 &&
+      ((st = check_ptr(g.dkp, "dk_prefix")) || (st = check_ptr(g.dvp, "dv_prefix"))))
+    return st;
+  if ((st = check_ptr(workspace, "workspace")) != PDY_OK) return st;
+  const CrossRowsPlan p = rows_plan(s, dq_key_tile);
+  const CrossKv kv = kv_launch(s);
+  const CrossBwdSpace sp = bwd_space(s, p, kv);
+  if (workspace_bytes < sp.total)
+    return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, %s needs %zu", workspace_bytes, who,
+                sp.total);
+  hipError_t e = init_cross_kernels();
+  if (e != hipSuccess) return hip_fail(e, "kernel attribute setup");
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+
+  uint8_t* w = reinterpret_cast<uint8_t*>(workspace);
+  auto take = [&](size_t bytes) {
+    uint8_t* r = w;
+    w += bytes;
+    return r;
+  };
+  float* dd = reinterpret_cast<float*>(take(sp.dd));
+  int32_t* counts_q = reinterpret_cast<int32_t*>(take(sp.counts_q));
+  int32_t* counts_k = reinterpret_cast<int32_t*>(take(sp.counts_k));
+  float* part_q = reinterpret_cast<float*>(take(sp.part_q));
+  float* part_k = reinterpret_cast<float*>(take(sp.part_kv));
+  float* part_v = reinterpret_cast<float*>(take(sp.part_kv));
+
+  pdy::CrossBwdArgs a;
+  a.q = static_cast<const uint16_t*>(x.q);
+  a.k = static_cast<const uint16_t*>(x.k);
+  a.v = static_cast<const uint16_t*>(x.v);
+  a.kp = static_cast<const uint16_t*>(x.kp);
+  a.vp = static_cast<const uint16_t*>(x.vp);
+  a.o = static_cast<const uint16_t*>(o);
+  a.dout = static_cast<const uint16_t*>(dout);
+  a.lse = lse;
+  a.dd = dd;
+  a.dq = g.dq;
+  a.dk = g.dk;
+  a.dv = g.dv;
+  a.dkp = g.dkp;
+  a.dvp = g.dvp;
+  a.out_bf16 = grad_bf16;
+  a.b = batch_of(x, s, causal);
+  a.scale = scale;
+  a.scale_log2 = scale * pdy::kLog2e;
+  a.pack_log2 = pack_log2(s);
+
+  // dQ first: it also writes D, which dK/dV reads
+  for (int i = 0; s.tq > 0 && i < p.launches; ++i) {
+    const CrossRows& f = p.l[i];
+    a.cut = f.cut;
+    a.part = part_q;
+    a.part2 = nullptr;
+    a.part_n = p.merge() ? counts_q + i * (part_n_bytes(s) / 4) : nullptr;
+    a.dd = i == 0 ? dd : nullptr;
+    const dim3 grid((unsigned)(f.wgs * s.hkv));
+    e = launch_timed(K_CROSS_DQ, hs,
+                     [&] { (void)cross_kernels(f.sh).dq[s.d == 128](&a, grid, hs); });
+    if (e != hipSuccess) return hip_fail(e, "cross_dq_kernel launch");
+  }
+  if (s.tk + s.prefix > 0) {
+    a.cut = kv.cut;
+    a.part = part_k;
+    a.part2 = part_v;
+    a.part_n = kv.cut.max_parts > 1 ? counts_k : nullptr;
+    a.dd = dd;
+    const dim3 grid((unsigned)(kv.wgs * s.hkv));
+    e = launch_timed(K_CROSS_DKDV, hs,
+                     [&] { (void)cross_kernels(kv.sh).dkdv[s.d == 128](&a, grid, hs); });
+    if (e != hipSuccess) return hip_fail(e, "cross_dkdv_kernel launch");
+  }
+  // the parts' sums, all in one launch
+  pdy::CrossSumArgs sum{};
+  sum.njobs = 0;
+  sum.out_bf16 = grad_bf16;
+  int64_t blocks = 0;
+  auto add = [&](const float* part, const int32_t* n0, const int32_t* n1, int max0, int max1,
+                 int64_t rows, int64_t first, int64_t count, int64_t heads, const int32_t* end,
+                 void* dst) {
+    if (count == 0) return;
+    const int b = (int)ceil_div(count * (s.d / 8), 256);
+    sum.job[sum.njobs++] =
+        pdy::CrossSumJob{part, n0, n1, max0, max1, rows, first, count, (int)heads, end, dst, b};
+    blocks += b;
+  };
+  if (s.tq > 0 && p.merge())
+    add(part_q, counts_q, p.launches > 1 ? counts_q + part_n_bytes(s) / 4 : nullptr,
+        p.l[0].cut.max_parts, p.launches > 1 ? p.l[1].cut.max_parts : 0, s.tq * s.hq, 0,
+        s.tq * s.hq, s.hq, x.cu_q + s.n, g.dq);
+  if (kv.cut.max_parts > 1) {
+    const int64_t rows = (s.prefix + s.tk) * s.hkv, pre = s.prefix * s.hkv;
+    for (int i = 0; i < 2; ++i) {
+      add(i ? part_v : part_k, counts_k, nullptr, kv.cut.max_parts, 0, rows, 0, pre, s.hkv, nullptr,
+          i ? g.dvp : g.dkp);
+      add(i ? part_v : part_k, counts_k, nullptr, kv.cut.max_parts, 0, rows, pre, s.tk * s.hkv,
+          s.hkv, x.cu_k + s.n, i ? g.dv : g.dk);
+    }
+  }
+  if (sum.njobs > 0) {
+    const dim3 grid((unsigned)blocks);
+    e = launch_timed(K_CROSS_SUM, hs, [&] {
+      if (s.d == 64) hipLaunchKernelGGL(pdy::cross_sum_kernel<64>, grid, dim3(256), 0, hs, sum);
+      else hipLaunchKernelGGL(pdy::cross_sum_kernel<128>, grid, dim3(256), 0, hs, sum);
+    });
+    if (e != hipSuccess) return hip_fail(e, "cross_sum_kernel launch");
+  }
+  return PDY_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -301,7 +512,7 @@ size_t attn_prefix_fwd_workspace_size(int32_t prefix_len, int32_t total_q, int32
   if (check_cross_sizes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k,
                         num_heads_q, num_heads_kv, head_dim, &s) != PDY_OK)
     return 0;
-  return s.tq == 0 ? 256 : fwd_bytes(s, fwd_plan(s));
+  return s.tq == 0 ? 256 : fwd_bytes(s, rows_plan(s, fwd_key_tile));
 }
 
 size_t attn_cross_fwd_workspace_size(int32_t total_q, int32_t total_k, int32_t num_seqs,
@@ -343,6 +554,60 @@ pdy_status attn_cross_fwd(const void* q, const void* k, const void* v, const int
   return cross_fwd_impl({q, k, v, nullptr, nullptr, cu_seqlens_q, cu_seqlens_k, seqlens_k}, s,
                         causal, scale, o, lse, workspace, workspace_bytes, stream,
                         "attn_cross_fwd");
+}
+
+size_t attn_prefix_bwd_workspace_size(int32_t prefix_len, int32_t total_q, int32_t total_k,
+                                      int32_t num_seqs, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                                      int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim) {
+  CrossSizes s;
+  if (check_cross_sizes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k,
+                        num_heads_q, num_heads_kv, head_dim, &s) != PDY_OK)
+    return 0;
+  return bwd_space(s, rows_plan(s, dq_key_tile), kv_launch(s)).total;
+}
+
+size_t attn_cross_bwd_workspace_size(int32_t total_q, int32_t total_k, int32_t num_seqs,
+                                     int32_t max_seqlen_q, int32_t max_seqlen_k,
+                                     int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim) {
+  return attn_prefix_bwd_workspace_size(0, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k,
+                                        num_heads_q, num_heads_kv, head_dim);
+}
+
+pdy_status attn_prefix_bwd(const void* q, const void* k, const void* v, const void* k_prefix,
+                           const void* v_prefix, const void* o, const float* lse, const void* dout,
+                           const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k,
+                           const int32_t* seqlens_k, int32_t prefix_len, int32_t num_seqs,
+                           int32_t total_q, int32_t total_k, int32_t max_seqlen_q,
+                           int32_t max_seqlen_k, int32_t num_heads_q, int32_t num_heads_kv,
+                           int32_t head_dim, int32_t causal, float scale, int32_t grad_bf16,
+                           void* dq, void* dk, void* dv, void* dk_prefix, void* dv_prefix,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  g_err[0] = 0;
+  CrossSizes s;
+  const pdy_status st = check_cross_sizes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q,
+                                          max_seqlen_k, num_heads_q, num_heads_kv, head_dim, &s);
+  if (st != PDY_OK) return st;
+  return cross_bwd_impl({q, k, v, k_prefix, v_prefix, cu_seqlens_q, cu_seqlens_k, seqlens_k}, o,
+                        lse, dout, s, causal, scale, grad_bf16, {dq, dk, dv, dk_prefix, dv_prefix},
+                        workspace, workspace_bytes, stream, "attn_prefix_bwd");
+}
+
+pdy_status attn_cross_bwd(const void* q, const void* k, const void* v, const void* o,
+                          const float* lse, const void* dout, const int32_t* cu_seqlens_q,
+                          const int32_t* cu_seqlens_k, const int32_t* seqlens_k, int32_t num_seqs,
+                          int32_t total_q, int32_t total_k, int32_t max_seqlen_q,
+                          int32_t max_seqlen_k, int32_t num_heads_q, int32_t num_heads_kv,
+                          int32_t head_dim, int32_t causal, float scale, int32_t grad_bf16,
+                          void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+  g_err[0] = 0;
+  CrossSizes s;
+  const pdy_status st = check_cross_sizes(0, total_q, total_k, num_seqs, max_seqlen_q,
+                                          max_seqlen_k, num_heads_q, num_heads_kv, head_dim, &s);
+  if (st != PDY_OK) return st;
+  return cross_bwd_impl({q, k, v, nullptr, nullptr, cu_seqlens_q, cu_seqlens_k, seqlens_k}, o, lse,
+                        dout, s, causal, scale, grad_bf16, {dq, dk, dv, nullptr, nullptr},
+                        workspace, workspace_bytes, stream, "attn_cross_bwd");
 }
 
 }  // extern "C"

@@ -32,9 +32,9 @@ struct CrossBatch {
   int causal;
 };
 
-// One sequence: rows of q and k, keys in use.
+// One sequence: rows of q and k, keys in use, and rows of k with those not in use.
 struct CrossSeq {
-  int q_lo, nq, k_lo, nk;
+  int q_lo, nq, k_lo, nk, room;
 };
 
 __device__ __forceinline__ CrossSeq cross_seq(const CrossBatch& b, int i) {
@@ -42,9 +42,13 @@ __device__ __forceinline__ CrossSeq cross_seq(const CrossBatch& b, int i) {
   s.q_lo = min(max(b.cu_q[i], 0), b.tq);
   s.nq = min(max(b.cu_q[i + 1], s.q_lo), b.tq) - s.q_lo;
   s.k_lo = min(max(b.cu_k[i], 0), b.tk);
-  s.nk = min(max(b.cu_k[i + 1], s.k_lo), b.tk) - s.k_lo;
+  s.nk = s.room = min(max(b.cu_k[i + 1], s.k_lo), b.tk) - s.k_lo;
   if (b.len_k) s.nk = min(max(b.len_k[i], 0), s.nk);
   return s;
+}
+// The whole batch as one sequence over the shared keys.
+__device__ __forceinline__ CrossSeq cross_shared_seq(const CrossBatch& b) {
+  return CrossSeq{0, min(max(b.cu_q[b.n], 0), b.tq), 0, b.prefix, b.prefix};
 }
 
 // Which rows and keys a launch covers.
@@ -55,19 +59,20 @@ enum CrossKeys : int {
 };
 
 // How a launch's rows and keys are cut.  An item is a tile of `rows` packed rows of
-// a sequence and kv head; its key tiles are cut into parts, one workgroup each,
-// whose partial results another kernel combines:
-//   units = sum over the sequences of row tiles x key tiles,
-//   a part has at most C = max(least, units * hkv / target) key tiles, so that the
+// a sequence and kv head (dK/dV: a tile of keys); its inner work, key tiles (row
+// tiles), is cut into parts, one workgroup each, whose partial results another
+// kernel combines:
+//   units = sum over the items of their inner tiles,
+//   a part has at most C = max(least, units * hkv / target) of them, so that the
 //   parts are alike whatever the lengths, there are about `target` of them, and
-//   a launch with that many items is not cut (C is then above their key tiles).
+//   a launch with that many items is not cut (C is then above their inner tiles).
 // Every workgroup computes C from the offsets, so that nothing waits for the host.
 struct CrossCut {
   int keys;         // CrossKeys
   int rows;         // packed rows per tile
   int key_tile;     // keys per tile
   int max_parts;    // 1: not cut
-  int least;        // fewest key tiles of a part
+  int least;        // fewest inner tiles of a part
   float per_head;   // parts wanted per kv head (target / hkv)
   int slice;        // first slice of the partial results
   int always_part;  // partial results also of items in one part
@@ -75,42 +80,34 @@ struct CrossCut {
 
 struct CrossPlace {
   CrossSeq s;
-  int tile;  // row tile of the sequence
+  int index;  // the sequence's place in the list
+  int tile;   // tile of the sequence
   int part, nparts;
 };
 
 __device__ __forceinline__ int cross_tiles(int x, int tile) { return (x + tile - 1) / tile; }
 
-// The sequence that lane l's place in the list stands for (CROSS_SHARED: sequence
-// 0 is the whole batch), and its row tiles and key tiles.
-__device__ __forceinline__ CrossSeq cross_lane_seq(const CrossBatch& b, const CrossCut& c, int i,
-                                                   int g, int& row_tiles, int& key_tiles) {
-  CrossSeq s = {0, 0, 0, 0};
-  row_tiles = key_tiles = 0;
-  if (i < (c.keys == CROSS_SHARED ? 1 : b.n)) {
-    if (c.keys == CROSS_SHARED) s.nq = min(max(b.cu_q[b.n], 0), b.tq);
-    else s = cross_seq(b, i);
-    row_tiles = cross_tiles(s.nq * g, c.rows);
-    key_tiles = cross_tiles(s.nk, c.key_tile) +
-                (c.keys == CROSS_OWN ? 0 : cross_tiles(b.prefix, c.key_tile));
-  }
-  return s;
-}
-
-// Sequence, row tile and part of entry `entry` of a kv head's list; false past its
-// end.  One pass over the sequences, 64 at a time (two where the launch is cut);
-// the results are wave-uniform.
-__device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut& c, int entry,
+// Sequence, tile and part of entry `entry` of a kv head's list; false past its end.
+// of(i, tiles, units): the i-th of the list's n sequences, its tiles and the units of
+// inner work of each.  One pass over the sequences, 64 at a time (two where the
+// launch is cut); the results are wave-uniform.
+template <class F>
+__device__ __forceinline__ bool cross_place(int n, const CrossCut& c, int entry, F&& of,
                                             CrossPlace& out) {
-  const int l = __lane_id(), g = b.hq / b.hkv;
-  const int n = c.keys == CROSS_SHARED ? 1 : b.n;
+  const int l = __lane_id();
+  auto lane = [&](int i, int& tiles, int& units) __attribute__((always_inline)) {
+    CrossSeq s = {0, 0, 0, 0, 0};
+    tiles = units = 0;
+    if (i < n) s = of(i, tiles, units);
+    return s;
+  };
   int cap = 1 << 30;
   if (c.max_parts > 1) {
     float units = 0.f;
     for (int i0 = 0; i0 < n; i0 += 64) {
-      int rt, kt;
-      cross_lane_seq(b, c, i0 + l, g, rt, kt);
-      units += (float)rt * (float)kt;
+      int t, u;
+      lane(i0 + l, t, u);
+      units += (float)t * (float)u;
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) units += __shfl_xor(units, off);
@@ -118,15 +115,15 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
   }
   int base = 0;
   for (int i0 = 0; i0 < n; i0 += 64) {
-    int rt, kt;
-    const CrossSeq s = cross_lane_seq(b, c, i0 + l, g, rt, kt);
-    const int parts = max(1, min(c.max_parts, cross_tiles(kt, cap)));
-    const int mine = rt * parts;
+    int t, u;
+    const CrossSeq s = lane(i0 + l, t, u);
+    const int parts = max(1, min(c.max_parts, cross_tiles(u, cap)));
+    const int mine = t * parts;
     int incl = mine;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
-      const int t = __shfl_up(incl, off);
-      if (l >= off) incl += t;
+      const int x = __shfl_up(incl, off);
+      if (l >= off) incl += x;
     }
     const int rel = entry - base;
     const uint64_t hit = __builtin_amdgcn_ballot_w64(rel >= incl - mine && rel < incl);
@@ -135,7 +132,8 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
       auto get = [&](int v) __attribute__((always_inline)) {
         return __builtin_amdgcn_readlane(v, src);
       };
-      out.s = CrossSeq{get(s.q_lo), get(s.nq), get(s.k_lo), get(s.nk)};
+      out.s = CrossSeq{get(s.q_lo), get(s.nq), get(s.k_lo), get(s.nk), get(s.room)};
+      out.index = i0 + src;
       out.nparts = get(parts);
       const int at = rel - get(incl - mine);
       out.tile = __builtin_amdgcn_readfirstlane(at / out.nparts);
@@ -147,6 +145,22 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
   return false;
 }
 
+// The same for tiles of packed rows (forward, dQ).
+__device__ __forceinline__ bool cross_place_rows(const CrossBatch& b, const CrossCut& c, int entry,
+                                                 CrossPlace& out) {
+  const bool shared = c.keys == CROSS_SHARED;
+  return cross_place(
+      shared ? 1 : b.n, c, entry,
+      [&](int i, int& tiles, int& units) __attribute__((always_inline)) {
+        const CrossSeq s = shared ? cross_shared_seq(b) : cross_seq(b, i);
+        tiles = cross_tiles(s.nq * (b.hq / b.hkv), c.rows);
+        units = cross_tiles(s.nk, c.key_tile) +
+                (c.keys == CROSS_FUSED ? cross_tiles(b.prefix, c.key_tile) : 0);
+        return s;
+      },
+      out);
+}
+
 // ---------------------------------------------------------------------------
 // Output tiles of packed rows: as store_rows_bf16 and store_rows_f32, with the
 // address of a row (0 .. 31 of the wave's tile) from `at`.
@@ -156,7 +170,7 @@ __device__ __forceinline__ void cross_store_bf16(const f32x16 (&acc)[D / 32], fl
                                                  uint16_t* lds, At&& at) {
   constexpr int P = kBf16Pitch<D>, LANES = D / 8, ROWS = 64 / LANES;
   if (nrows <= 0) return;  // wave-uniform
-  const int l = __lane_id();
+  const int l = fresh_lane_id();
   const int wr = (l & 31) * P + (l >> 5) * 4;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
@@ -191,7 +205,7 @@ __device__ __forceinline__ void cross_store_f32(const f32x16 (&acc)[D / 32], flo
                                                 float* lds, At&& at) {
   static_assert((D / 32) % PASS == 0, "whole passes");
   if (nrows <= 0) return;  // wave-uniform
-  const int l = __lane_id();
+  const int l = fresh_lane_id();
   const int wr = acc_slot_lane(l);
   const int rr = l >> 3, c = (l & 7) * 4;  // read: 8 lanes a row
   const uint32_t rd = lds_addr(lds) + (rr * kF32Pitch + c) * 4;

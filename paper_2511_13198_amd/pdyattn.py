@@ -27,7 +27,9 @@ SYMBOLS = ("attn_fwd_workspace_size", "attn_bwd_workspace_size", "attn_fwd", "at
            "attn_fwd_chunk_workspace_size", "attn_bwd_chunk_workspace_size", "attn_fwd_chunk",
            "attn_bwd_chunk", "attn_fwd_chunk_shared", "attn_bwd_chunk_shared", "attn_merge",
            "attn_cross_fwd_workspace_size", "attn_cross_fwd", "attn_prefix_fwd_workspace_size",
-           "attn_prefix_fwd", "attn_validate_cu_seqlens", "attn_bwd_noalloc", "pdy_launch_shapes",
+           "attn_prefix_fwd", "attn_cross_bwd_workspace_size", "attn_cross_bwd",
+           "attn_prefix_bwd_workspace_size", "attn_prefix_bwd", "attn_validate_cu_seqlens",
+           "attn_bwd_noalloc", "pdy_launch_shapes",
            "pdy_chunk_launch_shapes", "pdy_status_string", "pdy_last_error",
            "pdy_kernel_count", "pdy_kernel_name", "pdy_profile_start", "pdy_profile_stop")
 
@@ -85,6 +87,15 @@ def lib() -> ctypes.CDLL:
     L.attn_prefix_fwd_workspace_size.restype = sz
     L.attn_prefix_fwd.argtypes = [vp] * 8 + [i32] * 10 + [f32, vp, vp, vp, sz, vp]
     L.attn_prefix_fwd.restype = i32
+    L.attn_cross_bwd_workspace_size.argtypes = [i32] * 8
+    L.attn_cross_bwd_workspace_size.restype = sz
+    L.attn_cross_bwd.argtypes = [vp] * 9 + [i32] * 9 + [f32, i32, vp, vp, vp, vp, sz, vp]
+    L.attn_cross_bwd.restype = i32
+    L.attn_prefix_bwd_workspace_size.argtypes = [i32] * 9
+    L.attn_prefix_bwd_workspace_size.restype = sz
+    L.attn_prefix_bwd.argtypes = ([vp] * 11 + [i32] * 10 +
+                                  [f32, i32, vp, vp, vp, vp, vp, vp, sz, vp])
+    L.attn_prefix_bwd.restype = i32
     L.attn_validate_cu_seqlens.argtypes = [vp, i32, i32, ctypes.POINTER(i32), vp]
     L.attn_validate_cu_seqlens.restype = i32
     L.attn_bwd_noalloc.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
@@ -427,6 +438,18 @@ def prefix_fwd_workspace_size(prefix_len, total_q, total_k, num_seqs, max_seqlen
                                                     max_seqlen_q, max_seqlen_k, hq, hkv, d))
 
 
+def cross_bwd_workspace_size(total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k, hq, hkv,
+                             d) -> int:
+    return int(lib().attn_cross_bwd_workspace_size(total_q, total_k, num_seqs, max_seqlen_q,
+                                                   max_seqlen_k, hq, hkv, d))
+
+
+def prefix_bwd_workspace_size(prefix_len, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k,
+                              hq, hkv, d) -> int:
+    return int(lib().attn_prefix_bwd_workspace_size(prefix_len, total_q, total_k, num_seqs,
+                                                    max_seqlen_q, max_seqlen_k, hq, hkv, d))
+
+
 def _on_device(device):
     """The library launches on the current device: make it the tensors'."""
     import torch
@@ -540,3 +563,72 @@ def attn_prefix_fwd(q, k, v, k_prefix, v_prefix, cu_seqlens_q, cu_seqlens_k,
         raise ValueError("attn_prefix_fwd needs k_prefix and v_prefix")
     return _cross_fwd(q, k, v, k_prefix, v_prefix, cu_seqlens_q, cu_seqlens_k, max_seqlen_q,
                       max_seqlen_k, causal, scale, seqlens_k, out, lse, workspace)
+
+
+def _cross_bwd(q, k, v, kp, vp, o, lse, dout, cu_q, cu_k, max_q, max_k, causal, scale, seqlens_k,
+               grads, grad_dtype, workspace):
+    import torch
+    ptrs, offsets, pre, sizes, scale = _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k,
+                                                   scale, seqlens_k)
+    n, T, tk, max_q, max_k, hq, hkv, d = sizes
+    _check_tensor(o, "o", torch.bfloat16, 3)
+    _check_tensor(dout, "dout", torch.bfloat16, 3)
+    _check_tensor(lse, "lse", torch.float32, 2)
+    if o.shape != q.shape or dout.shape != q.shape or lse.shape != (hq, T):
+        raise ValueError("o and dout must match q, lse must be [Hq, T]")
+    given = [g for g in grads if g is not None]
+    dtype = given[0].dtype if given else grad_dtype
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"gradients must be torch.float32 or torch.bfloat16, got {dtype}")
+    names = ("dq", "dk", "dv", "dk_prefix", "dv_prefix")
+    out = []
+    for name, g, like in zip(names, grads, (q, k, v, kp, vp)):
+        if like is None:
+            continue
+        if g is None:
+            g = torch.empty(like.shape, dtype=dtype, device=q.device)
+        _check_tensor(g, name, dtype, 3)
+        if g.shape != like.shape:
+            raise ValueError(f"{name} must be {list(like.shape)}")
+        out.append(g)
+    if workspace is None:
+        size = prefix_bwd_workspace_size if pre else cross_bwd_workspace_size
+        workspace = _ws(size(*pre, T, tk, n, max_q, max_k, hq, hkv, d), q.device)
+    _same_device(q.device, o=o, lse=lse, dout=dout, workspace=workspace, **dict(zip(names, out)))
+    name = "attn_prefix_bwd" if pre else "attn_cross_bwd"
+    with _on_device(q.device):
+        st = getattr(lib(), name)(*ptrs, o.data_ptr(), lse.data_ptr(), dout.data_ptr(), *offsets,
+                                  *sizes, int(bool(causal)), scale, int(dtype == torch.bfloat16),
+                                  *(g.data_ptr() for g in out), workspace.data_ptr(),
+                                  workspace.numel() * workspace.element_size(),
+                                  _stream_handle(q.device))
+    _check(st, name)
+    return tuple(out)
+
+
+def attn_cross_bwd(q, k, v, o, lse, dout, cu_seqlens_q, cu_seqlens_k,
+                   max_seqlen_q: Optional[int] = None, max_seqlen_k: Optional[int] = None,
+                   causal: bool = False, scale: Optional[float] = None, seqlens_k=None, dq=None,
+                   dk=None, dv=None, grad_dtype=None, workspace=None) -> Tuple:
+    """dQ [Tq, Hq, d], dK, dV [Tk, Hkv, d] of sum(dout * O) of attn_cross_fwd, in the
+    dtype of the given gradients, else grad_dtype (torch.float32, the default, or
+    torch.bfloat16).  Keys not in use get 0; rows of no sequence are left."""
+    import torch
+    return _cross_bwd(q, k, v, None, None, o, lse, dout, cu_seqlens_q, cu_seqlens_k,
+                      max_seqlen_q, max_seqlen_k, causal, scale, seqlens_k,
+                      (dq, dk, dv, None, None), grad_dtype or torch.float32, workspace)
+
+
+def attn_prefix_bwd(q, k, v, k_prefix, v_prefix, o, lse, dout, cu_seqlens_q, cu_seqlens_k,
+                    max_seqlen_q: Optional[int] = None, max_seqlen_k: Optional[int] = None,
+                    causal: bool = True, scale: Optional[float] = None, seqlens_k=None, dq=None,
+                    dk=None, dv=None, dk_prefix=None, dv_prefix=None, grad_dtype=None,
+                    workspace=None) -> Tuple:
+    """attn_cross_bwd of attn_prefix_fwd: also dK, dV of the shared keys [P, Hkv, d],
+    summed over the rows of all sequences."""
+    import torch
+    if k_prefix is None or v_prefix is None:
+        raise ValueError("attn_prefix_bwd needs k_prefix and v_prefix")
+    return _cross_bwd(q, k, v, k_prefix, v_prefix, o, lse, dout, cu_seqlens_q, cu_seqlens_k,
+                      max_seqlen_q, max_seqlen_k, causal, scale, seqlens_k,
+                      (dq, dk, dv, dk_prefix, dv_prefix), grad_dtype or torch.float32, workspace)

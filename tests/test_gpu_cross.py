@@ -90,7 +90,11 @@ def forward(x, args, len_k, **kw):
     return pdyattn.attn_cross_fwd(x["q"], x["k"], x["v"], *args, seqlens_k=len_k, **kw)
 
 
-@pytest.mark.parametrize("case", CASES, ids=lambda c: f"q{sum(c[0])}k{sum(c[1])}p{c[3]}h{c[4]}kv{c[5]}d{c[6]}")
+def case_id(c):
+    return f"q{sum(c[0])}k{sum(c[1])}p{c[3]}h{c[4]}kv{c[5]}d{c[6]}"
+
+
+@pytest.mark.parametrize("case", CASES, ids=case_id)
 def test_forward(case):
     import torch
     x, ref, args, len_k = setup(case)
@@ -102,3 +106,40 @@ def test_forward(case):
     cu.check("o", o[:t], tuple(r[:t] for r in ref["o"]))
     cu.check("lse", lse[:, :t], tuple(r[:, :t] for r in ref["lse"]))
     assert (o[t:] == 7.0).all() and (lse[:, t:] == 7.0).all(), "rows of no sequence were written"
+
+
+def backward(x, o, lse, args, len_k, **kw):
+    from paper_2511_13198_amd import pdyattn
+    if "kp" in x:
+        return pdyattn.attn_prefix_bwd(x["q"], x["k"], x["v"], x["kp"], x["vp"], o, lse, x["do"],
+                                       *args, seqlens_k=len_k, **kw)
+    return pdyattn.attn_cross_bwd(x["q"], x["k"], x["v"], o, lse, x["do"], *args,
+                                  seqlens_k=len_k, **kw)
+
+
+GRADS = ("dq", "dk", "dv", "dkp", "dvp")
+
+
+def empties(x, dtype, value):
+    """Gradient tensors holding `value`, as the backward's keywords."""
+    import torch
+    names = {"dq": "q", "dk": "k", "dv": "v"}
+    if "kp" in x:
+        names.update(dk_prefix="kp", dv_prefix="vp")
+    return {n: torch.full_like(x[of], value, dtype=dtype) for n, of in names.items()}
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("case", CASES, ids=case_id)
+def test_gradients(case, dtype):
+    import torch
+    x, ref, args, len_k = setup(case, 1)
+    o, lse = forward(x, args, len_k)
+    out = empties(x, getattr(torch, dtype), 7.0)
+    got = backward(x, o, lse, args, len_k, **out)
+    torch.cuda.synchronize()
+    t, tk = sum(case[0]), sum(case[1])
+    for name, g in zip(GRADS, got):
+        end = t if name == "dq" else g.shape[0] if name.endswith("p") else tk
+        cu.check(name, g[:end], tuple(r[:end] for r in ref[name]))
+        assert (g[end:] == 7.0).all(), f"{name}: rows of no sequence were written"
