@@ -1,0 +1,115 @@
+// C-ABI of the rotary positions: argument checks, the frequencies as fractions of a
+// turn, and the launch.  The contract is in include/pdyattn.h.
+#include "../../include/pdyattn.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "host.hpp"
+#include "rotary.hpp"
+
+using namespace pdy_host;
+
+namespace {
+
+template <class In, class Out, int D>
+void launch_rotary(const pdy::RotaryArgs& a, bool inter, int64_t heads, hipStream_t st) {
+  constexpr int kTokens = 256 * 2 * (16 / (int)sizeof(In)) / D;
+  const dim3 grid((unsigned)((a.tokens + kTokens - 1) / kTokens),
+                  (unsigned)((heads + a.heads_per_block - 1) / a.heads_per_block));
+  if (inter)
+    hipLaunchKernelGGL((pdy::rotary_kernel<In, Out, D, true>), grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((pdy::rotary_kernel<In, Out, D, false>), grid, dim3(256), 0, st, a);
+}
+
+template <class In, class Out>
+void launch_rotary(const pdy::RotaryArgs& a, int d, bool inter, int64_t heads, hipStream_t st) {
+  if (d == 64) launch_rotary<In, Out, 64>(a, inter, heads, st);
+  else launch_rotary<In, Out, 128>(a, inter, heads, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
+                       int32_t total_tokens, int32_t num_axes, int32_t num_heads_q,
+                       int32_t num_heads_kv, int32_t head_dim, int32_t num_pairs,
+                       const double* freqs, const int32_t* pair_axes, int32_t interleaved,
+                       int32_t inverse, int32_t in_fp32, int32_t out_fp32, void* q_out,
+                       void* k_out, void* stream) {
+  g_err[0] = 0;
+  pdy_status st;
+  if (total_tokens < 0)
+    return fail(PDY_ERR_INVALID_ARG, "total_tokens must be >= 0 (got %d)", total_tokens);
+  if (num_axes < 1 || num_axes > pdy::kMaxAxes)
+    return fail(PDY_ERR_INVALID_ARG, "num_axes must be in [1, %d] (got %d)", pdy::kMaxAxes,
+                num_axes);
+  if (num_heads_q < 0 || num_heads_kv < 0 || (int64_t)num_heads_q + num_heads_kv < 1 ||
+      (int64_t)num_heads_q + num_heads_kv > 65535)
+    return fail(PDY_ERR_INVALID_ARG, "head counts must be >= 0 and 1 to 65,535 together (got %d, %d)",
+                num_heads_q, num_heads_kv);
+  if (head_dim != 64 && head_dim != 128)
+    return fail(PDY_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", head_dim);
+  if (num_pairs < 8 || num_pairs > head_dim / 2 || num_pairs % 8 != 0)
+    return fail(PDY_ERR_INVALID_ARG,
+                "num_pairs must be a multiple of 8 up to head_dim / 2 = %d (got %d)", head_dim / 2,
+                num_pairs);
+  if ((interleaved & ~1) || (inverse & ~1) || (in_fp32 & ~1) || (out_fp32 & ~1))
+    return fail(PDY_ERR_INVALID_ARG, "interleaved, inverse, in_fp32 and out_fp32 must be 0 or 1");
+  if (out_fp32 && !in_fp32)
+    return fail(PDY_ERR_UNSUPPORTED, "bf16 to fp32 is not supported (bf16, fp32, or fp32 to bf16)");
+  if (freqs == nullptr || pair_axes == nullptr)
+    return fail(PDY_ERR_INVALID_ARG, "freqs and pair_axes (host arrays) must not be NULL");
+  pdy::RotaryArgs a;
+  for (int p = 0; p < num_pairs; ++p) {
+    if (!std::isfinite(freqs[p]))
+      return fail(PDY_ERR_INVALID_ARG, "freqs[%d] is not finite", p);
+    if (pair_axes[p] < 0 || pair_axes[p] >= num_axes)
+      return fail(PDY_ERR_INVALID_ARG, "pair_axes[%d] must be in [0, %d) (got %d)", p, num_axes,
+                  pair_axes[p]);
+    // turns a position, without whole turns (a long double holds the 64 bits)
+    long double turns = (long double)freqs[p] * 0.15915494309189533576888376337251436L;
+    turns -= floorl(turns);
+    a.freq[p] = turns < 1.0L ? (uint64_t)(turns * 18446744073709551616.0L) : 0;
+    a.axis[p] = (uint8_t)pair_axes[p];
+  }
+  if (total_tokens == 0) return PDY_OK;
+  if (num_heads_q > 0 && ((st = check_ptr(q, "q")) || (st = check_ptr(q_out, "q_out")))) return st;
+  if (num_heads_kv > 0 && ((st = check_ptr(k, "k")) || (st = check_ptr(k_out, "k_out")))) return st;
+  if (positions == nullptr || (reinterpret_cast<uintptr_t>(positions) & 3u) != 0)
+    return fail(PDY_ERR_INVALID_ARG, "positions is NULL or not 4-byte aligned");
+  if (in_fp32 != out_fp32 && ((num_heads_q > 0 && q == q_out) || (num_heads_kv > 0 && k == k_out)))
+    return fail(PDY_ERR_INVALID_ARG, "in place needs one type for input and output");
+  a.in[0] = q;
+  a.in[1] = k;
+  a.out[0] = q_out;
+  a.out[1] = k_out;
+  a.heads[0] = num_heads_q;
+  a.heads[1] = num_heads_kv;
+  a.pos = positions;
+  a.tokens = total_tokens;
+  a.axes = num_axes;
+  a.pairs = num_pairs;
+  a.inverse = inverse;
+  // a block's tokens through all heads, so that angles are computed once, unless that
+  // leaves the chip idle: then fewer heads a block, down to one
+  const int64_t heads = (int64_t)num_heads_q + num_heads_kv;
+  const int64_t tokens_per_block = 512 * (in_fp32 ? 4 : 8) / head_dim;
+  const int64_t blocks = (total_tokens + tokens_per_block - 1) / tokens_per_block;
+  const int64_t cuts = std::min(heads, std::max<int64_t>(1, 1024 / blocks));
+  a.heads_per_block = (int)((heads + cuts - 1) / cuts);
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  const hipError_t e = launch_timed(K_ROTARY, hs, [&] {
+    if (!in_fp32) launch_rotary<uint16_t, uint16_t>(a, head_dim, interleaved, heads, hs);
+    else if (out_fp32) launch_rotary<float, float>(a, head_dim, interleaved, heads, hs);
+    else launch_rotary<float, uint16_t>(a, head_dim, interleaved, heads, hs);
+  });
+  if (e != hipSuccess) return hip_fail(e, "rotary_kernel launch");
+  return PDY_OK;
+}
+
+}  // extern "C"

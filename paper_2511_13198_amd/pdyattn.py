@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import math
 import os
 from typing import Optional, Tuple
@@ -28,8 +29,8 @@ SYMBOLS = ("attn_fwd_workspace_size", "attn_bwd_workspace_size", "attn_fwd", "at
            "attn_bwd_chunk", "attn_fwd_chunk_shared", "attn_bwd_chunk_shared", "attn_merge",
            "attn_cross_fwd_workspace_size", "attn_cross_fwd", "attn_prefix_fwd_workspace_size",
            "attn_prefix_fwd", "attn_cross_bwd_workspace_size", "attn_cross_bwd",
-           "attn_prefix_bwd_workspace_size", "attn_prefix_bwd", "attn_validate_cu_seqlens",
-           "attn_bwd_noalloc", "pdy_launch_shapes",
+           "attn_prefix_bwd_workspace_size", "attn_prefix_bwd", "attn_rotary",
+           "attn_validate_cu_seqlens", "attn_bwd_noalloc", "pdy_launch_shapes",
            "pdy_chunk_launch_shapes", "pdy_status_string", "pdy_last_error",
            "pdy_kernel_count", "pdy_kernel_name", "pdy_profile_start", "pdy_profile_stop")
 
@@ -96,6 +97,10 @@ def lib() -> ctypes.CDLL:
     L.attn_prefix_bwd.argtypes = ([vp] * 11 + [i32] * 10 +
                                   [f32, i32, vp, vp, vp, vp, vp, vp, sz, vp])
     L.attn_prefix_bwd.restype = i32
+    L.attn_rotary.argtypes = ([vp] * 3 + [i32] * 6 +
+                              [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32)] + [i32] * 4 +
+                              [vp] * 3)
+    L.attn_rotary.restype = i32
     L.attn_validate_cu_seqlens.argtypes = [vp, i32, i32, ctypes.POINTER(i32), vp]
     L.attn_validate_cu_seqlens.restype = i32
     L.attn_bwd_noalloc.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
@@ -632,3 +637,78 @@ def attn_prefix_bwd(q, k, v, k_prefix, v_prefix, o, lse, dout, cu_seqlens_q, cu_
     return _cross_bwd(q, k, v, k_prefix, v_prefix, o, lse, dout, cu_seqlens_q, cu_seqlens_k,
                       max_seqlen_q, max_seqlen_k, causal, scale, seqlens_k,
                       (dq, dk, dv, dk_prefix, dv_prefix), grad_dtype or torch.float32, workspace)
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions with several axes
+# ---------------------------------------------------------------------------
+@functools.lru_cache(maxsize=64)
+def _rotary_tables(sections: Tuple[int, ...], base: float, freqs: Optional[Tuple[float, ...]]):
+    """(frequencies, axes) of the pairs as C arrays."""
+    if any(n < 0 for n in sections):
+        raise ValueError(f"sections must be >= 0, got {sections}")
+    pairs = sum(sections)
+    if freqs is None:
+        freqs = tuple(base ** (-p / pairs) for p in range(pairs))
+    elif len(freqs) != pairs:
+        raise ValueError(f"freqs must have {pairs} values, one a pair, got {len(freqs)}")
+    axes = [a for a, n in enumerate(sections) for _ in range(n)]
+    return (ctypes.c_double * pairs)(*freqs), (ctypes.c_int32 * pairs)(*axes)
+
+
+def attn_rotary(q, k, positions, sections, base: float = 10000.0, freqs=None,
+                interleaved: bool = False, inverse: bool = False, out_q=None, out_k=None,
+                out_dtype=None):
+    """q [T, Hq, d] and k [T, Hkv, d] rotated by their positions (int32 [T, axes], or
+    [T] for one): sections[a] pairs of every head turn with axis a, in this order; the
+    frequencies are base ** (-p / sum(sections)) for pair p, or freqs[p] (numbers).  A
+    pair is elements p and p + sum(sections), or with interleaved 2 p and 2 p + 1;
+    elements behind the pairs are copied.  inverse undoes it: the gradients of q and k
+    from those of the rotated.  q or k may be None.  bf16, or float32 (out_dtype or
+    out_q, out_k bf16 round to it); out_q may be q, out_k k."""
+    import torch
+    given = [(t, n) for t, n in ((q, "q"), (k, "k")) if t is not None]
+    if not given:
+        raise ValueError("attn_rotary needs q or k")
+    first = given[0][0]
+    if first.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"{given[0][1]} must be torch.bfloat16 or torch.float32, got {first.dtype}")
+    T, d = first.shape[0], first.shape[-1]
+    outs = [o for o in (out_q, out_k) if o is not None]
+    dtype = outs[0].dtype if outs else out_dtype or first.dtype
+    res = []
+    for (t, name), o in zip(((q, "q"), (k, "k")), (out_q, out_k)):
+        if t is None:
+            if o is not None:
+                raise ValueError(f"out_{name} without {name}")
+            res.append(None)
+            continue
+        _check_tensor(t, name, first.dtype, 3)
+        if t.shape[0] != T or t.shape[2] != d:
+            raise ValueError("q and k must have the same tokens and head dimension")
+        if o is None:
+            o = torch.empty(t.shape, dtype=dtype, device=t.device)
+        _check_tensor(o, f"out_{name}", dtype, 3)
+        if o.shape != t.shape:
+            raise ValueError(f"out_{name} must have {name}'s shape")
+        res.append(o)
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"outputs must be torch.bfloat16 or torch.float32, got {dtype}")
+    if positions.dim() == 1:
+        positions = positions[:, None]
+    _check_tensor(positions, "positions", torch.int32, 2)
+    sections = tuple(int(n) for n in sections)
+    if positions.shape != (T, len(sections)):
+        raise ValueError(f"positions must be [{T}, {len(sections)}] (tokens, sections), got "
+                         f"{list(positions.shape)}")
+    _same_device(first.device, q=q, k=k, positions=positions, out_q=res[0], out_k=res[1])
+    w, axes = _rotary_tables(sections, float(base),
+                             None if freqs is None else tuple(float(f) for f in freqs))
+    with _on_device(first.device):
+        st = lib().attn_rotary(_ptr(q), _ptr(k), positions.data_ptr(), T, len(sections),
+                               0 if q is None else q.shape[1], 0 if k is None else k.shape[1], d,
+                               len(w), w, axes, int(bool(interleaved)), int(bool(inverse)),
+                               int(first.dtype == torch.float32), int(dtype == torch.float32),
+                               _ptr(res[0]), _ptr(res[1]), _stream_handle(first.device))
+    _check(st, "attn_rotary")
+    return res[0], res[1]
