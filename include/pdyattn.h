@@ -263,9 +263,9 @@ pdy_status attn_prefix_bwd(const void* q, const void* k, const void* v, const vo
 
 /* ---- Rotary positions with several axes ----
  * Rotates the first 2 num_pairs elements of every head of q and k in pairs: pair p by
- * the angle positions[t][pair_axes[p]] * freqs[p] (radians; num_axes int32 positions
- * a token, e.g. time, height, width; negative ones too), and copies the rest.  A pair
- * is elements p and p + num_pairs, or with interleaved = 1 elements 2 p and 2 p + 1:
+ * the angle positions[t][pair_axes[p]] * w_p (num_axes int32 positions a token, e.g.
+ * time, height, width; negative ones too), and copies the rest.  A pair is elements p
+ * and p + num_pairs, or with interleaved = 1 elements 2 p and 2 p + 1:
  *   (x, y) -> (x cos - y sin, x sin + y cos).
  * inverse = 1 takes the negative angle: it undoes the rotation, and turns the
  * gradients of rotated q and k into those of q and k.
@@ -273,14 +273,17 @@ pdy_status attn_prefix_bwd(const void* q, const void* k, const void* v, const vo
  *   bf16, or fp32 with in_fp32 (out_fp32 = 1, or bf16 with 0); out may be in where the
  *   types are the same.  With a head count of 0 that tensor is NULL.
  *   positions: int32 device array [total_tokens, num_axes], num_axes 1 to 4.
- *   num_pairs: a multiple of 8 up to head_dim / 2.  freqs, pair_axes: HOST arrays of
- *   num_pairs, read during the call (a captured graph keeps their values).
- * Angles are exact for every int32 position (64-bit fractions of a turn); products
- * are 32 bits, rounded once to a bf16 output.  Needs no workspace. */
+ *   num_pairs: a multiple of 8 up to head_dim / 2.
+ *   turns, pair_axes: HOST arrays of num_pairs, read during the call (a captured graph
+ *   keeps their values); turns[p] = w_p / 2 pi as a 64-bit fraction of a turn, which
+ *   attn_rotary_turns computes from the frequencies w_p (radians a position, finite).
+ * Angles are exact for every int32 position; products are 32 bits, rounded once to a
+ * bf16 output.  Needs no workspace. */
+pdy_status attn_rotary_turns(const double* freqs, int32_t num_pairs, uint64_t* turns);
 pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
                        int32_t total_tokens, int32_t num_axes, int32_t num_heads_q,
                        int32_t num_heads_kv, int32_t head_dim, int32_t num_pairs,
-                       const double* freqs, const int32_t* pair_axes, int32_t interleaved,
+                       const uint64_t* turns, const int32_t* pair_axes, int32_t interleaved,
                        int32_t inverse, int32_t in_fp32, int32_t out_fp32, void* q_out,
                        void* k_out, void* stream);
 

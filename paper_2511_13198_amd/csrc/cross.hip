@@ -67,18 +67,35 @@ int64_t most_items(const CrossSizes& s, int64_t n, int64_t max_q, int rows) {
 // ---- tiles of rows: forward and dQ ----
 
 // Rows of a sequence decide the workgroups' shape: the smallest tile that holds
-// them; few rows leave the waves to key groups.
+// them; few rows leave the waves to key groups.  4-wave workgroups share a CU by two,
+// so that one's start, end and products overlap the other's copies; 8 waves over 256
+// rows read K and V least often.  us at 32 / 64 / 128 rows a sequence with tiles of
+// 32 (4 key groups), 64 (2), 128 and 256 rows, d = 128:
+//   17 x 1-5 tokens, 24/8 heads, 900-9,000 keys (15 rows) 64 with 32-row tiles and two
+//   workgroups a CU, 80 with one; 32 x 8 tokens, 32/4 heads, 256-8,192 keys (64 rows)
+//   52 / 52 / 58 with 64, 128, 256; 32 x 32, 32/8 heads (128 rows) 97 / 82 / 91;
+//   a step of 8 x 256-2,048 over 1,024-8,192 keys, forward 332 / 257 / 251.
 CrossShape row_shape(int64_t rows) {
   if (rows <= 32) return {4, 4};
-  if (rows <= 64) return {8, 4};
-  if (rows <= 128) return {8, 2};
+  if (rows <= 64) return {4, 2};
+  if (rows <= 128) return {4, 1};
   return {8, 1};
 }
 
-int fwd_key_tile(const CrossSizes& s, const CrossShape& sh) {
-  return sh.groups > 1 || s.d == 128 ? 128 : 64;
-}
-int dq_key_tile(const CrossSizes&, const CrossShape&) { return 128; }
+// What the forward and the dQ kernel differ in.
+struct RowKernel {
+  bool dq;
+  int key_tile(const CrossSizes& s, const CrossShape& sh) const {
+    if (dq) return sh.nw == 8 ? 128 : 64;
+    if (sh.nw == 4) return sh.groups == 4 ? 128 : 64;
+    return s.d == 128 ? 128 : 64;
+  }
+  CrossShape shape(int64_t rows) const {
+    const CrossShape sh = row_shape(rows);
+    return dq && sh.groups == 4 ? CrossShape{4, 2} : sh;
+  }
+};
+constexpr RowKernel kFwd{false}, kDq{true};
 
 // One launch over tiles of rows.
 struct CrossRows {
@@ -90,63 +107,51 @@ struct CrossRows {
 constexpr int kMaxParts = 64;
 constexpr int64_t kPartBytes = (int64_t)256 << 20;  // partial results at most
 
-template <class KeyTile>
-CrossRows rows_launch(const CrossSizes& s, pdy::CrossKeys keys, KeyTile key_tile) {
-  const bool shared = keys == pdy::CROSS_SHARED;
-  const int64_t n = shared ? 1 : s.n, max_q = shared ? s.tq : s.max_q;
+// Few rows a sequence behind many shared keys: these once for the rows of all
+// sequences, apart from the sequences' own keys, with partial results of both.  Fused,
+// every sequence's tile of 32 rows or more streams them; us apart / fused, d = 128:
+//   64 sequences of 1 token, 32/8 heads, behind 32,768 keys 97 / 662, 1,024 49 / 59,
+//   512 49 / 48, 64 48 / 42; 32 of 8 tokens (32 rows) behind 8,000 64 / 78, of 16 (64
+//   rows) 99 / 138, of 32 (128 rows, 40 sequences, a step) 853 / 858.
+constexpr int64_t kApartRows = 64, kApartPrefix = 512;
+
+CrossRows rows_launch(const CrossSizes& s, const RowKernel& k) {
   CrossRows f;
-  f.sh = row_shape(max_q * s.g());
   pdy::CrossCut& c = f.cut;
-  c.keys = keys;
-  c.rows = f.sh.rows();
-  c.key_tile = key_tile(s, f.sh);
+  const int64_t slice = s.tq * s.hq * (s.d + 1) * 4;  // bytes of one slice of partial results
+  c.keys = s.prefix == 0 ? pdy::CROSS_OWN
+           : s.seq_rows() > kApartRows || s.prefix <= kApartPrefix || 2 * slice > kPartBytes
+               ? pdy::CROSS_FUSED
+               : pdy::CROSS_APART;
+  const bool apart = c.keys == pdy::CROSS_APART;
+  f.sh = k.shape(s.seq_rows());
+  if (apart) f.sh = k.shape(std::min<int64_t>(128, s.tq * s.g()));
+  const int rows = f.sh.rows(), keys_tile = k.key_tile(s, f.sh);
+  c.rows_log2 = __builtin_ctz((unsigned)rows);
+  c.key_log2 = __builtin_ctz((unsigned)keys_tile);
   c.least = 2;
-  c.slice = 0;
-  c.always_part = 0;
-  const int64_t items = most_items(s, n, max_q, c.rows);
-  const int64_t target = 2 * kCUs;
-  c.per_head = (float)((double)target / s.hkv);
-  const int64_t tiles = (shared ? 0 : ceil_div(s.max_k, c.key_tile)) +
-                        (keys == pdy::CROSS_OWN ? 0 : ceil_div(s.prefix, c.key_tile));
-  const int64_t slice = s.tq * s.hq * (s.d + 1) * 4;
-  int64_t parts = std::min<int64_t>({kMaxParts, tiles / c.least, kPartBytes / slice});
-  if (items * s.hkv >= target) parts = 1;
+  const int64_t items =
+      most_items(s, s.n, s.max_q, rows) + (apart ? ceil_div(s.tq * s.g(), rows) : 0);
+  const bool few = f.sh.groups == 4;  // (partial results are small then)
+  const int64_t target = (few ? 4 : 2) * kCUs;
+  c.share = (float)((double)s.hkv / target);
+  const int64_t own = ceil_div(s.max_k, keys_tile), pre = ceil_div(s.prefix, keys_tile);
+  const int64_t tiles = apart ? std::max(own, pre) : own + pre;
+  int64_t parts =
+      std::min<int64_t>({kMaxParts, tiles / c.least, kPartBytes / (slice * (apart ? 2 : 1))});
+  if (!apart && items * s.hkv >= (few ? 16 : 2) * kCUs) parts = 1;
   c.max_parts = (int)std::max<int64_t>(1, parts);
   f.wgs = items + (c.max_parts > 1 ? ceil_div(target, s.hkv) + 2 : 0);
   return f;
 }
 
-// The launches over all rows: own keys, or shared and own keys in one, or one each.
-struct CrossRowsPlan {
-  int launches;
-  CrossRows l[2];
-  bool merge() const { return launches > 1 || l[0].cut.max_parts > 1; }
-  int slices() const {
-    return merge() ? l[0].cut.max_parts + (launches > 1 ? l[1].cut.max_parts : 0) : 0;
-  }
-};
-
-template <class KeyTile>
-CrossRowsPlan rows_plan(const CrossSizes& s, KeyTile key_tile) {
-  CrossRowsPlan p;
-  if (s.prefix == 0) {
-    p.launches = 1;
-    p.l[0] = rows_launch(s, pdy::CROSS_OWN, key_tile);
-  } else if (s.seq_rows() > 64) {
-    p.launches = 1;
-    p.l[0] = rows_launch(s, pdy::CROSS_FUSED, key_tile);
-  } else {
-    // few rows a sequence: the shared keys once for the rows of all of them
-    p.launches = 2;
-    p.l[0] = rows_launch(s, pdy::CROSS_SHARED, key_tile);
-    p.l[1] = rows_launch(s, pdy::CROSS_OWN, key_tile);
-    p.l[0].cut.always_part = p.l[1].cut.always_part = 1;
-    p.l[1].cut.slice = p.l[0].cut.max_parts;
-  }
-  return p;
+// Partial results that a launch writes at most (0: none).
+int slices_of(const CrossRows& f) {
+  return f.cut.keys == pdy::CROSS_APART ? 2 * f.cut.max_parts
+                                        : f.cut.max_parts > 1 ? f.cut.max_parts : 0;
 }
 
-size_t part_n_bytes(const CrossSizes& s) { return align256((size_t)s.tq * 4); }
+size_t part_n_bytes(const CrossSizes& s) { return align256((size_t)s.tq * 2 * 4); }
 size_t part_o_bytes(const CrossSizes& s, int slices) {
   return align256((size_t)slices * s.tq * s.hq * s.d * 4);
 }
@@ -154,9 +159,9 @@ size_t part_lse_bytes(const CrossSizes& s, int slices) {
   return align256((size_t)slices * s.tq * s.hq * 4);
 }
 
-size_t fwd_bytes(const CrossSizes& s, const CrossRowsPlan& p) {
-  if (!p.merge()) return 256;
-  return 2 * part_n_bytes(s) + part_o_bytes(s, p.slices()) + part_lse_bytes(s, p.slices());
+size_t fwd_bytes(const CrossSizes& s, const CrossRows& f) {
+  const int n = slices_of(f);
+  return n == 0 ? 256 : part_n_bytes(s) + part_o_bytes(s, n) + part_lse_bytes(s, n);
 }
 
 // ---- tiles of keys: dK, dV ----
@@ -177,15 +182,19 @@ CrossKv kv_launch(const CrossSizes& s) {
   auto items = [&](int tile) {
     return std::min(s.tk / tile + s.n, s.n * ceil_div(s.max_k, tile)) + ceil_div(s.prefix, tile);
   };
-  k.sh = {8, items(256) * s.hkv >= kCUs ? 1 : 2};
+  // Few rows a sequence, so few steps a tile: two 4-wave workgroups a CU; else 256-key
+  // tiles where they fill the chip four times over, two query groups over 128 where not
+  // (16 sequences of 64-1,024 rows behind 4,096 keys, 32/8 heads: 564 + 29 us of sums
+  // with 256-key tiles, 546 + 19 with groups; 32 x 8-200 rows over 577-1,024 keys, 16
+  // heads of 64: 63 us, 110 with groups, 60 with 4 waves).
+  if (s.tq * s.g() <= 512 * s.n && items(128) * s.hkv >= 2 * kCUs) k.sh = {4, 1};
+  else k.sh = {8, items(256) * s.hkv >= 4 * kCUs ? 1 : 2};
   pdy::CrossCut& c = k.cut;
   c.keys = pdy::CROSS_FUSED;
-  c.rows = c.key_tile = k.sh.rows();
+  c.rows_log2 = c.key_log2 = __builtin_ctz((unsigned)k.sh.rows());
   c.least = 4;
-  c.slice = 0;
-  c.always_part = 0;
-  const int64_t n = items(c.rows), target = 2 * kCUs;
-  c.per_head = (float)((double)target / s.hkv);
+  const int64_t n = items(k.sh.rows()), target = 2 * kCUs;
+  c.share = (float)((double)s.hkv / target);
   const int64_t slice = (s.prefix + s.tk) * s.hkv * s.d * 8;
   int64_t parts = std::min<int64_t>(16, slice ? kPartBytes / slice : 1);
   // items alike in their rows need no cut once they fill the chip; a shared tile has
@@ -200,12 +209,12 @@ CrossKv kv_launch(const CrossSizes& s) {
 struct CrossBwdSpace {
   size_t dd, counts_q, counts_k, part_q, part_kv, total;
 };
-CrossBwdSpace bwd_space(const CrossSizes& s, const CrossRowsPlan& q, const CrossKv& kv) {
+CrossBwdSpace bwd_space(const CrossSizes& s, const CrossRows& q, const CrossKv& kv) {
   CrossBwdSpace x;
   x.dd = align256((size_t)s.hq * s.tq * 4);
-  x.counts_q = q.merge() ? 2 * part_n_bytes(s) : 0;
+  x.counts_q = slices_of(q) ? part_n_bytes(s) : 0;
   x.counts_k = kv.cut.max_parts > 1 ? align256((size_t)(s.prefix + s.tk) * 4) : 0;
-  x.part_q = part_o_bytes(s, q.slices());
+  x.part_q = part_o_bytes(s, slices_of(q));
   x.part_kv = kv.cut.max_parts > 1 ? align256((size_t)kv.cut.max_parts * (s.prefix + s.tk) *
                                               s.hkv * s.d * 4)
                                    : 0;
@@ -243,17 +252,22 @@ struct CrossKernels {
   hipError_t (*dkdv[2])(const pdy::CrossBwdArgs*, dim3, hipStream_t);
 };
 template <int NW, int G>
-constexpr CrossKernels cross_kernels_of() {
-  CrossKernels k{NW, G, {launch_fwd<64, NW, G>, launch_fwd<128, NW, G>},
-                 {launch_dq<64, NW, G>, launch_dq<128, NW, G>}, {nullptr, nullptr}};
-  if constexpr (G <= 2) {
-    k.dkdv[0] = launch_dkdv<64, NW, G>;
-    k.dkdv[1] = launch_dkdv<128, NW, G>;
-  }
+constexpr CrossKernels row_kernels() {
+  return {NW, G, {launch_fwd<64, NW, G>, launch_fwd<128, NW, G>},
+          {launch_dq<64, NW, G>, launch_dq<128, NW, G>}, {nullptr, nullptr}};
+}
+template <int NW, int G>
+constexpr CrossKernels with_dkdv(CrossKernels k) {
+  k.nw = NW;
+  k.groups = G;
+  k.dkdv[0] = launch_dkdv<64, NW, G>;
+  k.dkdv[1] = launch_dkdv<128, NW, G>;
   return k;
 }
-constexpr CrossKernels kCrossKernels[] = {cross_kernels_of<8, 1>(), cross_kernels_of<8, 2>(),
-                                          cross_kernels_of<8, 4>(), cross_kernels_of<4, 4>()};
+constexpr CrossKernels kCrossKernels[] = {
+    with_dkdv<8, 1>(row_kernels<8, 1>()), with_dkdv<4, 1>(row_kernels<4, 1>()),
+    row_kernels<4, 2>(), with_dkdv<8, 2>(CrossKernels{}),
+    CrossKernels{4, 4, {launch_fwd<64, 4, 4>, launch_fwd<128, 4, 4>}, {}, {}}};
 const CrossKernels& cross_kernels(const CrossShape& sh) {
   for (const CrossKernels& k : kCrossKernels)
     if (k.nw == sh.nw && k.groups == sh.groups) return k;
@@ -264,8 +278,9 @@ hipError_t init_cross_kernels() {
   static hipError_t status = [] {
     for (const CrossKernels& k : kCrossKernels)
       for (int d = 0; d < 2; ++d) {
-        hipError_t e = k.fwd[d](nullptr, dim3(), nullptr);
-        if (e == hipSuccess) e = k.dq[d](nullptr, dim3(), nullptr);
+        hipError_t e = hipSuccess;
+        if (k.fwd[d]) e = k.fwd[d](nullptr, dim3(), nullptr);
+        if (e == hipSuccess && k.dq[d]) e = k.dq[d](nullptr, dim3(), nullptr);
         if (e == hipSuccess && k.dkdv[d]) e = k.dkdv[d](nullptr, dim3(), nullptr);
         if (e != hipSuccess) return e;
       }
@@ -301,7 +316,8 @@ pdy_status check_cross_in(const CrossIn& x, const CrossSizes& s) {
 
 pdy::CrossBatch batch_of(const CrossIn& x, const CrossSizes& s, int32_t causal) {
   return pdy::CrossBatch{x.cu_q, x.cu_k, x.len_k, (int)s.n, (int)s.tq, (int)s.tk, (int)s.prefix,
-                         (int)s.hq, (int)s.hkv, causal};
+                         (int)s.hq, (int)s.hkv, (int)s.g(), (uint32_t)((1ull << 32) / s.g()),
+                         causal};
 }
 
 pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal, float scale,
@@ -313,8 +329,8 @@ pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal,
   if ((st = check_cross_in(x, s)) || (st = check_ptr(o, "o")) || (st = check_ptr(lse, "lse")) ||
       (st = check_ptr(workspace, "workspace")))
     return st;
-  const CrossRowsPlan p = rows_plan(s, fwd_key_tile);
-  const size_t need = fwd_bytes(s, p);
+  const CrossRows f = rows_launch(s, kFwd);
+  const size_t need = fwd_bytes(s, f);
   if (workspace_bytes < need)
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, %s needs %zu", workspace_bytes, who,
                 need);
@@ -322,6 +338,8 @@ pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal,
   if (e != hipSuccess) return hip_fail(e, "kernel attribute setup");
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
 
+  const int slices = slices_of(f);
+  uint8_t* const w = reinterpret_cast<uint8_t*>(workspace);
   pdy::CrossFwdArgs a;
   a.q = static_cast<const uint16_t*>(x.q);
   a.k = static_cast<const uint16_t*>(x.k);
@@ -331,45 +349,25 @@ pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal,
   a.o = static_cast<uint16_t*>(o);
   a.lse = lse;
   a.b = batch_of(x, s, causal);
+  a.cut = f.cut;
   a.scale_log2 = scale * pdy::kLog2e;
-  a.part_o = a.part_lse = nullptr;
-  a.part_n = nullptr;
-  int32_t* counts = reinterpret_cast<int32_t*>(workspace);
-  if (p.merge()) {
-    uint8_t* w = reinterpret_cast<uint8_t*>(workspace) + 2 * part_n_bytes(s);
-    a.part_o = reinterpret_cast<float*>(w);
-    a.part_lse = reinterpret_cast<float*>(w + part_o_bytes(s, p.slices()));
-  }
-  for (int i = 0; i < p.launches; ++i) {
-    const CrossRows& f = p.l[i];
-    a.cut = f.cut;
-    if (p.merge()) a.part_n = counts + i * (part_n_bytes(s) / 4);
-    const dim3 grid((unsigned)(f.wgs * s.hkv));
-    e = launch_timed(K_CROSS_FWD, hs,
-                     [&] { (void)cross_kernels(f.sh).fwd[s.d == 128](&a, grid, hs); });
-    if (e != hipSuccess) return hip_fail(e, "cross_fwd_kernel launch");
-  }
-  if (p.merge()) {
-    pdy::CrossMergeArgs m;
-    m.part_o = a.part_o;
-    m.part_lse = a.part_lse;
-    m.part_n = counts;
-    m.part_n1 = p.launches > 1 ? counts + part_n_bytes(s) / 4 : nullptr;
-    m.max0 = p.l[0].cut.max_parts;
-    m.max1 = p.launches > 1 ? p.l[1].cut.max_parts : 0;
-    m.cu_q = x.cu_q;
-    m.n = (int)s.n;
-    m.tq = (int)s.tq;
-    m.hq = (int)s.hq;
-    m.o = a.o;
-    m.lse = lse;
-    const dim3 blocks((unsigned)ceil_div(s.tq * s.hq * (s.d / 8), 256));
-    e = launch_timed(K_CROSS_MERGE, hs, [&] {
-      if (s.d == 64) hipLaunchKernelGGL(pdy::cross_merge_kernel<64>, blocks, dim3(256), 0, hs, m);
-      else hipLaunchKernelGGL(pdy::cross_merge_kernel<128>, blocks, dim3(256), 0, hs, m);
-    });
-    if (e != hipSuccess) return hip_fail(e, "cross_merge_kernel launch");
-  }
+  a.part_n = slices ? reinterpret_cast<int32_t*>(w) : nullptr;
+  a.part_o = reinterpret_cast<float*>(w + part_n_bytes(s));
+  a.part_lse = reinterpret_cast<float*>(w + part_n_bytes(s) + part_o_bytes(s, slices));
+  const dim3 grid((unsigned)(f.wgs * s.hkv));
+  e = launch_timed(K_CROSS_FWD, hs,
+                   [&] { (void)cross_kernels(f.sh).fwd[s.d == 128](&a, grid, hs); });
+  if (e != hipSuccess) return hip_fail(e, "cross_fwd_kernel launch");
+  if (slices == 0) return PDY_OK;
+  const pdy::CrossMergeArgs m{a.part_o, a.part_lse, a.part_n, f.cut.max_parts,
+                              f.cut.keys == pdy::CROSS_APART, x.cu_q, (int)s.n, (int)s.tq,
+                              (int)s.hq, a.o, lse};
+  const dim3 blocks((unsigned)ceil_div(s.tq * s.hq, 4));
+  e = launch_timed(K_CROSS_MERGE, hs, [&] {
+    if (s.d == 64) hipLaunchKernelGGL(pdy::cross_merge_kernel<64>, blocks, dim3(256), 0, hs, m);
+    else hipLaunchKernelGGL(pdy::cross_merge_kernel<128>, blocks, dim3(256), 0, hs, m);
+  });
+  if (e != hipSuccess) return hip_fail(e, "cross_merge_kernel launch");
   return PDY_OK;
 }
 
@@ -395,9 +393,9 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
       ((st = check_ptr(g.dkp, "dk_prefix")) || (st = check_ptr(g.dvp, "dv_prefix"))))
     return st;
   if ((st = check_ptr(workspace, "workspace")) != PDY_OK) return st;
-  const CrossRowsPlan p = rows_plan(s, dq_key_tile);
+  const CrossRows f = rows_launch(s, kDq);
   const CrossKv kv = kv_launch(s);
-  const CrossBwdSpace sp = bwd_space(s, p, kv);
+  const CrossBwdSpace sp = bwd_space(s, f, kv);
   if (workspace_bytes < sp.total)
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, %s needs %zu", workspace_bytes, who,
                 sp.total);
@@ -440,13 +438,11 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
   a.pack_log2 = pack_log2(s);
 
   // dQ first: it also writes D, which dK/dV reads
-  for (int i = 0; s.tq > 0 && i < p.launches; ++i) {
-    const CrossRows& f = p.l[i];
+  if (s.tq > 0) {
     a.cut = f.cut;
     a.part = part_q;
     a.part2 = nullptr;
-    a.part_n = p.merge() ? counts_q + i * (part_n_bytes(s) / 4) : nullptr;
-    a.dd = i == 0 ? dd : nullptr;
+    a.part_n = slices_of(f) ? counts_q : nullptr;
     const dim3 grid((unsigned)(f.wgs * s.hkv));
     e = launch_timed(K_CROSS_DQ, hs,
                      [&] { (void)cross_kernels(f.sh).dq[s.d == 128](&a, grid, hs); });
@@ -457,7 +453,6 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
     a.part = part_k;
     a.part2 = part_v;
     a.part_n = kv.cut.max_parts > 1 ? counts_k : nullptr;
-    a.dd = dd;
     const dim3 grid((unsigned)(kv.wgs * s.hkv));
     e = launch_timed(K_CROSS_DKDV, hs,
                      [&] { (void)cross_kernels(kv.sh).dkdv[s.d == 128](&a, grid, hs); });
@@ -468,26 +463,26 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
   sum.njobs = 0;
   sum.out_bf16 = grad_bf16;
   int64_t blocks = 0;
-  auto add = [&](const float* part, const int32_t* n0, const int32_t* n1, int max0, int max1,
-                 int64_t rows, int64_t first, int64_t count, int64_t heads, const int32_t* end,
+  auto add = [&](const float* part, const int32_t* n, const int32_t* n1, int max_parts,
+                 int64_t heads, int64_t rows, int64_t first, int64_t count, const int32_t* end,
                  void* dst) {
     if (count == 0) return;
     const int b = (int)ceil_div(count * (s.d / 8), 256);
-    sum.job[sum.njobs++] =
-        pdy::CrossSumJob{part, n0, n1, max0, max1, rows, first, count, (int)heads, end, dst, b};
+    sum.job[sum.njobs++] = pdy::CrossSumJob{part, n, n1, max_parts, (int)heads, rows, first, count,
+                                            end, dst, b};
     blocks += b;
   };
-  if (s.tq > 0 && p.merge())
-    add(part_q, counts_q, p.launches > 1 ? counts_q + part_n_bytes(s) / 4 : nullptr,
-        p.l[0].cut.max_parts, p.launches > 1 ? p.l[1].cut.max_parts : 0, s.tq * s.hq, 0,
-        s.tq * s.hq, s.hq, x.cu_q + s.n, g.dq);
+  if (s.tq > 0 && slices_of(f) > 0)
+    add(part_q, counts_q, f.cut.keys == pdy::CROSS_APART ? counts_q + s.tq : nullptr,
+        f.cut.max_parts, s.hq, s.tq * s.hq, 0, s.tq * s.hq, x.cu_q + s.n, g.dq);
   if (kv.cut.max_parts > 1) {
     const int64_t rows = (s.prefix + s.tk) * s.hkv, pre = s.prefix * s.hkv;
     for (int i = 0; i < 2; ++i) {
-      add(i ? part_v : part_k, counts_k, nullptr, kv.cut.max_parts, 0, rows, 0, pre, s.hkv, nullptr,
+      const float* part = i ? part_v : part_k;
+      add(part, counts_k, nullptr, kv.cut.max_parts, s.hkv, rows, 0, pre, nullptr,
           i ? g.dvp : g.dkp);
-      add(i ? part_v : part_k, counts_k, nullptr, kv.cut.max_parts, 0, rows, pre, s.tk * s.hkv,
-          s.hkv, x.cu_k + s.n, i ? g.dv : g.dk);
+      add(part, counts_k, nullptr, kv.cut.max_parts, s.hkv, rows, pre, s.tk * s.hkv, x.cu_k + s.n,
+          i ? g.dv : g.dk);
     }
   }
   if (sum.njobs > 0) {
@@ -512,7 +507,7 @@ size_t attn_prefix_fwd_workspace_size(int32_t prefix_len, int32_t total_q, int32
   if (check_cross_sizes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k,
                         num_heads_q, num_heads_kv, head_dim, &s) != PDY_OK)
     return 0;
-  return s.tq == 0 ? 256 : fwd_bytes(s, rows_plan(s, fwd_key_tile));
+  return s.tq == 0 ? 256 : fwd_bytes(s, rows_launch(s, kFwd));
 }
 
 size_t attn_cross_fwd_workspace_size(int32_t total_q, int32_t total_k, int32_t num_seqs,
@@ -563,7 +558,7 @@ size_t attn_prefix_bwd_workspace_size(int32_t prefix_len, int32_t total_q, int32
   if (check_cross_sizes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k,
                         num_heads_q, num_heads_kv, head_dim, &s) != PDY_OK)
     return 0;
-  return bwd_space(s, rows_plan(s, dq_key_tile), kv_launch(s)).total;
+  return bwd_space(s, rows_launch(s, kDq), kv_launch(s)).total;
 }
 
 size_t attn_cross_bwd_workspace_size(int32_t total_q, int32_t total_k, int32_t num_seqs,

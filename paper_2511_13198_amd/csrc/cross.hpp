@@ -29,6 +29,8 @@ struct CrossBatch {
   int tk;      // rows of k, v
   int prefix;  // shared keys
   int hq, hkv;
+  int g;           // hq / hkv
+  uint32_t g_inv;  // 2^32 / g, rounded down (g > 1)
   int causal;
 };
 
@@ -53,9 +55,11 @@ __device__ __forceinline__ CrossSeq cross_shared_seq(const CrossBatch& b) {
 
 // Which rows and keys a launch covers.
 enum CrossKeys : int {
-  CROSS_OWN = 0,     // a sequence's rows over its own keys
-  CROSS_FUSED = 1,   // over the shared keys, then its own
-  CROSS_SHARED = 2,  // all rows of the batch, as one sequence, over the shared keys
+  CROSS_OWN = 0,    // a sequence's rows over its own keys
+  CROSS_FUSED = 1,  // over the shared keys, then its own
+  CROSS_APART = 2,  // all rows of the batch, as one sequence, over the shared keys, and
+                    // beside it every sequence's rows over its own: partial results of
+                    // both, for few rows a sequence
 };
 
 // How a launch's rows and keys are cut.  An item is a tile of `rows` packed rows of
@@ -68,14 +72,12 @@ enum CrossKeys : int {
 //   a launch with that many items is not cut (C is then above their inner tiles).
 // Every workgroup computes C from the offsets, so that nothing waits for the host.
 struct CrossCut {
-  int keys;         // CrossKeys
-  int rows;         // packed rows per tile
-  int key_tile;     // keys per tile
-  int max_parts;    // 1: not cut
-  int least;        // fewest inner tiles of a part
-  float per_head;   // parts wanted per kv head (target / hkv)
-  int slice;        // first slice of the partial results
-  int always_part;  // partial results also of items in one part
+  int keys;       // CrossKeys
+  int rows_log2;  // packed rows per tile
+  int key_log2;   // keys per tile
+  int max_parts;  // of an item; 1: not cut
+  int least;      // fewest inner tiles of a part
+  float share;    // hkv / target
 };
 
 struct CrossPlace {
@@ -86,45 +88,70 @@ struct CrossPlace {
 };
 
 __device__ __forceinline__ int cross_tiles(int x, int tile) { return (x + tile - 1) / tile; }
+__device__ __forceinline__ int cross_tiles_log2(int x, int log2) {
+  return (x + (1 << log2) - 1) >> log2;
+}
+
+// Inclusive sum over the lanes up to this one, and over all (the last lane's): sums
+// within rows of 16 lanes, then of the rows before.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // 1 lane up in a row
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);  // 2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);  // 4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);  // 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // last lane of rows 0, 2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31
+  return x;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  auto add = [&](auto Ctrl, auto Rows) __attribute__((always_inline)) {
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(Ctrl)::value,
+                                                    decltype(Rows)::value, 0xf, false));
+  };
+  using std::integral_constant;
+  add(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});
+  add(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  add(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  add(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  add(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});
+  add(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
 
 // Sequence, tile and part of entry `entry` of a kv head's list; false past its end.
 // of(i, tiles, units): the i-th of the list's n sequences, its tiles and the units of
 // inner work of each.  One pass over the sequences, 64 at a time (two where the
-// launch is cut); the results are wave-uniform.
+// launch is cut and they are more); the results are wave-uniform.
 template <class F>
 __device__ __forceinline__ bool cross_place(int n, const CrossCut& c, int entry, F&& of,
                                             CrossPlace& out) {
   const int l = __lane_id();
-  auto lane = [&](int i, int& tiles, int& units) __attribute__((always_inline)) {
-    CrossSeq s = {0, 0, 0, 0, 0};
-    tiles = units = 0;
-    if (i < n) s = of(i, tiles, units);
-    return s;
+  CrossSeq s;
+  int t, u;
+  auto load = [&](int i) __attribute__((always_inline)) {
+    s = CrossSeq{0, 0, 0, 0, 0};
+    t = u = 0;
+    if (i < n) s = of(i, t, u);
   };
+  load(l);
   int cap = 1 << 30;
   if (c.max_parts > 1) {
-    float units = 0.f;
-    for (int i0 = 0; i0 < n; i0 += 64) {
-      int t, u;
-      lane(i0 + l, t, u);
+    float units = (float)t * (float)u;
+    for (int i0 = 64; i0 < n; i0 += 64) {
+      load(i0 + l);
       units += (float)t * (float)u;
     }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) units += __shfl_xor(units, off);
-    cap = max(c.least, (int)fminf(units / c.per_head + 1.f, 1e9f));
+    units = wave_sum(units);
+    cap = max(c.least, (int)fminf(units * c.share + 1.f, 1e9f));
+    if (n > 64) load(l);
   }
+  // ceil(u / cap) as a float product: exact enough, as any whole number near it does
+  const float inv = 1.f / (float)cap;
   int base = 0;
-  for (int i0 = 0; i0 < n; i0 += 64) {
-    int t, u;
-    const CrossSeq s = lane(i0 + l, t, u);
-    const int parts = max(1, min(c.max_parts, cross_tiles(u, cap)));
+  for (int i0 = 0;;) {
+    const int parts = max(1, min(c.max_parts, (int)ceilf((float)u * inv)));
     const int mine = t * parts;
-    int incl = mine;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int x = __shfl_up(incl, off);
-      if (l >= off) incl += x;
-    }
+    const int incl = wave_scan(mine);
     const int rel = entry - base;
     const uint64_t hit = __builtin_amdgcn_ballot_w64(rel >= incl - mine && rel < incl);
     if (hit) {
@@ -136,29 +163,39 @@ __device__ __forceinline__ bool cross_place(int n, const CrossCut& c, int entry,
       out.index = i0 + src;
       out.nparts = get(parts);
       const int at = rel - get(incl - mine);
-      out.tile = __builtin_amdgcn_readfirstlane(at / out.nparts);
-      out.part = __builtin_amdgcn_readfirstlane(at % out.nparts);
+      out.tile = out.nparts == 1 ? at : at / out.nparts;
+      out.part = at - out.tile * out.nparts;
       return true;
     }
     base += __builtin_amdgcn_readlane(incl, 63);
+    i0 += 64;
+    if (i0 >= n) return false;
+    load(i0 + l);
   }
-  return false;
 }
 
-// The same for tiles of packed rows (forward, dQ).
+// The same for tiles of packed rows (forward, dQ); CROSS_APART: the shared keys come
+// first in the list.
 __device__ __forceinline__ bool cross_place_rows(const CrossBatch& b, const CrossCut& c, int entry,
                                                  CrossPlace& out) {
-  const bool shared = c.keys == CROSS_SHARED;
+  const int apart = c.keys == CROSS_APART;
   return cross_place(
-      shared ? 1 : b.n, c, entry,
+      b.n + apart, c, entry,
       [&](int i, int& tiles, int& units) __attribute__((always_inline)) {
-        const CrossSeq s = shared ? cross_shared_seq(b) : cross_seq(b, i);
-        tiles = cross_tiles(s.nq * (b.hq / b.hkv), c.rows);
-        units = cross_tiles(s.nk, c.key_tile) +
-                (c.keys == CROSS_FUSED ? cross_tiles(b.prefix, c.key_tile) : 0);
+        const CrossSeq s = i < apart ? cross_shared_seq(b) : cross_seq(b, i - apart);
+        tiles = cross_tiles_log2(s.nq * b.g, c.rows_log2);
+        units = cross_tiles_log2(s.nk, c.key_log2) +
+                (c.keys == CROSS_FUSED ? cross_tiles_log2(b.prefix, c.key_log2) : 0);
         return s;
       },
       out);
+}
+
+// Token of packed row r (r >= 0): r / g by the reciprocal, off by at most one.
+__device__ __forceinline__ int cross_token(const CrossBatch& b, int r) {
+  if (b.g == 1) return r;  // uniform
+  const int t = (int)__umulhi((uint32_t)r, b.g_inv);
+  return r - t * b.g >= b.g ? t + 1 : t;
 }
 
 // ---------------------------------------------------------------------------

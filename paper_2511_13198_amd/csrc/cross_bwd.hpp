@@ -31,7 +31,7 @@ struct CrossBwdArgs {
   const uint16_t* o;
   const uint16_t* dout;
   const float* lse;  // [hq][tq]
-  float* dd;         // D, [hq][tq]: written by the dQ kernel (NULL: another launch does)
+  float* dd;         // D, [hq][tq]: written by the dQ kernel
   void* dq;          // float, or bf16 with out_bf16
   void* dk;
   void* dv;
@@ -45,7 +45,7 @@ struct CrossBwdArgs {
   int pack_log2;
   // partial gradients (fp32, scaled): part [slice][rows][D] -- rows are tq * hq pairs
   // for dQ, (prefix + tk) * hkv for dK (part) and dV (part2), the shared keys first --
-  // and how many slices from cut.slice on a token (key) has at part_n
+  // and how many slices a token (key) has at part_n; dQ with CROSS_APART as the forward
   float* part;
   float* part2;
   int32_t* part_n;
@@ -55,7 +55,8 @@ template <int D, int NW, int KG = 1>
 struct CrossDqCfg {
   static constexpr int RG = NW / KG;
   static constexpr int BQ = 32 * RG;
-  static constexpr int BK = 128;
+  // 4-wave workgroups keep 64 so that two of them fit a CU's LDS
+  static constexpr int BK = NW == 8 ? 128 : 64;
   static constexpr int WK = BK / KG;
   static constexpr int NT = NW * 64;
   using KL = DualLayout<D>;  // K is read as rows (S^T) and transposed (dQ^T)
@@ -71,7 +72,7 @@ struct CrossDqCfg {
 };
 
 template <int D, int NW, int KG>
-__global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : 1)
+__global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : NW == 4 ? 2 : 1)
     cross_dq_kernel(CrossBwdArgs a) {
   using C = CrossDqCfg<D, NW, KG>;
   using KL = typename C::KL;
@@ -83,7 +84,7 @@ __global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : 1
   xcd_order(blockIdx.x, gridDim.x, a.b.hkv, hk, entry);
   CrossPlace at;
   if (!cross_place_rows(a.b, a.cut, entry, at)) return;
-  const int g = a.b.hq / a.b.hkv;
+  const int g = a.b.g;
   const CrossSeq sq = at.s;
   const int row_end = (sq.q_lo + sq.nq) * g;
   const int row0 = sq.q_lo * g + at.tile * BQ;
@@ -98,7 +99,7 @@ __global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : 1
   const int wk0 = kg * C::WK;
   const int late = sq.nk - sq.nq - sq.q_lo + 1;  // as in the forward
   auto key_end = [&](int r) __attribute__((always_inline)) {
-    return a.b.causal ? min(sq.nk, min(r, row_end - 1) / g + late) : sq.nk;
+    return a.b.causal ? min(sq.nk, cross_token(a.b, max(min(r, row_end - 1), 0)) + late) : sq.nk;
   };
   const int lane_end = key_end(row);
   const int wave_first = __builtin_amdgcn_readfirstlane(key_end(wrow0));
@@ -106,12 +107,15 @@ __global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : 1
   const int wg_end = __builtin_amdgcn_readfirstlane(max(0, key_end(row0 + BQ - 1)));
   const size_t kvstride = (size_t)a.b.hkv * D;
   auto row_off = [&](int r) __attribute__((always_inline)) {
-    const int tok = r / g;
+    const int tok = cross_token(a.b, r);
     return ((size_t)tok * a.b.hq + hk * g + (r - tok * g)) * D;
   };
 
-  const int npre = a.cut.keys == CROSS_OWN ? 0 : cross_tiles(a.b.prefix, BK);
-  const int nown = a.cut.keys == CROSS_SHARED ? 0 : cross_tiles(wg_end, BK);
+  const bool apart = a.cut.keys == CROSS_APART;
+  const bool shared = apart && at.index == 0;  // this workgroup: shared keys alone
+  const bool second = apart && !shared;
+  const int npre = shared || a.cut.keys == CROSS_FUSED ? cross_tiles(a.b.prefix, BK) : 0;
+  const int nown = shared ? 0 : cross_tiles(wg_end, BK);
   const int ntiles = npre + nown;
   const int t_begin = (int)((int64_t)at.part * ntiles / at.nparts);
   const int t_end = (int)((int64_t)(at.part + 1) * ntiles / at.nparts);
@@ -168,7 +172,7 @@ __global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : 1
     for (int ks = 0; ks < D / 16; ++ks) of[ks] = load_bf16x8(a.o + roff + ks * 16, ok);
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) qf[ks] = load_bf16x8(a.q + roff + ks * 16, ok);
-    const int tok = r / g;
+    const int tok = cross_token(a.b, r);
     const size_t li = (size_t)(hk * g + (r - tok * g)) * a.b.tq + tok;
     if (ok) lse2 = a.lse[li];
     float dsum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -184,8 +188,9 @@ __global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : 1
       // a row without any visible key has LSE = -inf and no gradient
       if (lse2 == -INFINITY) lse2 = INFINITY;
       if (hh == 0 && at.part == 0 && kg == 0) {
-        if (a.dd) a.dd[li] = ddv;
-        if (a.part_n && hk == 0 && r == tok * g) a.part_n[tok] = at.nparts;
+        if (!second) a.dd[li] = ddv;
+        if (a.part_n && hk == 0 && r == tok * g)
+          a.part_n[(second ? a.b.tq : 0) + tok] = at.nparts;
       }
     }
   }
@@ -292,8 +297,9 @@ __global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : 1
   if (wrow0 >= row_end) return;
   __syncthreads();
 
-  const bool partial = a.cut.always_part || at.nparts > 1;
-  const size_t slice = (size_t)(a.cut.slice + at.part) * a.b.tq * a.b.hq * D;
+  const bool partial = apart || at.nparts > 1;
+  const size_t slice =
+      (size_t)(second ? a.cut.max_parts + at.part : at.part) * a.b.tq * a.b.hq * D;
   if constexpr (KG > 1) {
     float* slots = reinterpret_cast<float*>(smem) + rg * KG * (D / 32) * kF32Block;
     const int lane_off = acc_slot_lane();
@@ -381,7 +387,7 @@ __global__ void __launch_bounds__(NWAVES * 64, NWAVES == 4 ? 2 : D == 64 ? 3 : 1
 
   int hk, entry;
   xcd_order(blockIdx.x, gridDim.x, a.b.hkv, hk, entry);
-  const int g = a.b.hq / a.b.hkv;
+  const int g = a.b.g;
   const int sh = a.pack_log2, sweeps = g >> sh;  // head groups of `pack` heads
   // the list: the shared keys over the whole batch (if any), then the sequences
   const int first_own = a.b.prefix > 0 ? 1 : 0;
@@ -391,7 +397,7 @@ __global__ void __launch_bounds__(NWAVES * 64, NWAVES == 4 ? 2 : D == 64 ? 3 : 1
           [&](int i, int& tiles, int& units) __attribute__((always_inline)) {
             const CrossSeq s =
                 i < first_own ? cross_shared_seq(a.b) : cross_seq(a.b, i - first_own);
-            tiles = cross_tiles(s.room, BK);
+            tiles = cross_tiles_log2(s.room, a.cut.key_log2);
             units = s.nk > 0 ? cross_tiles(s.nq << sh, BQ) * sweeps : 0;
             return s;
           },
@@ -647,7 +653,7 @@ __global__ void __launch_bounds__(NWAVES * 64, NWAVES == 4 ? 2 : D == 64 ? 3 : 1
   const bool partial = at.nparts > 1;
   const int nrows = sq.room - kw0;
   const size_t off = (size_t)(sq.k_lo + kw0) * kvstride + (size_t)hk * D;
-  const size_t poff = ((size_t)(a.cut.slice + at.part) * (a.b.prefix + a.b.tk) +
+  const size_t poff = ((size_t)at.part * (a.b.prefix + a.b.tk) +
                        (shared ? 0 : a.b.prefix)) * kvstride + off;
   void* const dkout = shared ? a.dkp : a.dk;
   void* const dvout = shared ? a.dvp : a.dv;
@@ -689,21 +695,20 @@ __global__ void __launch_bounds__(NWAVES * 64, NWAVES == 4 ? 2 : D == 64 ? 3 : 1
   }
 }
 
-// Sums of partial gradients: row i of `rows` (a head's D floats; heads of them to a
-// token or key) has n0[token] slices from 0 on, and n1[token] from max0 on where the
-// shared and the own keys were two launches.  Rows with one slice and no second job
-// are written already.
+// Sums of partial gradients: row i (a head's D floats; `heads` of them to a token or
+// key) has n[token] slices from 0 on, and n1[token] from max_parts on where the shared
+// and the own keys were apart.  Rows with one slice are written already.
 struct CrossSumJob {
   const float* part;
-  const int32_t* n0;
-  const int32_t* n1;  // or NULL
-  int max0, max1;
-  int64_t rows;       // rows of a slice
-  int64_t first;      // first row to sum, and how many
-  int64_t count;
+  const int32_t* n;
+  const int32_t* n1;   // or NULL
+  int max_parts;
   int heads;
-  const int32_t* end; // tokens (keys) from *end on stay as they are; or NULL
-  void* dst;          // row `first`
+  int64_t rows;        // rows of a slice
+  int64_t first;       // first row to sum, and how many
+  int64_t count;
+  const int32_t* end;  // tokens (keys) from *end on stay as they are; or NULL
+  void* dst;           // row `first`
   int blocks;
 };
 struct CrossSumArgs {
@@ -725,8 +730,8 @@ __global__ void __launch_bounds__(256) cross_sum_kernel(CrossSumArgs a) {
   const int64_t row = b.first + i;
   const int tok = (int)(row / b.heads);
   if (b.end && (int)(i / b.heads) >= *b.end) return;
-  const int n0 = min(max(b.n0[tok], 0), b.max0);
-  const int n1 = b.n1 ? min(max(b.n1[tok], 0), b.max1) : 0;
+  const int n0 = min(max(b.n[tok], 0), b.max_parts);
+  const int n1 = b.n1 ? min(max(b.n1[tok], 0), b.max_parts) : 0;
   if (!b.n1 && n0 <= 1) return;
   float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   auto add = [&](int64_t slice) __attribute__((always_inline)) {
@@ -739,7 +744,7 @@ __global__ void __launch_bounds__(256) cross_sum_kernel(CrossSumArgs a) {
     }
   };
   for (int p = 0; p < n0; ++p) add(p);
-  for (int p = 0; p < n1; ++p) add(b.max0 + p);
+  for (int p = 0; p < n1; ++p) add(b.max_parts + p);
   if (a.out_bf16) cross_put8(x, (uint16_t*)b.dst + i * D + c);
   else cross_put8(x, (float*)b.dst + i * D + c);
 }

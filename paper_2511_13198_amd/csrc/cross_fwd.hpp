@@ -22,7 +22,8 @@ template <int D, int NW, int KG = 1>
 struct CrossFwdCfg {
   static constexpr int RG = NW / KG;
   static constexpr int BQ = 32 * RG;
-  static constexpr int BK = KG > 1 ? 128 : (D == 128 && NW == 8) ? 128 : 64;
+  static constexpr int BK = NW == 4 ? (KG == 4 ? 128 : 64)
+                            : KG > 1 || D == 128 ? 128 : 64;
   static constexpr int WK = BK / KG;
   static constexpr int BKS = WK < 64 ? WK : 64;
   static constexpr int NT = NW * 64;
@@ -30,14 +31,15 @@ struct CrossFwdCfg {
   using VL = DualLayout<D>;
   static constexpr int KTILE = KL::elems(BK);
   static constexpr int VTILE = VL::elems(BK);
-  static constexpr int STAGES = KG > 1 && D == 64 ? 4 : 2;
-  static constexpr int LDS_BYTES = STAGES * (KTILE + VTILE) * 2;
+  static constexpr int STAGES = NW == 4 && KG == 4 && D == 128 ? 1 : 2;
   static constexpr int F32_PASS = D == 128 ? 4 : 1;
+  // the output tile is turned in the tile buffers; key groups' partial O, then their
+  // row statistics
   static constexpr int STAT_OFF = NW * (D / 32) * kF32Block * 4;
-  static_assert(KG == 1 ? NW * F32_PASS * kF32Block * 4 <= LDS_BYTES &&
-                              NW * 32 * kBf16Pitch<D> * 2 <= LDS_BYTES
-                        : STAT_OFF + NW * 32 * 8 <= LDS_BYTES,
-                "the output tile is turned in the tile buffers");
+  static constexpr int OUT_BYTES = KG > 1 ? STAT_OFF + NW * 32 * 8 : NW * F32_PASS * kF32Block * 4;
+  static constexpr int TILE_BYTES = STAGES * (KTILE + VTILE) * 2;
+  static constexpr int LDS_BYTES = TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES;
+  static_assert(NW * 32 * kBf16Pitch<D> * 2 <= LDS_BYTES && LDS_BYTES <= 160 * 1024, "LDS");
 };
 
 struct CrossFwdArgs {
@@ -53,14 +55,15 @@ struct CrossFwdArgs {
   float scale_log2;
   // partial results: O (fp32, normalised by the part's own sums) and LSE of slice s
   // at part_o [s][tq * hq][D], part_lse [s][tq * hq] (NaN: a NaN or +inf logit), and
-  // how many slices from cut.slice on a token has at part_n [tq]
+  // how many slices a token has at part_n [tq].  CROSS_APART: part_n is of the shared
+  // keys, part_n + tq of a sequence's own, whose slices start at max_parts
   float* part_o;
   float* part_lse;
   int32_t* part_n;
 };
 
 template <int D, int NW, int KG>
-__global__ void __launch_bounds__(NW * 64, NW == 4 && KG == 1 ? 2 : 1)
+__global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1)
     cross_fwd_kernel(CrossFwdArgs a) {
   using C = CrossFwdCfg<D, NW, KG>;
   using KL = typename C::KL;
@@ -72,7 +75,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 && KG == 1 ? 2 : 1)
   xcd_order(blockIdx.x, gridDim.x, a.b.hkv, hk, entry);
   CrossPlace at;
   if (!cross_place_rows(a.b, a.cut, entry, at)) return;
-  const int g = a.b.hq / a.b.hkv;
+  const int g = a.b.g;
   const CrossSeq sq = at.s;
   const int row_end = (sq.q_lo + sq.nq) * g;  // packed rows of the sequence end
   const int row0 = sq.q_lo * g + at.tile * BQ;
@@ -88,7 +91,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 && KG == 1 ? 2 : 1)
   // first own key that a row's token does not see
   const int late = sq.nk - sq.nq - sq.q_lo + 1;  // key_end = token + late (causal)
   auto key_end = [&](int r) __attribute__((always_inline)) {
-    return a.b.causal ? min(sq.nk, min(r, row_end - 1) / g + late) : sq.nk;
+    return a.b.causal ? min(sq.nk, cross_token(a.b, max(min(r, row_end - 1), 0)) + late) : sq.nk;
   };
   const int lane_end = key_end(row);
   const int wave_first = __builtin_amdgcn_readfirstlane(key_end(wrow0));
@@ -98,7 +101,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 && KG == 1 ? 2 : 1)
   const size_t kvstride = (size_t)a.b.hkv * D;
   // element offset of packed row r
   auto row_off = [&](int r) __attribute__((always_inline)) {
-    const int tok = r / g;
+    const int tok = cross_token(a.b, r);
     return ((size_t)tok * a.b.hq + hk * g + (r - tok * g)) * D;
   };
 
@@ -118,8 +121,10 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 && KG == 1 ? 2 : 1)
   f32x16 s[BKS / 32];
 
   // key tiles: npre of the shared keys, then the sequence's own
-  const int npre = a.cut.keys == CROSS_OWN ? 0 : cross_tiles(a.b.prefix, BK);
-  const int nown = a.cut.keys == CROSS_SHARED ? 0 : cross_tiles(wg_end, BK);
+  const bool apart = a.cut.keys == CROSS_APART;
+  const bool shared = apart && at.index == 0;  // this workgroup: shared keys alone
+  const int npre = shared || a.cut.keys == CROSS_FUSED ? cross_tiles(a.b.prefix, BK) : 0;
+  const int nown = shared ? 0 : cross_tiles(wg_end, BK);
   const int ntiles = npre + nown;
   const int t_begin = (int)((int64_t)at.part * ntiles / at.nparts);
   const int t_end = (int)((int64_t)(at.part + 1) * ntiles / at.nparts);
@@ -255,11 +260,12 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 && KG == 1 ? 2 : 1)
 #pragma unroll
     for (int t = 0; t < S - 1; ++t)
       if (t_begin + t < t_end) issue(t_begin + t);
+    if (S == 1 && t_begin < t_end) issue(t_begin);
     for (int it = t_begin; it < t_end; ++it) {
-      if (it + S - 2 < t_end) wait_dma_n<(S - 2) * kMin>();
+      if (S > 2 && it + S - 2 < t_end) wait_dma_n<(S > 2 ? S - 2 : 0) * kMin>();
       else wait_dma();
       __syncthreads();
-      const int tn = it + S - 1;
+      const int tn = S == 1 ? it + 1 : it + S - 1;
       const bool more = tn < t_end;
       const bool pre = it < npre;
       const int k0t = (pre ? it : it - npre) * BK + wk0;  // this wave's first key
@@ -288,7 +294,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 && KG == 1 ? 2 : 1)
           if (sub == 0 || k0s < some) {
             compute_s(kbuf(it) + (wk0 + sub * BKS) * KL::ROW,
                       [&](auto KS) __attribute__((always_inline)) {
-                        if constexpr (sub == 0) {
+                        if constexpr (S > 1 && sub == 0) {
                           constexpr int ks = decltype(KS)::value;
                           if constexpr (ks < PK + PV - 1) copy(KS);
                           if constexpr (ks == D / 16 - 1)
@@ -301,9 +307,13 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 && KG == 1 ? 2 : 1)
                        vbuf(it) + (wk0 + sub * BKS) * VL::ROW);
           }
         });
-        copy(std::integral_constant<int, PK + PV - 1>{});
-      } else if (more) {
+        if constexpr (S > 1) copy(std::integral_constant<int, PK + PV - 1>{});
+      } else if (S > 1 && more) {
         issue(tn);
+      }
+      if constexpr (S == 1) {
+        __syncthreads();
+        if (more) issue(tn);
       }
     }
     wait_dma();
@@ -311,17 +321,20 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 && KG == 1 ? 2 : 1)
     __syncthreads();
   }
 
-  const bool partial = a.cut.always_part || at.nparts > 1;
+  const bool partial = apart || at.nparts > 1;
+  const bool second = apart && !shared;
   const size_t pairs = (size_t)a.b.tq * a.b.hq;
-  const size_t slice = (size_t)(a.cut.slice + at.part) * pairs;
-  if (a.part_n && hk == 0 && at.part == 0 && kg == 0 && hh == 0 && row < row_end && row % g == 0)
-    a.part_n[row / g] = at.nparts;
+  const size_t slice = (size_t)(second ? a.cut.max_parts + at.part : at.part) * pairs;
+  if (a.part_n && hk == 0 && at.part == 0 && kg == 0 && hh == 0 && row < row_end) {
+    const int tok = cross_token(a.b, row);
+    if (tok * g == row) a.part_n[(second ? a.b.tq : 0) + tok] = at.nparts;
+  }
   // LSE of a row from its offset m (base 2) and sum; a part hands a NaN sum on as NaN
   auto lse_of = [&](float m2, float tot) __attribute__((always_inline)) {
     return tot > 0.f ? (m2 + __builtin_log2f(tot)) * kLn2 : partial ? tot - INFINITY : -INFINITY;
   };
   auto put_lse = [&](int r, float x) __attribute__((always_inline)) {
-    const int tok = r / g, h = hk * g + (r - tok * g);
+    const int tok = cross_token(a.b, r), h = hk * g + (r - tok * g);
     if (partial) a.part_lse[slice + (size_t)tok * a.b.hq + h] = x;
     else a.lse[(size_t)h * a.b.tq + tok] = x;
   };
@@ -381,18 +394,20 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 && KG == 1 ? 2 : 1)
 }
 
 // Combine the partial results of the rows that have any: part_n[token] slices from
-// 0 on, and, where shared and own keys were two launches, part_n1[token] from slice
-// max0 on.
+// 0 on, and, where shared and own keys were apart, part_n[tq + token] from slice
+// max_parts on.
 //   LSE = log sum_p exp(LSE_p),  O = sum_p exp(LSE_p - LSE) O_p;
 // a part with LSE = -inf weighs nothing, one with NaN makes the row O = NaN, LSE =
-// -inf.  8 elements of a (token, head) pair per thread.
+// -inf.  A wave per (token, head) pair: a lane per slice for the weights (64 at a
+// time), then 64 / LANES slices at a time, 8 elements a lane, so that the reads of
+// many slices are in flight together.
 struct CrossMergeArgs {
   const float* part_o;
   const float* part_lse;
-  const int32_t* part_n;   // first job's slices of a token
-  const int32_t* part_n1;  // second job's, or NULL
-  int max0, max1;          // most slices of each; the second's start at max0
-  const int32_t* cu_q;     // rows end at cu_q[n]
+  const int32_t* part_n;
+  int max_parts;
+  int apart;
+  const int32_t* cu_q;  // rows end at cu_q[n]
   int n;
   int tq, hq;
   uint16_t* o;
@@ -401,52 +416,66 @@ struct CrossMergeArgs {
 
 template <int D>
 __global__ void __launch_bounds__(256) cross_merge_kernel(CrossMergeArgs a) {
-  constexpr int LANES = D / 8;
-  const size_t gid = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const size_t pair = gid / LANES;  // token * hq + head
-  const int c = (int)(gid % LANES) * 8;
-  const size_t pairs = (size_t)a.tq * a.hq;
+  constexpr int LANES = D / 8, GROUPS = 64 / LANES;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l = __lane_id();
+  const uint32_t pair = blockIdx.x * 4 + w;  // token * hq + head
+  const uint32_t pairs = (uint32_t)a.tq * a.hq;
   if (pair >= pairs) return;
-  const int tok = (int)(pair / a.hq), h = (int)(pair % a.hq);
-  if (tok >= a.cu_q[a.n]) return;  // rows behind the last sequence stay
-  const int n0 = min(max(a.part_n[tok], 0), a.max0);
-  const int n1 = a.part_n1 ? min(max(a.part_n1[tok], 0), a.max1) : 0;
-  if (!a.part_n1 && n0 == 1) return;  // written by its one part
-  float mx = -INFINITY;
-  bool bad = false;
-  auto each = [&](auto&& f) __attribute__((always_inline)) {
-    for (int p = 0; p < n0; ++p) f((size_t)p * pairs + pair);
-    for (int p = 0; p < n1; ++p) f((size_t)(a.max0 + p) * pairs + pair);
-  };
-  each([&](size_t i) {
-    const float x = a.part_lse[i];
-    bad |= x != x;
-    mx = fmaxf(mx, x);
-  });
+  const int tok = (int)(pair / (uint32_t)a.hq), h = (int)(pair - (uint32_t)tok * a.hq);
+  const int c = (l % LANES) * 8, grp = l / LANES;
+  const int end = a.cu_q[a.n];
+  const int n0 = min(max(a.part_n[tok], 0), a.max_parts);
+  const int n1 = a.apart ? min(max(a.part_n[a.tq + tok], 0), a.max_parts) : 0;
+  if (tok >= end) return;  // rows behind the last sequence stay
+  if (!a.apart && n0 == 1) return;  // written by its one part
+  const int parts = n0 + n1, gap = a.max_parts - n0;
+  float mx = -INFINITY, tot = 0.f;
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  float tot = 0.f;
-  if (bad) {
+  // (more than 64 slices: the sums so far are rescaled by each further 64)
+  for (int p0 = 0; p0 < parts; p0 += 64) {
+    const int p = p0 + l;
+    const float x = p < parts ? a.part_lse[(size_t)(p < n0 ? p : p + gap) * pairs + pair]
+                              : -INFINITY;
+    float top = x;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = NAN;
-  } else if (mx != -INFINITY) {
-    each([&](size_t i) {
-      const float wt = fast_exp2((a.part_lse[i] - mx) * kLog2e);
-      tot += wt;
-      const float* src = a.part_o + i * D + c;
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+    top = fmaxf(top, mx);
+    const float keep = mx == -INFINITY ? 0.f : fast_exp2((mx - top) * kLog2e);
+    // (NaN where x is NaN: fmaxf passes it over)
+    const float wt = x == -INFINITY ? 0.f : fast_exp2((x - top) * kLog2e);
+    mx = top;
+    float sum = wt;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+    tot = tot * keep + sum;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= keep;
+    const int m = min(64, parts - p0);
+#pragma unroll 4
+    for (int j0 = 0; j0 < m; j0 += GROUPS) {
+      // (every lane takes part in the exchange; past the last slice the weight is 0)
+      const float wj = __shfl(wt, j0 + grp);
+      const int pj = p0 + min(j0 + grp, m - 1);
+      const float* src = a.part_o + ((size_t)(pj < n0 ? pj : pj + gap) * pairs + pair) * D + c;
       const f32x4 x0 = *reinterpret_cast<const f32x4*>(src);
       const f32x4 x1 = *reinterpret_cast<const f32x4*>(src + 4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        acc[e] += wt * x0[e];
-        acc[4 + e] += wt * x1[e];
+        acc[e] += wj * x0[e];
+        acc[4 + e] += wj * x1[e];
       }
-    });
-    const float inv = 1.f / tot;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] *= inv;
+    }
   }
-  cross_put8(acc, a.o + pair * D + c);
-  if (c == 0)
+#pragma unroll
+  for (int off = LANES; off < 64; off <<= 1)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor(acc[e], off);
+  const float inv = tot > 0.f ? 1.f / tot : tot != tot ? NAN : 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] *= inv;
+  if (grp == 0) cross_put8(acc, a.o + (size_t)pair * D + c);
+  if (l == 0)
     a.lse[(size_t)h * a.tq + tok] = tot > 0.f ? mx + __builtin_log2f(tot) * kLn2 : -INFINITY;
 }
 

@@ -35,10 +35,24 @@ void launch_rotary(const pdy::RotaryArgs& a, int d, bool inter, int64_t heads, h
 
 extern "C" {
 
+pdy_status attn_rotary_turns(const double* freqs, int32_t num_pairs, uint64_t* turns) {
+  g_err[0] = 0;
+  if (num_pairs < 0 || (num_pairs > 0 && (freqs == nullptr || turns == nullptr)))
+    return fail(PDY_ERR_INVALID_ARG, "attn_rotary_turns: bad arrays");
+  for (int p = 0; p < num_pairs; ++p) {
+    if (!std::isfinite(freqs[p])) return fail(PDY_ERR_INVALID_ARG, "freqs[%d] is not finite", p);
+    // turns a position, without whole turns (a long double holds the 64 bits)
+    long double t = (long double)freqs[p] * 0.15915494309189533576888376337251436L;
+    t -= floorl(t);
+    turns[p] = t < 1.0L ? (uint64_t)(t * 18446744073709551616.0L) : 0;
+  }
+  return PDY_OK;
+}
+
 pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
                        int32_t total_tokens, int32_t num_axes, int32_t num_heads_q,
                        int32_t num_heads_kv, int32_t head_dim, int32_t num_pairs,
-                       const double* freqs, const int32_t* pair_axes, int32_t interleaved,
+                       const uint64_t* turns, const int32_t* pair_axes, int32_t interleaved,
                        int32_t inverse, int32_t in_fp32, int32_t out_fp32, void* q_out,
                        void* k_out, void* stream) {
   g_err[0] = 0;
@@ -62,19 +76,14 @@ pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
     return fail(PDY_ERR_INVALID_ARG, "interleaved, inverse, in_fp32 and out_fp32 must be 0 or 1");
   if (out_fp32 && !in_fp32)
     return fail(PDY_ERR_UNSUPPORTED, "bf16 to fp32 is not supported (bf16, fp32, or fp32 to bf16)");
-  if (freqs == nullptr || pair_axes == nullptr)
-    return fail(PDY_ERR_INVALID_ARG, "freqs and pair_axes (host arrays) must not be NULL");
+  if (turns == nullptr || pair_axes == nullptr)
+    return fail(PDY_ERR_INVALID_ARG, "turns and pair_axes (host arrays) must not be NULL");
   pdy::RotaryArgs a;
   for (int p = 0; p < num_pairs; ++p) {
-    if (!std::isfinite(freqs[p]))
-      return fail(PDY_ERR_INVALID_ARG, "freqs[%d] is not finite", p);
     if (pair_axes[p] < 0 || pair_axes[p] >= num_axes)
       return fail(PDY_ERR_INVALID_ARG, "pair_axes[%d] must be in [0, %d) (got %d)", p, num_axes,
                   pair_axes[p]);
-    // turns a position, without whole turns (a long double holds the 64 bits)
-    long double turns = (long double)freqs[p] * 0.15915494309189533576888376337251436L;
-    turns -= floorl(turns);
-    a.freq[p] = turns < 1.0L ? (uint64_t)(turns * 18446744073709551616.0L) : 0;
+    a.freq[p] = turns[p];
     a.axis[p] = (uint8_t)pair_axes[p];
   }
   if (total_tokens == 0) return PDY_OK;

@@ -9,7 +9,7 @@
 // of a head is copied.
 //
 // Angles.  A position of 10^5 and more times w in 32-bit floats would leave the angle
-// off by 10^-2.  The host gives w_p / 2 pi as a 64-bit fraction F of a turn; pos * F
+// off by 10^-2.  The caller gives w_p / 2 pi as a 64-bit fraction F of a turn; pos * F
 // mod 2^64 is then the angle in turns with whole turns gone, exact to pos * 2^-65.
 // Its upper 32 bits are split into the nearest eighth ... quarter turn and a
 // remainder of at most an eighth, whose sine and cosine are the Taylor sums to x^9

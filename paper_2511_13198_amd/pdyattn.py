@@ -7,7 +7,6 @@ fallback: if the library is missing or a call fails, an exception is raised.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import functools
 import math
@@ -29,7 +28,7 @@ SYMBOLS = ("attn_fwd_workspace_size", "attn_bwd_workspace_size", "attn_fwd", "at
            "attn_bwd_chunk", "attn_fwd_chunk_shared", "attn_bwd_chunk_shared", "attn_merge",
            "attn_cross_fwd_workspace_size", "attn_cross_fwd", "attn_prefix_fwd_workspace_size",
            "attn_prefix_fwd", "attn_cross_bwd_workspace_size", "attn_cross_bwd",
-           "attn_prefix_bwd_workspace_size", "attn_prefix_bwd", "attn_rotary",
+           "attn_prefix_bwd_workspace_size", "attn_prefix_bwd", "attn_rotary_turns", "attn_rotary",
            "attn_validate_cu_seqlens", "attn_bwd_noalloc", "pdy_launch_shapes",
            "pdy_chunk_launch_shapes", "pdy_status_string", "pdy_last_error",
            "pdy_kernel_count", "pdy_kernel_name", "pdy_profile_start", "pdy_profile_stop")
@@ -97,9 +96,9 @@ def lib() -> ctypes.CDLL:
     L.attn_prefix_bwd.argtypes = ([vp] * 11 + [i32] * 10 +
                                   [f32, i32, vp, vp, vp, vp, vp, vp, sz, vp])
     L.attn_prefix_bwd.restype = i32
-    L.attn_rotary.argtypes = ([vp] * 3 + [i32] * 6 +
-                              [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32)] + [i32] * 4 +
-                              [vp] * 3)
+    L.attn_rotary_turns.argtypes = [vp, i32, vp]
+    L.attn_rotary_turns.restype = i32
+    L.attn_rotary.argtypes = [vp] * 3 + [i32] * 6 + [vp] * 2 + [i32] * 4 + [vp] * 3
     L.attn_rotary.restype = i32
     L.attn_validate_cu_seqlens.argtypes = [vp, i32, i32, ctypes.POINTER(i32), vp]
     L.attn_validate_cu_seqlens.restype = i32
@@ -455,18 +454,30 @@ def prefix_bwd_workspace_size(prefix_len, total_q, total_k, num_seqs, max_seqlen
                                                     max_seqlen_q, max_seqlen_k, hq, hkv, d))
 
 
-def _on_device(device):
-    """The library launches on the current device: make it the tensors'."""
+def _launch(name: str, device, *args):
+    """Calls the library on the tensors' device and its current stream (the last
+    argument); the library launches on the current device."""
     import torch
-    if device.index is None or torch.cuda.current_device() == device.index:
-        return contextlib.nullcontext()
-    return torch.cuda.device(device)
+    index = device.index
+    if index is None or torch.cuda.current_device() == index:
+        st = getattr(lib(), name)(*args, _stream_handle(device))
+    else:
+        with torch.cuda.device(index):
+            st = getattr(lib(), name)(*args, _stream_handle(device))
+    if st != PDY_OK:
+        _check(st, name)
 
 
-def _same_device(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, q on {device}")
+def _check_tensors(device, *checks):
+    """(tensor, name, dtype, dims) of a call, all on one device."""
+    where = device.index if device.type == "cuda" else None
+    for t, name, dtype, ndim in checks:
+        # (the usual case in one line: this runs for every tensor of every call)
+        if (t.dtype is dtype and t.dim() == ndim and t.is_contiguous() and
+                t.get_device() == where):
+            continue
+        _check_tensor(t, name, dtype, ndim)
+        raise ValueError(f"{name} is on {t.device}, the call's first tensor on {device}")
 
 
 def _longest(cu, name: str, total: int) -> int:
@@ -480,68 +491,61 @@ def _longest(cu, name: str, total: int) -> int:
 def _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k, scale, seqlens_k):
     """Checked arguments of a call: the pointers and numbers of its inputs."""
     import torch
-    for t, name in ((q, "q"), (k, "k"), (v, "v")):
-        _check_tensor(t, name, torch.bfloat16, 3)
-    for t, name in ((cu_q, "cu_seqlens_q"), (cu_k, "cu_seqlens_k")):
-        _check_tensor(t, name, torch.int32, 1)
-    T, hq, d = q.shape
-    tk, hkv = k.shape[0], k.shape[1]
-    if k.shape[2] != d or v.shape != k.shape:
-        raise ValueError("k and v must be [Tk, Hkv, d] with q's d")
-    n = cu_q.numel() - 1
-    if n < 1 or cu_k.numel() != n + 1:
-        raise ValueError("cu_seqlens_q and cu_seqlens_k must have num_seqs + 1 >= 2 offsets each")
-    if seqlens_k is not None:
-        _check_tensor(seqlens_k, "seqlens_k", torch.int32, 1)
-        if seqlens_k.numel() != n:
-            raise ValueError("seqlens_k must have num_seqs lengths")
+    bf16, i32 = torch.bfloat16, torch.int32
     dev = q.device
-    _same_device(dev, k=k, v=v, cu_seqlens_q=cu_q, cu_seqlens_k=cu_k, seqlens_k=seqlens_k)
-    pre = ()
+    _check_tensors(dev, (q, "q", bf16, 3), (k, "k", bf16, 3), (v, "v", bf16, 3),
+                   (cu_q, "cu_seqlens_q", i32, 1), (cu_k, "cu_seqlens_k", i32, 1))
+    T, hq, d = q.shape
+    tk, hkv, dk = k.shape
+    if dk != d or v.shape != k.shape:
+        raise ValueError("k and v must be [Tk, Hkv, d] with q's d")
+    n = cu_q.shape[0] - 1
+    if n < 1 or cu_k.shape[0] != n + 1:
+        raise ValueError("cu_seqlens_q and cu_seqlens_k must have num_seqs + 1 >= 2 offsets each")
+    used = 0
+    if seqlens_k is not None:
+        _check_tensors(dev, (seqlens_k, "seqlens_k", i32, 1))
+        if seqlens_k.shape[0] != n:
+            raise ValueError("seqlens_k must have num_seqs lengths")
+        used = seqlens_k.data_ptr()
+    ptrs, pre = (q.data_ptr(), k.data_ptr(), v.data_ptr()), ()
     if kp is not None:
-        _check_tensor(kp, "k_prefix", torch.bfloat16, 3)
-        _check_tensor(vp, "v_prefix", torch.bfloat16, 3)
+        _check_tensors(dev, (kp, "k_prefix", bf16, 3), (vp, "v_prefix", bf16, 3))
         if kp.shape[1:] != (hkv, d) or vp.shape != kp.shape:
             raise ValueError("k_prefix and v_prefix must be [P, Hkv, d]")
-        _same_device(dev, k_prefix=kp, v_prefix=vp)
-        pre = (kp.shape[0],)
-    max_q = _longest(cu_q, "cu_seqlens_q", T) if max_q is None else int(max_q)
-    max_k = _longest(cu_k, "cu_seqlens_k", tk) if max_k is None else int(max_k)
-    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
-    ptrs = (q.data_ptr(), k.data_ptr(), v.data_ptr())
-    if pre:
-        ptrs += (kp.data_ptr(), vp.data_ptr())
-    offsets = (cu_q.data_ptr(), cu_k.data_ptr(), _ptr(seqlens_k), *pre)
-    return ptrs, offsets, pre, (n, T, tk, max_q, max_k, hq, hkv, d), scale
+        ptrs, pre = (*ptrs, kp.data_ptr(), vp.data_ptr()), (kp.shape[0],)
+    max_q = _longest(cu_q, "cu_seqlens_q", T) if max_q is None else max_q
+    max_k = _longest(cu_k, "cu_seqlens_k", tk) if max_k is None else max_k
+    return (dev, ptrs, (cu_q.data_ptr(), cu_k.data_ptr(), used, *pre), pre,
+            (n, T, tk, max_q, max_k, hq, hkv, d), 1.0 / math.sqrt(d) if scale is None else scale)
+
+
+def _cross_workspace(kind: str, pre, sizes, device):
+    """A workspace for a call of these sizes (kind "fwd" or "bwd")."""
+    n, T, tk, max_q, max_k, hq, hkv, d = sizes
+    name = f"attn_{'prefix' if pre else 'cross'}_{kind}_workspace_size"
+    return _ws(getattr(lib(), name)(*pre, T, tk, n, max_q, max_k, hq, hkv, d), device)
 
 
 def _cross_fwd(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k, causal, scale, seqlens_k, out, lse,
                workspace):
     import torch
-    ptrs, offsets, pre, sizes, scale = _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k,
-                                                   scale, seqlens_k)
-    n, T, tk, max_q, max_k, hq, hkv, d = sizes
+    dev, ptrs, offsets, pre, sizes, scale = _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k,
+                                                        scale, seqlens_k)
+    T, hq = sizes[1], sizes[5]
     if out is None:
         out = torch.empty_like(q)
-    else:
-        _check_tensor(out, "out", torch.bfloat16, 3)
     if lse is None:
-        lse = torch.empty((hq, T), dtype=torch.float32, device=q.device)
-    else:
-        _check_tensor(lse, "lse", torch.float32, 2)
+        lse = torch.empty((hq, T), dtype=torch.float32, device=dev)
+    if workspace is None:
+        workspace = _cross_workspace("fwd", pre, sizes, dev)
+    _check_tensors(dev, (out, "out", torch.bfloat16, 3), (lse, "lse", torch.float32, 2),
+                   (workspace, "workspace", workspace.dtype, workspace.dim()))
     if out.shape != q.shape or lse.shape != (hq, T):
         raise ValueError("out must be q's shape, lse [Hq, T]")
-    if workspace is None:
-        size = prefix_fwd_workspace_size if pre else cross_fwd_workspace_size
-        workspace = _ws(size(*pre, T, tk, n, max_q, max_k, hq, hkv, d), q.device)
-    _same_device(q.device, out=out, lse=lse, workspace=workspace)
-    name = "attn_prefix_fwd" if pre else "attn_cross_fwd"
-    with _on_device(q.device):
-        st = getattr(lib(), name)(*ptrs, *offsets, *sizes, int(bool(causal)), scale,
-                                  out.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
-                                  workspace.numel() * workspace.element_size(),
-                                  _stream_handle(q.device))
-    _check(st, name)
+    _launch("attn_prefix_fwd" if pre else "attn_cross_fwd", dev, *ptrs, *offsets, *sizes,
+            1 if causal else 0, scale, out.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
+            workspace.nbytes)
     return out, lse
 
 
@@ -573,41 +577,33 @@ def attn_prefix_fwd(q, k, v, k_prefix, v_prefix, cu_seqlens_q, cu_seqlens_k,
 def _cross_bwd(q, k, v, kp, vp, o, lse, dout, cu_q, cu_k, max_q, max_k, causal, scale, seqlens_k,
                grads, grad_dtype, workspace):
     import torch
-    ptrs, offsets, pre, sizes, scale = _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k,
-                                                   scale, seqlens_k)
-    n, T, tk, max_q, max_k, hq, hkv, d = sizes
-    _check_tensor(o, "o", torch.bfloat16, 3)
-    _check_tensor(dout, "dout", torch.bfloat16, 3)
-    _check_tensor(lse, "lse", torch.float32, 2)
-    if o.shape != q.shape or dout.shape != q.shape or lse.shape != (hq, T):
-        raise ValueError("o and dout must match q, lse must be [Hq, T]")
+    dev, ptrs, offsets, pre, sizes, scale = _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k,
+                                                        scale, seqlens_k)
     given = [g for g in grads if g is not None]
-    dtype = given[0].dtype if given else grad_dtype
+    dtype = given[0].dtype if given else grad_dtype or torch.float32
     if dtype not in (torch.float32, torch.bfloat16):
         raise TypeError(f"gradients must be torch.float32 or torch.bfloat16, got {dtype}")
-    names = ("dq", "dk", "dv", "dk_prefix", "dv_prefix")
     out = []
-    for name, g, like in zip(names, grads, (q, k, v, kp, vp)):
+    for name, g, like in zip(("dq", "dk", "dv", "dk_prefix", "dv_prefix"), grads, (q, k, v, kp, vp)):
         if like is None:
             continue
         if g is None:
-            g = torch.empty(like.shape, dtype=dtype, device=q.device)
-        _check_tensor(g, name, dtype, 3)
+            g = torch.empty(like.shape, dtype=dtype, device=dev)
+        _check_tensors(dev, (g, name, dtype, 3))
         if g.shape != like.shape:
             raise ValueError(f"{name} must be {list(like.shape)}")
         out.append(g)
     if workspace is None:
-        size = prefix_bwd_workspace_size if pre else cross_bwd_workspace_size
-        workspace = _ws(size(*pre, T, tk, n, max_q, max_k, hq, hkv, d), q.device)
-    _same_device(q.device, o=o, lse=lse, dout=dout, workspace=workspace, **dict(zip(names, out)))
-    name = "attn_prefix_bwd" if pre else "attn_cross_bwd"
-    with _on_device(q.device):
-        st = getattr(lib(), name)(*ptrs, o.data_ptr(), lse.data_ptr(), dout.data_ptr(), *offsets,
-                                  *sizes, int(bool(causal)), scale, int(dtype == torch.bfloat16),
-                                  *(g.data_ptr() for g in out), workspace.data_ptr(),
-                                  workspace.numel() * workspace.element_size(),
-                                  _stream_handle(q.device))
-    _check(st, name)
+        workspace = _cross_workspace("bwd", pre, sizes, dev)
+    _check_tensors(dev, (o, "o", torch.bfloat16, 3), (dout, "dout", torch.bfloat16, 3),
+                   (lse, "lse", torch.float32, 2),
+                   (workspace, "workspace", workspace.dtype, workspace.dim()))
+    if o.shape != q.shape or dout.shape != q.shape or lse.shape != (sizes[5], sizes[1]):
+        raise ValueError("o and dout must match q, lse must be [Hq, T]")
+    _launch("attn_prefix_bwd" if pre else "attn_cross_bwd", dev, *ptrs, o.data_ptr(),
+            lse.data_ptr(), dout.data_ptr(), *offsets, *sizes, 1 if causal else 0, scale,
+            1 if dtype is torch.bfloat16 else 0, *[g.data_ptr() for g in out],
+            workspace.data_ptr(), workspace.nbytes)
     return tuple(out)
 
 
@@ -618,10 +614,9 @@ def attn_cross_bwd(q, k, v, o, lse, dout, cu_seqlens_q, cu_seqlens_k,
     """dQ [Tq, Hq, d], dK, dV [Tk, Hkv, d] of sum(dout * O) of attn_cross_fwd, in the
     dtype of the given gradients, else grad_dtype (torch.float32, the default, or
     torch.bfloat16).  Keys not in use get 0; rows of no sequence are left."""
-    import torch
     return _cross_bwd(q, k, v, None, None, o, lse, dout, cu_seqlens_q, cu_seqlens_k,
                       max_seqlen_q, max_seqlen_k, causal, scale, seqlens_k,
-                      (dq, dk, dv, None, None), grad_dtype or torch.float32, workspace)
+                      (dq, dk, dv, None, None), grad_dtype, workspace)
 
 
 def attn_prefix_bwd(q, k, v, k_prefix, v_prefix, o, lse, dout, cu_seqlens_q, cu_seqlens_k,
@@ -631,12 +626,11 @@ def attn_prefix_bwd(q, k, v, k_prefix, v_prefix, o, lse, dout, cu_seqlens_q, cu_
                     workspace=None) -> Tuple:
     """attn_cross_bwd of attn_prefix_fwd: also dK, dV of the shared keys [P, Hkv, d],
     summed over the rows of all sequences."""
-    import torch
     if k_prefix is None or v_prefix is None:
         raise ValueError("attn_prefix_bwd needs k_prefix and v_prefix")
     return _cross_bwd(q, k, v, k_prefix, v_prefix, o, lse, dout, cu_seqlens_q, cu_seqlens_k,
                       max_seqlen_q, max_seqlen_k, causal, scale, seqlens_k,
-                      (dq, dk, dv, dk_prefix, dv_prefix), grad_dtype or torch.float32, workspace)
+                      (dq, dk, dv, dk_prefix, dv_prefix), grad_dtype, workspace)
 
 
 # ---------------------------------------------------------------------------
@@ -644,7 +638,8 @@ def attn_prefix_bwd(q, k, v, k_prefix, v_prefix, o, lse, dout, cu_seqlens_q, cu_
 # ---------------------------------------------------------------------------
 @functools.lru_cache(maxsize=64)
 def _rotary_tables(sections: Tuple[int, ...], base: float, freqs: Optional[Tuple[float, ...]]):
-    """(frequencies, axes) of the pairs as C arrays."""
+    """(pairs, turns, axes): the pairs' frequencies as fractions of a turn and their
+    axes, as C arrays, and the arrays' addresses."""
     if any(n < 0 for n in sections):
         raise ValueError(f"sections must be >= 0, got {sections}")
     pairs = sum(sections)
@@ -652,8 +647,11 @@ def _rotary_tables(sections: Tuple[int, ...], base: float, freqs: Optional[Tuple
         freqs = tuple(base ** (-p / pairs) for p in range(pairs))
     elif len(freqs) != pairs:
         raise ValueError(f"freqs must have {pairs} values, one a pair, got {len(freqs)}")
-    axes = [a for a, n in enumerate(sections) for _ in range(n)]
-    return (ctypes.c_double * pairs)(*freqs), (ctypes.c_int32 * pairs)(*axes)
+    turns = (ctypes.c_uint64 * pairs)()
+    axes = (ctypes.c_int32 * pairs)(*(a for a, n in enumerate(sections) for _ in range(n)))
+    w = (ctypes.c_double * pairs)(*freqs)
+    _check(lib().attn_rotary_turns(w, pairs, turns), "attn_rotary_turns")
+    return pairs, ctypes.addressof(turns), ctypes.addressof(axes), (turns, axes)
 
 
 def attn_rotary(q, k, positions, sections, base: float = 10000.0, freqs=None,
@@ -667,48 +665,46 @@ def attn_rotary(q, k, positions, sections, base: float = 10000.0, freqs=None,
     from those of the rotated.  q or k may be None.  bf16, or float32 (out_dtype or
     out_q, out_k bf16 round to it); out_q may be q, out_k k."""
     import torch
-    given = [(t, n) for t, n in ((q, "q"), (k, "k")) if t is not None]
-    if not given:
+    first = q if q is not None else k
+    if first is None:
         raise ValueError("attn_rotary needs q or k")
-    first = given[0][0]
-    if first.dtype not in (torch.bfloat16, torch.float32):
-        raise TypeError(f"{given[0][1]} must be torch.bfloat16 or torch.float32, got {first.dtype}")
-    T, d = first.shape[0], first.shape[-1]
-    outs = [o for o in (out_q, out_k) if o is not None]
-    dtype = outs[0].dtype if outs else out_dtype or first.dtype
-    res = []
-    for (t, name), o in zip(((q, "q"), (k, "k")), (out_q, out_k)):
+    types = (torch.bfloat16, torch.float32)
+    outs = out_q if out_q is not None else out_k
+    dtype = outs.dtype if outs is not None else out_dtype or first.dtype
+    if first.dtype not in types or dtype not in types:
+        raise TypeError("q, k and the outputs must be torch.bfloat16 or torch.float32, got "
+                        f"{first.dtype}, {dtype}")
+    dev = first.device
+    res, ptrs, heads = [], [], []
+    for name, t, o in (("q", q, out_q), ("k", k, out_k)):
         if t is None:
             if o is not None:
                 raise ValueError(f"out_{name} without {name}")
             res.append(None)
+            ptrs += [0, 0]
+            heads.append(0)
             continue
-        _check_tensor(t, name, first.dtype, 3)
-        if t.shape[0] != T or t.shape[2] != d:
-            raise ValueError("q and k must have the same tokens and head dimension")
         if o is None:
-            o = torch.empty(t.shape, dtype=dtype, device=t.device)
-        _check_tensor(o, f"out_{name}", dtype, 3)
+            o = torch.empty(t.shape, dtype=dtype, device=dev)
+        _check_tensors(dev, (t, name, first.dtype, 3), (o, f"out_{name}", dtype, 3))
         if o.shape != t.shape:
             raise ValueError(f"out_{name} must have {name}'s shape")
         res.append(o)
-    if dtype not in (torch.bfloat16, torch.float32):
-        raise TypeError(f"outputs must be torch.bfloat16 or torch.float32, got {dtype}")
+        ptrs += [t.data_ptr(), o.data_ptr()]
+        heads.append(t.shape[1])
+    T, d = first.shape[0], first.shape[2]
+    if q is not None and k is not None and (k.shape[0] != T or k.shape[2] != d):
+        raise ValueError("q and k must have the same tokens and head dimension")
     if positions.dim() == 1:
         positions = positions[:, None]
-    _check_tensor(positions, "positions", torch.int32, 2)
-    sections = tuple(int(n) for n in sections)
+    sections = tuple(sections)
+    _check_tensors(dev, (positions, "positions", torch.int32, 2))
     if positions.shape != (T, len(sections)):
         raise ValueError(f"positions must be [{T}, {len(sections)}] (tokens, sections), got "
                          f"{list(positions.shape)}")
-    _same_device(first.device, q=q, k=k, positions=positions, out_q=res[0], out_k=res[1])
-    w, axes = _rotary_tables(sections, float(base),
-                             None if freqs is None else tuple(float(f) for f in freqs))
-    with _on_device(first.device):
-        st = lib().attn_rotary(_ptr(q), _ptr(k), positions.data_ptr(), T, len(sections),
-                               0 if q is None else q.shape[1], 0 if k is None else k.shape[1], d,
-                               len(w), w, axes, int(bool(interleaved)), int(bool(inverse)),
-                               int(first.dtype == torch.float32), int(dtype == torch.float32),
-                               _ptr(res[0]), _ptr(res[1]), _stream_handle(first.device))
-    _check(st, "attn_rotary")
+    pairs, turns, axes, _ = _rotary_tables(sections, base, None if freqs is None else tuple(freqs))
+    _launch("attn_rotary", dev, ptrs[0], ptrs[2], positions.data_ptr(), T, len(sections), *heads,
+            d, pairs, turns, axes, 1 if interleaved else 0, 1 if inverse else 0,
+            1 if first.dtype is torch.float32 else 0, 1 if dtype is torch.float32 else 0, ptrs[1],
+            ptrs[3])
     return res[0], res[1]

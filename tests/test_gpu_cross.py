@@ -30,9 +30,12 @@ CASES = [
     ([70] * 60, [129] * 60, None, 0, 5, 1, 64, False),
     # more sequences than lanes
     ([1 + i % 3 for i in range(150)], [(37 * i) % 90 for i in range(150)], None, 0, 2, 1, 128, True),
-    # shared keys: few rows (two launches), many rows (one), one key, no own keys
+    # shared keys: few rows behind many of them (apart), others; one key, no own keys
     ([1] * 5, [40] * 5, [1, 40, 17, 0, 8], 333, 8, 2, 128, True),
     ([1] * 64, [9] * 64, None, 1000, 4, 4, 64, True),
+    ([1] * 9, [700] * 9, [700, 0, 1, 64, 128, 129, 650, 2, 90], 2500, 16, 2, 128, True),
+    ([16, 3, 0, 9], [20, 3, 1, 300], None, 900, 8, 2, 64, True),
+    ([20] * 12, [20] * 12, None, 600, 6, 2, 128, False),
     ([2, 1, 4], [2, 1, 4], None, 1, 8, 8, 64, True),
     ([4, 8, 1], [0, 0, 0], None, 130, 8, 4, 128, False),
     ([100, 33, 1, 250], [100, 33, 1, 250], None, 200, 8, 2, 128, True),
