@@ -14,11 +14,17 @@ using namespace pdy_host;
 
 namespace {
 
+constexpr int64_t kFill = 1024;  // workgroups
+
 template <class In, class Out, int D>
-void launch_rotary(const pdy::RotaryArgs& a, bool inter, int64_t heads, hipStream_t st) {
-  constexpr int kTokens = 256 * 2 * (16 / (int)sizeof(In)) / D;
-  const dim3 grid((unsigned)((a.tokens + kTokens - 1) / kTokens),
-                  (unsigned)((heads + a.heads_per_block - 1) / a.heads_per_block));
+void launch_rotary(pdy::RotaryArgs& a, bool inter, int64_t heads, hipStream_t st) {
+  constexpr int kHeads = 64 * 2 * (16 / (int)sizeof(In)) / D;  // of a wave's round
+  // a wave takes its token's heads all, so that the angles are computed once, unless
+  // that leaves the chip idle: then a part of the rounds each
+  const int64_t rounds = (heads + kHeads - 1) / kHeads, blocks = ((int64_t)a.tokens + 3) / 4;
+  const int64_t cuts = std::min(rounds, std::max<int64_t>(1, kFill / blocks));
+  a.rounds = (int)((rounds + cuts - 1) / cuts);
+  const dim3 grid((unsigned)blocks, (unsigned)((rounds + a.rounds - 1) / a.rounds));
   if (inter)
     hipLaunchKernelGGL((pdy::rotary_kernel<In, Out, D, true>), grid, dim3(256), 0, st, a);
   else
@@ -26,7 +32,7 @@ void launch_rotary(const pdy::RotaryArgs& a, bool inter, int64_t heads, hipStrea
 }
 
 template <class In, class Out>
-void launch_rotary(const pdy::RotaryArgs& a, int d, bool inter, int64_t heads, hipStream_t st) {
+void launch_rotary(pdy::RotaryArgs& a, int d, bool inter, int64_t heads, hipStream_t st) {
   if (d == 64) launch_rotary<In, Out, 64>(a, inter, heads, st);
   else launch_rotary<In, Out, 128>(a, inter, heads, st);
 }
@@ -104,13 +110,7 @@ pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
   a.axes = num_axes;
   a.pairs = num_pairs;
   a.inverse = inverse;
-  // a block's tokens through all heads, so that angles are computed once, unless that
-  // leaves the chip idle: then fewer heads a block, down to one
   const int64_t heads = (int64_t)num_heads_q + num_heads_kv;
-  const int64_t tokens_per_block = 512 * (in_fp32 ? 4 : 8) / head_dim;
-  const int64_t blocks = (total_tokens + tokens_per_block - 1) / tokens_per_block;
-  const int64_t cuts = std::min(heads, std::max<int64_t>(1, 1024 / blocks));
-  a.heads_per_block = (int)((heads + cuts - 1) / cuts);
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
   const hipError_t e = launch_timed(K_ROTARY, hs, [&] {
     if (!in_fp32) launch_rotary<uint16_t, uint16_t>(a, head_dim, interleaved, heads, hs);

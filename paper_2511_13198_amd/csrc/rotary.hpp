@@ -16,9 +16,13 @@
 // and x^10: the first terms left out are below 1.8e-9 and 1.2e-10 (x <= pi / 4), less
 // than a 32-bit rounding.
 //
-// Bound by memory: each element is read and written once.  A lane keeps the sines and
-// cosines of its 8 (4 of 32-bit elements) pairs of a token in registers and takes them
-// through the token's heads, so that they are computed once per token and lane.
+// Bound by memory: each element is read and written once.  A wave has one token: its
+// lanes compute the token's sines and cosines once, a pair each, and exchange them
+// through LDS; then D / (2 N) lanes take a head (16 bytes of input a lane and half), so
+// that the wave streams neighbouring heads, up to 2 KB at a time, with the next heads'
+// loads in flight.  65,536 tokens of 32/8 heads, bf16: 249 us (5.4 TB/s); with a lane's pairs
+// kept over one head after another of 8 tokens, 8 KB apart, 295 us.  131,072 of 4/4 in
+// 32 bits: 186 us (5.8).
 #pragma once
 #include "common.hpp"
 
@@ -34,7 +38,7 @@ struct RotaryArgs {
   const int32_t* pos;  // [tokens][axes]
   int tokens, axes;
   int pairs;
-  int heads_per_block;  // of q and k together; gridDim.y blocks of them
+  int rounds;  // of a wave over its token's heads; gridDim.y blocks of them
   int inverse;
   uint64_t freq[kMaxPairs];  // turns a position, as a fraction of 2^64
   uint8_t axis[kMaxPairs];
@@ -62,26 +66,10 @@ __device__ __forceinline__ void sincos_turn(uint32_t turn, float& sn, float& cs)
   cs = (quarter + 1) & 2 ? -b : b;
 }
 
-// N consecutive elements as floats, and back.
-template <int N>
-__device__ __forceinline__ void rot_load(const uint16_t* p, float (&x)[N]) {
-  static_assert(N == 8, "16 bytes");
-  const u32x4 v = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(v[i] << 16);
-    x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-  }
-}
-template <int N>
-__device__ __forceinline__ void rot_load(const float* p, float (&x)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    const f32x4 v = *reinterpret_cast<const f32x4*>(p + i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[i + e] = v[e];
-  }
-}
+__device__ __forceinline__ float rot_float(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+__device__ __forceinline__ float rot_float(float x) { return x; }
+
+// N consecutive outputs, rounded to nearest even.
 template <int N>
 __device__ __forceinline__ void rot_store(uint16_t* p, const float (&x)[N]) {
   uint32_t v[N / 2];
@@ -99,19 +87,22 @@ __device__ __forceinline__ void rot_store(float* p, const float (&x)[N]) {
     *reinterpret_cast<f32x4*>(p + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
 }
 
-// A lane has the units u and u + d / (2 N) of every head, of N elements each (16
-// bytes of input): as pairs p = u N + i, one element of each from either unit
-// (halves), or the N / 2 pairs of either unit (interleaved).  D / (2 N) lanes a
-// token; a workgroup takes 256 / that many tokens and heads_per_block heads of them.
-// Where `pairs` is below d / 2 the halves' second element is in unit (p + pairs) / N.
+// A lane has the units u and u + d / (2 N) of a head, of N elements each (16 bytes of
+// input): as pairs p = u N + i, one element of each from either unit (halves), or the
+// N / 2 pairs of either unit (interleaved).  Where `pairs` is below d / 2 the halves'
+// second elements are in unit (p + pairs) / N, and the lanes behind have the units that
+// are copied.
 template <class In, class Out, int D, bool INTER>
 __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a) {
   constexpr int N = 16 / sizeof(In);
   constexpr int LANES = D / (2 * N);
-  constexpr int TOKENS = 256 / LANES;
-  const int tok = blockIdx.x * TOKENS + threadIdx.x / LANES;
-  const int u = threadIdx.x % LANES;
+  constexpr int HEADS = 64 / LANES;  // a round
+  __shared__ f32x2 turn[4][kMaxPairs];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l = __lane_id();
+  const int tok = blockIdx.x * 4 + w;
   if (tok >= a.tokens) return;
+  const int u = l % LANES;
   // first elements of the lane's two units, and their first pairs (negative: copied)
   int e0, e1, p0, p1;
   const int rot = a.pairs / N;  // units of a half of the rotated part
@@ -129,58 +120,70 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a) {
     e1 = e0 + (D / 2 - a.pairs);
     p0 = p1 = -1;
   }
+  const int all = a.heads[0] + a.heads[1];
+  const int h_end = min(all, (int)(blockIdx.y + 1) * a.rounds * HEADS);
+  int h = blockIdx.y * a.rounds * HEADS + l / LANES;
+  // element offset of the lane's head, in q or k
+  auto at = [&](int head, int& t) __attribute__((always_inline)) {
+    t = head >= a.heads[0];
+    return ((size_t)tok * a.heads[t] + (t ? head - a.heads[0] : head)) * D;
+  };
+  In x[N], y[N];
+  auto load = [&](int head) __attribute__((always_inline)) {
+    int t;
+    const In* in = static_cast<const In*>(a.in[t = head >= a.heads[0]]) + at(head, t);
+    *reinterpret_cast<u32x4*>(x) = *reinterpret_cast<const u32x4*>(in + e0);
+    *reinterpret_cast<u32x4*>(y) = *reinterpret_cast<const u32x4*>(in + e1);
+  };
+  if (h < h_end) load(h);  // (on its way while the angles are computed)
+  if (l < a.pairs) {
+    const int64_t pos = a.pos[(size_t)tok * a.axes + a.axis[l]];
+    float sn, cs;
+    sincos_turn((uint32_t)(((uint64_t)pos * a.freq[l]) >> 32), sn, cs);
+    turn[w][l] = f32x2{a.inverse ? -sn : sn, cs};
+  }
+  wave_lds_fence();  // (a wave's own LDS operations complete in order)
   float sn[N], cs[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int p = INTER ? (i < N / 2 ? p0 : p1) : p0;
-    sn[i] = 0.f;
-    cs[i] = 1.f;
-    if (p >= 0) {
-      const int q = p + (INTER ? i % (N / 2) : i);
-      const int64_t at = a.pos[(size_t)tok * a.axes + a.axis[q]];
-      sincos_turn((uint32_t)(((uint64_t)at * a.freq[q]) >> 32), sn[i], cs[i]);
-      if (a.inverse) sn[i] = -sn[i];
-    }
+    const f32x2 v = turn[w][max(p, 0) + (INTER ? i % (N / 2) : i)];
+    sn[i] = v[0];
+    cs[i] = v[1];
   }
-  const int all = a.heads[0] + a.heads[1];
-  const int h_end = min(all, (int)(blockIdx.y + 1) * a.heads_per_block);
-  for (int h = blockIdx.y * a.heads_per_block; h < h_end; ++h) {
-    const int t = h >= a.heads[0];
-    const size_t off = ((size_t)tok * a.heads[t] + (t ? h - a.heads[0] : h)) * D;
-    const In* in = static_cast<const In*>(a.in[t]) + off;
-    Out* out = static_cast<Out*>(a.out[t]) + off;
-    float x[N], y[N], ox[N], oy[N];
-    rot_load(in + e0, x);
-    rot_load(in + e1, y);
+  for (; h < h_end; h += HEADS) {
+    float fx[N], fy[N], ox[N], oy[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      fx[i] = rot_float(x[i]);
+      fy[i] = rot_float(y[i]);
+    }
+    if (h + HEADS < h_end) load(h + HEADS);
     if (INTER) {
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) {
         const int j = N / 2 + i;
-        ox[2 * i] = x[2 * i] * cs[i] - x[2 * i + 1] * sn[i];
-        ox[2 * i + 1] = x[2 * i] * sn[i] + x[2 * i + 1] * cs[i];
-        oy[2 * i] = y[2 * i] * cs[j] - y[2 * i + 1] * sn[j];
-        oy[2 * i + 1] = y[2 * i] * sn[j] + y[2 * i + 1] * cs[j];
+        ox[2 * i] = fx[2 * i] * cs[i] - fx[2 * i + 1] * sn[i];
+        ox[2 * i + 1] = fx[2 * i] * sn[i] + fx[2 * i + 1] * cs[i];
+        oy[2 * i] = fy[2 * i] * cs[j] - fy[2 * i + 1] * sn[j];
+        oy[2 * i + 1] = fy[2 * i] * sn[j] + fy[2 * i + 1] * cs[j];
       }
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        ox[i] = x[i] * cs[i] - y[i] * sn[i];
-        oy[i] = x[i] * sn[i] + y[i] * cs[i];
+        ox[i] = fx[i] * cs[i] - fy[i] * sn[i];
+        oy[i] = fx[i] * sn[i] + fy[i] * cs[i];
       }
     }
-    if (!INTER && p0 < 0) {  // (copied as it is: a rotation by 0 would turn 0 * inf to NaN)
+    // (copied as it is: a rotation by 0 would turn infinities into NaN)
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        ox[i] = x[i];
-        oy[i] = y[i];
-      }
+    for (int i = 0; i < N; ++i) {
+      ox[i] = p0 < 0 ? fx[i] : ox[i];
+      oy[i] = p1 < 0 ? fy[i] : oy[i];
     }
-    if (INTER && p0 < 0)
-#pragma unroll
-      for (int i = 0; i < N; ++i) ox[i] = x[i];
-    if (INTER && p1 < 0)
-#pragma unroll
-      for (int i = 0; i < N; ++i) oy[i] = y[i];
+    int t;
+    const size_t off = at(h, t);
+    Out* out = static_cast<Out*>(a.out[t]) + off;
     rot_store(out + e0, ox);
     rot_store(out + e1, oy);
   }
