@@ -179,18 +179,38 @@ def forward_chains(steps: Sequence[Tuple[Range, Range, bool]], causal: bool
     return chains
 
 
+def _rotate_shards(q, k, ranges: Sequence[Sequence[Range]], devices, rotary: dict):
+    """q and k with every device's own ranges rotated by their positions."""
+    import torch
+    if devices is not None:
+        raise ValueError("rotary needs every device's shards: give rotated q and k instead of "
+                         "`devices`")
+    qr, kr = torch.empty_like(q), torch.empty_like(k)
+    rest = {n: x for n, x in rotary.items() if n != "positions"}
+    for own in ranges:
+        for a, b in own:
+            pdyattn.attn_rotary(q[a:b], k[a:b], rotary["positions"][a:b], out_q=qr[a:b],
+                                out_k=kr[a:b], **rest)
+    return qr, kr
+
+
 def ring_forward(q, k, v, p: int, causal: bool = True, scale: Optional[float] = None,
                  layout: str = "contiguous", devices: Optional[Iterable[int]] = None,
-                 out=None):
+                 out=None, rotary: Optional[dict] = None):
     """O [T, Hq, d] and {query range: LSE [Hq, len]} of the sequence, computed
     range pair by range pair in each device's ring order.  `devices` limits
     the work to those devices' query ranges (the rest of O is left as is).
+    rotary (positions [T, axes], sections, ...: the arguments of
+    pdyattn.attn_rotary): every device first rotates the q and k of its own
+    ranges, so that key shards travel rotated.
     A device's calls run as independent chains on two streams (a chain folds
     its pairs into its own partial result with attn_merge; the partials of a
     query range are merged at the end)."""
     import torch
     T, hq = q.shape[0], q.shape[1]
     ranges = device_ranges(T, p, layout)
+    if rotary is not None:
+        q, k = _rotate_shards(q, k, ranges, devices, rotary)
     o = torch.empty_like(q) if out is None else out
     lses: Dict[Range, object] = {}
     main = torch.cuda.current_stream(q.device)
@@ -243,16 +263,22 @@ def ring_forward(q, k, v, p: int, causal: bool = True, scale: Optional[float] = 
 
 def ring_backward(q, k, v, o, lses: Dict[Range, object], dout, p: int, causal: bool = True,
                   scale: Optional[float] = None, layout: str = "contiguous",
-                  devices: Optional[Iterable[int]] = None, grads=None):
+                  devices: Optional[Iterable[int]] = None, grads=None,
+                  rotary: Optional[dict] = None):
     """dQ [T, Hq, d], dK and dV [T, Hkv, d] (fp32) accumulated in the kernels
     over the range pairs, ring step by ring step.  With `devices` only those
     devices' calls run; a visiting shard's dK/dV then has to arrive in
     `grads` already holding the earlier devices' sums (zero for a timing).
-    Calls that write disjoint rows run two at a time on two streams."""
+    Calls that write disjoint rows run two at a time on two streams.
+    rotary: as in ring_forward, given the q and k from before the rotation;
+    the devices rotate the gradients of their own ranges back, so that dQ and
+    dK are those of the given q and k."""
     import torch
     T, hq, d = q.shape
     hkv = k.shape[1]
     ranges = device_ranges(T, p, layout)
+    if rotary is not None:
+        q, k = _rotate_shards(q, k, ranges, devices, rotary)
     if grads is None:
         grads = (torch.empty((T, hq, d), dtype=torch.float32, device=q.device),
                  torch.empty((T, hkv, d), dtype=torch.float32, device=q.device),
@@ -279,6 +305,12 @@ def ring_backward(q, k, v, o, lses: Dict[Range, object], dout, p: int, causal: b
                                                accumulate=accumulate, launches=len(group))
                 for i in range(len(group)):
                     main.wait_stream(side[i])
+    if rotary is not None:
+        rest = {n: x for n, x in rotary.items() if n != "positions"}
+        for own in ranges:
+            for a, b in own:
+                pdyattn.attn_rotary(dq[a:b], dk[a:b], rotary["positions"][a:b], inverse=True,
+                                    out_q=dq[a:b], out_k=dk[a:b], **rest)
     return dq, dk, dv
 
 

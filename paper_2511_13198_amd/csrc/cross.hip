@@ -118,7 +118,8 @@ constexpr int64_t kApartRows = 64, kApartPrefix = 512;
 CrossRows rows_launch(const CrossSizes& s, const RowKernel& k) {
   CrossRows f;
   pdy::CrossCut& c = f.cut;
-  const int64_t slice = s.tq * s.hq * (s.d + 1) * 4;  // bytes of one slice of partial results
+  // bytes of one slice of partial results (no queries: nothing is launched)
+  const int64_t slice = std::max<int64_t>(1, s.tq) * s.hq * (s.d + 1) * 4;
   c.keys = s.prefix == 0 ? pdy::CROSS_OWN
            : s.seq_rows() > kApartRows || s.prefix <= kApartPrefix || 2 * slice > kPartBytes
                ? pdy::CROSS_FUSED
@@ -499,6 +500,35 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
 }  // namespace
 
 extern "C" {
+
+pdy_status pdy_cross_launch_shapes(int32_t prefix_len, int32_t total_q, int32_t total_k,
+                                   int32_t num_seqs, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                                   int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim,
+                                   int32_t* shapes) {
+  g_err[0] = 0;
+  CrossSizes s;
+  const pdy_status st = check_cross_sizes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q,
+                                          max_seqlen_k, num_heads_q, num_heads_kv, head_dim, &s);
+  if (st != PDY_OK) return st;
+  if (shapes == nullptr) return fail(PDY_ERR_INVALID_ARG, "shapes is NULL");
+  std::fill(shapes, shapes + 10, 0);
+  auto put = [&](int i, const CrossShape& sh, const pdy::CrossCut& c) {
+    shapes[3 * i] = sh.nw;
+    shapes[3 * i + 1] = sh.groups;
+    shapes[3 * i + 2] = c.max_parts;
+  };
+  if (s.tq > 0) {
+    const CrossRows f = rows_launch(s, kFwd), q = rows_launch(s, kDq);
+    put(0, f.sh, f.cut);
+    put(1, q.sh, q.cut);
+    shapes[9] = f.cut.keys == pdy::CROSS_APART;
+  }
+  if (s.tk + s.prefix > 0) {
+    const CrossKv kv = kv_launch(s);
+    put(2, kv.sh, kv.cut);
+  }
+  return PDY_OK;
+}
 
 size_t attn_prefix_fwd_workspace_size(int32_t prefix_len, int32_t total_q, int32_t total_k,
                                       int32_t num_seqs, int32_t max_seqlen_q, int32_t max_seqlen_k,

@@ -119,21 +119,31 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // Sequence, tile and part of entry `entry` of a kv head's list; false past its end.
-// of(i, tiles, units): the i-th of the list's n sequences, its tiles and the units of
-// inner work of each.  One pass over the sequences, 64 at a time (two where the
-// launch is cut and they are more); the results are wave-uniform.
+// of(s, tiles, units): the tiles of a sequence and the units of inner work of each.
+// The list has the shared keys over the whole batch first where `shared` is set (index
+// 0), then the n sequences (index i, or i + 1): a lane each, 64 at a time in one pass
+// (two where the launch is cut and they are more).  The results are wave-uniform.
 template <class F>
-__device__ __forceinline__ bool cross_place(int n, const CrossCut& c, int entry, F&& of,
-                                            CrossPlace& out) {
-  const int l = __lane_id();
+__device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut& c, bool shared,
+                                            int entry, F&& of, CrossPlace& out) {
+  const int l = __lane_id(), n = b.n;
   CrossSeq s;
   int t, u;
   auto load = [&](int i) __attribute__((always_inline)) {
     s = CrossSeq{0, 0, 0, 0, 0};
     t = u = 0;
-    if (i < n) s = of(i, t, u);
+    if (i < n) {
+      s = cross_seq(b, i);
+      of(s, t, u);
+    }
   };
   load(l);
+  CrossSeq s0 = {0, 0, 0, 0, 0};
+  int t0 = 0, u0 = 0;
+  if (shared) {
+    s0 = cross_shared_seq(b);
+    of(s0, t0, u0);
+  }
   int cap = 1 << 30;
   if (c.max_parts > 1) {
     float units = (float)t * (float)u;
@@ -141,15 +151,33 @@ __device__ __forceinline__ bool cross_place(int n, const CrossCut& c, int entry,
       load(i0 + l);
       units += (float)t * (float)u;
     }
-    units = wave_sum(units);
+    units = wave_sum(units) + (float)t0 * (float)u0;
     cap = max(c.least, (int)fminf(units * c.share + 1.f, 1e9f));
     if (n > 64) load(l);
   }
-  // ceil(u / cap) as a float product: exact enough, as any whole number near it does
+  // ceil(u / cap) as a float product: any whole number near it does
   const float inv = 1.f / (float)cap;
+  auto parts_of = [&](int units) __attribute__((always_inline)) {
+    return max(1, min(c.max_parts, (int)ceilf((float)units * inv)));
+  };
+  auto place = [&](int at, int parts) __attribute__((always_inline)) {
+    out.nparts = parts;
+    out.tile = parts == 1 ? at : at / parts;
+    out.part = at - out.tile * parts;
+  };
   int base = 0;
+  if (shared) {
+    const int parts = parts_of(u0);
+    base = t0 * parts;
+    if (entry < base) {
+      out.s = s0;
+      out.index = 0;
+      place(entry, __builtin_amdgcn_readfirstlane(parts));
+      return true;
+    }
+  }
   for (int i0 = 0;;) {
-    const int parts = max(1, min(c.max_parts, (int)ceilf((float)u * inv)));
+    const int parts = parts_of(u);
     const int mine = t * parts;
     const int incl = wave_scan(mine);
     const int rel = entry - base;
@@ -160,11 +188,8 @@ __device__ __forceinline__ bool cross_place(int n, const CrossCut& c, int entry,
         return __builtin_amdgcn_readlane(v, src);
       };
       out.s = CrossSeq{get(s.q_lo), get(s.nq), get(s.k_lo), get(s.nk), get(s.room)};
-      out.index = i0 + src;
-      out.nparts = get(parts);
-      const int at = rel - get(incl - mine);
-      out.tile = out.nparts == 1 ? at : at / out.nparts;
-      out.part = at - out.tile * out.nparts;
+      out.index = i0 + src + (shared ? 1 : 0);
+      place(rel - get(incl - mine), get(parts));
       return true;
     }
     base += __builtin_amdgcn_readlane(incl, 63);
@@ -174,19 +199,15 @@ __device__ __forceinline__ bool cross_place(int n, const CrossCut& c, int entry,
   }
 }
 
-// The same for tiles of packed rows (forward, dQ); CROSS_APART: the shared keys come
-// first in the list.
+// The same for tiles of packed rows (forward, dQ).
 __device__ __forceinline__ bool cross_place_rows(const CrossBatch& b, const CrossCut& c, int entry,
                                                  CrossPlace& out) {
-  const int apart = c.keys == CROSS_APART;
+  const int pre = c.keys == CROSS_FUSED ? cross_tiles_log2(b.prefix, c.key_log2) : 0;
   return cross_place(
-      b.n + apart, c, entry,
-      [&](int i, int& tiles, int& units) __attribute__((always_inline)) {
-        const CrossSeq s = i < apart ? cross_shared_seq(b) : cross_seq(b, i - apart);
+      b, c, c.keys == CROSS_APART, entry,
+      [&](const CrossSeq& s, int& tiles, int& units) __attribute__((always_inline)) {
         tiles = cross_tiles_log2(s.nq * b.g, c.rows_log2);
-        units = cross_tiles_log2(s.nk, c.key_log2) +
-                (c.keys == CROSS_FUSED ? cross_tiles_log2(b.prefix, c.key_log2) : 0);
-        return s;
+        units = cross_tiles_log2(s.nk, c.key_log2) + pre;
       },
       out);
 }

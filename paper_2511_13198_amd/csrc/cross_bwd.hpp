@@ -390,20 +390,17 @@ __global__ void __launch_bounds__(NWAVES * 64, NWAVES == 4 ? 2 : D == 64 ? 3 : 1
   const int g = a.b.g;
   const int sh = a.pack_log2, sweeps = g >> sh;  // head groups of `pack` heads
   // the list: the shared keys over the whole batch (if any), then the sequences
-  const int first_own = a.b.prefix > 0 ? 1 : 0;
+  const bool pre = a.b.prefix > 0;
   CrossPlace at;
   if (!cross_place(
-          a.b.n + first_own, a.cut, entry,
-          [&](int i, int& tiles, int& units) __attribute__((always_inline)) {
-            const CrossSeq s =
-                i < first_own ? cross_shared_seq(a.b) : cross_seq(a.b, i - first_own);
+          a.b, a.cut, pre, entry,
+          [&](const CrossSeq& s, int& tiles, int& units) __attribute__((always_inline)) {
             tiles = cross_tiles_log2(s.room, a.cut.key_log2);
             units = s.nk > 0 ? cross_tiles(s.nq << sh, BQ) * sweeps : 0;
-            return s;
           },
           at))
     return;
-  const bool shared = at.index < first_own;
+  const bool shared = pre && at.index == 0;
   const CrossSeq sq = at.s;
   const uint16_t* const kin = shared ? a.kp : a.k;
   const uint16_t* const vin = shared ? a.vp : a.v;

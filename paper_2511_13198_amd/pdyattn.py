@@ -30,7 +30,7 @@ SYMBOLS = ("attn_fwd_workspace_size", "attn_bwd_workspace_size", "attn_fwd", "at
            "attn_prefix_fwd", "attn_cross_bwd_workspace_size", "attn_cross_bwd",
            "attn_prefix_bwd_workspace_size", "attn_prefix_bwd", "attn_rotary_turns", "attn_rotary",
            "attn_validate_cu_seqlens", "attn_bwd_noalloc", "pdy_launch_shapes",
-           "pdy_chunk_launch_shapes", "pdy_status_string", "pdy_last_error",
+           "pdy_chunk_launch_shapes", "pdy_cross_launch_shapes", "pdy_status_string", "pdy_last_error",
            "pdy_kernel_count", "pdy_kernel_name", "pdy_profile_start", "pdy_profile_stop")
 
 
@@ -109,6 +109,8 @@ def lib() -> ctypes.CDLL:
     L.pdy_launch_shapes.restype = i32
     L.pdy_chunk_launch_shapes.argtypes = [i32] * 9 + [ctypes.POINTER(i32)]
     L.pdy_chunk_launch_shapes.restype = i32
+    L.pdy_cross_launch_shapes.argtypes = [i32] * 9 + [ctypes.POINTER(i32)]
+    L.pdy_cross_launch_shapes.restype = i32
     L.pdy_status_string.argtypes = [i32]
     L.pdy_status_string.restype = ctypes.c_char_p
     L.pdy_last_error.argtypes = []
@@ -454,6 +456,18 @@ def prefix_bwd_workspace_size(prefix_len, total_q, total_k, num_seqs, max_seqlen
                                                     max_seqlen_q, max_seqlen_k, hq, hkv, d))
 
 
+def cross_launch_shapes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k, hq, hkv,
+                        d) -> dict:
+    """{kernel name: (waves, groups, parts at most)} of the launches of attn_cross_*
+    (prefix_len 0) and attn_prefix_*, and "apart": whether the shared keys are a list of
+    their own."""
+    out = (ctypes.c_int32 * 10)()
+    _check(lib().pdy_cross_launch_shapes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q,
+                                         max_seqlen_k, hq, hkv, d, out), "pdy_cross_launch_shapes")
+    names = ("cross_fwd_kernel", "cross_dq_kernel", "cross_dkdv_kernel")
+    return {**{n: tuple(out[3 * i:3 * i + 3]) for i, n in enumerate(names)}, "apart": bool(out[9])}
+
+
 def _launch(name: str, device, *args):
     """Calls the library on the tensors' device and its current stream (the last
     argument); the library launches on the current device."""
@@ -468,16 +482,19 @@ def _launch(name: str, device, *args):
         _check(st, name)
 
 
-def _check_tensors(device, *checks):
-    """(tensor, name, dtype, dims) of a call, all on one device."""
-    where = device.index if device.type == "cuda" else None
+def _fits(t, dtype, ndim: int, index) -> bool:
+    """Whether t is what a call asks for: type, dims, layout, device (by its index)."""
+    return (t.dtype is dtype and t.dim() == ndim and t.get_device() == index and
+            t.is_contiguous())
+
+
+def _refuse(device, *checks):
+    """Raises for the first (tensor, name, dtype, dims) that is not what a call asks for,
+    on a GPU and the one of the call's first tensor."""
     for t, name, dtype, ndim in checks:
-        # (the usual case in one line: this runs for every tensor of every call)
-        if (t.dtype is dtype and t.dim() == ndim and t.is_contiguous() and
-                t.get_device() == where):
-            continue
         _check_tensor(t, name, dtype, ndim)
-        raise ValueError(f"{name} is on {t.device}, the call's first tensor on {device}")
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the call's first tensor on {device}")
 
 
 def _longest(cu, name: str, total: int) -> int:
@@ -493,31 +510,39 @@ def _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k, scale, seqlens_k):
     import torch
     bf16, i32 = torch.bfloat16, torch.int32
     dev = q.device
-    _check_tensors(dev, (q, "q", bf16, 3), (k, "k", bf16, 3), (v, "v", bf16, 3),
-                   (cu_q, "cu_seqlens_q", i32, 1), (cu_k, "cu_seqlens_k", i32, 1))
+    index = dev.index
+    if not (_fits(q, bf16, 3, index) and _fits(k, bf16, 3, index) and _fits(v, bf16, 3, index) and
+            _fits(cu_q, i32, 1, index) and _fits(cu_k, i32, 1, index)):
+        _refuse(dev, (q, "q", bf16, 3), (k, "k", bf16, 3), (v, "v", bf16, 3),
+                (cu_q, "cu_seqlens_q", i32, 1), (cu_k, "cu_seqlens_k", i32, 1))
     T, hq, d = q.shape
-    tk, hkv, dk = k.shape
-    if dk != d or v.shape != k.shape:
+    tk, hkv, dk = shape = k.shape
+    if dk != d or v.shape != shape:
         raise ValueError("k and v must be [Tk, Hkv, d] with q's d")
-    n = cu_q.shape[0] - 1
-    if n < 1 or cu_k.shape[0] != n + 1:
+    n = cu_q.numel() - 1
+    if n < 1 or cu_k.numel() != n + 1:
         raise ValueError("cu_seqlens_q and cu_seqlens_k must have num_seqs + 1 >= 2 offsets each")
     used = 0
     if seqlens_k is not None:
-        _check_tensors(dev, (seqlens_k, "seqlens_k", i32, 1))
-        if seqlens_k.shape[0] != n:
+        if not _fits(seqlens_k, i32, 1, index):
+            _refuse(dev, (seqlens_k, "seqlens_k", i32, 1))
+        if seqlens_k.numel() != n:
             raise ValueError("seqlens_k must have num_seqs lengths")
         used = seqlens_k.data_ptr()
-    ptrs, pre = (q.data_ptr(), k.data_ptr(), v.data_ptr()), ()
-    if kp is not None:
-        _check_tensors(dev, (kp, "k_prefix", bf16, 3), (vp, "v_prefix", bf16, 3))
-        if kp.shape[1:] != (hkv, d) or vp.shape != kp.shape:
-            raise ValueError("k_prefix and v_prefix must be [P, Hkv, d]")
-        ptrs, pre = (*ptrs, kp.data_ptr(), vp.data_ptr()), (kp.shape[0],)
     max_q = _longest(cu_q, "cu_seqlens_q", T) if max_q is None else max_q
     max_k = _longest(cu_k, "cu_seqlens_k", tk) if max_k is None else max_k
-    return (dev, ptrs, (cu_q.data_ptr(), cu_k.data_ptr(), used, *pre), pre,
-            (n, T, tk, max_q, max_k, hq, hkv, d), 1.0 / math.sqrt(d) if scale is None else scale)
+    sizes = (n, T, tk, max_q, max_k, hq, hkv, d)
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    ptrs, offsets = (q.data_ptr(), k.data_ptr(), v.data_ptr()), (cu_q.data_ptr(), cu_k.data_ptr(), used)
+    if kp is None:
+        return dev, ptrs, offsets, (), sizes, scale
+    if not (_fits(kp, bf16, 3, index) and _fits(vp, bf16, 3, index)):
+        _refuse(dev, (kp, "k_prefix", bf16, 3), (vp, "v_prefix", bf16, 3))
+    shape = kp.shape
+    if shape[1] != hkv or shape[2] != d or vp.shape != shape:
+        raise ValueError("k_prefix and v_prefix must be [P, Hkv, d]")
+    return (dev, (*ptrs, kp.data_ptr(), vp.data_ptr()), (*offsets, shape[0]), (shape[0],), sizes,
+            scale)
 
 
 def _cross_workspace(kind: str, pre, sizes, device):
@@ -525,6 +550,18 @@ def _cross_workspace(kind: str, pre, sizes, device):
     n, T, tk, max_q, max_k, hq, hkv, d = sizes
     name = f"attn_{'prefix' if pre else 'cross'}_{kind}_workspace_size"
     return _ws(getattr(lib(), name)(*pre, T, tk, n, max_q, max_k, hq, hkv, d), device)
+
+
+def _check_outputs(dev, o, name: str, q, lse, workspace, hq: int, T: int):
+    """o like q, lse [Hq, T], a workspace, all on the device."""
+    import torch
+    index = dev.index
+    if not (_fits(o, torch.bfloat16, 3, index) and _fits(lse, torch.float32, 2, index) and
+            workspace.get_device() == index and workspace.is_contiguous()):
+        _refuse(dev, (o, name, torch.bfloat16, 3), (lse, "lse", torch.float32, 2),
+                (workspace, "workspace", workspace.dtype, workspace.dim()))
+    if o.shape != q.shape or lse.shape != (hq, T):
+        raise ValueError(f"{name} must be q's shape, lse [Hq, T]")
 
 
 def _cross_fwd(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k, causal, scale, seqlens_k, out, lse,
@@ -539,10 +576,7 @@ def _cross_fwd(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k, causal, scale, seqlens
         lse = torch.empty((hq, T), dtype=torch.float32, device=dev)
     if workspace is None:
         workspace = _cross_workspace("fwd", pre, sizes, dev)
-    _check_tensors(dev, (out, "out", torch.bfloat16, 3), (lse, "lse", torch.float32, 2),
-                   (workspace, "workspace", workspace.dtype, workspace.dim()))
-    if out.shape != q.shape or lse.shape != (hq, T):
-        raise ValueError("out must be q's shape, lse [Hq, T]")
+    _check_outputs(dev, out, "out", q, lse, workspace, hq, T)
     _launch("attn_prefix_fwd" if pre else "attn_cross_fwd", dev, *ptrs, *offsets, *sizes,
             1 if causal else 0, scale, out.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
             workspace.nbytes)
@@ -589,17 +623,18 @@ def _cross_bwd(q, k, v, kp, vp, o, lse, dout, cu_q, cu_k, max_q, max_k, causal, 
             continue
         if g is None:
             g = torch.empty(like.shape, dtype=dtype, device=dev)
-        _check_tensors(dev, (g, name, dtype, 3))
+        if not _fits(g, dtype, 3, dev.index):
+            _refuse(dev, (g, name, dtype, 3))
         if g.shape != like.shape:
             raise ValueError(f"{name} must be {list(like.shape)}")
         out.append(g)
     if workspace is None:
         workspace = _cross_workspace("bwd", pre, sizes, dev)
-    _check_tensors(dev, (o, "o", torch.bfloat16, 3), (dout, "dout", torch.bfloat16, 3),
-                   (lse, "lse", torch.float32, 2),
-                   (workspace, "workspace", workspace.dtype, workspace.dim()))
-    if o.shape != q.shape or dout.shape != q.shape or lse.shape != (sizes[5], sizes[1]):
-        raise ValueError("o and dout must match q, lse must be [Hq, T]")
+    if not _fits(dout, torch.bfloat16, 3, dev.index):
+        _refuse(dev, (dout, "dout", torch.bfloat16, 3))
+    if dout.shape != q.shape:
+        raise ValueError("dout must match q")
+    _check_outputs(dev, o, "o", q, lse, workspace, sizes[5], sizes[1])
     _launch("attn_prefix_bwd" if pre else "attn_cross_bwd", dev, *ptrs, o.data_ptr(),
             lse.data_ptr(), dout.data_ptr(), *offsets, *sizes, 1 if causal else 0, scale,
             1 if dtype is torch.bfloat16 else 0, *[g.data_ptr() for g in out],
@@ -668,43 +703,46 @@ def attn_rotary(q, k, positions, sections, base: float = 10000.0, freqs=None,
     first = q if q is not None else k
     if first is None:
         raise ValueError("attn_rotary needs q or k")
-    types = (torch.bfloat16, torch.float32)
+    dev, tin = first.device, first.dtype
+    index, types = dev.index, (torch.bfloat16, torch.float32)
     outs = out_q if out_q is not None else out_k
-    dtype = outs.dtype if outs is not None else out_dtype or first.dtype
-    if first.dtype not in types or dtype not in types:
+    tout = outs.dtype if outs is not None else out_dtype or tin
+    if tin not in types or tout not in types:
         raise TypeError("q, k and the outputs must be torch.bfloat16 or torch.float32, got "
-                        f"{first.dtype}, {dtype}")
-    dev = first.device
-    res, ptrs, heads = [], [], []
-    for name, t, o in (("q", q, out_q), ("k", k, out_k)):
+                        f"{tin}, {tout}")
+
+    if (q is None and out_q is not None) or (k is None and out_k is not None):
+        raise ValueError("out_q without q" if q is None else "out_k without k")
+
+    def side(name, t, o):
+        """(output, pointers of input and output, heads) of q or k."""
         if t is None:
-            if o is not None:
-                raise ValueError(f"out_{name} without {name}")
-            res.append(None)
-            ptrs += [0, 0]
-            heads.append(0)
-            continue
+            return None, 0, 0, 0
         if o is None:
-            o = torch.empty(t.shape, dtype=dtype, device=dev)
-        _check_tensors(dev, (t, name, first.dtype, 3), (o, f"out_{name}", dtype, 3))
+            o = torch.empty(t.shape, dtype=tout, device=dev)
+        if not (_fits(t, tin, 3, index) and _fits(o, tout, 3, index)):
+            _refuse(dev, (t, name, tin, 3), (o, f"out_{name}", tout, 3))
         if o.shape != t.shape:
             raise ValueError(f"out_{name} must have {name}'s shape")
-        res.append(o)
-        ptrs += [t.data_ptr(), o.data_ptr()]
-        heads.append(t.shape[1])
-    T, d = first.shape[0], first.shape[2]
+        return o, t.data_ptr(), o.data_ptr(), t.shape[1]
+
+    out_q, q_in, q_to, hq = side("q", q, out_q)
+    out_k, k_in, k_to, hkv = side("k", k, out_k)
+    T, _, d = first.shape
     if q is not None and k is not None and (k.shape[0] != T or k.shape[2] != d):
         raise ValueError("q and k must have the same tokens and head dimension")
     if positions.dim() == 1:
         positions = positions[:, None]
+    if not _fits(positions, torch.int32, 2, index):
+        _refuse(dev, (positions, "positions", torch.int32, 2))
     sections = tuple(sections)
-    _check_tensors(dev, (positions, "positions", torch.int32, 2))
-    if positions.shape != (T, len(sections)):
-        raise ValueError(f"positions must be [{T}, {len(sections)}] (tokens, sections), got "
+    axes = len(sections)
+    if positions.shape != (T, axes):
+        raise ValueError(f"positions must be [{T}, {axes}] (tokens, sections), got "
                          f"{list(positions.shape)}")
-    pairs, turns, axes, _ = _rotary_tables(sections, base, None if freqs is None else tuple(freqs))
-    _launch("attn_rotary", dev, ptrs[0], ptrs[2], positions.data_ptr(), T, len(sections), *heads,
-            d, pairs, turns, axes, 1 if interleaved else 0, 1 if inverse else 0,
-            1 if first.dtype is torch.float32 else 0, 1 if dtype is torch.float32 else 0, ptrs[1],
-            ptrs[3])
-    return res[0], res[1]
+    pairs, turns, pair_axes, _ = _rotary_tables(sections, base,
+                                                None if freqs is None else tuple(freqs))
+    _launch("attn_rotary", dev, q_in, k_in, positions.data_ptr(), T, axes, hq, hkv, d, pairs,
+            turns, pair_axes, 1 if interleaved else 0, 1 if inverse else 0,
+            1 if tin is torch.float32 else 0, 1 if tout is torch.float32 else 0, q_to, k_to)
+    return out_q, out_k

@@ -28,6 +28,11 @@ CASES = [
     ([300, 0, 515], [777, 5, 2049], None, 0, 4, 4, 128, False),
     ([1200], [3000], None, 0, 6, 2, 64, True),
     ([70] * 60, [129] * 60, None, 0, 5, 1, 64, False),
+    ([20, 9, 1], [300, 700, 65], None, 0, 4, 2, 64, True),
+    # enough key tiles to fill the chip: short rows, long ones
+    ([30, 1, 17, 8, 30, 30, 2, 9], [500] * 8, [500, 499, 1, 0, 256, 128, 300, 500], 0, 16, 16, 128, False),
+    ([600, 700], [9000, 7500], None, 0, 16, 16, 128, True),
+    ([530, 601], [9100, 7401], None, 0, 16, 16, 64, False),
     # more sequences than lanes
     ([1 + i % 3 for i in range(150)], [(37 * i) % 90 for i in range(150)], None, 0, 2, 1, 128, True),
     # shared keys: few rows behind many of them (apart), others; one key, no own keys
@@ -146,3 +151,118 @@ def test_gradients(case, dtype):
         end = t if name == "dq" else g.shape[0] if name.endswith("p") else tk
         cu.check(name, g[:end], tuple(r[:end] for r in ref[name]))
         assert (g[end:] == 7.0).all(), f"{name}: rows of no sequence were written"
+
+
+def test_results_repeat_bit_for_bit():
+    import torch
+    for case in (CASES[2], CASES[11], CASES[-5]):
+        x, _, args, len_k = setup(case, 2)
+        runs = []
+        for _ in range(3):
+            o, lse = forward(x, args, len_k)
+            runs.append((o, lse) + backward(x, o, lse, args, len_k))
+        t, tk = sum(case[0]), sum(case[1])
+        for a in runs[1:]:
+            for i, (p, r) in enumerate(zip(a, runs[0])):
+                n = (slice(None), slice(0, t)) if i == 1 else slice(0, tk if i in (3, 4) else t if i < 3 else None)
+                assert torch.equal(p[n], r[n])
+
+
+def test_nothing_in_use():
+    """No queries: gradients of the keys are zero.  No keys at all: o = 0, lse = -inf."""
+    import torch
+    from paper_2511_13198_amd import pdyattn
+    k = torch.randn(40, 2, 64, device="cuda").to(torch.bfloat16)
+    none = torch.empty(0, 4, 64, dtype=torch.bfloat16, device="cuda")
+    lse0 = torch.empty(4, 0, device="cuda")
+    cq, ck = cu.offsets([0, 0], "cuda"), cu.offsets([30, 10], "cuda")
+    dq, dk, dv, dkp, dvp = pdyattn.attn_prefix_bwd(none, k, k, k, k, none, lse0, none, cq, ck,
+                                                   dk=torch.full_like(k, 7.0))
+    assert dq.shape == none.shape
+    for g in (dk, dv, dkp, dvp):
+        assert (g == 0).all()
+    q = torch.randn(5, 4, 64, device="cuda").to(torch.bfloat16)
+    nokeys = torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    cq, ck = cu.offsets([2, 3], "cuda"), cu.offsets([0, 0], "cuda")
+    o, lse = pdyattn.attn_cross_fwd(q, nokeys, nokeys, cq, ck)
+    assert (o == 0).all() and (lse == -math.inf).all()
+    dq, dk, dv = pdyattn.attn_cross_bwd(q, nokeys, nokeys, o, lse, q, cq, ck)
+    assert (dq == 0).all() and dk.shape == nokeys.shape
+
+
+def test_not_a_number_and_infinite_logits():
+    """A row that sees a NaN or +inf logit gets o = NaN, lse = -inf, whole or in parts;
+    one whose logits are all -inf sees nothing; other rows are as without."""
+    import torch
+    from paper_2511_13198_amd import pdyattn
+    for lk in (100, 9000):
+        x = make([4], [lk], 0, 2, 2, 128, 3, behind=0)
+        cq, ck = cu.offsets([4], "cuda"), cu.offsets([lk], "cuda")
+        clean = pdyattn.attn_cross_fwd(x["q"], x["k"], x["v"], cq, ck)
+        x["q"][1, 0, 5] = math.nan
+        x["q"][2, 1] = math.inf
+        o, lse = pdyattn.attn_cross_fwd(x["q"], x["k"], x["v"], cq, ck)
+        for t, h in ((1, 0), (2, 1)):
+            assert torch.isnan(o[t, h]).all() and lse[h, t] == -math.inf
+            o[t, h], lse[h, t] = clean[0][t, h], clean[1][h, t]
+        assert torch.equal(o, clean[0]) and torch.equal(lse, clean[1])
+        k = x["k"].clone()
+        k[:, 0] = -math.inf
+        q = x["q"].clone()
+        q[:, 0] = 1.0
+        o, lse = pdyattn.attn_cross_fwd(q, k, x["v"], cq, ck)
+        assert (o[:, 0] == 0).all() and (lse[0] == -math.inf).all()
+
+
+def test_wrong_offsets_stay_inside():
+    """Offsets that fall, leave the tensors or contradict max_seqlen give some result,
+    without touching the rows they cannot mean."""
+    import torch
+    from paper_2511_13198_amd import pdyattn
+    x = make([20, 30], [100, 200], 0, 4, 2, 64, 4, behind=0)
+    for cq, ck in (([0, 40, 20], [0, 100, 300]), ([0, 20, 5000], [0, 100, 9000]),
+                   ([0, -5, 50], [50, 20, 300]), ([0, 1, 50], [0, 0, -1])):
+        cq = torch.tensor(cq, dtype=torch.int32, device="cuda")
+        ck = torch.tensor(ck, dtype=torch.int32, device="cuda")
+        used = torch.tensor([10 ** 9, -7], dtype=torch.int32, device="cuda")
+        for len_k in (None, used):
+            o, lse = pdyattn.attn_cross_fwd(x["q"], x["k"], x["v"], cq, ck, 30, 200, True,
+                                            seqlens_k=len_k)
+            pdyattn.attn_cross_bwd(x["q"], x["k"], x["v"], x["q"], torch.zeros_like(lse), x["do"],
+                                   cq, ck, 30, 200, True, seqlens_k=len_k)
+        torch.cuda.synchronize()
+
+
+def test_cache_beyond_32_bit_offsets():
+    """Keys whose element offsets pass 2^31, at the cache's end."""
+    import torch
+    from paper_2511_13198_amd import pdyattn
+    hkv, d, slots, n = 8, 128, 1 << 18, 9  # 2.4e9 elements
+    free, _ = torch.cuda.mem_get_info()
+    if free < 24 << 30:
+        pytest.skip("needs 24 GiB of device memory")
+    k = torch.zeros((n * slots, hkv, d), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    used = [3, 0, 5, 1, 0, 0, 0, 7, 700]
+    for s, u in enumerate(used):
+        for t in (k, v):
+            t[s * slots:s * slots + u] = torch.randn((u, hkv, d), generator=g, device="cuda").to(
+                torch.bfloat16)
+    q = torch.randn((n, 16, d), generator=g, device="cuda").to(torch.bfloat16)
+    do = torch.randn((n, 16, d), generator=g, device="cuda").to(torch.bfloat16)
+    cq, ck = cu.offsets([1] * n, "cuda"), cu.offsets([slots] * n, "cuda")
+    len_k = torch.tensor(used, dtype=torch.int32, device="cuda")
+    o, lse = pdyattn.attn_cross_fwd(q, k, v, cq, ck, 1, slots, True, seqlens_k=len_k)
+    at = torch.cat([torch.arange(s * slots, s * slots + u) for s, u in enumerate(used)]).cuda()
+    ref = cu.reference(q, k[at], v[at], cu.offsets([1] * n), cu.offsets(used), True, d ** -0.5,
+                       do=do)
+    cu.check("o", o, ref["o"])
+    cu.check("lse", lse, ref["lse"])
+    dq, dk, dv = pdyattn.attn_cross_bwd(q, k, v, o, lse, do, cq, ck, 1, slots, True,
+                                        seqlens_k=len_k, grad_dtype=torch.bfloat16)
+    cu.check("dq", dq, ref["dq"])
+    cu.check("dk", dk[at], ref["dk"])
+    cu.check("dv", dv[at], ref["dv"])
+    dk[at] = 0
+    assert not dk.any()
