@@ -337,7 +337,7 @@ pdy_status pdy_chunk_launch_shapes(int32_t tq, int32_t tk, int32_t q_offset, int
 pdy_status pdy_cross_launch_shapes(int32_t prefix_len, int32_t total_q, int32_t total_k,
                                    int32_t num_seqs, int32_t max_seqlen_q, int32_t max_seqlen_k,
                                    int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim,
-                                   int32_t* shapes);
+                                   int32_t causal, int32_t* shapes);
 
 /* Static text for a status code. */
 const char* pdy_status_string(int32_t status);

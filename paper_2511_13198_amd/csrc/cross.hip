@@ -66,20 +66,17 @@ int64_t most_items(const CrossSizes& s, int64_t n, int64_t max_q, int rows) {
 
 // ---- tiles of rows: forward and dQ ----
 
-// Rows of a sequence decide the workgroups' shape: the smallest tile that holds
-// them; few rows leave the waves to key groups.  4-wave workgroups share a CU by two,
-// so that one's start, end and products overlap the other's copies; 8 waves over 256
-// rows read K and V least often.  us at 32 / 64 / 128 rows a sequence with tiles of
-// 32 (4 key groups), 64 (2), 128 and 256 rows, d = 128:
+// Workgroup shapes: 32 rows in 4 key groups, 64 in 2, 128, and 8 waves over 256.  4-wave
+// workgroups share a CU by two, so that one's start, end and products overlap the
+// other's copies; 8 waves over 256 rows read K and V least often.  Up to 64 rows a
+// sequence the smallest tile that holds them is taken.  us with tiles of 32, 64, 128
+// and 256 rows, forward, d = 128:
 //   17 x 1-5 tokens, 24/8 heads, 900-9,000 keys (15 rows) 64 with 32-row tiles and two
 //   workgroups a CU, 80 with one; 32 x 8 tokens, 32/4 heads, 256-8,192 keys (64 rows)
-//   52 / 52 / 58 with 64, 128, 256; 32 x 32, 32/8 heads (128 rows) 97 / 82 / 91;
-//   a step of 8 x 256-2,048 over 1,024-8,192 keys, forward 332 / 257 / 251.
-CrossShape row_shape(int64_t rows) {
+//   52 / 52 / 58 with 64, 128, 256 rows; 32 x 32, 32/8 heads (128 rows) 97 / 82 / 91.
+CrossShape few_rows_shape(int64_t rows) {
   if (rows <= 32) return {4, 4};
-  if (rows <= 64) return {4, 2};
-  if (rows <= 128) return {4, 1};
-  return {8, 1};
+  return rows <= 64 ? CrossShape{4, 2} : CrossShape{4, 1};
 }
 
 // What the forward and the dQ kernel differ in.
@@ -90,9 +87,22 @@ struct RowKernel {
     if (sh.nw == 4) return sh.groups == 4 ? 128 : 64;
     return s.d == 128 ? 128 : 64;
   }
-  CrossShape shape(int64_t rows) const {
-    const CrossShape sh = row_shape(rows);
-    return dq && sh.groups == 4 ? CrossShape{4, 2} : sh;
+  // workgroups of a shape on the chip at a time (d = 64: by registers and LDS)
+  int64_t slots(const CrossSizes& s, const CrossShape& sh) const {
+    if (sh.nw == 8) return s.d == 64 ? 2 * kCUs : kCUs;
+    return s.d == 64 && !dq ? 3 * kCUs : 2 * kCUs;
+  }
+  // a workgroup's time on 64 keys, alone on its CU or beside others: d = 128, 200 rows x
+  // 30,810 keys x 16 heads (64 x 484 such units) and 8 x 256-2,048 rows over 1,024-8,192
+  // keys, 32/8 heads (a full chip); d = 64, 4 x 281-1,127 rows behind 24,028 keys
+  double unit_us(const CrossSizes& s, const CrossShape& sh, bool full) const {
+    if (s.d == 64) {
+      if (sh.nw == 8) return full ? 1.9 : 1.2;
+      return sh.groups == 1 ? (full ? 1.9 : 1.1) : full ? 0.95 : 0.85;
+    }
+    if (sh.nw == 8) return dq ? 1.75 : 1.48;
+    if (sh.groups == 1) return dq ? (full ? 2.0 : 1.4) : full ? 1.6 : 1.46;
+    return dq ? (full ? 1.1 : 0.85) : 1.1;
   }
 };
 constexpr RowKernel kFwd{false}, kDq{true};
@@ -106,6 +116,7 @@ struct CrossRows {
 
 constexpr int kMaxParts = 64;
 constexpr int64_t kPartBytes = (int64_t)256 << 20;  // partial results at most
+constexpr double kMoveBytesPerUs = 4.0e6;           // partial results written and read back
 
 // Few rows a sequence behind many shared keys: these once for the rows of all
 // sequences, apart from the sequences' own keys, with partial results of both.  Fused,
@@ -115,7 +126,47 @@ constexpr int64_t kPartBytes = (int64_t)256 << 20;  // partial results at most
 //   rows) 99 / 138, of 32 (128 rows, 40 sequences, a step) 853 / 858.
 constexpr int64_t kApartRows = 64, kApartPrefix = 512;
 
-CrossRows rows_launch(const CrossSizes& s, const RowKernel& k) {
+// Shape and parts of a launch over sequences of more than 64 rows: the ones of least
+// estimated time, from the average rows and keys of a sequence.  With I items of u
+// units in p parts, on `slots` workgroups at a time,
+//   rounds = ceil(I p / slots), time = rounds (start + u / p unit) + partial results.
+// parts = 1: whole.  us measured, 256-row tiles / 128 whole / 128 in parts (their sums
+// included): 9 x 427 rows x 4 heads 56 / 59 / 57, 51 x 79 x 16 64 / 49 / 57, 2,000 x 8
+// over 3,000 keys 79 / 76 / 54, 4 x 1,041 x 8 causal 37 / 38 / 44.
+struct RowsChoice {
+  CrossShape sh;
+  int parts;
+  int64_t entries;  // of all heads: whole rounds
+};
+RowsChoice choose_rows(const CrossSizes& s, const RowKernel& k, bool causal) {
+  const double own = std::min<double>((double)s.max_k, (double)s.tk / s.n);
+  const double seen = causal ? std::max(own - 0.5 * s.tq / s.n, 0.5 * own) : own;
+  const double keys = seen + s.prefix, rows = (double)s.tq * s.g();
+  RowsChoice best{{8, 1}, 1, 0};
+  double least = 1e30;
+  for (const CrossShape& sh : {CrossShape{8, 1}, CrossShape{4, 1}, CrossShape{4, 2}}) {
+    if (sh.rows() >= 2 * s.seq_rows()) continue;
+    const int64_t slots = k.slots(s, sh);
+    const double items = std::min(rows / sh.rows() + 0.5 * s.n,
+                                  (double)most_items(s, s.n, s.max_q, sh.rows())) * s.hkv;
+    const double units = std::max(1.0, keys / 64);
+    for (int p = 1; p <= kMaxParts && p <= std::max(1.0, units / 4); ++p) {
+      const double bytes = (double)p * rows * s.hkv * s.d * 4;
+      if (p > 1 && bytes > kPartBytes) break;
+      const double rounds = std::ceil(items * p / slots);
+      const double unit = k.unit_us(s, sh, items * p > kCUs);
+      const double t = rounds * (7.0 + units / p * unit) +
+                       (p > 1 ? 5.0 + 2.0 * bytes / kMoveBytesPerUs : 0.0);
+      if (t < (p > 1 ? 0.95 : 1.0) * least) {
+        least = t;
+        best = {sh, p, (int64_t)rounds * slots};
+      }
+    }
+  }
+  return best;
+}
+
+CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
   CrossRows f;
   pdy::CrossCut& c = f.cut;
   // bytes of one slice of partial results (no queries: nothing is launched)
@@ -125,24 +176,35 @@ CrossRows rows_launch(const CrossSizes& s, const RowKernel& k) {
                ? pdy::CROSS_FUSED
                : pdy::CROSS_APART;
   const bool apart = c.keys == pdy::CROSS_APART;
-  f.sh = k.shape(s.seq_rows());
-  if (apart) f.sh = k.shape(std::min<int64_t>(128, s.tq * s.g()));
+  int64_t most = kMaxParts, entries;  // parts of an item, and of all
+  if (s.seq_rows() > 64) {
+    const RowsChoice r = choose_rows(s, k, causal);
+    f.sh = r.sh;
+    entries = r.entries;
+    if (r.parts == 1) most = 1;
+  } else {
+    f.sh = few_rows_shape(apart ? s.tq * s.g() : s.seq_rows());
+    // (few rows are bound by reading keys, of lengths that the host does not know:
+    // more parts than fit at a time even them out)
+    const bool few = f.sh.groups == 4;
+    if (k.dq && few) f.sh = {4, 2};
+    entries = (few ? 4 : 2) * kCUs;
+    if (!apart && most_items(s, s.n, s.max_q, f.sh.rows()) * s.hkv >= (few ? 16 : 2) * kCUs)
+      most = 1;
+  }
   const int rows = f.sh.rows(), keys_tile = k.key_tile(s, f.sh);
   c.rows_log2 = __builtin_ctz((unsigned)rows);
   c.key_log2 = __builtin_ctz((unsigned)keys_tile);
   c.least = 2;
   const int64_t items =
       most_items(s, s.n, s.max_q, rows) + (apart ? ceil_div(s.tq * s.g(), rows) : 0);
-  const bool few = f.sh.groups == 4;  // (partial results are small then)
-  const int64_t target = (few ? 4 : 2) * kCUs;
-  c.share = (float)((double)s.hkv / target);
+  c.entries = (int)ceil_div(entries, s.hkv);
+  c.even = s.seq_rows() > 64;
   const int64_t own = ceil_div(s.max_k, keys_tile), pre = ceil_div(s.prefix, keys_tile);
   const int64_t tiles = apart ? std::max(own, pre) : own + pre;
-  int64_t parts =
-      std::min<int64_t>({kMaxParts, tiles / c.least, kPartBytes / (slice * (apart ? 2 : 1))});
-  if (!apart && items * s.hkv >= (few ? 16 : 2) * kCUs) parts = 1;
-  c.max_parts = (int)std::max<int64_t>(1, parts);
-  f.wgs = items + (c.max_parts > 1 ? ceil_div(target, s.hkv) + 2 : 0);
+  most = std::min<int64_t>({most, tiles / c.least, kPartBytes / (slice * (apart ? 2 : 1))});
+  c.max_parts = (int)std::max<int64_t>(1, most);
+  f.wgs = items + (c.max_parts > 1 ? c.entries + 2 : 0);
   return f;
 }
 
@@ -183,26 +245,29 @@ CrossKv kv_launch(const CrossSizes& s) {
   auto items = [&](int tile) {
     return std::min(s.tk / tile + s.n, s.n * ceil_div(s.max_k, tile)) + ceil_div(s.prefix, tile);
   };
-  // Few rows a sequence, so few steps a tile: two 4-wave workgroups a CU; else 256-key
-  // tiles where they fill the chip four times over, two query groups over 128 where not
-  // (16 sequences of 64-1,024 rows behind 4,096 keys, 32/8 heads: 564 + 29 us of sums
-  // with 256-key tiles, 546 + 19 with groups; 32 x 8-200 rows over 577-1,024 keys, 16
-  // heads of 64: 63 us, 110 with groups, 60 with 4 waves).
-  if (s.tq * s.g() <= 512 * s.n && items(128) * s.hkv >= 2 * kCUs) k.sh = {4, 1};
+  // Few rows a sequence, so few steps a tile, or d = 64: two 4-wave workgroups a CU; else
+  // 256-key tiles where they fill the chip four times over, two query groups over 128
+  // where not.  us with 4 waves, 8, and 8 in groups: 16 sequences of 64-1,024 rows behind
+  // 4,096 keys, 32/8 heads 616 / 607 / 580; 9 x 427 rows x 273-2,190 keys, 16/4 heads 84 /
+  // 93 / 76; 51 x 79 behind 385, 16 heads 70 / 77 / 84; d = 64, 32 x 8-200 rows over
+  // 577-1,024 keys, 16 heads 60 / 63 / 110, 4 x 281-1,127 behind 24,028, 16/8 heads 419 /
+  // 438 / 487.
+  if (items(128) * s.hkv >= 2 * kCUs && (s.d == 64 || s.tq * s.g() <= 512 * s.n)) k.sh = {4, 1};
   else k.sh = {8, items(256) * s.hkv >= 4 * kCUs ? 1 : 2};
   pdy::CrossCut& c = k.cut;
   c.keys = pdy::CROSS_FUSED;
   c.rows_log2 = c.key_log2 = __builtin_ctz((unsigned)k.sh.rows());
   c.least = 4;
-  const int64_t n = items(k.sh.rows()), target = 2 * kCUs;
-  c.share = (float)((double)s.hkv / target);
+  const int64_t n = items(k.sh.rows()), target = kCUs;
+  c.entries = (int)ceil_div(target, s.hkv);
+  c.even = 0;
   const int64_t slice = (s.prefix + s.tk) * s.hkv * s.d * 8;
   int64_t parts = std::min<int64_t>(16, slice ? kPartBytes / slice : 1);
   // items alike in their rows need no cut once they fill the chip; a shared tile has
   // the rows of all sequences
   if (n * s.hkv >= target && (s.prefix == 0 || s.n == 1)) parts = 1;
   c.max_parts = (int)std::max<int64_t>(1, parts);
-  k.wgs = n + (c.max_parts > 1 ? ceil_div(target, s.hkv) + 2 : 0);
+  k.wgs = n + (c.max_parts > 1 ? c.entries + 2 : 0);
   return k;
 }
 
@@ -257,11 +322,12 @@ constexpr CrossKernels row_kernels() {
   return {NW, G, {launch_fwd<64, NW, G>, launch_fwd<128, NW, G>},
           {launch_dq<64, NW, G>, launch_dq<128, NW, G>}, {nullptr, nullptr}};
 }
+// (dK/dV of d = 64 has no 256-key tiles: no launch takes them)
 template <int NW, int G>
 constexpr CrossKernels with_dkdv(CrossKernels k) {
   k.nw = NW;
   k.groups = G;
-  k.dkdv[0] = launch_dkdv<64, NW, G>;
+  if constexpr (NW == 4 || G > 1) k.dkdv[0] = launch_dkdv<64, NW, G>;
   k.dkdv[1] = launch_dkdv<128, NW, G>;
   return k;
 }
@@ -330,7 +396,7 @@ pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal,
   if ((st = check_cross_in(x, s)) || (st = check_ptr(o, "o")) || (st = check_ptr(lse, "lse")) ||
       (st = check_ptr(workspace, "workspace")))
     return st;
-  const CrossRows f = rows_launch(s, kFwd);
+  const CrossRows f = rows_launch(s, kFwd, causal != 0);
   const size_t need = fwd_bytes(s, f);
   if (workspace_bytes < need)
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, %s needs %zu", workspace_bytes, who,
@@ -394,7 +460,7 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
       ((st = check_ptr(g.dkp, "dk_prefix")) || (st = check_ptr(g.dvp, "dv_prefix"))))
     return st;
   if ((st = check_ptr(workspace, "workspace")) != PDY_OK) return st;
-  const CrossRows f = rows_launch(s, kDq);
+  const CrossRows f = rows_launch(s, kDq, causal != 0);
   const CrossKv kv = kv_launch(s);
   const CrossBwdSpace sp = bwd_space(s, f, kv);
   if (workspace_bytes < sp.total)
@@ -504,12 +570,13 @@ extern "C" {
 pdy_status pdy_cross_launch_shapes(int32_t prefix_len, int32_t total_q, int32_t total_k,
                                    int32_t num_seqs, int32_t max_seqlen_q, int32_t max_seqlen_k,
                                    int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim,
-                                   int32_t* shapes) {
+                                   int32_t causal, int32_t* shapes) {
   g_err[0] = 0;
   CrossSizes s;
   const pdy_status st = check_cross_sizes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q,
                                           max_seqlen_k, num_heads_q, num_heads_kv, head_dim, &s);
   if (st != PDY_OK) return st;
+  if (causal != 0 && causal != 1) return fail(PDY_ERR_INVALID_ARG, "causal must be 0 or 1");
   if (shapes == nullptr) return fail(PDY_ERR_INVALID_ARG, "shapes is NULL");
   std::fill(shapes, shapes + 10, 0);
   auto put = [&](int i, const CrossShape& sh, const pdy::CrossCut& c) {
@@ -518,7 +585,7 @@ pdy_status pdy_cross_launch_shapes(int32_t prefix_len, int32_t total_q, int32_t 
     shapes[3 * i + 2] = c.max_parts;
   };
   if (s.tq > 0) {
-    const CrossRows f = rows_launch(s, kFwd), q = rows_launch(s, kDq);
+    const CrossRows f = rows_launch(s, kFwd, causal != 0), q = rows_launch(s, kDq, causal != 0);
     put(0, f.sh, f.cut);
     put(1, q.sh, q.cut);
     shapes[9] = f.cut.keys == pdy::CROSS_APART;
@@ -537,7 +604,10 @@ size_t attn_prefix_fwd_workspace_size(int32_t prefix_len, int32_t total_q, int32
   if (check_cross_sizes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k,
                         num_heads_q, num_heads_kv, head_dim, &s) != PDY_OK)
     return 0;
-  return s.tq == 0 ? 256 : fwd_bytes(s, rows_launch(s, kFwd));
+  // (enough for both masks)
+  return s.tq == 0 ? 256
+                   : std::max(fwd_bytes(s, rows_launch(s, kFwd, false)),
+                              fwd_bytes(s, rows_launch(s, kFwd, true)));
 }
 
 size_t attn_cross_fwd_workspace_size(int32_t total_q, int32_t total_k, int32_t num_seqs,
@@ -588,7 +658,9 @@ size_t attn_prefix_bwd_workspace_size(int32_t prefix_len, int32_t total_q, int32
   if (check_cross_sizes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k,
                         num_heads_q, num_heads_kv, head_dim, &s) != PDY_OK)
     return 0;
-  return bwd_space(s, rows_launch(s, kDq), kv_launch(s)).total;
+  const CrossKv kv = kv_launch(s);
+  return std::max(bwd_space(s, rows_launch(s, kDq, false), kv).total,
+                  bwd_space(s, rows_launch(s, kDq, true), kv).total);
 }
 
 size_t attn_cross_bwd_workspace_size(int32_t total_q, int32_t total_k, int32_t num_seqs,

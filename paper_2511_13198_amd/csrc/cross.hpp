@@ -66,10 +66,13 @@ enum CrossKeys : int {
 // a sequence and kv head (dK/dV: a tile of keys); its inner work, key tiles (row
 // tiles), is cut into parts, one workgroup each, whose partial results another
 // kernel combines:
-//   units = sum over the items of their inner tiles,
-//   a part has at most C = max(least, units * hkv / target) of them, so that the
-//   parts are alike whatever the lengths, there are about `target` of them, and
-//   a launch with that many items is not cut (C is then above their inner tiles).
+//   a part has at most C = max(least, units / entries) inner tiles, the units being all
+//   items' of a kv head: about `entries` parts, alike whatever the lengths, and up to
+//   one an item more.
+// EVEN and `even` (tiles of many rows, up to 64 sequences): C is the least from there on with which
+// the parts are no more than `entries`, so that they fit the rounds on the chip that
+// the host planned for (6 sequences of 500-2,000 rows behind 16,384 keys, 4 heads: 648
+// parts where 512 fit, 299 us, 432 of them 264).
 // Every workgroup computes C from the offsets, so that nothing waits for the host.
 struct CrossCut {
   int keys;       // CrossKeys
@@ -77,7 +80,8 @@ struct CrossCut {
   int key_log2;   // keys per tile
   int max_parts;  // of an item; 1: not cut
   int least;      // fewest inner tiles of a part
-  float share;    // hkv / target
+  int entries;    // parts of a kv head
+  int even;       // whole rounds (EVEN)
 };
 
 struct CrossPlace {
@@ -103,6 +107,16 @@ __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31
   return x;
 }
+// The largest of the lanes' values (>= 0).
+__device__ __forceinline__ int wave_max(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(x, 63);
+}
 __device__ __forceinline__ float wave_sum(float v) {
   auto add = [&](auto Ctrl, auto Rows) __attribute__((always_inline)) {
     v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(Ctrl)::value,
@@ -123,7 +137,7 @@ __device__ __forceinline__ float wave_sum(float v) {
 // The list has the shared keys over the whole batch first where `shared` is set (index
 // 0), then the n sequences (index i, or i + 1): a lane each, 64 at a time in one pass
 // (two where the launch is cut and they are more).  The results are wave-uniform.
-template <class F>
+template <bool EVEN, class F>
 __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut& c, bool shared,
                                             int entry, F&& of, CrossPlace& out) {
   const int l = __lane_id(), n = b.n;
@@ -152,18 +166,34 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
       units += (float)t * (float)u;
     }
     units = wave_sum(units) + (float)t0 * (float)u0;
-    cap = max(c.least, (int)fminf(units * c.share + 1.f, 1e9f));
-    if (n > 64) load(l);
+    cap = max(c.least, (int)fminf(units / (float)c.entries + 1.f, 1e9f));
+    if (n > 64) {
+      load(l);
+    } else if (EVEN && c.even) {
+      // the least C from there on whose parts are few enough: by bisection, at most
+      // up to the largest item (the parts get fewer as C grows)
+      int hi = max(u0, wave_max(t > 0 ? u : 0));
+      while (cap < hi) {
+        const int mid = (cap + hi) >> 1;
+        const float inv = 1.f / (float)mid;
+        const int e = __builtin_amdgcn_readlane(wave_scan(t * (int)ceilf((float)u * inv)), 63) +
+                      t0 * (int)ceilf((float)u0 * inv);
+        if (e <= c.entries) hi = mid;
+        else cap = mid + 1;
+      }
+    }
   }
   // ceil(u / cap) as a float product: any whole number near it does
   const float inv = 1.f / (float)cap;
   auto parts_of = [&](int units) __attribute__((always_inline)) {
     return max(1, min(c.max_parts, (int)ceilf((float)units * inv)));
   };
-  auto place = [&](int at, int parts) __attribute__((always_inline)) {
+  // a part's tiles one after another: workgroups that run at a time then stream the
+  // same keys (rows), which L2 holds once
+  auto place = [&](int at, int tiles, int parts) __attribute__((always_inline)) {
     out.nparts = parts;
-    out.tile = parts == 1 ? at : at / parts;
-    out.part = at - out.tile * parts;
+    out.part = parts == 1 ? 0 : at / tiles;
+    out.tile = at - out.part * tiles;
   };
   int base = 0;
   if (shared) {
@@ -172,7 +202,7 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
     if (entry < base) {
       out.s = s0;
       out.index = 0;
-      place(entry, __builtin_amdgcn_readfirstlane(parts));
+      place(entry, t0, __builtin_amdgcn_readfirstlane(parts));
       return true;
     }
   }
@@ -189,7 +219,7 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
       };
       out.s = CrossSeq{get(s.q_lo), get(s.nq), get(s.k_lo), get(s.nk), get(s.room)};
       out.index = i0 + src + (shared ? 1 : 0);
-      place(rel - get(incl - mine), get(parts));
+      place(rel - get(incl - mine), get(t), get(parts));
       return true;
     }
     base += __builtin_amdgcn_readlane(incl, 63);
@@ -200,10 +230,11 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
 }
 
 // The same for tiles of packed rows (forward, dQ).
+template <bool EVEN>
 __device__ __forceinline__ bool cross_place_rows(const CrossBatch& b, const CrossCut& c, int entry,
                                                  CrossPlace& out) {
   const int pre = c.keys == CROSS_FUSED ? cross_tiles_log2(b.prefix, c.key_log2) : 0;
-  return cross_place(
+  return cross_place<EVEN>(
       b, c, c.keys == CROSS_APART, entry,
       [&](const CrossSeq& s, int& tiles, int& units) __attribute__((always_inline)) {
         tiles = cross_tiles_log2(s.nq * b.g, c.rows_log2);

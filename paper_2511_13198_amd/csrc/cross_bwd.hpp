@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : N
   int hk, entry;
   xcd_order(blockIdx.x, gridDim.x, a.b.hkv, hk, entry);
   CrossPlace at;
-  if (!cross_place_rows(a.b, a.cut, entry, at)) return;
+  if (!cross_place_rows<KG == 1>(a.b, a.cut, entry, at)) return;
   const int g = a.b.g;
   const CrossSeq sq = at.s;
   const int row_end = (sq.q_lo + sq.nq) * g;
@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(NWAVES * 64, NWAVES == 4 ? 2 : D == 64 ? 3 : 1
   // the list: the shared keys over the whole batch (if any), then the sequences
   const bool pre = a.b.prefix > 0;
   CrossPlace at;
-  if (!cross_place(
+  if (!cross_place<false>(
           a.b, a.cut, pre, entry,
           [&](const CrossSeq& s, int& tiles, int& units) __attribute__((always_inline)) {
             tiles = cross_tiles_log2(s.room, a.cut.key_log2);

@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1)
   int hk, entry;
   xcd_order(blockIdx.x, gridDim.x, a.b.hkv, hk, entry);
   CrossPlace at;
-  if (!cross_place_rows(a.b, a.cut, entry, at)) return;
+  if (!cross_place_rows<KG == 1>(a.b, a.cut, entry, at)) return;
   const int g = a.b.g;
   const CrossSeq sq = at.s;
   const int row_end = (sq.q_lo + sq.nq) * g;  // packed rows of the sequence end

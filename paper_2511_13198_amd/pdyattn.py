@@ -109,7 +109,7 @@ def lib() -> ctypes.CDLL:
     L.pdy_launch_shapes.restype = i32
     L.pdy_chunk_launch_shapes.argtypes = [i32] * 9 + [ctypes.POINTER(i32)]
     L.pdy_chunk_launch_shapes.restype = i32
-    L.pdy_cross_launch_shapes.argtypes = [i32] * 9 + [ctypes.POINTER(i32)]
+    L.pdy_cross_launch_shapes.argtypes = [i32] * 10 + [ctypes.POINTER(i32)]
     L.pdy_cross_launch_shapes.restype = i32
     L.pdy_status_string.argtypes = [i32]
     L.pdy_status_string.restype = ctypes.c_char_p
@@ -457,13 +457,14 @@ def prefix_bwd_workspace_size(prefix_len, total_q, total_k, num_seqs, max_seqlen
 
 
 def cross_launch_shapes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k, hq, hkv,
-                        d) -> dict:
+                        d, causal: bool = False) -> dict:
     """{kernel name: (waves, groups, parts at most)} of the launches of attn_cross_*
     (prefix_len 0) and attn_prefix_*, and "apart": whether the shared keys are a list of
     their own."""
     out = (ctypes.c_int32 * 10)()
     _check(lib().pdy_cross_launch_shapes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q,
-                                         max_seqlen_k, hq, hkv, d, out), "pdy_cross_launch_shapes")
+                                         max_seqlen_k, hq, hkv, d, int(bool(causal)), out),
+           "pdy_cross_launch_shapes")
     names = ("cross_fwd_kernel", "cross_dq_kernel", "cross_dkdv_kernel")
     return {**{n: tuple(out[3 * i:3 * i + 3]) for i, n in enumerate(names)}, "apart": bool(out[9])}
 

@@ -101,37 +101,48 @@ def test_workspace_sizes():
 def test_shapes_of_launches_and_what_the_gpu_cases_cover():
     """The rules' two sides, and that the GPU tests' cases reach every kernel and
     combining path at both head dimensions."""
-    shape = lambda n, q, k, hq, hkv, d, pre=0: P.cross_launch_shapes(  # noqa: E731
-        pre, n * q, n * k, n, q, k, hq, hkv, d)
-    for rows, fwd, dq in ((32, (4, 4), (4, 2)), (33, (4, 2), (4, 2)), (64, (4, 2), (4, 2)),
-                          (65, (4, 1), (4, 1)), (128, (4, 1), (4, 1)), (129, (8, 1), (8, 1))):
+    def shape(n, q, k, hq, hkv, d, pre=0, causal=False):
+        return P.cross_launch_shapes(pre, n * q, n * k, n, q, k, hq, hkv, d, causal)
+
+    # up to 64 rows the smallest tile that holds them; a group's heads are rows
+    for rows, fwd, dq in ((32, (4, 4), (4, 2)), (33, (4, 2), (4, 2)), (64, (4, 2), (4, 2))):
         s = shape(2, rows, 500, 4, 4, 128)
         assert s["cross_fwd_kernel"][:2] == fwd and s["cross_dq_kernel"][:2] == dq
-    assert shape(2, 8, 500, 32, 8, 64)["cross_fwd_kernel"][:2] == (4, 4)  # a group's heads are rows
+        assert shape(2, rows // 4, 500, 16, 4, 128)["cross_fwd_kernel"][:2] == few(rows // 4 * 4)
+    # then by the estimate: small tiles for launches that do not fill the chip, the
+    # largest, whole, for those that do, parts where few rows see many keys
+    assert shape(4, 300, 600, 3, 1, 128)["cross_fwd_kernel"] == (4, 2, 1)
+    assert shape(50, 80, 464, 16, 16, 128)["cross_fwd_kernel"] == (4, 1, 1)
+    assert shape(64, 512, 512, 32, 32, 128)["cross_fwd_kernel"] == (8, 1, 1)
+    assert shape(1, 200, 30000, 16, 16, 128)["cross_fwd_kernel"][2] > 8
     assert shape(4, 1, 100, 8, 2, 128, 513)["apart"] and not shape(4, 1, 100, 8, 2, 128, 512)["apart"]
     assert not shape(4, 17, 100, 8, 2, 128, 4000)["apart"]
-    assert shape(64, 512, 512, 32, 32, 128)["cross_fwd_kernel"][2] == 1  # fills the chip: no parts
     seen = set()
     for lq, lk, used, prefix, hq, hkv, d, causal in gpu.CASES:
         s = P.cross_launch_shapes(prefix, sum(lq) + 3, sum(lk) + 3, len(lq), max(lq), max(lk), hq,
-                                  hkv, d)
+                                  hkv, d, causal)
         for kernel in ("cross_fwd_kernel", "cross_dq_kernel", "cross_dkdv_kernel"):
             w, g, parts = s[kernel]
             seen |= {(kernel, w, g, d), (kernel, "parts" if parts > 1 else "whole", d)}
         seen.add(("apart", s["apart"], d))
     want = {("cross_fwd_kernel", *s, d) for s in ((4, 4), (4, 2), (4, 1), (8, 1)) for d in (64, 128)}
     want |= {("cross_dq_kernel", *s, d) for s in ((4, 2), (4, 1), (8, 1)) for d in (64, 128)}
-    want |= {("cross_dkdv_kernel", *s, d) for s in ((4, 1), (8, 1), (8, 2)) for d in (64, 128)}
+    want |= {("cross_dkdv_kernel", *s, d) for s in ((4, 1), (8, 2)) for d in (64, 128)}
+    want.add(("cross_dkdv_kernel", 8, 1, 128))
     want |= {(k, p, d) for k in ("cross_fwd_kernel", "cross_dq_kernel", "cross_dkdv_kernel")
              for p in ("parts", "whole") for d in (64, 128)}
     want |= {("apart", a, d) for a in (True, False) for d in (64, 128)}
     assert not want - seen, sorted(map(str, want - seen))
 
 
+def few(rows):
+    return (4, 4) if rows <= 32 else (4, 2)
+
+
 def test_shape_query_refusals():
     with pytest.raises(P.PdyError):
         P.cross_launch_shapes(0, 10, 10, 2, 11, 5, 8, 8, 128)
-    assert P.lib().pdy_cross_launch_shapes(0, 10, 10, 2, 5, 5, 8, 8, 128, None) == P.PDY_ERR_INVALID_ARG
+    assert P.lib().pdy_cross_launch_shapes(0, 10, 10, 2, 5, 5, 8, 8, 128, 0, None) == P.PDY_ERR_INVALID_ARG
     assert set(P.cross_launch_shapes(0, 0, 0, 2, 0, 0, 8, 8, 128).values()) == {(0, 0, 0), False}
 
 

@@ -9,7 +9,7 @@ from tests import test_isa_lds_waits as isa
 CSRC = os.path.dirname(isa.SRC)
 
 
-@pytest.mark.parametrize("src,reads,kernels", [("cross.hip", 1000, 20), ("rotary.hip", 0, 12)])
+@pytest.mark.parametrize("src,reads,kernels", [("cross.hip", 1000, 19), ("rotary.hip", 0, 12)])
 def test_lds_waits_and_no_scratch(src, reads, kernels):
     asm = isa.device_asm(os.path.join(CSRC, src))
     hazards, checked = isa.lds_wait_hazards(asm)
