@@ -200,6 +200,7 @@ CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
       most_items(s, s.n, s.max_q, rows) + (apart ? ceil_div(s.tq * s.g(), rows) : 0);
   c.entries = (int)ceil_div(entries, s.hkv);
   c.even = s.seq_rows() > 64;
+  c.list = nullptr;
   const int64_t own = ceil_div(s.max_k, keys_tile), pre = ceil_div(s.prefix, keys_tile);
   const int64_t tiles = apart ? std::max(own, pre) : own + pre;
   most = std::min<int64_t>({most, tiles / c.least, kPartBytes / (slice * (apart ? 2 : 1))});
@@ -214,6 +215,10 @@ int slices_of(const CrossRows& f) {
                                         : f.cut.max_parts > 1 ? f.cut.max_parts : 0;
 }
 
+// The list of a launch over more sequences than lanes.
+size_t list_bytes(const CrossSizes& s) {
+  return s.n > pdy::kListLanes ? align256((size_t)(s.n + 2) * 4) : 0;
+}
 size_t part_n_bytes(const CrossSizes& s) { return align256((size_t)s.tq * 2 * 4); }
 size_t part_o_bytes(const CrossSizes& s, int slices) {
   return align256((size_t)slices * s.tq * s.hq * s.d * 4);
@@ -224,7 +229,8 @@ size_t part_lse_bytes(const CrossSizes& s, int slices) {
 
 size_t fwd_bytes(const CrossSizes& s, const CrossRows& f) {
   const int n = slices_of(f);
-  return n == 0 ? 256 : part_n_bytes(s) + part_o_bytes(s, n) + part_lse_bytes(s, n);
+  return list_bytes(s) +
+         (n == 0 ? 256 : part_n_bytes(s) + part_o_bytes(s, n) + part_lse_bytes(s, n));
 }
 
 // ---- tiles of keys: dK, dV ----
@@ -256,7 +262,9 @@ CrossKv kv_launch(const CrossSizes& s) {
   else k.sh = {8, items(256) * s.hkv >= 4 * kCUs ? 1 : 2};
   pdy::CrossCut& c = k.cut;
   c.keys = pdy::CROSS_FUSED;
-  c.rows_log2 = c.key_log2 = __builtin_ctz((unsigned)k.sh.rows());
+  c.key_log2 = __builtin_ctz((unsigned)k.sh.rows());
+  c.rows_log2 = k.sh.nw == 4 && s.d == 128 ? 5 : 6;  // CrossDkdvCfg::BQ
+  c.list = nullptr;
   c.least = 4;
   const int64_t n = items(k.sh.rows()), target = kCUs;
   c.entries = (int)ceil_div(target, s.hkv);
@@ -271,12 +279,14 @@ CrossKv kv_launch(const CrossSizes& s) {
   return k;
 }
 
-// Workspace of a backward: D, the counts of parts, the partial dQ, and dK and dV.
+// Workspace of a backward: the lists, D, the counts of parts, the partial dQ, and dK and
+// dV.
 struct CrossBwdSpace {
-  size_t dd, counts_q, counts_k, part_q, part_kv, total;
+  size_t list, dd, counts_q, counts_k, part_q, part_kv, total;
 };
 CrossBwdSpace bwd_space(const CrossSizes& s, const CrossRows& q, const CrossKv& kv) {
   CrossBwdSpace x;
+  x.list = list_bytes(s);
   x.dd = align256((size_t)s.hq * s.tq * 4);
   x.counts_q = slices_of(q) ? part_n_bytes(s) : 0;
   x.counts_k = kv.cut.max_parts > 1 ? align256((size_t)(s.prefix + s.tk) * 4) : 0;
@@ -284,7 +294,7 @@ CrossBwdSpace bwd_space(const CrossSizes& s, const CrossRows& q, const CrossKv& 
   x.part_kv = kv.cut.max_parts > 1 ? align256((size_t)kv.cut.max_parts * (s.prefix + s.tk) *
                                               s.hkv * s.d * 4)
                                    : 0;
-  x.total = std::max<size_t>(256, x.dd + x.counts_q + x.counts_k + x.part_q + 2 * x.part_kv);
+  x.total = std::max<size_t>(256, 2 * x.list + x.dd + x.counts_q + x.counts_k + x.part_q + 2 * x.part_kv);
   return x;
 }
 
@@ -387,6 +397,21 @@ pdy::CrossBatch batch_of(const CrossIn& x, const CrossSizes& s, int32_t causal) 
                          causal};
 }
 
+// The lists of a launch over rows, over keys (NULL: none), or both.
+hipError_t launch_lists(const pdy::CrossBatch& b, const pdy::CrossCut* q, const pdy::CrossCut* kv,
+                        int pack_log2, hipStream_t hs) {
+  pdy::CrossListArgs l{b, {}, {}, pack_log2};
+  int n = 0;
+  if (q) l.cut[n++] = *q;
+  if (kv) {
+    l.kv[n] = 1;
+    l.cut[n++] = *kv;
+  }
+  return launch_timed(K_CROSS_LIST, hs, [&] {
+    hipLaunchKernelGGL(pdy::cross_list_kernel, dim3(n), dim3(pdy::kListThreads), 0, hs, l);
+  });
+}
+
 pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal, float scale,
                           void* o, float* lse, void* workspace, size_t workspace_bytes,
                           void* stream, const char* who) {
@@ -396,7 +421,7 @@ pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal,
   if ((st = check_cross_in(x, s)) || (st = check_ptr(o, "o")) || (st = check_ptr(lse, "lse")) ||
       (st = check_ptr(workspace, "workspace")))
     return st;
-  const CrossRows f = rows_launch(s, kFwd, causal != 0);
+  CrossRows f = rows_launch(s, kFwd, causal != 0);
   const size_t need = fwd_bytes(s, f);
   if (workspace_bytes < need)
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, %s needs %zu", workspace_bytes, who,
@@ -406,7 +431,8 @@ pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal,
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
 
   const int slices = slices_of(f);
-  uint8_t* const w = reinterpret_cast<uint8_t*>(workspace);
+  uint8_t* const lists = reinterpret_cast<uint8_t*>(workspace);
+  uint8_t* const w = lists + list_bytes(s);
   pdy::CrossFwdArgs a;
   a.q = static_cast<const uint16_t*>(x.q);
   a.k = static_cast<const uint16_t*>(x.k);
@@ -416,6 +442,11 @@ pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal,
   a.o = static_cast<uint16_t*>(o);
   a.lse = lse;
   a.b = batch_of(x, s, causal);
+  if (list_bytes(s)) {
+    f.cut.list = reinterpret_cast<int32_t*>(lists);
+    e = launch_lists(a.b, &f.cut, nullptr, 0, hs);
+    if (e != hipSuccess) return hip_fail(e, "cross_list_kernel launch");
+  }
   a.cut = f.cut;
   a.scale_log2 = scale * pdy::kLog2e;
   a.part_n = slices ? reinterpret_cast<int32_t*>(w) : nullptr;
@@ -460,8 +491,8 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
       ((st = check_ptr(g.dkp, "dk_prefix")) || (st = check_ptr(g.dvp, "dv_prefix"))))
     return st;
   if ((st = check_ptr(workspace, "workspace")) != PDY_OK) return st;
-  const CrossRows f = rows_launch(s, kDq, causal != 0);
-  const CrossKv kv = kv_launch(s);
+  CrossRows f = rows_launch(s, kDq, causal != 0);
+  CrossKv kv = kv_launch(s);
   const CrossBwdSpace sp = bwd_space(s, f, kv);
   if (workspace_bytes < sp.total)
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, %s needs %zu", workspace_bytes, who,
@@ -476,6 +507,7 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
     w += bytes;
     return r;
   };
+  uint8_t* const lists = take(2 * sp.list);
   float* dd = reinterpret_cast<float*>(take(sp.dd));
   int32_t* counts_q = reinterpret_cast<int32_t*>(take(sp.counts_q));
   int32_t* counts_k = reinterpret_cast<int32_t*>(take(sp.counts_k));
@@ -503,9 +535,16 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
   a.scale = scale;
   a.scale_log2 = scale * pdy::kLog2e;
   a.pack_log2 = pack_log2(s);
+  const bool rows = s.tq > 0, keys = s.tk + s.prefix > 0;
+  if (sp.list) {
+    f.cut.list = reinterpret_cast<int32_t*>(lists);
+    kv.cut.list = reinterpret_cast<int32_t*>(lists + sp.list);
+    e = launch_lists(a.b, rows ? &f.cut : nullptr, keys ? &kv.cut : nullptr, a.pack_log2, hs);
+    if (e != hipSuccess) return hip_fail(e, "cross_list_kernel launch");
+  }
 
   // dQ first: it also writes D, which dK/dV reads
-  if (s.tq > 0) {
+  if (rows) {
     a.cut = f.cut;
     a.part = part_q;
     a.part2 = nullptr;
@@ -515,7 +554,7 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
                      [&] { (void)cross_kernels(f.sh).dq[s.d == 128](&a, grid, hs); });
     if (e != hipSuccess) return hip_fail(e, "cross_dq_kernel launch");
   }
-  if (s.tk + s.prefix > 0) {
+  if (keys) {
     a.cut = kv.cut;
     a.part = part_k;
     a.part2 = part_v;
@@ -539,7 +578,7 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
                                             end, dst, b};
     blocks += b;
   };
-  if (s.tq > 0 && slices_of(f) > 0)
+  if (rows && slices_of(f) > 0)
     add(part_q, counts_q, f.cut.keys == pdy::CROSS_APART ? counts_q + s.tq : nullptr,
         f.cut.max_parts, s.hq, s.tq * s.hq, 0, s.tq * s.hq, x.cu_q + s.n, g.dq);
   if (kv.cut.max_parts > 1) {

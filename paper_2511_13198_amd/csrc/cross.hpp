@@ -69,19 +69,28 @@ enum CrossKeys : int {
 //   a part has at most C = max(least, units / entries) inner tiles, the units being all
 //   items' of a kv head: about `entries` parts, alike whatever the lengths, and up to
 //   one an item more.
-// EVEN and `even` (tiles of many rows, up to 64 sequences): C is the least from there on with which
+// EVEN and `even` (tiles of many rows, up to kListLanes sequences): C is the least from there on with which
 // the parts are no more than `entries`, so that they fit the rounds on the chip that
 // the host planned for (6 sequences of 500-2,000 rows behind 16,384 keys, 4 heads: 648
 // parts where 512 fit, 299 us, 432 of them 264).
-// Every workgroup computes C from the offsets, so that nothing waits for the host.
+// C follows from the offsets on the GPU, so that nothing waits for the host: every
+// workgroup computes it, and its place in the list, with a lane per sequence; of more
+// sequences than lanes cross_list_kernel writes the list once and a workgroup searches
+// it, 64 starts at a time (fwd + bwd of sequences of 1-32 rows over 1-64 keys, 8 heads,
+// d = 64, us with every workgroup passing over all sequences / with the list: 128 of
+// them 38 / 43, 256 71 / 72, 1,024 331 / 240, 16,384 31,600 / 3,880).
+constexpr int kListLanes = 64;
 struct CrossCut {
   int keys;       // CrossKeys
-  int rows_log2;  // packed rows per tile
+  int rows_log2;  // packed rows per tile (dK/dV: per step)
   int key_log2;   // keys per tile
   int max_parts;  // of an item; 1: not cut
   int least;      // fewest inner tiles of a part
   int entries;    // parts of a kv head
   int even;       // whole rounds (EVEN)
+  // more than kListLanes sequences: entries of a kv head before each sequence's (after
+  // the shared keys') [n], their number, and C; else NULL
+  int32_t* list;
 };
 
 struct CrossPlace {
@@ -132,44 +141,105 @@ __device__ __forceinline__ float wave_sum(float v) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
+// Tiles of a sequence and the units of inner work of each: tiles of packed rows over
+// keys (forward, dQ), and tiles of keys over steps of rows (dK/dV; 2^pack_log2 heads of
+// the group to a step).
+__device__ __forceinline__ void cross_row_units(const CrossBatch& b, const CrossCut& c,
+                                                const CrossSeq& s, int& tiles, int& units) {
+  const int pre = c.keys == CROSS_FUSED ? cross_tiles_log2(b.prefix, c.key_log2) : 0;
+  tiles = cross_tiles_log2(s.nq * b.g, c.rows_log2);
+  units = cross_tiles_log2(s.nk, c.key_log2) + pre;
+}
+__device__ __forceinline__ void cross_key_units(const CrossBatch& b, const CrossCut& c,
+                                                int pack_log2, const CrossSeq& s, int& tiles,
+                                                int& units) {
+  tiles = cross_tiles_log2(s.room, c.key_log2);
+  units = s.nk > 0 ? cross_tiles_log2(s.nq << pack_log2, c.rows_log2) * (b.g >> pack_log2) : 0;
+}
+
+// C for items of so many units of inner work.
+__device__ __forceinline__ int cross_cap(const CrossCut& c, float units) {
+  return c.max_parts > 1 ? max(c.least, (int)fminf(units / (float)c.entries + 1.f, 1e9f)) : 1 << 30;
+}
+// Parts of an item of `units`: ceil(units / cap) as a float product (any whole number
+// near it does).
+__device__ __forceinline__ int cross_parts(const CrossCut& c, float inv_cap, int units) {
+  return max(1, min(c.max_parts, (int)ceilf((float)units * inv_cap)));
+}
+
 // Sequence, tile and part of entry `entry` of a kv head's list; false past its end.
-// of(s, tiles, units): the tiles of a sequence and the units of inner work of each.
-// The list has the shared keys over the whole batch first where `shared` is set (index
-// 0), then the n sequences (index i, or i + 1): a lane each, 64 at a time in one pass
-// (two where the launch is cut and they are more).  The results are wave-uniform.
+// of(s, tiles, units): as above.  The list has the shared keys over the whole batch first
+// where `shared` is set (index 0), then the n sequences (index i, or i + 1).  The
+// results are wave-uniform.
 template <bool EVEN, class F>
 __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut& c, bool shared,
                                             int entry, F&& of, CrossPlace& out) {
   const int l = __lane_id(), n = b.n;
-  CrossSeq s;
-  int t, u;
-  auto load = [&](int i) __attribute__((always_inline)) {
-    s = CrossSeq{0, 0, 0, 0, 0};
-    t = u = 0;
-    if (i < n) {
-      s = cross_seq(b, i);
-      of(s, t, u);
-    }
-  };
-  load(l);
   CrossSeq s0 = {0, 0, 0, 0, 0};
   int t0 = 0, u0 = 0;
   if (shared) {
     s0 = cross_shared_seq(b);
     of(s0, t0, u0);
   }
+  // a part's tiles one after another: workgroups that run at a time then stream the
+  // same keys (rows), which L2 holds once
+  auto place = [&](int at, int tiles, int parts) __attribute__((always_inline)) {
+    out.nparts = parts;
+    out.part = parts == 1 ? 0 : at / tiles;
+    out.tile = at - out.part * tiles;
+  };
+  auto in_shared = [&](float inv) __attribute__((always_inline)) {
+    const int parts = __builtin_amdgcn_readfirstlane(cross_parts(c, inv, u0));
+    if (entry < t0 * parts) {
+      out.s = s0;
+      out.index = 0;
+      place(entry, t0, parts);
+    }
+    return t0 * parts;
+  };
+  if (c.list) {
+    const float inv = 1.f / (float)c.list[n + 1];
+    int rel = entry;
+    if (shared) {
+      const int base = in_shared(inv);
+      if (entry < base) return true;
+      rel -= base;
+    }
+    if (rel >= c.list[n]) return false;
+    // the last sequence that starts at `rel` or before: of 64 evenly spaced ones, of
+    // the 64th part behind the one found, ...
+    int lo = 0, span = n, start = 0;
+    while (true) {
+      const int step = (span + 63) >> 6;
+      const int x = l * step < span ? c.list[lo + l * step] : 0x7fffffff;
+      const int k = max(0, __builtin_popcountll(__builtin_amdgcn_ballot_w64(x <= rel)) - 1);
+      start = __builtin_amdgcn_readlane(x, k);
+      lo += k * step;
+      span = min(step, span - k * step);
+      if (step == 1) break;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    const CrossSeq s = cross_seq(b, lo);
+    int t, u;
+    of(s, t, u);
+    const int parts = cross_parts(c, inv, u);
+    // (always, unless the offsets are wrong)
+    if ((uint32_t)(rel - start) >= (uint32_t)(t * parts)) return false;
+    out.s = CrossSeq{s.q_lo, s.nq, s.k_lo, s.nk, s.room};
+    out.index = lo + (shared ? 1 : 0);
+    place(rel - start, __builtin_amdgcn_readfirstlane(t), __builtin_amdgcn_readfirstlane(parts));
+    return true;
+  }
+  CrossSeq s = {0, 0, 0, 0, 0};
+  int t = 0, u = 0;
+  if (l < n) {
+    s = cross_seq(b, l);
+    of(s, t, u);
+  }
   int cap = 1 << 30;
   if (c.max_parts > 1) {
-    float units = (float)t * (float)u;
-    for (int i0 = 64; i0 < n; i0 += 64) {
-      load(i0 + l);
-      units += (float)t * (float)u;
-    }
-    units = wave_sum(units) + (float)t0 * (float)u0;
-    cap = max(c.least, (int)fminf(units / (float)c.entries + 1.f, 1e9f));
-    if (n > 64) {
-      load(l);
-    } else if (EVEN && c.even) {
+    cap = cross_cap(c, wave_sum((float)t * (float)u) + (float)t0 * (float)u0);
+    if (EVEN && c.even) {
       // the least C from there on whose parts are few enough: by bisection, at most
       // up to the largest item (the parts get fewer as C grows)
       int hi = max(u0, wave_max(t > 0 ? u : 0));
@@ -183,64 +253,108 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
       }
     }
   }
-  // ceil(u / cap) as a float product: any whole number near it does
   const float inv = 1.f / (float)cap;
-  auto parts_of = [&](int units) __attribute__((always_inline)) {
-    return max(1, min(c.max_parts, (int)ceilf((float)units * inv)));
-  };
-  // a part's tiles one after another: workgroups that run at a time then stream the
-  // same keys (rows), which L2 holds once
-  auto place = [&](int at, int tiles, int parts) __attribute__((always_inline)) {
-    out.nparts = parts;
-    out.part = parts == 1 ? 0 : at / tiles;
-    out.tile = at - out.part * tiles;
-  };
-  int base = 0;
+  int rel = entry;
   if (shared) {
-    const int parts = parts_of(u0);
-    base = t0 * parts;
-    if (entry < base) {
-      out.s = s0;
-      out.index = 0;
-      place(entry, t0, __builtin_amdgcn_readfirstlane(parts));
-      return true;
-    }
+    const int base = in_shared(inv);
+    if (entry < base) return true;
+    rel -= base;
   }
-  for (int i0 = 0;;) {
-    const int parts = parts_of(u);
-    const int mine = t * parts;
-    const int incl = wave_scan(mine);
-    const int rel = entry - base;
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(rel >= incl - mine && rel < incl);
-    if (hit) {
-      const int src = __builtin_ctzll(hit);
-      auto get = [&](int v) __attribute__((always_inline)) {
-        return __builtin_amdgcn_readlane(v, src);
-      };
-      out.s = CrossSeq{get(s.q_lo), get(s.nq), get(s.k_lo), get(s.nk), get(s.room)};
-      out.index = i0 + src + (shared ? 1 : 0);
-      place(rel - get(incl - mine), get(t), get(parts));
-      return true;
-    }
-    base += __builtin_amdgcn_readlane(incl, 63);
-    i0 += 64;
-    if (i0 >= n) return false;
-    load(i0 + l);
-  }
+  const int parts = cross_parts(c, inv, u);
+  const int mine = t * parts;
+  const int incl = wave_scan(mine);
+  const uint64_t hit = __builtin_amdgcn_ballot_w64(rel >= incl - mine && rel < incl);
+  if (!hit) return false;
+  const int src = __builtin_ctzll(hit);
+  auto get = [&](int v) __attribute__((always_inline)) {
+    return __builtin_amdgcn_readlane(v, src);
+  };
+  out.s = CrossSeq{get(s.q_lo), get(s.nq), get(s.k_lo), get(s.nk), get(s.room)};
+  out.index = src + (shared ? 1 : 0);
+  place(rel - get(incl - mine), get(t), get(parts));
+  return true;
 }
 
 // The same for tiles of packed rows (forward, dQ).
 template <bool EVEN>
 __device__ __forceinline__ bool cross_place_rows(const CrossBatch& b, const CrossCut& c, int entry,
                                                  CrossPlace& out) {
-  const int pre = c.keys == CROSS_FUSED ? cross_tiles_log2(b.prefix, c.key_log2) : 0;
   return cross_place<EVEN>(
       b, c, c.keys == CROSS_APART, entry,
       [&](const CrossSeq& s, int& tiles, int& units) __attribute__((always_inline)) {
-        tiles = cross_tiles_log2(s.nq * b.g, c.rows_log2);
-        units = cross_tiles_log2(s.nk, c.key_log2) + pre;
+        cross_row_units(b, c, s, tiles, units);
       },
       out);
+}
+
+// The lists of one or two launches (a workgroup each): a thread per run of consecutive
+// sequences, their units summed for C, then their entries scanned.
+struct CrossListArgs {
+  CrossBatch b;
+  CrossCut cut[2];
+  int kv[2];  // dK/dV
+  int pack_log2;
+};
+constexpr int kListThreads = 1024;
+__global__ void __launch_bounds__(kListThreads) cross_list_kernel(CrossListArgs a) {
+  constexpr int kWaves = kListThreads / 64;
+  __shared__ float wave_units[kWaves];
+  __shared__ int64_t wave_entries[kWaves];
+  const CrossBatch& b = a.b;
+  const CrossCut& c = a.cut[blockIdx.x];
+  const int kv = a.kv[blockIdx.x], t = threadIdx.x, w = t >> 6;
+  const int run = (b.n + kListThreads - 1) / kListThreads;
+  const int first = min(b.n, t * run), last = min(b.n, first + run);
+  auto of = [&](const CrossSeq& s, int& tiles, int& units) __attribute__((always_inline)) {
+    if (kv) cross_key_units(b, c, a.pack_log2, s, tiles, units);
+    else cross_row_units(b, c, s, tiles, units);
+  };
+  int tiles, units, cap = cross_cap(c, 0.f);
+  if (c.max_parts > 1) {
+    float sum = 0.f;
+    for (int i = first; i < last; ++i) {
+      of(cross_seq(b, i), tiles, units);
+      sum += (float)tiles * (float)units;
+    }
+    sum = wave_sum(sum);
+    if ((t & 63) == 0) wave_units[w] = sum;
+    __syncthreads();
+    sum = 0.f;
+    for (int i = 0; i < kWaves; ++i) sum += wave_units[i];
+    if (kv ? b.prefix > 0 : c.keys == CROSS_APART) {
+      of(cross_shared_seq(b), tiles, units);
+      sum += (float)tiles * (float)units;
+    }
+    cap = cross_cap(c, sum);
+  }
+  const float inv = 1.f / (float)cap;
+  auto entries = [&](int i) __attribute__((always_inline)) {
+    of(cross_seq(b, i), tiles, units);
+    return (int64_t)tiles * cross_parts(c, inv, units);
+  };
+  int64_t mine = 0;
+  for (int i = first; i < last; ++i) mine += entries(i);
+  int64_t at = mine;  // inclusive sum over the wave's lanes
+  for (int off = 1; off < 64; off <<= 1) {
+    const int64_t y = __shfl_up(at, off, 64);
+    if ((t & 63) >= off) at += y;
+  }
+  if ((t & 63) == 63) wave_entries[w] = at;
+  __syncthreads();
+  at -= mine;
+  for (int i = 0; i < w; ++i) at += wave_entries[i];
+  // (past 31 bits, with wrong offsets alone, the list ends)
+  auto put = [&](int i) __attribute__((always_inline)) {
+    c.list[i] = (int)min(at, (int64_t)0x7fffffff);
+  };
+  for (int i = first; i < last; ++i) {
+    put(i);
+    at += entries(i);
+  }
+  if (t == kListThreads - 1) {
+    put(b.n);
+    c.list[b.n + 1] = cap;
+  }
 }
 
 // Token of packed row r (r >= 0): r / g by the reciprocal, off by at most one.

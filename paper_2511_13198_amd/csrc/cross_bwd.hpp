@@ -395,8 +395,7 @@ __global__ void __launch_bounds__(NWAVES * 64, NWAVES == 4 ? 2 : D == 64 ? 3 : 1
   if (!cross_place<false>(
           a.b, a.cut, pre, entry,
           [&](const CrossSeq& s, int& tiles, int& units) __attribute__((always_inline)) {
-            tiles = cross_tiles_log2(s.room, a.cut.key_log2);
-            units = s.nk > 0 ? cross_tiles(s.nq << sh, BQ) * sweeps : 0;
+            cross_key_units(a.b, a.cut, sh, s, tiles, units);
           },
           at))
     return;

@@ -34,15 +34,16 @@ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // Optional per-thread kernel timing: while enabled, every launch is bracketed
 // by two events on its own stream; pdy_profile_stop reduces them per kernel.
 // ---------------------------------------------------------------------------
-enum KernelId { K_PLAN = 0, K_FWD, K_DKDV, K_DQ, K_SPLIT_MERGE, K_SPLIT_SUM, K_CROSS_FWD,
-                K_CROSS_MERGE, K_CROSS_DQ, K_CROSS_DKDV, K_CROSS_SUM, K_ROTARY,
+enum KernelId { K_PLAN = 0, K_FWD, K_DKDV, K_DQ, K_SPLIT_MERGE, K_SPLIT_SUM, K_CROSS_LIST,
+                K_CROSS_FWD, K_CROSS_MERGE, K_CROSS_DQ, K_CROSS_DKDV, K_CROSS_SUM, K_ROTARY,
                 K_COUNT };
 const char* const kKernelNames[K_COUNT] = {"plan_kernel",     "fwd_kernel",
                                            "bwd_dkdv_kernel", "bwd_dq_kernel",
                                            "split_merge_kernel", "split_sum_kernel",
-                                           "cross_fwd_kernel", "cross_merge_kernel",
-                                           "cross_dq_kernel", "cross_dkdv_kernel",
-                                           "cross_sum_kernel",   "rotary_kernel"};
+                                           "cross_list_kernel", "cross_fwd_kernel",
+                                           "cross_merge_kernel", "cross_dq_kernel",
+                                           "cross_dkdv_kernel", "cross_sum_kernel",
+                                           "rotary_kernel"};
 struct ProfRec {
   int kid;
   hipEvent_t a, b;

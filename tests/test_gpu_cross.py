@@ -46,6 +46,13 @@ CASES = [
     ([100, 33, 1, 250], [100, 33, 1, 250], None, 200, 8, 2, 128, True),
     ([300, 129], [300, 400], None, 1, 3, 1, 64, True),
     ([90, 120], [64, 64], [10, 64], 65, 2, 2, 128, True),
+    # more sequences than lanes: shared keys with them and apart, long rows, a list of
+    # three levels
+    ([1 + i % 2 for i in range(300)], [i % 20 for i in range(300)], None, 700, 4, 2, 64, True),
+    ([1] * 65, [3] * 65, [i % 4 for i in range(65)], 1500, 8, 1, 128, True),
+    ([i % 90 for i in range(100)], [(i * 7) % 160 for i in range(100)], None, 40, 4, 2, 128, True),
+    ([0] * 66 + [200, 0, 31], [9] * 66 + [1500, 0, 1], None, 0, 2, 2, 64, False),
+    ([i % 3 for i in range(4200)], [(i * 5) % 4 for i in range(4200)], None, 0, 2, 2, 64, False),
 ]
 
 
