@@ -216,7 +216,7 @@ pdy_status attn_merge(const void* o_a, const float* lse_a, const void* o_b, cons
  * q, o bf16 [total_q, Hq, d]; k, v bf16 [total_k, Hkv, d] (NULL if total_k = 0); lse
  * fp32 [Hq, total_q].  Launch shapes and the parts of rows with few keys follow from
  * the sizes and the offsets' values: results of a sequence depend on its batch in
- * rounding only.  Other rules as above. */
+ * rounding only.  Hq * d is below 2^24, Hkv * d below 2^22.  Other rules as above. */
 size_t attn_cross_fwd_workspace_size(int32_t total_q, int32_t total_k, int32_t num_seqs,
                                      int32_t max_seqlen_q, int32_t max_seqlen_k,
                                      int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim);
@@ -278,7 +278,7 @@ pdy_status attn_prefix_bwd(const void* q, const void* k, const void* v, const vo
  *   keeps their values); turns[p] = w_p / 2 pi as a 64-bit fraction of a turn, which
  *   attn_rotary_turns computes from the frequencies w_p (radians a position, finite).
  * Angles are exact for every int32 position; products are 32 bits, rounded once to a
- * bf16 output.  Needs no workspace. */
+ * bf16 output.  Needs no workspace; total_tokens is below 2^26 - 4. */
 pdy_status attn_rotary_turns(const double* freqs, int32_t num_pairs, uint64_t* turns);
 pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
                        int32_t total_tokens, int32_t num_axes, int32_t num_heads_q,

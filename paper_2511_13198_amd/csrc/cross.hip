@@ -44,6 +44,9 @@ pdy_status check_cross_sizes(int32_t prefix, int32_t tq, int32_t tk, int32_t n, 
   // sequence an unfilled tile at most)
   if (((int64_t)tq + n) * hq >= (int64_t)1 << 31 || ((int64_t)tk + prefix) * hkv >= (int64_t)1 << 31)
     return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
+  // (a tile's copies address its 64 tokens of q or 256 keys by bytes in 31 bits)
+  if ((int64_t)hq * d >= 1 << 24 || (int64_t)hkv * d >= 1 << 22)
+    return fail(PDY_ERR_INVALID_ARG, "too many heads for one launch (Hq=%d, Hkv=%d)", hq, hkv);
   *out = CrossSizes{tq, tk, n, max_q, max_k, prefix, hq, hkv, d};
   return PDY_OK;
 }
@@ -208,6 +211,9 @@ CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
   f.wgs = items + (c.max_parts > 1 ? c.entries + 2 : 0);
   return f;
 }
+
+// Whether a grid's threads can be counted in 32 bits, as a launch's are.
+bool fits_grid(int64_t wgs, int threads) { return wgs * threads < (int64_t)1 << 32; }
 
 // Partial results that a launch writes at most (0: none).
 int slices_of(const CrossRows& f) {
@@ -426,6 +432,8 @@ pdy_status cross_fwd_impl(const CrossIn& x, const CrossSizes& s, int32_t causal,
   if (workspace_bytes < need)
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, %s needs %zu", workspace_bytes, who,
                 need);
+  if (!fits_grid(f.wgs * s.hkv, f.sh.nw * 64))
+    return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
   hipError_t e = init_cross_kernels();
   if (e != hipSuccess) return hip_fail(e, "kernel attribute setup");
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
@@ -497,6 +505,8 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
   if (workspace_bytes < sp.total)
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, %s needs %zu", workspace_bytes, who,
                 sp.total);
+  if (!fits_grid(f.wgs * s.hkv, f.sh.nw * 64) || !fits_grid(kv.wgs * s.hkv, kv.sh.nw * 64))
+    return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
   hipError_t e = init_cross_kernels();
   if (e != hipSuccess) return hip_fail(e, "kernel attribute setup");
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);

@@ -63,8 +63,10 @@ pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
                        void* k_out, void* stream) {
   g_err[0] = 0;
   pdy_status st;
-  if (total_tokens < 0)
-    return fail(PDY_ERR_INVALID_ARG, "total_tokens must be >= 0 (got %d)", total_tokens);
+  // (a launch's threads, 64 a token, are counted in 32 bits)
+  if (total_tokens < 0 || total_tokens >= (1 << 26) - 4)
+    return fail(PDY_ERR_INVALID_ARG, "total_tokens must be >= 0 and below 2^26 - 4 (got %d)",
+                total_tokens);
   if (num_axes < 1 || num_axes > pdy::kMaxAxes)
     return fail(PDY_ERR_INVALID_ARG, "num_axes must be in [1, %d] (got %d)", pdy::kMaxAxes,
                 num_axes);

@@ -41,6 +41,8 @@ BAD = [
     (dict(len_k=FAKE + 1), "seqlens_k"), (dict(q=0), "q is NULL"), (dict(k=FAKE + 8), "aligned"),
     (dict(v=0), "v is NULL"), (dict(o=0), "o is NULL"), (dict(lse=FAKE + 4), "aligned"),
     (dict(ws=0), "workspace"), (dict(tq=1 << 27, hq=32), "too large"),
+    (dict(hq=1 << 17, hkv=2), "too many heads"), (dict(hq=1 << 15, hkv=1 << 15), "too many heads"),
+    (dict(n=1 << 25), "too large"),
 ]
 BAD_BWD = [(dict(do=0), "dout is NULL"), (dict(dq=FAKE + 2), "aligned"), (dict(dk=0), "dk is NULL"),
            (dict(dv=0), "dv is NULL"), (dict(bf16=2), "grad_bf16")]
@@ -179,7 +181,7 @@ def rotary(**kw):
 
 
 @pytest.mark.parametrize("kw,text", [
-    (dict(t=-1), "total_tokens"), (dict(axes=0), "num_axes"), (dict(axes=5), "num_axes"),
+    (dict(t=-1), "total_tokens"), (dict(t=1 << 26), "total_tokens"), (dict(axes=0), "num_axes"), (dict(axes=5), "num_axes"),
     (dict(hq=0, hkv=0), "head counts"), (dict(hq=-1), "head counts"), (dict(pairs=33), "num_pairs"),
     (dict(pairs=12), "num_pairs"), (dict(pairs=0), "num_pairs"), (dict(pairs=40), "num_pairs"),
     (dict(inter=2), "interleaved"), (dict(inv=-1), "inverse"), (dict(turns=None), "turns"),
