@@ -333,7 +333,8 @@ pdy_status pdy_chunk_launch_shapes(int32_t tq, int32_t tk, int32_t q_offset, int
 /* The same for attn_cross_* (prefix_len = 0) and attn_prefix_*: three values each for the
  * forward, dQ and dK/dV kernels (a launch is cut into that many parts per item at most,
  * as the offsets have it), then 1 where the shared keys are a list of their own beside
- * the sequences' (partial results of both), 10 values. */
+ * the sequences' (partial results of both), and 1 each where the forward and dQ keep
+ * their first items whole: 12 values. */
 pdy_status pdy_cross_launch_shapes(int32_t prefix_len, int32_t total_q, int32_t total_k,
                                    int32_t num_seqs, int32_t max_seqlen_q, int32_t max_seqlen_k,
                                    int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim,

@@ -118,6 +118,9 @@ struct CrossRows {
 };
 
 constexpr int kMaxParts = 64;
+// Sequences that every workgroup puts in order for whole rounds, at about 0.1 us each: 51
+// sequences' forward 47 us unsorted, 55 sorted.
+constexpr int64_t kSorted = 32;
 constexpr int64_t kPartBytes = (int64_t)256 << 20;  // partial results at most
 constexpr double kMoveBytesPerUs = 4.0e6;           // partial results written and read back
 
@@ -131,22 +134,28 @@ constexpr int64_t kApartRows = 64, kApartPrefix = 512;
 
 // Shape and parts of a launch over sequences of more than 64 rows: the ones of least
 // estimated time, from the average rows and keys of a sequence.  With I items of u
-// units in p parts, on `slots` workgroups at a time,
-//   rounds = ceil(I p / slots), time = rounds (start + u / p unit) + partial results.
-// parts = 1: whole.  us measured, 256-row tiles / 128 whole / 128 in parts (their sums
-// included): 9 x 427 rows x 4 heads 56 / 59 / 57, 51 x 79 x 16 64 / 49 / 57, 2,000 x 8
-// over 3,000 keys 79 / 76 / 54, 4 x 1,041 x 8 causal 37 / 38 / 44.
+// units, on `slots` workgroups at a time,
+//   whole: ceil(I / slots) (start + u unit), and no less than the longest item's;
+//   in p parts: ceil(I p / slots) (start + u / p unit) + partial results;
+//   whole rounds, the rest in parts: I (start + u unit) / slots + start + partial results.
+// us measured, 256-row tiles / 128 whole / 128 in parts (their sums included): 9 x 427
+// rows x 4 heads 56 / 59 / 57, 51 x 79 x 16 64 / 49 / 57, 2,000 x 8 over 3,000 keys 79 / 76
+// / 54, 4 x 1,041 x 8 causal 37 / 38 / 44; 21 x 208 rows over 1-5,792 keys, one head, whole
+// 67, in parts 26.
 struct RowsChoice {
   CrossShape sh;
-  int parts;
+  int parts;        // 1: whole
   int64_t entries;  // of all heads: whole rounds
+  int64_t round;    // of all heads: whole rounds, then parts (0: all alike)
 };
 RowsChoice choose_rows(const CrossSizes& s, const RowKernel& k, bool causal) {
   const double own = std::min<double>((double)s.max_k, (double)s.tk / s.n);
   const double seen = causal ? std::max(own - 0.5 * s.tq / s.n, 0.5 * own) : own;
   const double keys = seen + s.prefix, rows = (double)s.tq * s.g();
-  RowsChoice best{{8, 1}, 1, 0};
+  const double longest = (double)(s.max_k + s.prefix) / 64;
+  RowsChoice best{{8, 1}, 1, 0, 0};
   double least = 1e30;
+  constexpr double kStart = 7.0, kMerge = 5.0;
   for (const CrossShape& sh : {CrossShape{8, 1}, CrossShape{4, 1}, CrossShape{4, 2}}) {
     if (sh.rows() >= 2 * s.seq_rows()) continue;
     const int64_t slots = k.slots(s, sh);
@@ -158,12 +167,22 @@ RowsChoice choose_rows(const CrossSizes& s, const RowKernel& k, bool causal) {
       if (p > 1 && bytes > kPartBytes) break;
       const double rounds = std::ceil(items * p / slots);
       const double unit = k.unit_us(s, sh, items * p > kCUs);
-      const double t = rounds * (7.0 + units / p * unit) +
-                       (p > 1 ? 5.0 + 2.0 * bytes / kMoveBytesPerUs : 0.0);
+      double t = rounds * (kStart + units / p * unit);
+      if (p > 1) t += kMerge + 2.0 * bytes / kMoveBytesPerUs;
+      else t = std::max(t, kStart + longest * unit);
       if (t < (p > 1 ? 0.95 : 1.0) * least) {
         least = t;
-        best = {sh, p, (int64_t)rounds * slots};
+        best = {sh, p, (int64_t)rounds * slots, 0};
       }
+    }
+    // (more than a round, or parts would do as well)
+    const double bytes = std::min<double>((double)slots * sh.rows(), kMaxParts * rows * s.hkv) *
+                         s.d * 4;
+    const double t = items * (kStart + units * k.unit_us(s, sh, true)) / slots + kStart + kMerge +
+                     2.0 * bytes / kMoveBytesPerUs;
+    if (items > slots && s.n <= kSorted && t < 0.85 * least) {
+      least = t;
+      best = {sh, 2, slots, slots};
     }
   }
   return best;
@@ -179,11 +198,12 @@ CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
                ? pdy::CROSS_FUSED
                : pdy::CROSS_APART;
   const bool apart = c.keys == pdy::CROSS_APART;
-  int64_t most = kMaxParts, entries;  // parts of an item, and of all
+  int64_t most = kMaxParts, entries, round = 0;  // parts of an item, and of all
   if (s.seq_rows() > 64) {
     const RowsChoice r = choose_rows(s, k, causal);
     f.sh = r.sh;
     entries = r.entries;
+    round = r.round;
     if (r.parts == 1) most = 1;
   } else {
     f.sh = few_rows_shape(apart ? s.tq * s.g() : s.seq_rows());
@@ -203,6 +223,7 @@ CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
       most_items(s, s.n, s.max_q, rows) + (apart ? ceil_div(s.tq * s.g(), rows) : 0);
   c.entries = (int)ceil_div(entries, s.hkv);
   c.even = s.seq_rows() > 64;
+  c.round = (int)ceil_div(round, s.hkv);
   c.list = nullptr;
   const int64_t own = ceil_div(s.max_k, keys_tile), pre = ceil_div(s.prefix, keys_tile);
   const int64_t tiles = apart ? std::max(own, pre) : own + pre;
@@ -225,7 +246,7 @@ int slices_of(const CrossRows& f) {
 size_t list_bytes(const CrossSizes& s) {
   return s.n > pdy::kListLanes ? align256((size_t)(s.n + 2) * 4) : 0;
 }
-size_t part_n_bytes(const CrossSizes& s) { return align256((size_t)s.tq * 2 * 4); }
+size_t part_n_bytes(const CrossSizes& s) { return align256((size_t)s.tq * s.hq * 2 * 4); }
 size_t part_o_bytes(const CrossSizes& s, int slices) {
   return align256((size_t)slices * s.tq * s.hq * s.d * 4);
 }
@@ -274,7 +295,7 @@ CrossKv kv_launch(const CrossSizes& s) {
   c.least = 4;
   const int64_t n = items(k.sh.rows()), target = kCUs;
   c.entries = (int)ceil_div(target, s.hkv);
-  c.even = 0;
+  c.even = c.round = 0;
   const int64_t slice = (s.prefix + s.tk) * s.hkv * s.d * 8;
   int64_t parts = std::min<int64_t>(16, slice ? kPartBytes / slice : 1);
   // items alike in their rows need no cut once they fill the chip; a shared tile has
@@ -580,24 +601,24 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
   sum.out_bf16 = grad_bf16;
   int64_t blocks = 0;
   auto add = [&](const float* part, const int32_t* n, const int32_t* n1, int max_parts,
-                 int64_t heads, int64_t rows, int64_t first, int64_t count, const int32_t* end,
+                 int64_t heads, int64_t each, int64_t rows, int64_t first, int64_t count, const int32_t* end,
                  void* dst) {
     if (count == 0) return;
     const int b = (int)ceil_div(count * (s.d / 8), 256);
-    sum.job[sum.njobs++] = pdy::CrossSumJob{part, n, n1, max_parts, (int)heads, rows, first, count,
+    sum.job[sum.njobs++] = pdy::CrossSumJob{part, n, n1, max_parts, (int)heads, (int)each, rows, first, count,
                                             end, dst, b};
     blocks += b;
   };
   if (rows && slices_of(f) > 0)
-    add(part_q, counts_q, f.cut.keys == pdy::CROSS_APART ? counts_q + s.tq : nullptr,
-        f.cut.max_parts, s.hq, s.tq * s.hq, 0, s.tq * s.hq, x.cu_q + s.n, g.dq);
+    add(part_q, counts_q, f.cut.keys == pdy::CROSS_APART ? counts_q + s.tq * s.hq : nullptr,
+        f.cut.max_parts, s.hq, 1, s.tq * s.hq, 0, s.tq * s.hq, x.cu_q + s.n, g.dq);
   if (kv.cut.max_parts > 1) {
     const int64_t rows = (s.prefix + s.tk) * s.hkv, pre = s.prefix * s.hkv;
     for (int i = 0; i < 2; ++i) {
       const float* part = i ? part_v : part_k;
-      add(part, counts_k, nullptr, kv.cut.max_parts, s.hkv, rows, 0, pre, nullptr,
+      add(part, counts_k, nullptr, kv.cut.max_parts, s.hkv, s.hkv, rows, 0, pre, nullptr,
           i ? g.dvp : g.dkp);
-      add(part, counts_k, nullptr, kv.cut.max_parts, s.hkv, rows, pre, s.tk * s.hkv, x.cu_k + s.n,
+      add(part, counts_k, nullptr, kv.cut.max_parts, s.hkv, s.hkv, rows, pre, s.tk * s.hkv, x.cu_k + s.n,
           i ? g.dv : g.dk);
     }
   }
@@ -627,7 +648,7 @@ pdy_status pdy_cross_launch_shapes(int32_t prefix_len, int32_t total_q, int32_t 
   if (st != PDY_OK) return st;
   if (causal != 0 && causal != 1) return fail(PDY_ERR_INVALID_ARG, "causal must be 0 or 1");
   if (shapes == nullptr) return fail(PDY_ERR_INVALID_ARG, "shapes is NULL");
-  std::fill(shapes, shapes + 10, 0);
+  std::fill(shapes, shapes + 12, 0);
   auto put = [&](int i, const CrossShape& sh, const pdy::CrossCut& c) {
     shapes[3 * i] = sh.nw;
     shapes[3 * i + 1] = sh.groups;
@@ -638,6 +659,8 @@ pdy_status pdy_cross_launch_shapes(int32_t prefix_len, int32_t total_q, int32_t 
     put(0, f.sh, f.cut);
     put(1, q.sh, q.cut);
     shapes[9] = f.cut.keys == pdy::CROSS_APART;
+    shapes[10] = f.cut.round > 0;
+    shapes[11] = q.cut.round > 0;
   }
   if (s.tk + s.prefix > 0) {
     const CrossKv kv = kv_launch(s);

@@ -69,10 +69,16 @@ enum CrossKeys : int {
 //   a part has at most C = max(least, units / entries) inner tiles, the units being all
 //   items' of a kv head: about `entries` parts, alike whatever the lengths, and up to
 //   one an item more.
-// EVEN and `even` (tiles of many rows, up to kListLanes sequences): C is the least from there on with which
-// the parts are no more than `entries`, so that they fit the rounds on the chip that
-// the host planned for (6 sequences of 500-2,000 rows behind 16,384 keys, 4 heads: 648
-// parts where 512 fit, 299 us, 432 of them 264).
+// EVEN and `even` (tiles of many rows, up to kListLanes sequences): under a causal mask
+// a sequence's last tiles come first, and C is the least from there on with which the
+// parts are no more than `entries`, so that they fit the rounds on the chip that the
+// host planned for (6 sequences of 500-2,000 rows behind 16,384 keys, 4 heads: 648 parts
+// where 512 fit, 299 us, 432 of them 264).
+//   round > 0 (workgroups of a kv head at a time): the sequences of most keys come first,
+// their items whole, as many rounds of them as end before an even share of all work
+// would, and the others' parts fill the rest of the chip.  16 sequences of 69-759 rows
+// behind 4,096 keys, 32/8 heads, 2.2 rounds of 256 rows: forward 342 us whole, 297 and 18
+// for the sums with the last 0.2 in parts; dQ 458 with tiles of 64 rows, 405 and 7.
 // C follows from the offsets on the GPU, so that nothing waits for the host: every
 // workgroup computes it, and its place in the list, with a lane per sequence; of more
 // sequences than lanes cross_list_kernel writes the list once and a workgroup searches
@@ -87,7 +93,8 @@ struct CrossCut {
   int max_parts;  // of an item; 1: not cut
   int least;      // fewest inner tiles of a part
   int entries;    // parts of a kv head
-  int even;       // whole rounds (EVEN)
+  int even;       // parts to `entries` (EVEN)
+  int round;      // whole items, then parts (EVEN; 0: all in parts)
   // more than kListLanes sequences: entries of a kv head before each sequence's (after
   // the shared keys') [n], their number, and C; else NULL
   int32_t* list;
@@ -236,24 +243,82 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
     s = cross_seq(b, l);
     of(s, t, u);
   }
-  int cap = 1 << 30;
-  if (c.max_parts > 1) {
-    cap = cross_cap(c, wave_sum((float)t * (float)u) + (float)t0 * (float)u0);
-    if (EVEN && c.even) {
-      // the least C from there on whose parts are few enough: by bisection, at most
-      // up to the largest item (the parts get fewer as C grows)
-      int hi = max(u0, wave_max(t > 0 ? u : 0));
-      while (cap < hi) {
-        const int mid = (cap + hi) >> 1;
-        const float inv = 1.f / (float)mid;
-        const int e = __builtin_amdgcn_readlane(wave_scan(t * (int)ceilf((float)u * inv)), 63) +
-                      t0 * (int)ceilf((float)u0 * inv);
-        if (e <= c.entries) hi = mid;
-        else cap = mid + 1;
+  auto get = [&](int v, int src) __attribute__((always_inline)) {
+    return __builtin_amdgcn_readlane(v, src);
+  };
+  auto found = [&](int src) __attribute__((always_inline)) {
+    out.s = CrossSeq{get(s.q_lo, src), get(s.nq, src), get(s.k_lo, src), get(s.nk, src),
+                     get(s.room, src)};
+    out.index = src + (shared ? 1 : 0);
+  };
+  if constexpr (EVEN) {
+    if (c.even) {
+      int first = wave_scan(t) - t;  // items before this sequence's
+      const int total = get(first + t, 63);
+      if (c.max_parts > 1 && c.round) {
+        // (6 bits order equal ones; u is below 2^25)
+        const int key = (u << 6) | (63 - l);
+        first = 0;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) first += get(key, j) > key ? get(t, j) : 0;
       }
+      auto holds = [&](int item) __attribute__((always_inline)) {
+        return __builtin_amdgcn_ballot_w64(first <= item && item < first + t);
+      };
+      int whole = c.max_parts > 1 ? 0 : total, entries = c.entries;
+      if (c.max_parts > 1 && c.round) {
+        // (a workgroup's start and end cost what 320 keys do)
+        const float start = (float)(320 >> c.key_log2);
+        const float share = wave_sum((float)t * ((float)u + start)) / (float)c.round;
+        float end = 0.f;
+        while (whole < total) {
+          end += (float)get(u, __builtin_ctzll(holds(whole))) + start;
+          if (end > share) break;
+          whole += c.round;
+        }
+        whole = min(whole, total);
+        entries = c.round * ((total - whole + c.round - 1) / c.round);
+      }
+      const int cut = min(t, max(0, first + t - whole));  // the sequence's items in parts
+      int cap = 1 << 30;
+      if (whole < total) {
+        cap = max(c.least, (int)fminf(wave_sum((float)cut * (float)u) / (float)entries + 1.f, 1e9f));
+        // by bisection, at most up to the largest item (the parts get fewer as C grows)
+        int hi = wave_max(cut > 0 ? u : 0);
+        while (cap < hi) {
+          const int mid = (cap + hi) >> 1;
+          const float inv = 1.f / (float)mid;
+          const int e = get(wave_scan(cut * max(1, (int)ceilf((float)u * inv))), 63);
+          if (e <= entries) hi = mid;
+          else cap = mid + 1;
+        }
+      }
+      const int parts = cross_parts(c, 1.f / (float)cap, u);
+      int rel = entry, before = first, mine = t - cut;
+      if (entry >= whole) {
+        rel -= whole;
+        mine = cut * parts;
+        before = wave_scan(mine) - mine;
+      }
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(rel >= before && rel < before + mine);
+      if (!hit) return false;
+      const int src = __builtin_ctzll(hit);
+      found(src);
+      const int tiles = get(t, src), cuts = get(cut, src), at = rel - get(before, src);
+      if (entry < whole) {
+        out.nparts = 1;
+        out.part = 0;
+        out.tile = at;
+      } else {
+        place(at, cuts, get(parts, src));
+        out.tile += tiles - cuts;
+      }
+      if (b.causal) out.tile = tiles - 1 - out.tile;
+      return true;
     }
   }
-  const float inv = 1.f / (float)cap;
+  const float units = wave_sum((float)t * (float)u) + (float)t0 * (float)u0;
+  const float inv = 1.f / (float)cross_cap(c, units);
   int rel = entry;
   if (shared) {
     const int base = in_shared(inv);
@@ -266,12 +331,8 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
   const uint64_t hit = __builtin_amdgcn_ballot_w64(rel >= incl - mine && rel < incl);
   if (!hit) return false;
   const int src = __builtin_ctzll(hit);
-  auto get = [&](int v) __attribute__((always_inline)) {
-    return __builtin_amdgcn_readlane(v, src);
-  };
-  out.s = CrossSeq{get(s.q_lo), get(s.nq), get(s.k_lo), get(s.nk), get(s.room)};
-  out.index = src + (shared ? 1 : 0);
-  place(rel - get(incl - mine), get(t), get(parts));
+  found(src);
+  place(rel - get(incl - mine, src), get(t, src), get(parts, src));
   return true;
 }
 

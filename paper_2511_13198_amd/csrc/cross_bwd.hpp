@@ -45,7 +45,8 @@ struct CrossBwdArgs {
   int pack_log2;
   // partial gradients (fp32, scaled): part [slice][rows][D] -- rows are tq * hq pairs
   // for dQ, (prefix + tk) * hkv for dK (part) and dV (part2), the shared keys first --
-  // and how many slices a token (key) has at part_n; dQ with CROSS_APART as the forward
+  // and how many slices a row of dQ (a key) has at part_n; dQ with CROSS_APART as the
+  // forward
   float* part;
   float* part2;
   int32_t* part_n;
@@ -83,7 +84,7 @@ __global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : N
   int hk, entry;
   xcd_order(blockIdx.x, gridDim.x, a.b.hkv, hk, entry);
   CrossPlace at;
-  if (!cross_place_rows<KG == 1>(a.b, a.cut, entry, at)) return;
+  if (!cross_place_rows<KG <= 2>(a.b, a.cut, entry, at)) return;
   const int g = a.b.g;
   const CrossSeq sq = at.s;
   const int row_end = (sq.q_lo + sq.nq) * g;
@@ -189,8 +190,9 @@ __global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : N
       if (lse2 == -INFINITY) lse2 = INFINITY;
       if (hh == 0 && at.part == 0 && kg == 0) {
         if (!second) a.dd[li] = ddv;
-        if (a.part_n && hk == 0 && r == tok * g)
-          a.part_n[(second ? a.b.tq : 0) + tok] = at.nparts;
+        if (a.part_n)
+          a.part_n[(second ? (size_t)a.b.tq * a.b.hq : 0) + (size_t)tok * a.b.hq + hk * g +
+                   (r - tok * g)] = at.nparts;
       }
     }
   }
@@ -692,14 +694,15 @@ __global__ void __launch_bounds__(NWAVES * 64, NWAVES == 4 ? 2 : D == 64 ? 3 : 1
 }
 
 // Sums of partial gradients: row i (a head's D floats; `heads` of them to a token or
-// key) has n[token] slices from 0 on, and n1[token] from max_parts on where the shared
-// and the own keys were apart.  Rows with one slice are written already.
+// key) has n[i / each] slices from 0 on, and n1[i / each] from max_parts on where the
+// shared and the own keys were apart.  Rows with one slice are written already.
 struct CrossSumJob {
   const float* part;
   const int32_t* n;
   const int32_t* n1;   // or NULL
   int max_parts;
   int heads;
+  int each;            // rows to a count
   int64_t rows;        // rows of a slice
   int64_t first;       // first row to sum, and how many
   int64_t count;
@@ -724,10 +727,10 @@ __global__ void __launch_bounds__(256) cross_sum_kernel(CrossSumArgs a) {
   const int c = (int)(gid % LANES) * 8;
   if (i >= b.count) return;
   const int64_t row = b.first + i;
-  const int tok = (int)(row / b.heads);
+  const int64_t count = row / b.each;
   if (b.end && (int)(i / b.heads) >= *b.end) return;
-  const int n0 = min(max(b.n[tok], 0), b.max_parts);
-  const int n1 = b.n1 ? min(max(b.n1[tok], 0), b.max_parts) : 0;
+  const int n0 = min(max(b.n[count], 0), b.max_parts);
+  const int n1 = b.n1 ? min(max(b.n1[count], 0), b.max_parts) : 0;
   if (!b.n1 && n0 <= 1) return;
   float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   auto add = [&](int64_t slice) __attribute__((always_inline)) {

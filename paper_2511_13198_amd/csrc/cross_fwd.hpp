@@ -55,8 +55,8 @@ struct CrossFwdArgs {
   float scale_log2;
   // partial results: O (fp32, normalised by the part's own sums) and LSE of slice s
   // at part_o [s][tq * hq][D], part_lse [s][tq * hq] (NaN: a NaN or +inf logit), and
-  // how many slices a token has at part_n [tq].  CROSS_APART: part_n is of the shared
-  // keys, part_n + tq of a sequence's own, whose slices start at max_parts
+  // how many slices a row has at part_n [tq * hq].  CROSS_APART: part_n is of the shared
+  // keys, part_n + tq * hq of a sequence's own, whose slices start at max_parts
   float* part_o;
   float* part_lse;
   int32_t* part_n;
@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1)
   int hk, entry;
   xcd_order(blockIdx.x, gridDim.x, a.b.hkv, hk, entry);
   CrossPlace at;
-  if (!cross_place_rows<KG == 1>(a.b, a.cut, entry, at)) return;
+  if (!cross_place_rows<KG <= 2>(a.b, a.cut, entry, at)) return;
   const int g = a.b.g;
   const CrossSeq sq = at.s;
   const int row_end = (sq.q_lo + sq.nq) * g;  // packed rows of the sequence end
@@ -325,9 +325,9 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1)
   const bool second = apart && !shared;
   const size_t pairs = (size_t)a.b.tq * a.b.hq;
   const size_t slice = (size_t)(second ? a.cut.max_parts + at.part : at.part) * pairs;
-  if (a.part_n && hk == 0 && at.part == 0 && kg == 0 && hh == 0 && row < row_end) {
+  if (a.part_n && at.part == 0 && kg == 0 && hh == 0 && row < row_end) {
     const int tok = cross_token(a.b, row);
-    if (tok * g == row) a.part_n[(second ? a.b.tq : 0) + tok] = at.nparts;
+    a.part_n[(second ? pairs : 0) + (size_t)tok * a.b.hq + hk * g + (row - tok * g)] = at.nparts;
   }
   // LSE of a row from its offset m (base 2) and sum; a part hands a NaN sum on as NaN
   auto lse_of = [&](float m2, float tot) __attribute__((always_inline)) {
@@ -393,9 +393,9 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1)
   }
 }
 
-// Combine the partial results of the rows that have any: part_n[token] slices from
-// 0 on, and, where shared and own keys were apart, part_n[tq + token] from slice
-// max_parts on.
+// Combine the partial results of the rows that have any: part_n[row] slices from 0 on,
+// and, where shared and own keys were apart, part_n[tq * hq + row] from slice max_parts
+// on.
 //   LSE = log sum_p exp(LSE_p),  O = sum_p exp(LSE_p - LSE) O_p;
 // a part with LSE = -inf weighs nothing, one with NaN makes the row O = NaN, LSE =
 // -inf.  A wave per (token, head) pair: a lane per slice for the weights (64 at a
@@ -425,8 +425,8 @@ __global__ void __launch_bounds__(256) cross_merge_kernel(CrossMergeArgs a) {
   const int tok = (int)(pair / (uint32_t)a.hq), h = (int)(pair - (uint32_t)tok * a.hq);
   const int c = (l % LANES) * 8, grp = l / LANES;
   const int end = a.cu_q[a.n];
-  const int n0 = min(max(a.part_n[tok], 0), a.max_parts);
-  const int n1 = a.apart ? min(max(a.part_n[a.tq + tok], 0), a.max_parts) : 0;
+  const int n0 = min(max(a.part_n[pair], 0), a.max_parts);
+  const int n1 = a.apart ? min(max(a.part_n[(size_t)pairs + pair], 0), a.max_parts) : 0;
   if (tok >= end) return;  // rows behind the last sequence stay
   if (!a.apart && n0 == 1) return;  // written by its one part
   const int parts = n0 + n1, gap = a.max_parts - n0;

@@ -459,14 +459,16 @@ def prefix_bwd_workspace_size(prefix_len, total_q, total_k, num_seqs, max_seqlen
 def cross_launch_shapes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k, hq, hkv,
                         d, causal: bool = False) -> dict:
     """{kernel name: (waves, groups, parts at most)} of the launches of attn_cross_*
-    (prefix_len 0) and attn_prefix_*, and "apart": whether the shared keys are a list of
-    their own."""
-    out = (ctypes.c_int32 * 10)()
+    (prefix_len 0) and attn_prefix_*; "apart": whether the shared keys are a list of
+    their own; "fwd_whole_first", "dq_whole_first": whether the first items stay whole and
+    the last ones alone are cut."""
+    out = (ctypes.c_int32 * 12)()
     _check(lib().pdy_cross_launch_shapes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q,
                                          max_seqlen_k, hq, hkv, d, int(bool(causal)), out),
            "pdy_cross_launch_shapes")
     names = ("cross_fwd_kernel", "cross_dq_kernel", "cross_dkdv_kernel")
-    return {**{n: tuple(out[3 * i:3 * i + 3]) for i, n in enumerate(names)}, "apart": bool(out[9])}
+    return {**{n: tuple(out[3 * i:3 * i + 3]) for i, n in enumerate(names)}, "apart": bool(out[9]),
+            "fwd_whole_first": bool(out[10]), "dq_whole_first": bool(out[11])}
 
 
 def _launch(name: str, device, *args):

@@ -126,14 +126,16 @@ def test_shapes_of_launches_and_what_the_gpu_cases_cover():
         for kernel in ("cross_fwd_kernel", "cross_dq_kernel", "cross_dkdv_kernel"):
             w, g, parts = s[kernel]
             seen |= {(kernel, w, g, d), (kernel, "parts" if parts > 1 else "whole", d)}
-        seen.add(("apart", s["apart"], d))
+        seen |= {("apart", s["apart"], d), ("fwd whole first", s["fwd_whole_first"], d),
+                 ("dq whole first", s["dq_whole_first"], d)}
     want = {("cross_fwd_kernel", *s, d) for s in ((4, 4), (4, 2), (4, 1), (8, 1)) for d in (64, 128)}
     want |= {("cross_dq_kernel", *s, d) for s in ((4, 2), (4, 1), (8, 1)) for d in (64, 128)}
     want |= {("cross_dkdv_kernel", *s, d) for s in ((4, 1), (8, 2)) for d in (64, 128)}
     want.add(("cross_dkdv_kernel", 8, 1, 128))
     want |= {(k, p, d) for k in ("cross_fwd_kernel", "cross_dq_kernel", "cross_dkdv_kernel")
              for p in ("parts", "whole") for d in (64, 128)}
-    want |= {("apart", a, d) for a in (True, False) for d in (64, 128)}
+    want |= {(what, a, d) for a in (True, False) for d in (64, 128)
+             for what in ("apart", "fwd whole first", "dq whole first")}
     assert not want - seen, sorted(map(str, want - seen))
 
 
