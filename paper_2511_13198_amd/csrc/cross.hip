@@ -152,7 +152,8 @@ RowsChoice choose_rows(const CrossSizes& s, const RowKernel& k, bool causal) {
   const double own = std::min<double>((double)s.max_k, (double)s.tk / s.n);
   const double seen = causal ? std::max(own - 0.5 * s.tq / s.n, 0.5 * own) : own;
   const double keys = seen + s.prefix, rows = (double)s.tq * s.g();
-  const double longest = (double)(s.max_k + s.prefix) / 64;
+  const double longest = std::max(1.0, (double)(s.max_k + s.prefix) / 64);
+  const double alike = std::min(1.0, (own + s.prefix) / (64 * longest));
   RowsChoice best{{8, 1}, 1, 0, 0};
   double least = 1e30;
   constexpr double kStart = 7.0, kMerge = 5.0;
@@ -167,10 +168,14 @@ RowsChoice choose_rows(const CrossSizes& s, const RowKernel& k, bool causal) {
       if (p > 1 && bytes > kPartBytes) break;
       const double rounds = std::ceil(items * p / slots);
       const double unit = k.unit_us(s, sh, items * p > kCUs);
-      double t = rounds * (kStart + units / p * unit);
-      if (p > 1) t += kMerge + 2.0 * bytes / kMoveBytesPerUs;
+      // (items that differ in length do not end in rounds)
+      const double lasts = p > 1 ? rounds : alike * rounds + (1 - alike) * (items / slots + 0.5);
+      double t = lasts * (kStart + units / p * unit);
+      // (parts have to be better by 5%, whole rounds and parts by 8%: the estimates are
+      // that wrong)
+      if (p > 1) t = (t + kMerge + 2.0 * bytes / kMoveBytesPerUs) / 0.95;
       else t = std::max(t, kStart + longest * unit);
-      if (t < (p > 1 ? 0.95 : 1.0) * least) {
+      if (t < least) {
         least = t;
         best = {sh, p, (int64_t)rounds * slots, 0};
       }
@@ -178,9 +183,9 @@ RowsChoice choose_rows(const CrossSizes& s, const RowKernel& k, bool causal) {
     // (more than a round, or parts would do as well)
     const double bytes = std::min<double>((double)slots * sh.rows(), kMaxParts * rows * s.hkv) *
                          s.d * 4;
-    const double t = items * (kStart + units * k.unit_us(s, sh, true)) / slots + kStart + kMerge +
-                     2.0 * bytes / kMoveBytesPerUs;
-    if (items > slots && s.n <= kSorted && t < 0.85 * least) {
+    const double t = (items * (kStart + units * k.unit_us(s, sh, true)) / slots + kStart + kMerge +
+                      2.0 * bytes / kMoveBytesPerUs) / 0.92;
+    if (items > slots && s.n <= kSorted && t < least) {
       least = t;
       best = {sh, 2, slots, slots};
     }

@@ -51,6 +51,8 @@ CASES = [
     ([864, 500, 1, 735, 600], [864, 500, 1, 735, 600], None, 1500, 24, 8, 128, True),
     ([384, 200, 10, 303, 384, 95, 300, 250, 384, 90], [390, 200, 0, 303, 700, 95, 1, 250, 384, 90], None,
      1200, 48, 16, 64, True),
+    ([480, 200, 10, 303, 480, 300, 400, 227], [480, 200, 10, 303, 480, 300, 400, 227], None, 1500, 48, 16,
+     64, True),
     # more sequences than lanes: shared keys with them and apart, long rows, a list of
     # three levels
     ([1 + i % 2 for i in range(300)], [i % 20 for i in range(300)], None, 700, 4, 2, 64, True),
