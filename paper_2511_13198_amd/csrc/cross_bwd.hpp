@@ -52,12 +52,17 @@ struct CrossBwdArgs {
   int32_t* part_n;
 };
 
+// Rows that see so many keys at most have D from P and dP (cross_dq_kernel); no more than
+// a tile of the smallest.
+constexpr int kCrossFewKeys = 64;
+
 template <int D, int NW, int KG = 1>
 struct CrossDqCfg {
   static constexpr int RG = NW / KG;
   static constexpr int BQ = 32 * RG;
   // 4-wave workgroups keep 64 so that two of them fit a CU's LDS
   static constexpr int BK = NW == 8 ? 128 : 64;
+  static_assert(kCrossFewKeys <= BK, "few keys are in one tile");
   static constexpr int WK = BK / KG;
   static constexpr int NT = NW * 64;
   using KL = DualLayout<D>;  // K is read as rows (S^T) and transposed (dQ^T)
@@ -159,7 +164,15 @@ __global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : N
     kd.issue(x.k, kvstride, x.keys, kbuf(t));
     vd.issue(x.v, kvstride, x.keys, vbuf(t));
   };
-  if (t_begin < t_end) issue(t_begin);
+  // some row sees few keys (the first has the fewest): its D is summed from P and dP, below
+  const bool few = ntiles > 0 && a.b.prefix + max(0, __builtin_amdgcn_readfirstlane(key_end(row0))) <=
+                                     kCrossFewKeys;
+  if (few) {
+    issue(0);
+    if (npre > 0) issue(1);
+  } else if (t_begin < t_end) {
+    issue(t_begin);
+  }
   bf16x8 qf[D / 16], gf[D / 16];
   float lse2 = 0.f, ddv = 0.f;
   {
@@ -189,60 +202,112 @@ __global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : N
       // a row without any visible key has LSE = -inf and no gradient
       if (lse2 == -INFINITY) lse2 = INFINITY;
       if (hh == 0 && at.part == 0 && kg == 0) {
-        if (!second) a.dd[li] = ddv;
+        if (!second && !few) a.dd[li] = ddv;
         if (a.part_n)
           a.part_n[(second ? (size_t)a.b.tq * a.b.hq : 0) + (size_t)tok * a.b.hq + hk * g +
                    (r - tok * g)] = at.nparts;
       }
     }
   }
+
+  // S^T and dP^T of 32 keys of tile `it`, from key kb * 32 of this wave's on; hook(N) runs
+  // after the products of the N-th K-step
+  auto products = [&](auto KB, int it, f32x16& s, f32x16& dp, auto&& hook)
+                      __attribute__((always_inline)) {
+    constexpr int kb = decltype(KB)::value;
+    constexpr int NKS = D / 16, PIPE = D == 64 && NW == 8 && KG == 1 ? 1 : 2;
+    const uint32_t kra = lds_addr(kbuf(it)) + (k_row + wk0 * KL::ROW) * 2;
+    const uint32_t vra = lds_addr(vbuf(it)) + (v_row + wk0 * VL::ROW) * 2;
+    s = zero16();
+    dp = zero16();
+    u32x4 rk[PIPE + 1], rv[PIPE + 1];
+    auto rd = [&](auto KS) __attribute__((always_inline)) {
+      constexpr int ks = decltype(KS)::value, sl = ks % (PIPE + 1);
+      row_issue<KL, kb * 32, ks * 16>(kra, rk[sl]);
+      row_issue<VL, kb * 32, ks * 16>(vra, rv[sl]);
+    };
+    static_for<PIPE>([&](auto KS) { rd(KS); });
+    static_for<NKS>([&](auto KS) {
+      constexpr int ks = decltype(KS)::value, sl = ks % (PIPE + 1);
+      if constexpr (ks + PIPE < NKS) {
+        rd(std::integral_constant<int, ks + PIPE>{});
+        row_wait<2 * PIPE>(rk[sl], rv[sl]);
+      } else {
+        row_wait<2 * (NKS - 1 - ks)>(rk[sl], rv[sl]);
+      }
+      s = mfma32(as_bf16x8(rk[sl]), qf[ks], s);
+      dp = mfma32(as_bf16x8(rv[sl]), gf[ks], dp);
+      hook(std::integral_constant<int, kb * NKS + ks>{});
+    });
+  };
+  auto mask = [&](f32x16& s, int lim) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (acc_row_off(r) >= lim) s[r] = -INFINITY;
+  };
+
+  if (few) {
+    // D = sum_j P_ij dP_ij in 32 bits over the first tile of the shared and of the own
+    // keys, for the rows that see no others.  D from O carries O's rounding into
+    // dS = P (dP - D): of a row with one key, whose dS is 0, that is all there is, and up
+    // to some ten keys it shows beside dS's own rounding (dQ of 50 sequences of 21-338
+    // causal rows off by 2.7e-3 of its norm, 2.4e-3 so).
+    float dot = 0.f;
+    wait_dma();
+    __syncthreads();
+    for (int it = 0; it <= npre; ++it) {
+      const int end = (it < npre ? a.b.prefix : lane_end) - wk0;
+      // keys of the tile that such a row of this wave sees end here
+      const int some = (it < npre ? a.b.prefix : min(wave_end, kCrossFewKeys - a.b.prefix)) - wk0;
+      static_for<(C::WK < kCrossFewKeys ? C::WK : kCrossFewKeys) / 32>([&](auto KB) {
+        if (decltype(KB)::value * 32 >= some) return;
+        f32x16 s, dp;
+        products(KB, it, s, dp, [](auto) {});
+        mask(s, end - (decltype(KB)::value * 32 + hh * 4));
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          dot = __builtin_fmaf(fast_exp2(__builtin_fmaf(s[r], a.scale_log2, -lse2)), dp[r], dot);
+      });
+    }
+    dot += partner32(dot);
+    if constexpr (KG > 1) {
+      // (in the second buffer: the first tile is the one that the loop begins with)
+      __syncthreads();
+      float* sums = reinterpret_cast<float*>(kbuf(1)) + rg * KG * 32;
+      if (l < 32) sums[kg * 32 + l] = dot;
+      __syncthreads();
+      dot = 0.f;
+#pragma unroll
+      for (int j = 0; j < KG; ++j) dot += sums[j * 32 + (l & 31)];
+    }
+    if (a.b.prefix + max(0, lane_end) <= kCrossFewKeys) ddv = dot;
+    if (hh == 0 && at.part == 0 && kg == 0 && !second && row < row_end) {
+      const int tok = cross_token(a.b, row);
+      a.dd[(size_t)(hk * g + (row - tok * g)) * a.b.tq + tok] = ddv;
+    }
+    if (t_begin > 0) {
+      __syncthreads();
+      if (t_begin < t_end) issue(t_begin);
+    }
+  }
   f32x16 dqa[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dqa[i] = zero16();
 
-  // keys of tile `it` for this wave (returns false where it has none); hook(N) runs
-  // after the products of the N-th K-step
+  // keys of tile `it` for this wave (returns false where it has none)
   auto compute = [&](int it, auto&& hook) __attribute__((always_inline)) {
     const bool pre = it < npre;
     const int k0 = (pre ? it : it - npre) * BK + wk0;
     const int some = pre ? a.b.prefix : wave_end, every = pre ? a.b.prefix : wave_first;
     if (wrow0 >= row_end || k0 >= some) return false;
     const int end = pre ? a.b.prefix : lane_end;
-    const uint32_t kra = lds_addr(kbuf(it)) + (k_row + wk0 * KL::ROW) * 2;
     const uint32_t ka = lds_addr(kbuf(it)) + (k_tr + wk0 * KL::ROW) * 2;
-    const uint32_t vra = lds_addr(vbuf(it)) + (v_row + wk0 * VL::ROW) * 2;
     const bool need_mask = k0 + C::WK > every;
     static_for<C::WK / 32>([&](auto KB) {
       constexpr int kb = decltype(KB)::value;
-      f32x16 s = zero16(), dp = zero16();
-      {
-        constexpr int NKS = D / 16, PIPE = D == 64 && NW == 8 && KG == 1 ? 1 : 2;
-        u32x4 rk[PIPE + 1], rv[PIPE + 1];
-        auto rd = [&](auto KS) __attribute__((always_inline)) {
-          constexpr int ks = decltype(KS)::value, sl = ks % (PIPE + 1);
-          row_issue<KL, kb * 32, ks * 16>(kra, rk[sl]);
-          row_issue<VL, kb * 32, ks * 16>(vra, rv[sl]);
-        };
-        static_for<PIPE>([&](auto KS) { rd(KS); });
-        static_for<NKS>([&](auto KS) {
-          constexpr int ks = decltype(KS)::value, sl = ks % (PIPE + 1);
-          if constexpr (ks + PIPE < NKS) {
-            rd(std::integral_constant<int, ks + PIPE>{});
-            row_wait<2 * PIPE>(rk[sl], rv[sl]);
-          } else {
-            row_wait<2 * (NKS - 1 - ks)>(rk[sl], rv[sl]);
-          }
-          s = mfma32(as_bf16x8(rk[sl]), qf[ks], s);
-          dp = mfma32(as_bf16x8(rv[sl]), gf[ks], dp);
-          hook(std::integral_constant<int, kb * NKS + ks>{});
-        });
-      }
-      if (need_mask) {
-        const int lim = end - (k0 + kb * 32 + hh * 4);
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (acc_row_off(r) >= lim) s[r] = -INFINITY;
-      }
+      f32x16 s, dp;
+      products(KB, it, s, dp, hook);
+      if (need_mask) mask(s, end - (k0 + kb * 32 + hh * 4));
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float pv = fast_exp2(__builtin_fmaf(s[r], a.scale_log2, -lse2));

@@ -33,7 +33,9 @@ from typing import Dict, List
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIBRARY_KERNELS = ("plan_kernel", "fwd_kernel", "bwd_dkdv_kernel", "bwd_dq_kernel",
-                   "split_merge_kernel", "split_sum_kernel")
+                   "split_merge_kernel", "split_sum_kernel", "cross_list_kernel",
+                   "cross_fwd_kernel", "cross_merge_kernel", "cross_dq_kernel",
+                   "cross_dkdv_kernel", "cross_sum_kernel", "rotary_kernel")
 
 
 def code_text(src: str) -> str:

@@ -280,3 +280,40 @@ def test_cache_beyond_32_bit_offsets():
     cu.check("dv", dv[at], ref["dv"])
     dk[at] = 0
     assert not dk.any()
+
+
+@pytest.mark.parametrize("prefix", [0, 1])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [(3, 1, 17), (300, 2, 70)])
+def test_a_row_with_one_key_has_no_gradient(rows, d, prefix):
+    """Its P is 1 whatever the key, so dS = P (dP - D) is 0: what is left is P's own
+    distance from 1.  The exponent is the difference of the logit m (base 2) and of LSE,
+    two products from each other and back, five roundings of 2^-24 |m|; with the power's
+    2^-22 and the sum's 2^-24 that is under (1 + |m| / 4) 2^-20 of dP, and dS enters the
+    product rounded to bf16.  (With D from a bf16 O it would be up to 2^-8.)"""
+    import torch
+    from paper_2511_13198_amd import pdyattn
+    lk = [0] * len(rows) if prefix else [1] * len(rows)
+    hq, hkv, g = 4, 2, 2
+    x = make(rows, lk, prefix, hq, hkv, d, seed=d + prefix, behind=0)
+    rest = (cu.offsets(rows, "cuda"), cu.offsets(lk, "cuda"), max(rows), max(1, max(lk)) if not prefix
+            else 0)
+    scale = 1 / math.sqrt(d)
+    if prefix:
+        ins = (x["q"], x["k"], x["v"], x["kp"], x["vp"])
+        o, lse = pdyattn.attn_prefix_fwd(*ins, *rest, scale=scale)
+        dq = pdyattn.attn_prefix_bwd(*ins, o, lse, x["do"], *rest, scale=scale)[0]
+        key, val = x["kp"][:1].expand(len(rows), -1, -1), x["vp"][:1].expand(len(rows), -1, -1)
+    else:
+        ins = (x["q"], x["k"], x["v"])
+        o, lse = pdyattn.attn_cross_fwd(*ins, *rest, scale=scale)
+        dq = pdyattn.attn_cross_bwd(*ins, o, lse, x["do"], *rest, scale=scale)[0]
+        key, val = x["k"], x["v"]
+    at = torch.repeat_interleave(torch.arange(len(rows)), torch.tensor(rows)).cuda()
+    k, v = (t[at].double().repeat_interleave(g, 1) for t in (key, val))
+    m = (x["q"].double() * k).sum(2) * scale / math.log(2)
+    dp = (x["do"].double() * v).sum(2)
+    bound = scale * dp.abs() * (1 + m.abs() / 4) * 2.0 ** -20 * (1 + 2.0 ** -8)
+    off = dq.double().abs() / (bound[:, :, None] * k.abs()).clamp_min(1e-30)
+    print(f"    worst {float(off.max()):.3f} of its bound", flush=True)
+    assert float(off.max()) <= 1.0
