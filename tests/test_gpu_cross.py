@@ -46,6 +46,10 @@ CASES = [
     ([100, 33, 1, 250], [100, 33, 1, 250], None, 200, 8, 2, 128, True),
     ([300, 129], [300, 400], None, 1, 3, 1, 64, True),
     ([90, 120], [64, 64], [10, 64], 65, 2, 2, 128, True),
+    # many heads to a group, and a prime number of them
+    ([3, 9, 1], [40, 300, 7], None, 20, 64, 1, 64, True),
+    ([40, 5], [100, 260], None, 0, 48, 1, 128, True),
+    ([70, 12], [90, 150], [90, 0], 0, 7, 1, 64, False),
     # a little more than whole rounds of tiles: the last items alone in parts, tiles that
     # end inside a token's heads
     ([864, 500, 1, 735, 600], [864, 500, 1, 735, 600], None, 1500, 24, 8, 128, True),
@@ -317,3 +321,16 @@ def test_a_row_with_one_key_has_no_gradient(rows, d, prefix):
     off = dq.double().abs() / (bound[:, :, None] * k.abs()).clamp_min(1e-30)
     print(f"    worst {float(off.max()):.3f} of its bound", flush=True)
     assert float(off.max()) <= 1.0
+
+
+def test_no_keys_at_all():
+    """Empty k and v: o = 0, lse = -inf, dq = 0."""
+    import torch
+    from paper_2511_13198_amd import pdyattn
+    q = torch.ones((5, 4, 64), dtype=torch.bfloat16, device="cuda")
+    k = torch.empty((0, 2, 64), dtype=torch.bfloat16, device="cuda")
+    cq, ck = cu.offsets([2, 3], "cuda"), cu.offsets([0, 0], "cuda")
+    o, lse = pdyattn.attn_cross_fwd(q, k, k, cq, ck)
+    assert not bool(o.any()) and bool((lse == -math.inf).all())
+    dq, dk, dv = pdyattn.attn_cross_bwd(q, k, k, o, lse, q, cq, ck)
+    assert not bool(dq.any()) and dk.shape == dv.shape == k.shape
