@@ -17,6 +17,12 @@
 // dK/dV row steps.  A step is BQ rows: `pack` heads of the group (the largest power
 // of two that divides it, at most 32) by BQ / pack tokens, so that a sequence of few
 // tokens still fills a step, and a step's rows have one address pattern.
+//
+// Bound by the products: 8 sequences of 256-2,048 rows over 1,024-8,192 keys, 32/8 heads,
+// dQ 345 us (3 products, 1,065 TFLOP/s), dK/dV 503 us (4 products, 975 TFLOP/s; matrix
+// cores busy 54 % and 47 % of the time at 1.8-1.9 GHz).  Short rows over many keys are
+// bound by reading keys and writing gradients: 32 x 8-200 rows over 577-1,024 keys, 16
+// heads, d = 64, bf16 gradients, 34 and 60 us (dK/dV moves 0.24 GB).
 #pragma once
 #include "cross.hpp"
 
