@@ -132,6 +132,12 @@ constexpr double kMoveBytesPerUs = 4.0e6;           // partial results written a
 //   rows) 99 / 138, of 32 (128 rows, 40 sequences, a step) 853 / 858.
 constexpr int64_t kApartRows = 64, kApartPrefix = 512;
 
+// Few rows over so many keys at most are not cut: the launch that combines parts takes
+// longer than they save.  us with parts / whole, a token for each of 1-60 sequences over
+// 400, 800, 1,500 keys: d = 64 10.6 / 7.8, 11.0 / 9.9, 10.7 / 14.0; d = 128 11.6 / 10.2,
+// 12.5 / 13.9, 11.8 / 20.5.
+constexpr int64_t kWholeKeys64 = 1024, kWholeKeys128 = 512;
+
 // Shape and parts of a launch over sequences of more than 64 rows: the ones of least
 // estimated time, from the average rows and keys of a sequence.  With I items of u
 // units, on `slots` workgroups at a time,
@@ -217,7 +223,8 @@ CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
     const bool few = f.sh.groups == 4;
     if (k.dq && few) f.sh = {4, 2};
     entries = (few ? 4 : 2) * kCUs;
-    if (!apart && most_items(s, s.n, s.max_q, f.sh.rows()) * s.hkv >= (few ? 16 : 2) * kCUs)
+    if (!apart && (most_items(s, s.n, s.max_q, f.sh.rows()) * s.hkv >= (few ? 16 : 2) * kCUs ||
+                   s.max_k + s.prefix <= (s.d == 64 ? kWholeKeys64 : kWholeKeys128)))
       most = 1;
   }
   const int rows = f.sh.rows(), keys_tile = k.key_tile(s, f.sh);
