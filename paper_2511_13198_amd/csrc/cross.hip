@@ -132,11 +132,17 @@ constexpr double kMoveBytesPerUs = 4.0e6;           // partial results written a
 //   rows) 99 / 138, of 32 (128 rows, 40 sequences, a step) 853 / 858.
 constexpr int64_t kApartRows = 64, kApartPrefix = 512;
 
-// Few rows over so many keys at most are not cut: the launch that combines parts takes
-// longer than they save.  us with parts / whole, a token for each of 1-60 sequences over
-// 400, 800, 1,500 keys: d = 64 10.6 / 7.8, 11.0 / 9.9, 10.7 / 14.0; d = 128 11.6 / 10.2,
-// 12.5 / 13.9, 11.8 / 20.5.
-constexpr int64_t kWholeKeys64 = 1024, kWholeKeys128 = 512;
+// Few rows over so many keys at most, shared ones among them, are one whole item a tile:
+// the launch that combines partial results takes longer than these save.  us with parts /
+// whole, a token for each of 1-60 sequences over 400, 800, 1,500 keys: d = 64 10.6 / 7.8,
+// 11.0 / 9.9, 10.7 / 14.0; d = 128 11.6 / 10.2, 12.5 / 13.9, 11.8 / 20.5.  Apart / whole,
+// over 100 own and 520, 700, 1,000 shared keys: 16 sequences, 8 kv heads of 64, 11.8 / 9.8,
+// 11.8 / 10.6, 11.8 / 12.2; 64 of 128, which fill the chip, 19.7 / 15.5, 20.7 / 16.5, 20.7 /
+// 19.2.
+bool short_keys(const CrossSizes& s) {
+  const bool more = s.d == 64 || (s.prefix > 0 && s.n * s.hkv >= 2 * kCUs);
+  return s.max_k + s.prefix <= (more ? 1024 : 512);
+}
 
 // Shape and parts of a launch over sequences of more than 64 rows: the ones of least
 // estimated time, from the average rows and keys of a sequence.  With I items of u
@@ -205,7 +211,8 @@ CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
   // bytes of one slice of partial results (no queries: nothing is launched)
   const int64_t slice = std::max<int64_t>(1, s.tq) * s.hq * (s.d + 1) * 4;
   c.keys = s.prefix == 0 ? pdy::CROSS_OWN
-           : s.seq_rows() > kApartRows || s.prefix <= kApartPrefix || 2 * slice > kPartBytes
+           : s.seq_rows() > kApartRows || s.prefix <= kApartPrefix || short_keys(s) ||
+                   2 * slice > kPartBytes
                ? pdy::CROSS_FUSED
                : pdy::CROSS_APART;
   const bool apart = c.keys == pdy::CROSS_APART;
@@ -224,7 +231,7 @@ CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
     if (k.dq && few) f.sh = {4, 2};
     entries = (few ? 4 : 2) * kCUs;
     if (!apart && (most_items(s, s.n, s.max_q, f.sh.rows()) * s.hkv >= (few ? 16 : 2) * kCUs ||
-                   s.max_k + s.prefix <= (s.d == 64 ? kWholeKeys64 : kWholeKeys128)))
+                   short_keys(s)))
       most = 1;
   }
   const int rows = f.sh.rows(), keys_tile = k.key_tile(s, f.sh);
