@@ -514,12 +514,15 @@ def _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k, scale, seqlens_k):
     bf16, i32 = torch.bfloat16, torch.int32
     dev = q.device
     index = dev.index
-    if not (_fits(q, bf16, 3, index) and _fits(k, bf16, 3, index) and _fits(v, bf16, 3, index) and
+    shape_q, shape = q.shape, k.shape
+    if not (len(shape_q) == 3 and len(shape) == 3 and q.dtype is bf16 and k.dtype is bf16 and
+            v.dtype is bf16 and q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and
+            q.get_device() == index and k.get_device() == index and v.get_device() == index and
             _fits(cu_q, i32, 1, index) and _fits(cu_k, i32, 1, index)):
         _refuse(dev, (q, "q", bf16, 3), (k, "k", bf16, 3), (v, "v", bf16, 3),
                 (cu_q, "cu_seqlens_q", i32, 1), (cu_k, "cu_seqlens_k", i32, 1))
-    T, hq, d = q.shape
-    tk, hkv, dk = shape = k.shape
+    T, hq, d = shape_q
+    tk, hkv, dk = shape
     if dk != d or v.shape != shape:
         raise ValueError("k and v must be [Tk, Hkv, d] with q's d")
     n = cu_q.numel() - 1
@@ -539,9 +542,10 @@ def _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k, scale, seqlens_k):
     ptrs, offsets = (q.data_ptr(), k.data_ptr(), v.data_ptr()), (cu_q.data_ptr(), cu_k.data_ptr(), used)
     if kp is None:
         return dev, ptrs, offsets, (), sizes, scale
-    if not (_fits(kp, bf16, 3, index) and _fits(vp, bf16, 3, index)):
-        _refuse(dev, (kp, "k_prefix", bf16, 3), (vp, "v_prefix", bf16, 3))
     shape = kp.shape
+    if not (len(shape) == 3 and kp.dtype is bf16 and vp.dtype is bf16 and kp.is_contiguous() and
+            vp.is_contiguous() and kp.get_device() == index and vp.get_device() == index):
+        _refuse(dev, (kp, "k_prefix", bf16, 3), (vp, "v_prefix", bf16, 3))
     if shape[1] != hkv or shape[2] != d or vp.shape != shape:
         raise ValueError("k_prefix and v_prefix must be [P, Hkv, d]")
     return (dev, (*ptrs, kp.data_ptr(), vp.data_ptr()), (*offsets, shape[0]), (shape[0],), sizes,
@@ -555,15 +559,16 @@ def _cross_workspace(kind: str, pre, sizes, device):
     return _ws(getattr(lib(), name)(*pre, T, tk, n, max_q, max_k, hq, hkv, d), device)
 
 
-def _check_outputs(dev, o, name: str, q, lse, workspace, hq: int, T: int):
-    """o like q, lse [Hq, T], a workspace, all on the device."""
+def _check_outputs(dev, o, name: str, lse, workspace, T: int, hq: int, d: int):
+    """o [T, Hq, d], lse [Hq, T], a workspace, all on the device."""
     import torch
     index = dev.index
-    if not (_fits(o, torch.bfloat16, 3, index) and _fits(lse, torch.float32, 2, index) and
-            workspace.get_device() == index and workspace.is_contiguous()):
+    if not (o.dtype is torch.bfloat16 and lse.dtype is torch.float32 and o.is_contiguous() and
+            lse.is_contiguous() and workspace.is_contiguous() and o.get_device() == index and
+            lse.get_device() == index and workspace.get_device() == index):
         _refuse(dev, (o, name, torch.bfloat16, 3), (lse, "lse", torch.float32, 2),
                 (workspace, "workspace", workspace.dtype, workspace.dim()))
-    if o.shape != q.shape or lse.shape != (hq, T):
+    if o.shape != (T, hq, d) or lse.shape != (hq, T):
         raise ValueError(f"{name} must be q's shape, lse [Hq, T]")
 
 
@@ -572,14 +577,14 @@ def _cross_fwd(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k, causal, scale, seqlens
     import torch
     dev, ptrs, offsets, pre, sizes, scale = _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k,
                                                         scale, seqlens_k)
-    T, hq = sizes[1], sizes[5]
+    _, T, _, _, _, hq, _, d = sizes
     if out is None:
         out = torch.empty_like(q)
     if lse is None:
         lse = torch.empty((hq, T), dtype=torch.float32, device=dev)
     if workspace is None:
         workspace = _cross_workspace("fwd", pre, sizes, dev)
-    _check_outputs(dev, out, "out", q, lse, workspace, hq, T)
+    _check_outputs(dev, out, "out", lse, workspace, T, hq, d)
     _launch("attn_prefix_fwd" if pre else "attn_cross_fwd", dev, *ptrs, *offsets, *sizes,
             1 if causal else 0, scale, out.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
             workspace.nbytes)
@@ -620,24 +625,27 @@ def _cross_bwd(q, k, v, kp, vp, o, lse, dout, cu_q, cu_k, max_q, max_k, causal, 
     dtype = given[0].dtype if given else grad_dtype or torch.float32
     if dtype not in (torch.float32, torch.bfloat16):
         raise TypeError(f"gradients must be torch.float32 or torch.bfloat16, got {dtype}")
+    _, T, tk, _, _, hq, hkv, d = sizes
+    index, own = dev.index, (tk, hkv, d)
+    shapes = ((T, hq, d), own, own, (pre[0], hkv, d), (pre[0], hkv, d)) if pre else ((T, hq, d), own, own)
     out = []
-    for name, g, like in zip(("dq", "dk", "dv", "dk_prefix", "dv_prefix"), grads, (q, k, v, kp, vp)):
-        if like is None:
-            continue
+    for i, shape in enumerate(shapes):
+        g = grads[i]
         if g is None:
-            g = torch.empty(like.shape, dtype=dtype, device=dev)
-        if not _fits(g, dtype, 3, dev.index):
+            g = torch.empty(shape, dtype=dtype, device=dev)
+        elif not (g.dtype is dtype and g.shape == shape and g.is_contiguous() and
+                  g.get_device() == index):
+            name = ("dq", "dk", "dv", "dk_prefix", "dv_prefix")[i]
             _refuse(dev, (g, name, dtype, 3))
-        if g.shape != like.shape:
-            raise ValueError(f"{name} must be {list(like.shape)}")
+            raise ValueError(f"{name} must be {list(shape)}")
         out.append(g)
     if workspace is None:
         workspace = _cross_workspace("bwd", pre, sizes, dev)
-    if not _fits(dout, torch.bfloat16, 3, dev.index):
+    if not _fits(dout, torch.bfloat16, 3, index):
         _refuse(dev, (dout, "dout", torch.bfloat16, 3))
-    if dout.shape != q.shape:
+    if dout.shape != shapes[0]:
         raise ValueError("dout must match q")
-    _check_outputs(dev, o, "o", q, lse, workspace, sizes[5], sizes[1])
+    _check_outputs(dev, o, "o", lse, workspace, T, hq, d)
     _launch("attn_prefix_bwd" if pre else "attn_cross_bwd", dev, *ptrs, o.data_ptr(),
             lse.data_ptr(), dout.data_ptr(), *offsets, *sizes, 1 if causal else 0, scale,
             1 if dtype is torch.bfloat16 else 0, *[g.data_ptr() for g in out],
@@ -717,23 +725,28 @@ def attn_rotary(q, k, positions, sections, base: float = 10000.0, freqs=None,
     if (q is None and out_q is not None) or (k is None and out_k is not None):
         raise ValueError("out_q without q" if q is None else "out_k without k")
 
-    def side(name, t, o):
-        """(output, pointers of input and output, heads) of q or k."""
+    T = d = None
+    heads, ptrs, filled = [0, 0], [0, 0, 0, 0], [out_q, out_k]
+    for i, t in enumerate((q, k)):
         if t is None:
-            return None, 0, 0, 0
+            continue
+        o = filled[i]
         if o is None:
-            o = torch.empty(t.shape, dtype=tout, device=dev)
-        if not (_fits(t, tin, 3, index) and _fits(o, tout, 3, index)):
+            o = filled[i] = torch.empty(t.shape, dtype=tout, device=dev)
+        shape = t.shape
+        if not (len(shape) == 3 and t.dtype is tin and o.dtype is tout and t.is_contiguous() and
+                o.is_contiguous() and t.get_device() == index and o.get_device() == index):
+            name = "qk"[i]
             _refuse(dev, (t, name, tin, 3), (o, f"out_{name}", tout, 3))
-        if o.shape != t.shape:
-            raise ValueError(f"out_{name} must have {name}'s shape")
-        return o, t.data_ptr(), o.data_ptr(), t.shape[1]
-
-    out_q, q_in, q_to, hq = side("q", q, out_q)
-    out_k, k_in, k_to, hkv = side("k", k, out_k)
-    T, _, d = first.shape
-    if q is not None and k is not None and (k.shape[0] != T or k.shape[2] != d):
-        raise ValueError("q and k must have the same tokens and head dimension")
+        if o.shape != shape:
+            raise ValueError(f"out_{'qk'[i]} must have {'qk'[i]}'s shape")
+        if T is None:
+            T, heads[i], d = shape
+        elif shape[0] != T or shape[2] != d:
+            raise ValueError("q and k must have the same tokens and head dimension")
+        else:
+            heads[i] = shape[1]
+        ptrs[i], ptrs[2 + i] = t.data_ptr(), o.data_ptr()
     if positions.dim() == 1:
         positions = positions[:, None]
     if not _fits(positions, torch.int32, 2, index):
@@ -745,7 +758,7 @@ def attn_rotary(q, k, positions, sections, base: float = 10000.0, freqs=None,
                          f"{list(positions.shape)}")
     pairs, turns, pair_axes, _ = _rotary_tables(sections, base,
                                                 None if freqs is None else tuple(freqs))
-    _launch("attn_rotary", dev, q_in, k_in, positions.data_ptr(), T, axes, hq, hkv, d, pairs,
-            turns, pair_axes, 1 if interleaved else 0, 1 if inverse else 0,
-            1 if tin is torch.float32 else 0, 1 if tout is torch.float32 else 0, q_to, k_to)
-    return out_q, out_k
+    _launch("attn_rotary", dev, ptrs[0], ptrs[1], positions.data_ptr(), T, axes, heads[0], heads[1],
+            d, pairs, turns, pair_axes, 1 if interleaved else 0, 1 if inverse else 0,
+            1 if tin is torch.float32 else 0, 1 if tout is torch.float32 else 0, ptrs[2], ptrs[3])
+    return filled[0], filled[1]
