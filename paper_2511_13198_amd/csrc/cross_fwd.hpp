@@ -259,18 +259,13 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1)
       kd.issue(x.k, kvstride, x.keys, kbuf(t));
       vd.issue(x.v, kvstride, x.keys, vbuf(t));
     };
-    constexpr int S = C::STAGES;
+    constexpr int S = C::STAGES;  // 1: a tile's copies begin when its products have ended
     constexpr int PK = TileDma<KL, BK, NW>::PER_WAVE, PV = TileDma<VL, BK, NW>::PER_WAVE;
-    constexpr int kMin = TileDma<KL, BK, NW>::INSTS / NW + TileDma<VL, BK, NW>::INSTS / NW;
-#pragma unroll
-    for (int t = 0; t < S - 1; ++t)
-      if (t_begin + t < t_end) issue(t_begin + t);
-    if (S == 1 && t_begin < t_end) issue(t_begin);
+    if (t_begin < t_end) issue(t_begin);
     for (int it = t_begin; it < t_end; ++it) {
-      if (S > 2 && it + S - 2 < t_end) wait_dma_n<(S > 2 ? S - 2 : 0) * kMin>();
-      else wait_dma();
+      wait_dma();
       __syncthreads();
-      const int tn = S == 1 ? it + 1 : it + S - 1;
+      const int tn = it + 1;
       const bool more = tn < t_end;
       const bool pre = it < npre;
       const int k0t = (pre ? it : it - npre) * BK + wk0;  // this wave's first key
