@@ -320,6 +320,13 @@ CrossKv kv_launch(const CrossSizes& s) {
   // items alike in their rows need no cut once they fill the chip; a shared tile has
   // the rows of all sequences
   if (n * s.hkv >= target && (s.prefix == 0 || s.n == 1)) parts = 1;
+  // Items of few steps are not cut: the launch that sums parts takes longer than they
+  // save.  us of a backward with parts / whole, longest items of 1, 4, 8 and 16 steps: 4
+  // sequences over 300 keys, 8 heads, d = 64 18.6 / 16.1, 23.5 / 21.0, 28.9 / 22.4, 36.2 /
+  // 24.7; 8 query heads to one of 128 28.7 / 25.7 (2), 35.6 / 34.9 (8), 36.9 / 47.8 (16).
+  const int sh = pack_log2(s);
+  const int64_t rows = s.prefix > 0 ? s.tq : s.max_q;  // that see the longest
+  if (ceil_div(rows << sh, 1 << c.rows_log2) * (s.g() >> sh) <= 8) parts = 1;
   c.max_parts = (int)std::max<int64_t>(1, parts);
   k.wgs = n + (c.max_parts > 1 ? c.entries + 2 : 0);
   return k;
