@@ -130,18 +130,25 @@ constexpr double kMoveBytesPerUs = 4.0e6;           // partial results written a
 //   64 sequences of 1 token, 32/8 heads, behind 32,768 keys 97 / 662, 1,024 49 / 59,
 //   512 49 / 48, 64 48 / 42; 32 of 8 tokens (32 rows) behind 8,000 64 / 78, of 16 (64
 //   rows) 99 / 138, of 32 (128 rows, 40 sequences, a step) 853 / 858.
-constexpr int64_t kApartRows = 64, kApartPrefix = 512;
+// With more (sequence, kv head) pairs than 4 a CU fused takes rounds that apart does not:
+// 256 and 512 sequences, 8 kv heads, 30 own keys, d = 64, us apart / fused behind 128 shared
+// keys 26 / 29, 43 / 54, 256 27 / 33, 44 / 62; over 400 own 54 / 51, 115 / 120 and 56 / 55,
+// 115 / 129.
+constexpr int64_t kApartRows = 64, kApartPrefix = 512, kApartPrefixMany = 256;
 
 // Few rows over so many keys at most, shared ones among them, are one whole item a tile:
 // the launch that combines partial results takes longer than these save.  us with parts /
 // whole, a token for each of 1-60 sequences over 400, 800, 1,500 keys: d = 64 10.6 / 7.8,
 // 11.0 / 9.9, 10.7 / 14.0; d = 128 11.6 / 10.2, 12.5 / 13.9, 11.8 / 20.5.  Apart / whole,
-// over 100 own and 520, 700, 1,000 shared keys: 16 sequences, 8 kv heads of 64, 11.8 / 9.8,
-// 11.8 / 10.6, 11.8 / 12.2; 64 of 128, which fill the chip, 19.7 / 15.5, 20.7 / 16.5, 20.7 /
-// 19.2.
+// over 100 own and 520, 700, 900 shared keys, up to two pairs a CU: 64 sequences, 8 kv heads
+// of 64, 12.2 / 11.3, 12.2 / 12.2, 12.4 / 14.1 (128 sequences 20.6 / 24.5, 20.6 / 25.9); 60
+// sequences of 8 heads to one of 128 15.7 / 13.3, 15.8 / 14.9, 16.3 / 17.4, 3 of 8 to 8 12.6 /
+// 12.8, 11.4 / 14.3.  Parts / whole behind 256 shared and 400 own keys, 32/8 heads of 128, 64
+// sequences 30.0 / 25.8, 1,024 of 8/1 52.8 / 50.0.
 bool short_keys(const CrossSizes& s) {
-  const bool more = s.d == 64 || (s.prefix > 0 && s.n * s.hkv >= 2 * kCUs);
-  return s.max_k + s.prefix <= (more ? 1024 : 512);
+  const int64_t most = s.prefix > kApartPrefix ? (s.d == 64 ? 800 : 640)
+                       : s.d == 64 || (s.prefix > 0 && s.n * s.hkv >= 2 * kCUs) ? 1024 : 512;
+  return s.max_k + s.prefix <= most;
 }
 
 // Shape and parts of a launch over sequences of more than 64 rows: the ones of least
@@ -210,9 +217,11 @@ CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
   pdy::CrossCut& c = f.cut;
   // bytes of one slice of partial results (no queries: nothing is launched)
   const int64_t slice = std::max<int64_t>(1, s.tq) * s.hq * (s.d + 1) * 4;
+  const int64_t pairs = s.n * s.hkv;
   c.keys = s.prefix == 0 ? pdy::CROSS_OWN
-           : s.seq_rows() > kApartRows || s.prefix <= kApartPrefix || short_keys(s) ||
-                   2 * slice > kPartBytes
+           : s.seq_rows() > kApartRows || 2 * slice > kPartBytes ||
+                   s.prefix <= (pairs > 4 * kCUs ? kApartPrefixMany : kApartPrefix) ||
+                   (pairs <= 2 * kCUs && short_keys(s))
                ? pdy::CROSS_FUSED
                : pdy::CROSS_APART;
   const bool apart = c.keys == pdy::CROSS_APART;

@@ -117,7 +117,11 @@ def test_shapes_of_launches_and_what_the_gpu_cases_cover():
     assert shape(50, 80, 464, 16, 16, 128)["cross_fwd_kernel"] == (4, 1, 1)
     assert shape(64, 512, 512, 32, 32, 128)["cross_fwd_kernel"] == (8, 1, 1)
     assert shape(1, 200, 30000, 16, 16, 128)["cross_fwd_kernel"][2] > 8
-    assert shape(4, 1, 100, 8, 2, 128, 513)["apart"] and not shape(4, 1, 100, 8, 2, 128, 512)["apart"]
+    # shared keys apart for few rows behind many of them; not where all keys are few, nor
+    # (more of them) where the sequences fill the chip several times
+    assert shape(4, 1, 200, 8, 2, 128, 513)["apart"] and not shape(4, 1, 200, 8, 2, 128, 512)["apart"]
+    assert not shape(4, 1, 100, 8, 2, 128, 540)["apart"] and shape(4, 1, 101, 8, 2, 128, 540)["apart"]
+    assert shape(300, 1, 10, 8, 4, 128, 257)["apart"] and not shape(200, 1, 10, 8, 4, 128, 257)["apart"]
     assert not shape(4, 17, 100, 8, 2, 128, 4000)["apart"]
     seen = set()
     for lq, lk, used, prefix, hq, hkv, d, causal in gpu.CASES:
