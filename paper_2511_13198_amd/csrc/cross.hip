@@ -601,8 +601,9 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
   a.scale = scale;
   a.scale_log2 = scale * pdy::kLog2e;
   a.pack_log2 = pack_log2(s);
-  const bool rows = s.tq > 0, keys = s.tk + s.prefix > 0;
-  if (sp.list) {
+  // (keys of no sequence alone: no tile of keys)
+  const bool rows = s.tq > 0, keys = kv.wgs > 0;
+  if (sp.list && (rows || keys)) {
     f.cut.list = reinterpret_cast<int32_t*>(lists);
     kv.cut.list = reinterpret_cast<int32_t*>(lists + sp.list);
     e = launch_lists(a.b, rows ? &f.cut : nullptr, keys ? &kv.cut : nullptr, a.pack_log2, hs);
