@@ -535,7 +535,8 @@ def _cross_args(q, k, v, kp, vp, cu_q, cu_k, max_q, max_k, scale, seqlens_k):
         if seqlens_k.numel() != n:
             raise ValueError("seqlens_k must have num_seqs lengths")
         used = seqlens_k.data_ptr()
-    max_q = _longest(cu_q, "cu_seqlens_q", T) if max_q is None else max_q
+    if max_q is None:  # (the library wants at least 1 where there are rows, of a sequence or not)
+        max_q = max(_longest(cu_q, "cu_seqlens_q", T), min(1, T))
     max_k = _longest(cu_k, "cu_seqlens_k", tk) if max_k is None else max_k
     sizes = (n, T, tk, max_q, max_k, hq, hkv, d)
     scale = 1.0 / math.sqrt(d) if scale is None else scale

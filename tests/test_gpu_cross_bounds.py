@@ -31,3 +31,23 @@ def test_keys_of_no_sequence_alone(n):
         dk, dv = filled(k.shape, torch.float32), filled(k.shape, torch.float32)
         dq, _, _ = pdyattn.attn_cross_bwd(q, k, k, o, lse, q, cq, ck, dk=dk, dv=dv)
         assert (dq == 0).all() and (dk == 7).all() and (dv == 7).all()
+
+
+@pytest.mark.parametrize("prefix", [0, 5])
+def test_rows_of_no_sequence_alone(prefix):
+    """Sequences without queries beside rows of q that belong to none, the longest length
+    left to the call: o, lse and dq stay as they were, the keys' gradients are 0."""
+    import torch
+    from paper_2511_13198_amd import pdyattn
+    q, k = filled((5, 4, 64), torch.bfloat16), filled((6, 2, 64), torch.bfloat16)
+    kp = filled((prefix, 2, 64), torch.bfloat16)
+    cq, ck = cu.offsets([0, 0], "cuda"), cu.offsets([4, 2], "cuda")
+    o, lse, dq = filled(q.shape, torch.bfloat16), filled((4, 5), torch.float32), filled(q.shape, torch.float32)
+    if prefix:
+        pdyattn.attn_prefix_fwd(q, k, k, kp, kp, cq, ck, out=o, lse=lse)
+        grads = pdyattn.attn_prefix_bwd(q, k, k, kp, kp, o, lse, q, cq, ck, dq=dq)
+    else:
+        pdyattn.attn_cross_fwd(q, k, k, cq, ck, out=o, lse=lse)
+        grads = pdyattn.attn_cross_bwd(q, k, k, o, lse, q, cq, ck, dq=dq)
+    assert (o == 7).all() and (lse == 7).all() and (dq == 7).all()
+    assert all((g == 0).all() for g in grads[1:])
