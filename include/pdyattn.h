@@ -207,9 +207,12 @@ pdy_status attn_merge(const void* o_a, const float* lse_a, const void* o_b, cons
  *     v_prefix, bf16 [prefix_len, Hkv, d] (causal or not), which are read once for
  *     all rows where these are few a sequence.  prefix_len = 0 is attn_cross_*.
  *   - A row that sees no key gets o = 0, lse = -inf, and no gradient.
- *   - max_seqlen_q, max_seqlen_k: upper bounds of the sequences' queries and keys;
- *     rows beyond max_seqlen_q may stay unwritten.  Offsets are trusted as above,
- *     but clamped to the tensors: wrong ones give wrong results, no stray access.
+ *   - max_seqlen_q, max_seqlen_k: upper bounds of the sequences' queries and keys; with
+ *     seqlens_k the latter may bound the keys in use alone.  Of a sequence with more,
+ *     the rows beyond max_seqlen_q, and so the gradients of the keys that these see, and
+ *     dk, dv beyond max_seqlen_k may stay unwritten or are wrong; other sequences have
+ *     theirs.  Offsets are trusted as above, but clamped to the tensors: wrong ones give
+ *     wrong results, no stray access.
  *   - Gradients of sum(dout * o), given o and lse as the forward wrote them; with
  *     grad_bf16 = 0 fp32, with 1 bf16 (rounded once, from 32-bit sums).  dk and dv of
  *     keys not in use are 0; dk_prefix and dv_prefix sum the rows of all sequences.

@@ -246,6 +246,7 @@ CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
   const int rows = f.sh.rows(), keys_tile = k.key_tile(s, f.sh);
   c.rows_log2 = __builtin_ctz((unsigned)rows);
   c.key_log2 = __builtin_ctz((unsigned)keys_tile);
+  c.max_tiles = (int)ceil_div(s.seq_rows(), rows);
   c.least = 2;
   const int64_t items =
       most_items(s, s.n, s.max_q, rows) + (apart ? ceil_div(s.tq * s.g(), rows) : 0);
@@ -301,7 +302,8 @@ int pack_log2(const CrossSizes& s) {
   return n;
 }
 
-CrossKv kv_launch(const CrossSizes& s) {
+// rooms: max_k may bound the keys in use alone, and tiles cover those not in use too.
+CrossKv kv_launch(const CrossSizes& s, bool rooms) {
   CrossKv k;
   auto items = [&](int tile) {
     return std::min(s.tk / tile + s.n, s.n * ceil_div(s.max_k, tile)) + ceil_div(s.prefix, tile);
@@ -319,6 +321,7 @@ CrossKv kv_launch(const CrossSizes& s) {
   c.keys = pdy::CROSS_FUSED;
   c.key_log2 = __builtin_ctz((unsigned)k.sh.rows());
   c.rows_log2 = k.sh.nw == 4 && s.d == 128 ? 5 : 6;  // CrossDkdvCfg::BQ
+  c.max_tiles = 0;  // (of rows)
   c.list = nullptr;
   c.least = 4;
   const int64_t n = items(k.sh.rows()), target = kCUs;
@@ -337,7 +340,8 @@ CrossKv kv_launch(const CrossSizes& s) {
   const int64_t rows = s.prefix > 0 ? s.tq : s.max_q;  // that see the longest
   if (ceil_div(rows << sh, 1 << c.rows_log2) * (s.g() >> sh) <= 8) parts = 1;
   c.max_parts = (int)std::max<int64_t>(1, parts);
-  k.wgs = n + (c.max_parts > 1 ? c.entries + 2 : 0);
+  const int64_t tiles = rooms ? s.tk / k.sh.rows() + s.n + ceil_div(s.prefix, k.sh.rows()) : n;
+  k.wgs = tiles + (c.max_parts > 1 ? c.entries + 2 : 0);
   return k;
 }
 
@@ -456,7 +460,7 @@ pdy_status check_cross_in(const CrossIn& x, const CrossSizes& s) {
 pdy::CrossBatch batch_of(const CrossIn& x, const CrossSizes& s, int32_t causal) {
   return pdy::CrossBatch{x.cu_q, x.cu_k, x.len_k, (int)s.n, (int)s.tq, (int)s.tk, (int)s.prefix,
                          (int)s.hq, (int)s.hkv, (int)s.g(), (uint32_t)((1ull << 32) / s.g()),
-                         causal};
+                         causal, (int)(x.len_k ? s.tk : s.max_k)};
 }
 
 // The lists of a launch over rows, over keys (NULL: none), or both.
@@ -556,7 +560,7 @@ pdy_status cross_bwd_impl(const CrossIn& x, const void* o, const float* lse, con
     return st;
   if ((st = check_ptr(workspace, "workspace")) != PDY_OK) return st;
   CrossRows f = rows_launch(s, kDq, causal != 0);
-  CrossKv kv = kv_launch(s);
+  CrossKv kv = kv_launch(s, x.len_k != nullptr);
   const CrossBwdSpace sp = bwd_space(s, f, kv);
   if (workspace_bytes < sp.total)
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, %s needs %zu", workspace_bytes, who,
@@ -699,7 +703,7 @@ pdy_status pdy_cross_launch_shapes(int32_t prefix_len, int32_t total_q, int32_t 
     shapes[11] = q.cut.round > 0;
   }
   if (s.tk + s.prefix > 0) {
-    const CrossKv kv = kv_launch(s);
+    const CrossKv kv = kv_launch(s, false);
     put(2, kv.sh, kv.cut);
   }
   return PDY_OK;
@@ -766,7 +770,7 @@ size_t attn_prefix_bwd_workspace_size(int32_t prefix_len, int32_t total_q, int32
   if (check_cross_sizes(prefix_len, total_q, total_k, num_seqs, max_seqlen_q, max_seqlen_k,
                         num_heads_q, num_heads_kv, head_dim, &s) != PDY_OK)
     return 0;
-  const CrossKv kv = kv_launch(s);
+  const CrossKv kv = kv_launch(s, false);  // (its parts, whatever max_k bounds)
   return std::max(bwd_space(s, rows_launch(s, kDq, false), kv).total,
                   bwd_space(s, rows_launch(s, kDq, true), kv).total);
 }

@@ -14,7 +14,9 @@
 // sequence still fills g rows of the matrix product.
 //
 // Offsets read from cu_q, cu_k and len_k are clamped to the tensors, so that no
-// value in them makes a kernel leave its tensors.
+// value in them makes a kernel leave its tensors.  Tiles end at the lengths that the
+// host sized the grid for: a sequence that is longer than it was said to be loses its
+// own last tiles, not those of the sequences behind it.
 #pragma once
 #include "common.hpp"
 
@@ -32,9 +34,11 @@ struct CrossBatch {
   int g;           // hq / hkv
   uint32_t g_inv;  // 2^32 / g, rounded down (g > 1)
   int causal;
+  int max_k;  // keys of a sequence (in use or not) that get a gradient
 };
 
-// One sequence: rows of q and k, keys in use, and rows of k with those not in use.
+// One sequence: rows of q and k, keys in use, and rows of k that get a gradient (those
+// not in use too).
 struct CrossSeq {
   int q_lo, nq, k_lo, nk, room;
 };
@@ -46,6 +50,7 @@ __device__ __forceinline__ CrossSeq cross_seq(const CrossBatch& b, int i) {
   s.k_lo = min(max(b.cu_k[i], 0), b.tk);
   s.nk = s.room = min(max(b.cu_k[i + 1], s.k_lo), b.tk) - s.k_lo;
   if (b.len_k) s.nk = min(max(b.len_k[i], 0), s.nk);
+  s.room = min(s.room, b.max_k);
   return s;
 }
 // The whole batch as one sequence over the shared keys.
@@ -90,6 +95,7 @@ struct CrossCut {
   int keys;       // CrossKeys
   int rows_log2;  // packed rows per tile (dK/dV: per step)
   int key_log2;   // keys per tile
+  int max_tiles;  // of a sequence's rows
   int max_parts;  // of an item; 1: not cut
   int least;      // fewest inner tiles of a part
   int entries;    // parts of a kv head
@@ -152,9 +158,11 @@ __device__ __forceinline__ float wave_sum(float v) {
 // keys (forward, dQ), and tiles of keys over steps of rows (dK/dV; 2^pack_log2 heads of
 // the group to a step).
 __device__ __forceinline__ void cross_row_units(const CrossBatch& b, const CrossCut& c,
-                                                const CrossSeq& s, int& tiles, int& units) {
+                                                const CrossSeq& s, bool whole_batch, int& tiles,
+                                                int& units) {
   const int pre = c.keys == CROSS_FUSED ? cross_tiles_log2(b.prefix, c.key_log2) : 0;
   tiles = cross_tiles_log2(s.nq * b.g, c.rows_log2);
+  if (!whole_batch) tiles = min(tiles, c.max_tiles);
   units = cross_tiles_log2(s.nk, c.key_log2) + pre;
 }
 __device__ __forceinline__ void cross_key_units(const CrossBatch& b, const CrossCut& c,
@@ -175,7 +183,7 @@ __device__ __forceinline__ int cross_parts(const CrossCut& c, float inv_cap, int
 }
 
 // Sequence, tile and part of entry `entry` of a kv head's list; false past its end.
-// of(s, tiles, units): as above.  The list has the shared keys over the whole batch first
+// of(s, whole_batch, tiles, units): as above.  The list has the shared keys over the whole batch first
 // where `shared` is set (index 0), then the n sequences (index i, or i + 1).  The
 // results are wave-uniform.
 template <bool EVEN, class F>
@@ -186,7 +194,7 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
   int t0 = 0, u0 = 0;
   if (shared) {
     s0 = cross_shared_seq(b);
-    of(s0, t0, u0);
+    of(s0, true, t0, u0);
   }
   // a part's tiles one after another: workgroups that run at a time then stream the
   // same keys (rows), which L2 holds once
@@ -228,7 +236,7 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
     lo = __builtin_amdgcn_readfirstlane(lo);
     const CrossSeq s = cross_seq(b, lo);
     int t, u;
-    of(s, t, u);
+    of(s, false, t, u);
     const int parts = cross_parts(c, inv, u);
     // (always, unless the offsets are wrong)
     if ((uint32_t)(rel - start) >= (uint32_t)(t * parts)) return false;
@@ -241,7 +249,7 @@ __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut&
   int t = 0, u = 0;
   if (l < n) {
     s = cross_seq(b, l);
-    of(s, t, u);
+    of(s, false, t, u);
   }
   auto get = [&](int v, int src) __attribute__((always_inline)) {
     return __builtin_amdgcn_readlane(v, src);
@@ -342,8 +350,9 @@ __device__ __forceinline__ bool cross_place_rows(const CrossBatch& b, const Cros
                                                  CrossPlace& out) {
   return cross_place<EVEN>(
       b, c, c.keys == CROSS_APART, entry,
-      [&](const CrossSeq& s, int& tiles, int& units) __attribute__((always_inline)) {
-        cross_row_units(b, c, s, tiles, units);
+      [&](const CrossSeq& s, bool whole_batch, int& tiles, int& units)
+          __attribute__((always_inline)) {
+        cross_row_units(b, c, s, whole_batch, tiles, units);
       },
       out);
 }
@@ -366,15 +375,16 @@ __global__ void __launch_bounds__(kListThreads) cross_list_kernel(CrossListArgs 
   const int kv = a.kv[blockIdx.x], t = threadIdx.x, w = t >> 6;
   const int run = (b.n + kListThreads - 1) / kListThreads;
   const int first = min(b.n, t * run), last = min(b.n, first + run);
-  auto of = [&](const CrossSeq& s, int& tiles, int& units) __attribute__((always_inline)) {
+  auto of = [&](const CrossSeq& s, bool whole_batch, int& tiles, int& units)
+                __attribute__((always_inline)) {
     if (kv) cross_key_units(b, c, a.pack_log2, s, tiles, units);
-    else cross_row_units(b, c, s, tiles, units);
+    else cross_row_units(b, c, s, whole_batch, tiles, units);
   };
   int tiles, units, cap = cross_cap(c, 0.f);
   if (c.max_parts > 1) {
     float sum = 0.f;
     for (int i = first; i < last; ++i) {
-      of(cross_seq(b, i), tiles, units);
+      of(cross_seq(b, i), false, tiles, units);
       sum += (float)tiles * (float)units;
     }
     sum = wave_sum(sum);
@@ -383,14 +393,14 @@ __global__ void __launch_bounds__(kListThreads) cross_list_kernel(CrossListArgs 
     sum = 0.f;
     for (int i = 0; i < kWaves; ++i) sum += wave_units[i];
     if (kv ? b.prefix > 0 : c.keys == CROSS_APART) {
-      of(cross_shared_seq(b), tiles, units);
+      of(cross_shared_seq(b), true, tiles, units);
       sum += (float)tiles * (float)units;
     }
     cap = cross_cap(c, sum);
   }
   const float inv = 1.f / (float)cap;
   auto entries = [&](int i) __attribute__((always_inline)) {
-    of(cross_seq(b, i), tiles, units);
+    of(cross_seq(b, i), false, tiles, units);
     return (int64_t)tiles * cross_parts(c, inv, units);
   };
   int64_t mine = 0;

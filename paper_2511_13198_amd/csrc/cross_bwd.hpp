@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(NWAVES * 64, NWAVES == 4 ? 2 : D == 64 ? 3 : 1
   CrossPlace at;
   if (!cross_place<false>(
           a.b, a.cut, pre, entry,
-          [&](const CrossSeq& s, int& tiles, int& units) __attribute__((always_inline)) {
+          [&](const CrossSeq& s, bool, int& tiles, int& units) __attribute__((always_inline)) {
             cross_key_units(a.b, a.cut, sh, s, tiles, units);
           },
           at))

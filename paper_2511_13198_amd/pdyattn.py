@@ -599,8 +599,11 @@ def attn_cross_fwd(q, k, v, cu_seqlens_q, cu_seqlens_k, max_seqlen_q: Optional[i
     """O [Tq, Hq, d] bf16 and LSE [Hq, Tq] fp32 of every sequence's queries over
     its own keys: q [Tq, Hq, d] cut by cu_seqlens_q, k, v [Tk, Hkv, d] by
     cu_seqlens_k (int32 [N + 1]).  seqlens_k (int32 [N]): only the first so many
-    keys of each are in use.  causal aligns the ends: the last query sees every
-    key.  Rows without a key get O = 0, LSE = -inf; rows of no sequence are left."""
+    keys of each are in use.  max_seqlen_q, max_seqlen_k: upper bounds of the
+    lengths, max_seqlen_k with seqlens_k of these alone (None: read from the
+    offsets, waiting for them); a sequence that is longer loses results of its own.
+    causal aligns the ends: the last query sees every key.  Rows without a key get
+    O = 0, LSE = -inf; rows of no sequence are left."""
     return _cross_fwd(q, k, v, None, None, cu_seqlens_q, cu_seqlens_k, max_seqlen_q,
                       max_seqlen_k, causal, scale, seqlens_k, out, lse, workspace)
 

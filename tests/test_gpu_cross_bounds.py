@@ -6,6 +6,7 @@ import math
 import pytest
 
 from tests import cross_util as cu
+from tests import test_gpu_cross as gpu
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +52,84 @@ def test_rows_of_no_sequence_alone(prefix):
         grads = pdyattn.attn_cross_bwd(q, k, k, o, lse, q, cq, ck, dq=dq)
     assert (o == 7).all() and (lse == 7).all() and (dq == 7).all()
     assert all((g == 0).all() for g in grads[1:])
+
+
+# (query lengths, key lengths, used or None, prefix, Hq, Hkv, d, causal)
+BOUNDS = [
+    # padded batches and caches, the longest length that of the keys in use
+    ([1, 5, 1, 3], [1024] * 4, [300, 7, 0, 299], 0, 8, 2, 128, True),
+    ([30, 200, 8, 100], [1500] * 4, [900, 11, 64, 650], 0, 4, 4, 64, False),
+    ([40, 1, 300], [700] * 3, [1, 90, 33], 200, 4, 2, 128, True),
+    ([1 + i % 3 for i in range(80)], [300] * 80, [i % 50 for i in range(80)], 0, 4, 1, 64, True),
+]
+
+
+@pytest.mark.parametrize("case", BOUNDS, ids=gpu.case_id)
+def test_the_longest_length_of_the_keys_in_use_will_do(case):
+    """With seqlens_k a max_seqlen_k that bounds these alone gives every result, zeros for
+    the keys not in use among them."""
+    import torch
+    x, ref, args, len_k = gpu.setup(case, 4)
+    args = (*args[:3], max(case[2]), *args[4:])
+    o, lse = gpu.forward(x, args, len_k)
+    got = gpu.backward(x, o, lse, args, len_k, **gpu.empties(x, torch.float32, 7.0))
+    t, tk = sum(case[0]), sum(case[1])
+    cu.check("o", o[:t], tuple(r[:t] for r in ref["o"]))
+    for name, g in zip(gpu.GRADS, got):
+        end = t if name == "dq" else g.shape[0] if name.endswith("p") else tk
+        cu.check(name, g[:end], tuple(r[:end] for r in ref[name]))
+        assert (g[end:] == 7.0).all(), f"{name}: rows of no sequence were written"
+
+
+# (the first sequence is the one that is longer than it was said to be)
+SHORT = [
+    ([40, 1, 30, 9], [300] * 4, None, 0, 8, 2, 128, True),
+    ([600, 90, 100, 33], [500, 600, 2, 90], None, 0, 4, 4, 64, False),
+    ([700, 300, 290], [900, 650, 400], None, 150, 2, 2, 128, True),
+    ([9, 2, 1, 2], [40, 10, 0, 3], None, 1100, 4, 4, 128, True),
+    ([200] + [3] * 75, [90] + [60] * 75, None, 0, 4, 2, 128, True),
+    ([5] + [1] * 99, [90] + [6] * 99, None, 1300, 8, 2, 64, True),
+]
+
+
+@pytest.mark.parametrize("case", SHORT, ids=gpu.case_id)
+def test_a_longest_query_length_too_small_costs_its_own_sequence_alone(case):
+    """Every other sequence has its results; of the longer one the first max_seqlen_q rows
+    have theirs, and no row of none is written."""
+    import torch
+    x, ref, args, len_k = gpu.setup(case, 5)
+    most, first, t, tk = max(case[0][1:]), case[0][0], sum(case[0]), sum(case[1])
+    args = (*args[:2], most, *args[3:])
+    o, lse = filled(x["q"].shape, torch.bfloat16), filled((case[4], t + 3), torch.float32)
+    gpu.forward(x, args, len_k, out=o, lse=lse)
+    keep = torch.tensor([i for i in range(t) if i < most or i >= first], device="cuda")
+    cu.check("o", o, ref["o"], keep)
+    cu.check("lse", lse.T, tuple(r.T for r in ref["lse"]), keep)
+    assert (o[t:] == 7).all() and (lse[:, t:] == 7).all()
+    dq, dk, dv = gpu.backward(x, o, lse, args, len_k, **gpu.empties(x, torch.float32, 7.0))[:3]
+    cu.check("dq", dq, ref["dq"], keep)
+    for name, g in (("dk", dk), ("dv", dv)):
+        cu.check(name, g, ref[name], torch.arange(case[1][0], tk, device="cuda"))
+        assert (g[tk:] == 7).all()
+    assert (dq[t:] == 7).all()
+
+
+@pytest.mark.parametrize("case", [c for c in SHORT if c[1][0] > max(c[1][1:])] +
+                         [([9, 4, 30], [1000, 260, 300], None, 0, 4, 2, 64, True)], ids=gpu.case_id)
+def test_a_longest_key_length_too_small_costs_its_own_gradients_alone(case):
+    """Rows attend to all keys whatever the bound; dk and dv of the longer sequence's first
+    max_seqlen_k keys and of all others are there."""
+    import torch
+    x, ref, args, len_k = gpu.setup(case, 6)
+    most, first, t, tk = max(case[1][1:]), case[1][0], sum(case[0]), sum(case[1])
+    args = (*args[:3], most, *args[4:])
+    o, lse = gpu.forward(x, args, len_k)
+    cu.check("o", o[:t], tuple(r[:t] for r in ref["o"]))
+    got = gpu.backward(x, o, lse, args, len_k, **gpu.empties(x, torch.float32, 7.0))
+    keep = torch.tensor([i for i in range(tk) if i < most or i >= first], device="cuda")
+    for name, g in zip(gpu.GRADS, got):
+        cu.check(name, g[:t] if name == "dq" else g,
+                 tuple(r[:t] for r in ref[name]) if name == "dq" else ref[name],
+                 keep if name in ("dk", "dv") else None)
+        if name in ("dk", "dv"):
+            assert (g[tk:] == 7).all()
