@@ -279,9 +279,11 @@ pdy_status attn_prefix_bwd(const void* q, const void* k, const void* v, const vo
  *   num_pairs: a multiple of 8 up to head_dim / 2.
  *   turns, pair_axes: HOST arrays of num_pairs, read during the call (a captured graph
  *   keeps their values); turns[p] = w_p / 2 pi as a 64-bit fraction of a turn, which
- *   attn_rotary_turns computes from the frequencies w_p (radians a position, finite).
- * Angles are exact for every int32 position; products are 32 bits, rounded once to a
- * bf16 output.  Needs no workspace; total_tokens is below 2^26 - 4. */
+ *   attn_rotary_turns computes from the frequencies w_p (radians a position, finite),
+ *   rounded to the nearest.
+ * For every int32 position and frequency the angle is off by less than 2^-31 of a turn
+ * from positions * w_p (w_p as the double that it is); products are 32 bits, rounded
+ * once to a bf16 output.  Needs no workspace; total_tokens is below 2^26 - 4. */
 pdy_status attn_rotary_turns(const double* freqs, int32_t num_pairs, uint64_t* turns);
 pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
                        int32_t total_tokens, int32_t num_axes, int32_t num_heads_q,

@@ -16,6 +16,35 @@ namespace {
 
 constexpr int64_t kFill = 1024;  // workgroups
 
+// 1 / (2 pi) as a binary fraction, the first 64 bits first: enough that the largest
+// double's whole turns are known.
+constexpr uint64_t kInvTwoPi[] = {
+    0x28be60db9391054a, 0x7f09d5f47d4d3770, 0x36d8a5664f10e410, 0x7f9458eaf7aef158,
+    0x6dc91b8e909374b8, 0x01924bba82746487, 0x3f877ac72c4a69cf, 0xba208d7d4baed121,
+    0x3a671c09ad17df90, 0x4e64758e60d4ce7d, 0x272117e2ef7e4a0e, 0xc7fe25fff7816603,
+    0xfbcbc462d6829b47, 0xdb4d9fb3c9f2c26d, 0xd3d18fd9a797fa8b, 0x5d49eeb1faf97c5e,
+    0xcf41ce7de294a4ba, 0x9afed7ec47e35742, 0x1580cc11bf1edaea};
+
+// w / 2 pi modulo 1 as a fraction of 2^64, to the nearest.  With w = m 2^e, m of 53 bits,
+// the bits of 1 / (2 pi) up to weight 2^-e give whole turns, and of those behind 192 leave
+// the product off by less than 2^-138.
+uint64_t turn_of(double w) {
+  int e;
+  const uint64_t m = (uint64_t)std::ldexp(std::frexp(std::fabs(w), &e), 53);
+  e -= 53;
+  // 64 bits from weight 2^-(at + 1) on (those in front of the point are 0)
+  auto bits = [](int at) -> uint64_t {
+    if (at <= -64) return 0;
+    if (at < 0) return kInvTwoPi[0] >> -at;
+    const int j = at / 64, s = at % 64;
+    return s == 0 ? kInvTwoPi[j] : kInvTwoPi[j] << s | kInvTwoPi[j + 1] >> (64 - s);
+  };
+  typedef unsigned __int128 u128;
+  const u128 low = (u128)m * bits(e + 128), mid = (u128)m * bits(e + 64) + (uint64_t)(low >> 64);
+  const uint64_t turn = m * bits(e) + (uint64_t)(mid >> 64) + ((uint64_t)mid >> 63);
+  return w < 0 ? -turn : turn;
+}
+
 template <class In, class Out, int D>
 void launch_rotary(pdy::RotaryArgs& a, bool inter, int64_t heads, hipStream_t st) {
   constexpr int kHeads = 64 * 2 * (16 / (int)sizeof(In)) / D;  // of a wave's round
@@ -47,10 +76,7 @@ pdy_status attn_rotary_turns(const double* freqs, int32_t num_pairs, uint64_t* t
     return fail(PDY_ERR_INVALID_ARG, "attn_rotary_turns: bad arrays");
   for (int p = 0; p < num_pairs; ++p) {
     if (!std::isfinite(freqs[p])) return fail(PDY_ERR_INVALID_ARG, "freqs[%d] is not finite", p);
-    // turns a position, without whole turns (a long double holds the 64 bits)
-    long double t = (long double)freqs[p] * 0.15915494309189533576888376337251436L;
-    t -= floorl(t);
-    turns[p] = t < 1.0L ? (uint64_t)(t * 18446744073709551616.0L) : 0;
+    turns[p] = turn_of(freqs[p]);
   }
   return PDY_OK;
 }

@@ -9,9 +9,9 @@
 // of a head is copied.
 //
 // Angles.  A position of 10^5 and more times w in 32-bit floats would leave the angle
-// off by 10^-2.  The caller gives w_p / 2 pi as a 64-bit fraction F of a turn; pos * F
-// mod 2^64 is then the angle in turns with whole turns gone, exact to pos * 2^-65.
-// Its upper 32 bits are split into the nearest eighth ... quarter turn and a
+// off by 10^-2.  The caller gives w_p / 2 pi as a 64-bit fraction F of a turn, rounded to
+// the nearest; pos * F mod 2^64 is then the angle in turns with whole turns gone, off by
+// at most |pos| 2^-65 of a turn, 2^-34.  Its upper 32 bits (off by 2^-32) are split into the nearest eighth ... quarter turn and a
 // remainder of at most an eighth, whose sine and cosine are the Taylor sums to x^9
 // and x^10: the first terms left out are below 1.8e-9 and 1.2e-10 (x <= pi / 4), less
 // than a 32-bit rounding.
