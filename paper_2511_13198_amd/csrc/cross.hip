@@ -127,27 +127,49 @@ constexpr double kMoveBytesPerUs = 4.0e6;           // partial results written a
 // Few rows a sequence behind many shared keys: these once for the rows of all
 // sequences, apart from the sequences' own keys, with partial results of both.  Fused,
 // every sequence's tile of 32 rows or more streams them; us apart / fused, d = 128:
-//   64 sequences of 1 token, 32/8 heads, behind 32,768 keys 97 / 662, 1,024 49 / 59,
-//   512 49 / 48, 64 48 / 42; 32 of 8 tokens (32 rows) behind 8,000 64 / 78, of 16 (64
-//   rows) 99 / 138, of 32 (128 rows, 40 sequences, a step) 853 / 858.
-// With more (sequence, kv head) pairs than 4 a CU fused takes rounds that apart does not:
-// 256 and 512 sequences, 8 kv heads, 30 own keys, d = 64, us apart / fused behind 128 shared
-// keys 26 / 29, 43 / 54, 256 27 / 33, 44 / 62; over 400 own 54 / 51, 115 / 120 and 56 / 55,
-// 115 / 129.
-constexpr int64_t kApartRows = 64, kApartPrefix = 512, kApartPrefixMany = 256;
+//   64 sequences of 1 token, 32/8 heads, behind 32,768 keys 97 / 662; 32 of 8 tokens (32
+//   rows) behind 8,000 64 / 78, of 16 (64 rows) 99 / 138, of 32 (128 rows, 40 sequences,
+//   a step) 853 / 858.
+// Where the (sequence, kv head) pairs are more than 4 a CU, fused takes rounds that apart
+// does not.  Apart saves what a tile has beyond a sequence's R rows and costs partial
+// results a row, so the keys from which it pays grow with R / (tile - R).  us fused / apart
+// (or their ratio) behind so many shared keys, 1,280-4,096 pairs:
+//   d = 128: R = 1, 512 sequences of 8/8 heads over 100 own keys: 128 79 / 79, 256 91 / 79;
+//   R = 4, 32/8 heads: 128 80 / 88, 256 93 / 89; R = 8, 2,048 of 16/2 over 400: 256 0.94;
+//   R = 16, 256 of 8/8 over 400: 200 97 / 113, 700 123 / 119; R = 32, 160 of 32/8 over 30:
+//   1,000 66 / 80, 2,000 101 / 98; R = 64, 256 of 16/8 over 100: 1,000 124 / 191, 3,500
+//   312 / 346
+//   d = 64: R = 1: 128 55 / 42; R = 4: 128 57 / 51, 256 64 / 52; R = 8: 128 0.95, 192 1.02;
+//   R = 16: 200 62 / 72, 400 71 / 75, 700 80 / 76; R = 32: 1,000 49 / 54, 2,000 69 / 63;
+//   R = 64: 1,000 67 / 131, 3,500 176 / 217
+constexpr int64_t kApartRows = 64, kApartPrefix = 512;
+int64_t fused_keys(const CrossSizes& s) {
+  if (s.n * s.hkv <= 4 * kCUs) return kApartPrefix;
+  const int64_t rows = s.seq_rows();  // (at most kApartRows)
+  return (s.d == 64 ? 0 : 128) + 500 * rows / ((rows <= 32 ? 44 : 72) - rows);
+}
 
 // Few rows over so many keys at most, shared ones among them, are one whole item a tile:
 // the launch that combines partial results takes longer than these save.  us with parts /
 // whole, a token for each of 1-60 sequences over 400, 800, 1,500 keys: d = 64 10.6 / 7.8,
-// 11.0 / 9.9, 10.7 / 14.0; d = 128 11.6 / 10.2, 12.5 / 13.9, 11.8 / 20.5.  Apart / whole,
-// over 100 own and 520, 700, 900 shared keys, up to two pairs a CU: 64 sequences, 8 kv heads
-// of 64, 12.2 / 11.3, 12.2 / 12.2, 12.4 / 14.1 (128 sequences 20.6 / 24.5, 20.6 / 25.9); 60
-// sequences of 8 heads to one of 128 15.7 / 13.3, 15.8 / 14.9, 16.3 / 17.4, 3 of 8 to 8 12.6 /
-// 12.8, 11.4 / 14.3.  Parts / whole behind 256 shared and 400 own keys, 32/8 heads of 128, 64
-// sequences 30.0 / 25.8, 1,024 of 8/1 52.8 / 50.0.
+// 11.0 / 9.9, 10.7 / 14.0; d = 128 11.6 / 10.2, 12.5 / 13.9, 11.8 / 20.5.  Parts / whole behind
+// 256 shared and 400 own keys, 32/8 heads of 128, 64 sequences 28.7 / 24.0, 512 167 / 167.
+// Apart / whole, up to a pair a CU, over 100 own and 520, 700 shared keys: 8 sequences of 32/8
+// heads of 128 13.2 / 13.4, 12.0 / 14.9, of 64 11.1 / 9.9, 10.4 / 10.7; 32 of them 17.1 / 16.2,
+// 17.1 / 18.0 and d = 64 whole / apart 0.82, 0.89.
+// From one to two pairs a CU the line grows with a sequence's rows R, as above.  Time whole
+// over time apart, 384 and 512 pairs over 100 and 400 own keys:
+//   d = 128, R = 1: behind 520 keys 0.98-1.14, 600 0.98-1.21; R = 4: 520 0.88-1.00, 700
+//   0.90-1.09, 800 0.95-1.16; R = 8: 700 0.79-1.00, 900 0.89-0.97; R = 16: 700 0.79; R = 64:
+//   700 0.50
+//   d = 64, R = 1: 520 0.96-1.06, 600 0.96-1.05; R = 4: 700 0.91-1.04, 800 0.96-1.07; R = 8:
+//   900 0.92-0.98; R = 16: 700 0.78; R = 64: 700 0.56
 bool short_keys(const CrossSizes& s) {
+  const int64_t pairs = s.n * s.hkv;
+  if (s.prefix > kApartPrefix && pairs > kCUs && pairs <= 2 * kCUs)
+    return s.prefix <= 500 + 60 * s.seq_rows() && s.max_k <= 512;
   const int64_t most = s.prefix > kApartPrefix ? (s.d == 64 ? 800 : 640)
-                       : s.d == 64 || (s.prefix > 0 && s.n * s.hkv >= 2 * kCUs) ? 1024 : 512;
+                       : s.d == 64 || (s.prefix > 0 && pairs >= 2 * kCUs) ? 1024 : 512;
   return s.max_k + s.prefix <= most;
 }
 
@@ -219,8 +241,7 @@ CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
   const int64_t slice = std::max<int64_t>(1, s.tq) * s.hq * (s.d + 1) * 4;
   const int64_t pairs = s.n * s.hkv;
   c.keys = s.prefix == 0 ? pdy::CROSS_OWN
-           : s.seq_rows() > kApartRows || 2 * slice > kPartBytes ||
-                   s.prefix <= (pairs > 4 * kCUs ? kApartPrefixMany : kApartPrefix) ||
+           : s.seq_rows() > kApartRows || 2 * slice > kPartBytes || s.prefix <= fused_keys(s) ||
                    (pairs <= 2 * kCUs && short_keys(s))
                ? pdy::CROSS_FUSED
                : pdy::CROSS_APART;
