@@ -234,6 +234,19 @@ RowsChoice choose_rows(const CrossSizes& s, const RowKernel& k, bool causal) {
   return best;
 }
 
+// Whether the longest of `items` whole items takes longer than all of them side by side, by
+// more than the launch that combines parts (16 units of 64 keys): one long sequence among
+// short ones.  us whole / in parts: 512 x 1 token, 32/8 heads of 128, over 1,000 keys and one
+// of 131,072 2,826 / 497, of 32,768 985 / 469, of 8,192 520 / 457, of 4,096 444 / 447; 32 x 64,
+// 16/16 heads, over 300 keys and one of 16,384 275 / 60, of 2,048 49 / 38, of 1,024 34 / 38.
+// Even lengths behind too large a bound pay for it: the 512 over 300 keys, 16,384 said, 144 /
+// 148; 64 x 64 over 300, 4,096 said, 40 / 47.
+bool outlasts(const CrossSizes& s, const RowKernel& k, const CrossShape& sh, int64_t items) {
+  const double mean = std::min<double>((double)s.max_k, (double)s.tk / s.n) + s.prefix;
+  const double longest = (double)(s.max_k + s.prefix);
+  return longest > 0.8 * (double)items * mean / (double)k.slots(s, sh) + 16 * 64;
+}
+
 CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
   CrossRows f;
   pdy::CrossCut& c = f.cut;
@@ -260,8 +273,9 @@ CrossRows rows_launch(const CrossSizes& s, const RowKernel& k, bool causal) {
     const bool few = f.sh.groups == 4;
     if (k.dq && few) f.sh = {4, 2};
     entries = (few ? 4 : 2) * kCUs;
-    if (!apart && (most_items(s, s.n, s.max_q, f.sh.rows()) * s.hkv >= (few ? 16 : 2) * kCUs ||
-                   short_keys(s)))
+    const int64_t items = most_items(s, s.n, s.max_q, f.sh.rows()) * s.hkv;
+    if (!apart && (items >= (few ? 16 : 2) * kCUs || short_keys(s)) &&
+        !outlasts(s, k, f.sh, items))
       most = 1;
   }
   const int rows = f.sh.rows(), keys_tile = k.key_tile(s, f.sh);
@@ -350,9 +364,17 @@ CrossKv kv_launch(const CrossSizes& s, bool rooms) {
   c.even = c.round = 0;
   const int64_t slice = (s.prefix + s.tk) * s.hkv * s.d * 8;
   int64_t parts = std::min<int64_t>(16, slice ? kPartBytes / slice : 1);
-  // items alike in their rows need no cut once they fill the chip; a shared tile has
-  // the rows of all sequences
-  if (n * s.hkv >= target && (s.prefix == 0 || s.n == 1)) parts = 1;
+  // Items alike in their rows need no cut once they fill the chip; a shared tile has
+  // the rows of all sequences, and one sequence may have many more rows than the others:
+  // its items' steps against an even share of all, as for rows above.  us of a backward with
+  // parts / whole: 300 x 16 tokens over 60 keys, 8/1 heads of 128, one of 8,192 tokens 173 /
+  // 1,439, of 512 60 / 129, of 128 55 / 65; 256 x 16 of 32/8 over as many keys, one of 512 134 /
+  // 169, of 128 110 / 105; even lengths, 2,048 said, 215 / 213.
+  const int64_t steps_of = (int64_t)1 << c.rows_log2;
+  const double slots = (k.sh.nw == 4 ? 2.0 : 1.0) * kCUs;
+  const double share = std::max(1.0, (double)(s.tq * s.g()) / (s.n * steps_of)) * n * s.hkv / slots;
+  const bool alike = s.prefix == 0 && (double)(s.max_q * s.g()) / steps_of <= share + 8;
+  if (n * s.hkv >= target && (alike || s.n == 1)) parts = 1;
   // Items of few steps are not cut: the launch that sums parts takes longer than they
   // save.  us of a backward with parts / whole, longest items of 1, 4, 8 and 16 steps: 4
   // sequences over 300 keys, 8 heads, d = 64 18.6 / 16.1, 23.5 / 21.0, 28.9 / 22.4, 36.2 /

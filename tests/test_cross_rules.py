@@ -21,3 +21,25 @@ def shapes(n, q, k, prefix, hq, hkv, d, causal=True):
 ])
 def test_shared_keys_apart_or_with_each_sequence(n, q, k, prefix, hq, hkv, d, apart):
     assert shapes(n, q, k, prefix, hq, hkv, d)["apart"] == apart
+
+
+@pytest.mark.parametrize("n,q,k,longest,hq,hkv,d,cut", [
+    (512, 1, 1000, 131072, 32, 8, 128, True), (512, 1, 1000, 8192, 32, 8, 128, True),
+    (512, 1, 1000, 4096, 32, 8, 128, False), (512, 1, 1000, 32768, 32, 8, 64, True),
+    (32, 64, 300, 16384, 16, 16, 128, True), (32, 64, 300, 2048, 16, 16, 64, True),
+    (32, 64, 300, 1024, 16, 16, 128, False), (512, 1, 1000, 1000, 32, 8, 128, False),
+])
+def test_one_long_cache_among_short_ones_is_cut(n, q, k, longest, hq, hkv, d, cut):
+    s = P.cross_launch_shapes(0, n * q, (n - 1) * k + longest, n, q, max(k, longest), hq, hkv, d, False)
+    assert (s["cross_fwd_kernel"][2] > 1) == cut and (s["cross_dq_kernel"][2] > 1) == cut
+
+
+@pytest.mark.parametrize("n,q,longest,k,hq,hkv,d,cut", [
+    (300, 16, 8192, 60, 8, 1, 128, True), (300, 16, 128, 60, 8, 1, 64, True),
+    (256, 16, 512, 16, 32, 8, 128, True), (256, 16, 128, 16, 32, 8, 128, False),
+    (32, 16, 2048, 1000, 8, 8, 64, True), (32, 16, 512, 1000, 8, 8, 64, False),
+    (300, 16, 16, 60, 8, 1, 128, False),
+])
+def test_keys_that_one_long_sequence_sees_are_cut(n, q, longest, k, hq, hkv, d, cut):
+    s = P.cross_launch_shapes(0, (n - 1) * q + longest, n * k, n, longest, k, hq, hkv, d, False)
+    assert (s["cross_dkdv_kernel"][2] > 1) == cut
