@@ -1,7 +1,11 @@
 """Launch rules of cross attention at sizes whose both sides were timed."""
+import math
+import random
+
 import pytest
 
 from paper_2511_13198_amd import pdyattn as P
+from tests import test_gpu_cross, test_gpu_cross_plans
 
 
 def shapes(n, q, k, prefix, hq, hkv, d, causal=True):
@@ -43,3 +47,38 @@ def test_one_long_cache_among_short_ones_is_cut(n, q, k, longest, hq, hkv, d, cu
 def test_keys_that_one_long_sequence_sees_are_cut(n, q, longest, k, hq, hkv, d, cut):
     s = P.cross_launch_shapes(0, (n - 1) * q + longest, n * k, n, longest, k, hq, hkv, d, False)
     assert (s["cross_dkdv_kernel"][2] > 1) == cut
+
+
+def plans(prefix, tq, tk, n, mq, mk, hq, hkv, d, causal):
+    """(kernel, waves, groups, d, plan, shared keys or not, a list or not) of each launch."""
+    s = P.cross_launch_shapes(prefix, tq, tk, n, mq, mk, hq, hkv, d, causal)
+    out = set()
+    for kernel, first in (("fwd", "fwd_whole_first"), ("dq", "dq_whole_first"), ("dkdv", None)):
+        w, g, parts = s[f"cross_{kernel}_kernel"]
+        plan = "parts" if parts > 1 else "whole"
+        if first:
+            plan = "apart" if s["apart"] else "whole first" if s[first] else plan
+        out.add((kernel, w, g, d, plan, prefix > 0, n > 64))
+    return out
+
+
+def test_the_gpu_cases_reach_what_random_sizes_reach():
+    """Every kernel, tile shape and plan together, not one by one."""
+    seen = set()
+    for lq, lk, _, prefix, hq, hkv, d, causal in test_gpu_cross.CASES + test_gpu_cross_plans.CASES:
+        seen |= plans(prefix, sum(lq) + 3, sum(lk) + 3, len(lq), max(lq), max(lk), hq, hkv, d, causal)
+    rng = random.Random(0)
+
+    def log(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    reached = set()
+    for _ in range(20000):
+        n, hkv, d = log(1, rng.choice([64, 3000])), rng.choice([1, 2, 4, 8, 16]), rng.choice([64, 128])
+        hq, q, k = rng.choice([1, 2, 3, 4, 8, 16]) * hkv, log(1, 3000), log(1, 30000)
+        prefix = log(1, 30000) if rng.random() < 0.5 else 0
+        tq = max(q, int(n * q * rng.choice([1, 1, 0.6, 0.3, 0.05])))
+        tk = max(k, int(n * k * rng.choice([1, 1, 0.6, 0.3, 0.05])))
+        if max((tq + n) * hq, (tk + prefix) * hkv) < 1 << 31:
+            reached |= plans(prefix, tq, tk, n, q, k, hq, hkv, d, rng.random() < 0.5)
+    assert len(reached) > 170 and not reached - seen, sorted(map(str, reached - seen))
