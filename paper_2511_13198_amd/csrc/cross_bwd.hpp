@@ -287,7 +287,8 @@ __global__ void __launch_bounds__(NW * 64, D == 64 && NW == 8 && KG == 1 ? 4 : N
       for (int j = 0; j < KG; ++j) dot += sums[j * 32 + (l & 31)];
     }
     if (a.b.prefix + max(0, lane_end) <= kCrossFewKeys) ddv = dot;
-    if (hh == 0 && at.part == 0 && kg == 0 && !second && row < row_end) {
+    // (no workgroup of apart lists: few keys are fused)
+    if (hh == 0 && at.part == 0 && kg == 0 && row < row_end) {
       const int tok = cross_token(a.b, row);
       a.dd[(size_t)(hk * g + (row - tok * g)) * a.b.tq + tok] = ddv;
     }
