@@ -216,6 +216,12 @@ pdy_status attn_merge(const void* o_a, const float* lse_a, const void* o_b, cons
  *   - Gradients of sum(dout * o), given o and lse as the forward wrote them; with
  *     grad_bf16 = 0 fp32, with 1 bf16 (rounded once, from 32-bit sums).  dk and dv of
  *     keys not in use are 0; dk_prefix and dv_prefix sum the rows of all sequences.
+ *   - Probabilities (before the products with v and dout) and the logits' gradients
+ *     (before those with k and q) are rounded to bf16, and the backward takes
+ *     <dout, o> from the rounded o for rows with more than 64 keys; logits, sums and
+ *     lse are 32 bits.
+ *   - An infinity or NaN in a v in use, or in dout, may also reach rows (keys) of its
+ *     sequence that the causal mask parts from it, as in attn_fwd and attn_bwd.
  * q, o bf16 [total_q, Hq, d]; k, v bf16 [total_k, Hkv, d] (NULL if total_k = 0); lse
  * fp32 [Hq, total_q].  Launch shapes and the parts of rows with few keys follow from
  * the sizes and the offsets' values: results of a sequence depend on its batch in

@@ -83,7 +83,8 @@ enum CrossKeys : int {
 // their items whole, as many rounds of them as end before an even share of all work
 // would, and the others' parts fill the rest of the chip.  16 sequences of 69-759 rows
 // behind 4,096 keys, 32/8 heads, 2.2 rounds of 256 rows: forward 342 us whole, 297 and 18
-// for the sums with the last 0.2 in parts; dQ 458 with tiles of 64 rows, 405 and 7.
+// for the sums with the last 0.2 in parts; dQ 458 with tiles of 64 rows, 405 and 7 (in a
+// running loop; a profiled dozen passes 326 and 437).
 // C follows from the offsets on the GPU, so that nothing waits for the host: every
 // workgroup computes it, and its place in the list, with a lane per sequence; of more
 // sequences than lanes cross_list_kernel writes the list once and a workgroup searches
@@ -183,9 +184,9 @@ __device__ __forceinline__ int cross_parts(const CrossCut& c, float inv_cap, int
 }
 
 // Sequence, tile and part of entry `entry` of a kv head's list; false past its end.
-// of(s, whole_batch, tiles, units): as above.  The list has the shared keys over the whole batch first
-// where `shared` is set (index 0), then the n sequences (index i, or i + 1).  The
-// results are wave-uniform.
+// of(s, whole_batch, tiles, units): as above.  The list has the shared keys over the whole
+// batch first where `shared` is set (index 0), then the n sequences (index i, or i + 1).
+// The results are wave-uniform.
 template <bool EVEN, class F>
 __device__ __forceinline__ bool cross_place(const CrossBatch& b, const CrossCut& c, bool shared,
                                             int entry, F&& of, CrossPlace& out) {

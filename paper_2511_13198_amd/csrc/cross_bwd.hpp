@@ -11,18 +11,21 @@
 //                        sequence's, all in one launch, so that they fill the chip
 //                        together and the shared tiles' long loops are cut into
 //                        parts of about the own tiles' length.
-// P and dS enter the products as bf16 (off by at most 2^-8 of each), sums are 32
-// bits; gradients are written in 32 bits or rounded to bf16 once.
+// P and dS enter the products as bf16 (off by at most 2^-8 of each), which is the matrix
+// cores' full rate, and D of rows with more than 64 keys comes from the rounded O, which
+// is what the forward keeps; sums are 32 bits, gradients are written in 32 bits or rounded
+// to bf16 once (off by 2.4e-3 of their norm, 1.7e-3 of which that rounding is).
 //
 // dK/dV row steps.  A step is BQ rows: `pack` heads of the group (the largest power
 // of two that divides it, at most 32) by BQ / pack tokens, so that a sequence of few
 // tokens still fills a step, and a step's rows have one address pattern.
 //
 // Bound by the products: 8 sequences of 256-2,048 rows over 1,024-8,192 keys, 32/8 heads,
-// dQ 345 us (3 products, 1,065 TFLOP/s), dK/dV 503 us (4 products, 975 TFLOP/s; matrix
-// cores busy 54 % and 47 % of the time at 1.8-1.9 GHz).  Short rows over many keys are
-// bound by reading keys and writing gradients: 32 x 8-200 rows over 577-1,024 keys, 16
-// heads, d = 64, bf16 gradients, 34 and 60 us (dK/dV moves 0.24 GB).
+// dQ 343 us (3 products, 1,071 TFLOP/s), dK/dV 490 us (4 products, 1,001 TFLOP/s) in a
+// running loop (387 and 573 in a profiled dozen passes, matrix cores busy 53 % and 47 % of
+// the time at 1.9 GHz).  Short rows over many keys are bound by reading keys and writing
+// gradients: 32 x 8-200 rows over 577-1,024 keys, 16 heads, d = 64, bf16 gradients, 33 and
+// 58 us (dK/dV moves 0.24 GB), 32-bit ones 33 and 71.
 #pragma once
 #include "cross.hpp"
 

@@ -6,18 +6,23 @@
 // The products, the online softmax and the copies are those of the self-attention
 // forward: S^T = K Q^T on 32x32x16 matrix instructions with a row per lane, P
 // rounded to bf16 and fed back as an operand, K/V tiles copied to LDS a tile or
-// more ahead.  What differs is where rows and keys come from: packed rows (all
-// heads of a group side by side), keys with offsets of their own, shared key tiles
-// before a sequence's own, and parts of the keys where rows are few (CrossCut).
+// more ahead.  P in bf16 is the matrix cores' full rate (two halves of it would be twice
+// the products): O is off by 2.3e-3 of its norm, 1.7e-3 of which its own rounding is;
+// sums, maxima and LSE are 32 bits.
+//
+// What differs is where rows and keys come from: packed rows (all heads of a group side
+// by side), keys with offsets of their own, shared key tiles before a sequence's own, and
+// parts of the keys where rows are few (CrossCut).
 //
 // KG key groups: the waves are NW / KG row blocks times KG groups that take 1 / KG
 // of every key tile; few rows per workgroup, as a token or some of a sequence
 // give, still use every wave.
 //
 // Few rows are bound by reading keys: one token for each of 64 sequences over caches of
-// 256-16,384 keys, 32/8 heads, 182 us, 4.9 TB/s.  Many are bound by the products and
+// 256-16,384 keys, 32/8 heads, 183 us, 4.9 TB/s.  Many are bound by the products and
 // the softmax beside them: 8 sequences of 256-2,048 rows over 1,024-8,192 keys, 32/8
-// heads, 257 us, 955 TFLOP/s (matrix cores busy 46 % of the time at 1.9 GHz).
+// heads, 250 us in a running loop, 982 TFLOP/s (287 in a profiled dozen passes, matrix
+// cores busy 46 % of the time at 2.0 GHz).
 #pragma once
 #include "cross.hpp"
 
