@@ -135,18 +135,25 @@ constexpr double kMoveBytesPerUs = 4.0e6;           // partial results written a
 // results a row, so the keys from which it pays grow with R / (tile - R).  us fused / apart
 // (or their ratio) behind so many shared keys, 1,280-4,096 pairs:
 //   d = 128: R = 1, 512 sequences of 8/8 heads over 100 own keys: 128 79 / 79, 256 91 / 79;
-//   R = 4, 32/8 heads: 128 80 / 88, 256 93 / 89; R = 8, 2,048 of 16/2 over 400: 256 0.94;
+//   R = 4, 32/8 heads: 128 80 / 88, 256 93 / 89; R = 8, 2,048 of 16/2 over 400: 256 0.94,
+//   512 of 32/4 over 1,000-2,000: 250 317 / 338;
 //   R = 16, 256 of 8/8 over 400: 200 97 / 113, 700 123 / 119; R = 32, 160 of 32/8 over 30:
 //   1,000 66 / 80, 2,000 101 / 98; R = 64, 256 of 16/8 over 100: 1,000 124 / 191, 3,500
 //   312 / 346
-//   d = 64: R = 1: 128 55 / 42; R = 4: 128 57 / 51, 256 64 / 52; R = 8: 128 0.95, 192 1.02;
+//   d = 64: R = 1: 128 55 / 42; R = 4: 128 57 / 51, 256 64 / 52; R = 8: 128 0.95, 192 1.02,
+//   over 1,000-2,000 120 168 / 182;
 //   R = 16: 200 62 / 72, 400 71 / 75, 700 80 / 76; R = 32: 1,000 49 / 54, 2,000 69 / 63;
 //   R = 64: 1,000 67 / 131, 3,500 176 / 217
-constexpr int64_t kApartRows = 64, kApartPrefix = 512;
+// Up to 6 pairs a CU fused keeps 256 keys, which long own keys want: 140 sequences of 8/8
+// heads over 3,000-6,000 keys, d = 64, behind 16-120 286 / 331, d = 128, behind 160-250 481 /
+// 515 (over up to 2,000 35 / 34 and 63 / 62; 130 over 30 keys of d = 64 behind 128 1.14).
+constexpr int64_t kApartRows = 64, kApartPrefix = 512, kApartPrefixMany = 256;
 int64_t fused_keys(const CrossSizes& s) {
-  if (s.n * s.hkv <= 4 * kCUs) return kApartPrefix;
-  const int64_t rows = s.seq_rows();  // (at most kApartRows)
-  return (s.d == 64 ? 0 : 128) + 500 * rows / ((rows <= 32 ? 44 : 72) - rows);
+  const int64_t pairs = s.n * s.hkv, rows = s.seq_rows();  // (rows: at most kApartRows)
+  if (pairs <= 4 * kCUs) return kApartPrefix;
+  const int64_t line = (s.d == 64 ? 0 : 128) +
+                       (rows <= 32 ? 800 * rows / (54 - rows) : 500 * rows / (72 - rows));
+  return pairs <= 6 * kCUs ? std::max(kApartPrefixMany, line) : line;
 }
 
 // Few rows over so many keys at most, shared ones among them, are one whole item a tile:

@@ -22,6 +22,7 @@ def shapes(n, q, k, prefix, hq, hkv, d, causal=True):
     (512, 1, 30, 256, 8, 8, 128, True), (512, 1, 30, 128, 32, 8, 128, False),
     (256, 32, 200, 400, 16, 8, 128, False), (256, 32, 200, 700, 16, 8, 64, False),
     (256, 16, 200, 256, 8, 8, 64, False),
+    (140, 1, 6000, 120, 8, 8, 64, False), (140, 1, 6000, 250, 8, 8, 128, False),
 ])
 def test_shared_keys_apart_or_with_each_sequence(n, q, k, prefix, hq, hkv, d, apart):
     assert shapes(n, q, k, prefix, hq, hkv, d)["apart"] == apart
