@@ -84,7 +84,7 @@ enum CrossKeys : int {
 // would, and the others' parts fill the rest of the chip.  16 sequences of 69-759 rows
 // behind 4,096 keys, 32/8 heads, 2.2 rounds of 256 rows: forward 342 us whole, 297 and 18
 // for the sums with the last 0.2 in parts; dQ 458 with tiles of 64 rows, 405 and 7 (in a
-// running loop; a profiled dozen passes 326 and 437).
+// running loop; a profiled dozen passes 324 and 434).
 // C follows from the offsets on the GPU, so that nothing waits for the host: every
 // workgroup computes it, and its place in the list, with a lane per sequence; of more
 // sequences than lanes cross_list_kernel writes the list once and a workgroup searches

@@ -22,7 +22,7 @@
 //
 // Bound by the products: 8 sequences of 256-2,048 rows over 1,024-8,192 keys, 32/8 heads,
 // dQ 343 us (3 products, 1,071 TFLOP/s), dK/dV 490 us (4 products, 1,001 TFLOP/s) in a
-// running loop (387 and 573 in a profiled dozen passes, matrix cores busy 53 % and 47 % of
+// running loop (381 and 565 in a profiled dozen passes, matrix cores busy 53 % and 47 % of
 // the time at 1.9 GHz).  Short rows over many keys are bound by reading keys and writing
 // gradients: 32 x 8-200 rows over 577-1,024 keys, 16 heads, d = 64, bf16 gradients, 33 and
 // 58 us (dK/dV moves 0.24 GB), 32-bit ones 33 and 71.

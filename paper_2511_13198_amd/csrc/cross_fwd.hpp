@@ -21,7 +21,7 @@
 // Few rows are bound by reading keys: one token for each of 64 sequences over caches of
 // 256-16,384 keys, 32/8 heads, 183 us, 4.9 TB/s.  Many are bound by the products and
 // the softmax beside them: 8 sequences of 256-2,048 rows over 1,024-8,192 keys, 32/8
-// heads, 250 us in a running loop, 982 TFLOP/s (287 in a profiled dozen passes, matrix
+// heads, 250 us in a running loop, 982 TFLOP/s (283 in a profiled dozen passes, matrix
 // cores busy 46 % of the time at 2.0 GHz).
 #pragma once
 #include "cross.hpp"
