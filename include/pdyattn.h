@@ -298,6 +298,79 @@ pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
                        int32_t inverse, int32_t in_fp32, int32_t out_fp32, void* q_out,
                        void* k_out, void* stream);
 
+/* ---- A paged key/value cache ----
+ * A pool of num_pages pages of page_size keys (a multiple of 16):
+ *   k_pages, v_pages [num_pages, Hkv, page_size, d], bf16, or with cache_e4m3 = 1 8-bit
+ *   floats (e4m3, largest 448): a value is its byte's times k_scale (v_scale) of the head,
+ *   fp32 device arrays [Hkv] (NULL with bf16);
+ *   scores fp32 [num_pages, Hkv, page_size]: a running weight of every key, where kept.
+ * page_table: int32 device array [num_seqs, max_pages]; key j of sequence i is key
+ * j % page_size of page page_table[i][j / page_size].  seqlens_k: int32 device array
+ * [num_seqs], the keys in use.  Entries behind the last page in use are not read.
+ *   - Pages may be shared by sequences (a common beginning) in calls that only read them;
+ *     what a call writes (new keys, scores, kept keys) is in pages of one sequence.
+ *   - Tables and lengths are trusted, but clamped to the tensors: wrong ones give wrong
+ *     results, no stray access (keys in no page of the pool are not written).
+ *   - Slots that hold no key in use may hold anything, NaN among it.
+ *   - num_pages * Hkv * page_size / 16 and max_pages * page_size are below 2^31.
+ * Other rules as above. */
+
+/* New keys and values into their pages: token t of the nq = cu_seqlens[i+1] -
+ * cu_seqlens[i] tokens of sequence i becomes its key seqlens_k[i] - nq + t (seqlens_k
+ * counts the new ones; tokens that would lie in front of key 0 are dropped).
+ *   k, v bf16 [total_tokens, Hkv, d]; tokens from cu_seqlens[num_seqs] on are no
+ *   sequence's.  e4m3: x / scale, up to 448, rounded once to the nearest (ties to even).
+ *   scores (or NULL): 0 for the new keys.
+ * total_tokens is below 2^26 - 4.  Needs no workspace. */
+pdy_status attn_paged_write(const void* k, const void* v, const int32_t* cu_seqlens,
+                            const int32_t* page_table, const int32_t* seqlens_k,
+                            const float* k_scale, const float* v_scale, int32_t num_seqs,
+                            int32_t total_tokens, int32_t num_pages, int32_t page_size,
+                            int32_t max_pages, int32_t num_heads_kv, int32_t head_dim,
+                            int32_t cache_e4m3, void* k_pages, void* v_pages, float* scores,
+                            void* stream);
+
+/* attn_cross_fwd over a paged cache: the queries cu_seqlens_q[i] .. cu_seqlens_q[i+1]-1 of
+ * sequence i over its first seqlens_k[i] keys (max_seqlen_k where these are more); the rules
+ * of rows, masks and results are those of attn_cross_fwd.  Meant for one or few queries a
+ * sequence (any number is right).
+ *   scores (or NULL): adds to every key in use its weight, the sum over the sequence's
+ *   rows and the heads of its group of exp(S - lse), with logits S and lse as above; rows
+ *   with lse = -inf add nothing.
+ * Probabilities (before the product with v) are rounded to bf16; logits, sums, weights and
+ * lse are 32 bits.  with_scores: whether scores will be given. */
+size_t attn_paged_fwd_workspace_size(int32_t total_q, int32_t num_seqs, int32_t max_seqlen_q,
+                                     int32_t max_seqlen_k, int32_t num_heads_q,
+                                     int32_t num_heads_kv, int32_t head_dim,
+                                     int32_t with_scores);
+pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_pages,
+                          const int32_t* page_table, const int32_t* cu_seqlens_q,
+                          const int32_t* seqlens_k, const float* k_scale, const float* v_scale,
+                          int32_t num_seqs, int32_t total_q, int32_t num_pages, int32_t page_size,
+                          int32_t max_pages, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                          int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim,
+                          int32_t cache_e4m3, int32_t causal, float scale, void* o, float* lse,
+                          float* scores, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Shortens every sequence of more than `budget` keys to so many, each kv head by its own
+ * scores: the first `first` and the last `recent` keys stay, and of those between the ones of
+ * the highest scores (equal ones: the earlier; a NaN is below every number).  What stays, of
+ * the shorter sequences everything, is copied in its order, keys, values and scores, to the
+ * pages of new_table, int32 device array [num_seqs, new_max_pages], which must be none that
+ * the sequences use.  (Keys keep what they were rotated by.)
+ *   kept int32 [num_seqs, Hkv, budget] (out): the old number of each key, -1 behind the
+ *   last.  new_lens int32 [num_seqs] (out): min(seqlens_k, budget); may be seqlens_k.
+ * first + recent <= budget <= new_max_pages * page_size (or max_seqlen_k is). */
+size_t attn_paged_evict_workspace_size(int32_t num_seqs, int32_t max_seqlen_k,
+                                       int32_t num_heads_kv, int32_t budget);
+pdy_status attn_paged_evict(void* k_pages, void* v_pages, float* scores, const int32_t* page_table,
+                            const int32_t* seqlens_k, const int32_t* new_table, int32_t num_seqs,
+                            int32_t num_pages, int32_t page_size, int32_t max_pages,
+                            int32_t new_max_pages, int32_t max_seqlen_k, int32_t num_heads_kv,
+                            int32_t head_dim, int32_t cache_e4m3, int32_t budget, int32_t recent,
+                            int32_t first, int32_t* kept, int32_t* new_lens, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
 /* Debug helper: copies cu_seqlens to the host (synchronising `stream`) and
  * checks cu[0] = 0, monotonicity and cu[num_seqs] = total_tokens.  On success
  * writes the longest segment length to *max_seqlen_out (may be NULL). */

@@ -11,10 +11,11 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpdyattn.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("pdyattn.hip", "cross.hip", "rotary.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("pdyattn.hip", "cross.hip", "rotary.hip",
+                                           "paged.hip")]
 HEADERS = [os.path.join(CSRC, f) for f in ("common.hpp", "host.hpp", "plan.hpp", "fwd.hpp",
                                            "bwd.hpp", "cross.hpp", "cross_fwd.hpp", "cross_bwd.hpp",
-                                           "rotary.hpp")] + [
+                                           "rotary.hpp", "paged.hpp")] + [
     os.path.join(ROOT, "include", "pdyattn.h")]
 
 ARCH = "gfx950"

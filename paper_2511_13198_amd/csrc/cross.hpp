@@ -119,42 +119,6 @@ __device__ __forceinline__ int cross_tiles_log2(int x, int log2) {
   return (x + (1 << log2) - 1) >> log2;
 }
 
-// Inclusive sum over the lanes up to this one, and over all (the last lane's): sums
-// within rows of 16 lanes, then of the rows before.
-__device__ __forceinline__ int wave_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // 1 lane up in a row
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);  // 2
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);  // 4
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);  // 8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // last lane of rows 0, 2
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31
-  return x;
-}
-// The largest of the lanes' values (>= 0).
-__device__ __forceinline__ int wave_max(int x) {
-  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
-  return __builtin_amdgcn_readlane(x, 63);
-}
-__device__ __forceinline__ float wave_sum(float v) {
-  auto add = [&](auto Ctrl, auto Rows) __attribute__((always_inline)) {
-    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(Ctrl)::value,
-                                                    decltype(Rows)::value, 0xf, false));
-  };
-  using std::integral_constant;
-  add(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});
-  add(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
-  add(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
-  add(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
-  add(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});
-  add(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
-}
-
 // Tiles of a sequence and the units of inner work of each: tiles of packed rows over
 // keys (forward, dQ), and tiles of keys over steps of rows (dK/dV; 2^pack_log2 heads of
 // the group to a step).
@@ -502,20 +466,6 @@ __device__ __forceinline__ void cross_store_f32(const f32x16 (&acc)[D / 32], flo
     });
     wave_lds_fence();
   });
-}
-
-// 8 floats to consecutive bf16 (rounded to nearest even) or to float.
-__device__ __forceinline__ void cross_put8(const float (&x)[8], uint16_t* to) {
-  u32x4 v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    v[i] = __builtin_bit_cast(uint32_t,
-                              __builtin_convertvector(f32x2{x[2 * i], x[2 * i + 1]}, bf16x2));
-  *reinterpret_cast<u32x4*>(to) = v;
-}
-__device__ __forceinline__ void cross_put8(const float (&x)[8], float* to) {
-  *reinterpret_cast<f32x4*>(to) = f32x4{x[0], x[1], x[2], x[3]};
-  *reinterpret_cast<f32x4*>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
 }
 
 }  // namespace pdy

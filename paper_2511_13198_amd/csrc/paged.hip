@@ -1,0 +1,344 @@
+// C-ABI of the paged key/value cache: argument checks, launch shapes, workspace and
+// launches.  The contract is in include/pdyattn.h.
+#include "../../include/pdyattn.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "host.hpp"
+#include "paged.hpp"
+
+using namespace pdy_host;
+
+namespace {
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// The pool and its tables, checked.
+struct PagedSizes {
+  int64_t n, num_pages, page, max_pages, max_k, hkv, d;
+  bool e4m3;
+  int64_t row_bytes() const { return d * (e4m3 ? 1 : 2); }
+};
+
+pdy_status check_ints(const int32_t* p, const char* name) {
+  if (p == nullptr) return fail(PDY_ERR_INVALID_ARG, "%s is NULL", name);
+  if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0)
+    return fail(PDY_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
+  return PDY_OK;
+}
+
+pdy_status check_heads(int32_t n, int32_t hkv, int32_t d) {
+  if (n < 1) return fail(PDY_ERR_INVALID_ARG, "num_seqs must be >= 1 (got %d)", n);
+  if (hkv < 1) return fail(PDY_ERR_INVALID_ARG, "head counts must be >= 1 (got Hkv=%d)", hkv);
+  if (d != 64 && d != 128)
+    return fail(PDY_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", d);
+  if ((int64_t)hkv * d >= 1 << 22)
+    return fail(PDY_ERR_INVALID_ARG, "too many heads for one launch (Hkv=%d)", hkv);
+  return PDY_OK;
+}
+
+pdy_status check_pool(const void* k, const void* v, const float* k_scale, const float* v_scale,
+                      const int32_t* table, const int32_t* len, int32_t n, int32_t num_pages,
+                      int32_t page, int32_t max_pages, int32_t max_k, int32_t hkv, int32_t d,
+                      int32_t e4m3, bool scales, PagedSizes* out) {
+  pdy_status st = check_heads(n, hkv, d);
+  if (st != PDY_OK) return st;
+  if (page < 16 || page % 16 != 0)
+    return fail(PDY_ERR_INVALID_ARG, "page_size must be a multiple of 16 (got %d)", page);
+  if (num_pages < 0 || max_pages < 0)
+    return fail(PDY_ERR_INVALID_ARG, "num_pages and max_pages must be >= 0 (got %d, %d)",
+                num_pages, max_pages);
+  // runs of 16 keys are counted in 32 bits, over the pool and over a sequence
+  if ((int64_t)num_pages * hkv * (page / 16) >= (int64_t)1 << 31 ||
+      (int64_t)max_pages * page >= (int64_t)1 << 31)
+    return fail(PDY_ERR_INVALID_ARG, "too many pages (num_pages=%d, max_pages=%d)", num_pages,
+                max_pages);
+  if (max_k < 0 || max_k > (int64_t)max_pages * page)
+    return fail(PDY_ERR_INVALID_ARG,
+                "max_seqlen_k must be in [0, max_pages * page_size] (got %d, %d * %d)", max_k,
+                max_pages, page);
+  if (e4m3 & ~1) return fail(PDY_ERR_INVALID_ARG, "cache_e4m3 must be 0 or 1");
+  if ((st = check_ints(len, "seqlens_k")) != PDY_OK) return st;
+  if (max_pages > 0 && (st = check_ints(table, "page_table"))) return st;
+  if (num_pages > 0 && ((st = check_ptr(k, "k_pages")) || (st = check_ptr(v, "v_pages")))) return st;
+  if (scales && e4m3) {
+    if ((st = check_ints(reinterpret_cast<const int32_t*>(k_scale), "k_scale")) ||
+        (st = check_ints(reinterpret_cast<const int32_t*>(v_scale), "v_scale")))
+      return st;
+  } else if (scales && (k_scale || v_scale)) {
+    return fail(PDY_ERR_INVALID_ARG, "k_scale and v_scale are of an e4m3 cache (a bf16 one has none)");
+  }
+  *out = PagedSizes{n, num_pages, page, max_pages, max_k, hkv, d, e4m3 != 0};
+  return PDY_OK;
+}
+
+pdy::PagedCache cache_of(const PagedSizes& s, const int32_t* table, const int32_t* len) {
+  const int64_t runs = s.page / 16;
+  return pdy::PagedCache{table, len, (int)s.n, (int)s.num_pages, (int)s.page, (int)s.max_pages,
+                         (int)s.max_k, (int)s.hkv, (int)runs, (uint32_t)((1ull << 32) / runs)};
+}
+
+// Whether a grid's threads can be counted in 32 bits, as a launch's are.
+bool fits_grid(int64_t wgs, int threads) { return wgs * threads < (int64_t)1 << 32; }
+
+// ---- attention ----
+struct PagedRows {
+  int64_t tq, max_q, hq;
+};
+
+pdy_status check_rows(int32_t tq, int32_t n, int32_t max_q, int32_t hq, int32_t hkv, int32_t d,
+                      PagedRows* out) {
+  if (tq < 0) return fail(PDY_ERR_INVALID_ARG, "total_q must be >= 0 (got %d)", tq);
+  if (max_q < 0 || max_q > tq || (tq > 0 && max_q < 1))
+    return fail(PDY_ERR_INVALID_ARG, "max_seqlen_q must be in [1, total_q] (got %d, total_q=%d)",
+                max_q, tq);
+  if (hq < 1 || hq % hkv != 0)
+    return fail(PDY_ERR_INVALID_ARG, "num_heads_q (%d) must be a multiple of num_heads_kv (%d)",
+                hq, hkv);
+  if (((int64_t)tq + n) * hq >= (int64_t)1 << 31)
+    return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
+  if ((int64_t)hq * d >= 1 << 24)
+    return fail(PDY_ERR_INVALID_ARG, "too many heads for one launch (Hq=%d)", hq);
+  *out = PagedRows{tq, max_q, hq};
+  return PDY_OK;
+}
+
+template <int D, bool F8, int RB, int NW>
+hipError_t launch_fwd(const pdy::PagedFwdArgs* a, dim3 grid, hipStream_t st) {
+  using C = pdy::PagedFwdCfg<D, F8, RB, NW>;
+  if (a == nullptr) return set_lds(pdy::paged_fwd_kernel<D, F8, RB, NW>, C::LDS_BYTES);
+  hipLaunchKernelGGL((pdy::paged_fwd_kernel<D, F8, RB, NW>), grid, dim3(C::NT), C::LDS_BYTES, st, *a);
+  return hipSuccess;
+}
+using LaunchFwd = hipError_t (*)(const pdy::PagedFwdArgs*, dim3, hipStream_t);
+// [d = 64, 128][bf16, e4m3][16, 32, 64 rows]
+template <int D, bool F8>
+constexpr LaunchFwd kFwdOf[3] = {launch_fwd<D, F8, 1, 4>, launch_fwd<D, F8, 2, 4>,
+                                 launch_fwd<D, F8, 4, 4>};
+const LaunchFwd* const kFwd[2][2] = {{kFwdOf<64, false>, kFwdOf<64, true>},
+                                     {kFwdOf<128, false>, kFwdOf<128, true>}};
+
+hipError_t init_paged_kernels() {
+  static hipError_t status = [] {
+    for (const auto& d : kFwd)
+      for (const LaunchFwd* f : d)
+        for (int i = 0; i < 3; ++i) {
+          const hipError_t e = f[i](nullptr, dim3(), nullptr);
+          if (e != hipSuccess) return e;
+        }
+    return hipSuccess;
+  }();
+  return status;
+}
+
+}  // namespace
+
+extern "C" {
+
+pdy_status attn_paged_write(const void* k, const void* v, const int32_t* cu_seqlens,
+                            const int32_t* page_table, const int32_t* seqlens_k,
+                            const float* k_scale, const float* v_scale, int32_t num_seqs,
+                            int32_t total_tokens, int32_t num_pages, int32_t page_size,
+                            int32_t max_pages, int32_t num_heads_kv, int32_t head_dim,
+                            int32_t cache_e4m3, void* k_pages, void* v_pages, float* scores,
+                            void* stream) {
+  g_err[0] = 0;
+  PagedSizes s;
+  pdy_status st;
+  if (total_tokens < 0 || total_tokens >= (1 << 26) - 4)
+    return fail(PDY_ERR_INVALID_ARG, "total_tokens must be >= 0 and below 2^26 - 4 (got %d)",
+                total_tokens);
+  const int64_t room = std::min<int64_t>((int64_t)std::max(max_pages, 0) * std::max(page_size, 0),
+                                         0x7fffffff);
+  if ((st = check_pool(k_pages, v_pages, k_scale, v_scale, page_table, seqlens_k, num_seqs,
+                       num_pages, page_size, max_pages, (int32_t)room, num_heads_kv, head_dim,
+                       cache_e4m3, true, &s)))
+    return st;
+  if (total_tokens == 0) return PDY_OK;
+  if ((st = check_ints(cu_seqlens, "cu_seqlens")) || (st = check_ptr(k, "k")) ||
+      (st = check_ptr(v, "v")))
+    return st;
+  if (scores && (st = check_ptr(scores, "scores"))) return st;
+  pdy::PagedWriteArgs a;
+  a.c = cache_of(s, page_table, seqlens_k);
+  a.in[0] = static_cast<const uint16_t*>(k);
+  a.in[1] = static_cast<const uint16_t*>(v);
+  a.pages[0] = k_pages;
+  a.pages[1] = v_pages;
+  a.scale[0] = k_scale;
+  a.scale[1] = v_scale;
+  a.scores = scores;
+  a.cu = cu_seqlens;
+  a.tokens = total_tokens;
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  const dim3 grid((unsigned)ceil_div(total_tokens, 4));
+  const hipError_t e = launch_timed(K_PAGED_WRITE, hs, [&] {
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, hs, a); };
+    if (head_dim == 64)
+      s.e4m3 ? go(pdy::paged_write_kernel<64, true>) : go(pdy::paged_write_kernel<64, false>);
+    else
+      s.e4m3 ? go(pdy::paged_write_kernel<128, true>) : go(pdy::paged_write_kernel<128, false>);
+  });
+  if (e != hipSuccess) return hip_fail(e, "paged_write_kernel launch");
+  return PDY_OK;
+}
+
+size_t attn_paged_fwd_workspace_size(int32_t total_q, int32_t num_seqs, int32_t max_seqlen_q,
+                                     int32_t max_seqlen_k, int32_t num_heads_q,
+                                     int32_t num_heads_kv, int32_t head_dim, int32_t with_scores) {
+  g_err[0] = 0;
+  PagedRows r;
+  if (check_heads(num_seqs, num_heads_kv, head_dim) != PDY_OK || max_seqlen_k < 0 ||
+      (with_scores & ~1) ||
+      check_rows(total_q, num_seqs, max_seqlen_q, num_heads_q, num_heads_kv, head_dim, &r) != PDY_OK)
+    return 0;
+  return 256;
+}
+
+pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_pages,
+                          const int32_t* page_table, const int32_t* cu_seqlens_q,
+                          const int32_t* seqlens_k, const float* k_scale, const float* v_scale,
+                          int32_t num_seqs, int32_t total_q, int32_t num_pages, int32_t page_size,
+                          int32_t max_pages, int32_t max_seqlen_q, int32_t max_seqlen_k,
+                          int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim,
+                          int32_t cache_e4m3, int32_t causal, float scale, void* o, float* lse,
+                          float* scores, void* workspace, size_t workspace_bytes, void* stream) {
+  g_err[0] = 0;
+  PagedSizes s;
+  PagedRows r;
+  pdy_status st;
+  if ((st = check_pool(k_pages, v_pages, k_scale, v_scale, page_table, seqlens_k, num_seqs,
+                       num_pages, page_size, max_pages, max_seqlen_k, num_heads_kv, head_dim,
+                       cache_e4m3, true, &s)) ||
+      (st = check_rows(total_q, num_seqs, max_seqlen_q, num_heads_q, num_heads_kv, head_dim, &r)) ||
+      (st = check_scale(scale, causal)))
+    return st;
+  if (total_q == 0) return PDY_OK;
+  if ((st = check_ints(cu_seqlens_q, "cu_seqlens_q")) || (st = check_ptr(q, "q")) ||
+      (st = check_ptr(o, "o")) || (st = check_ptr(lse, "lse")) ||
+      (st = check_ptr(workspace, "workspace")))
+    return st;
+  if (scores && (st = check_ptr(scores, "scores"))) return st;
+  if (workspace_bytes < 256)
+    return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, attn_paged_fwd needs %zu",
+                workspace_bytes, (size_t)256);
+  const int64_t g = r.hq / s.hkv, rows = r.max_q * g;
+  const int shape = rows <= 16 ? 0 : rows <= 32 ? 1 : 2;
+  pdy::PagedFwdArgs a;
+  a.c = cache_of(s, page_table, seqlens_k);
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = k_pages;
+  a.v = v_pages;
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
+  a.cu_q = cu_seqlens_q;
+  a.tq = total_q;
+  a.hq = num_heads_q;
+  a.g = (int)g;
+  a.g_inv = (uint32_t)((1ull << 32) / g);
+  a.causal = causal;
+  a.max_tiles = (int)ceil_div(rows, 16 << shape);
+  a.scale_log2 = scale * pdy::kLog2e;
+  a.o = static_cast<uint16_t*>(o);
+  a.lse = lse;
+  const int64_t wgs = s.n * a.max_tiles * s.hkv;
+  if (!fits_grid(wgs, 256)) return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
+  hipError_t e = init_paged_kernels();
+  if (e != hipSuccess) return hip_fail(e, "kernel attribute setup");
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  e = launch_timed(K_PAGED_FWD, hs, [&] {
+    (void)kFwd[s.d == 128][s.e4m3][shape](&a, dim3((unsigned)wgs), hs);
+  });
+  if (e != hipSuccess) return hip_fail(e, "paged_fwd_kernel launch");
+  if (scores) {
+    pdy::PagedWeighArgs b{a.c, a.q, a.k, a.k_scale, a.cu_q, a.lse, a.tq, a.hq, a.g, a.g_inv,
+                          a.causal, a.scale_log2, scores};
+    const dim3 grid((unsigned)ceil_div(ceil_div(std::max<int64_t>(s.max_k, 1), 16),
+                                       4 * pdy::kWeighRuns), (unsigned)s.hkv, (unsigned)s.n);
+    e = launch_timed(K_PAGED_WEIGH, hs, [&] {
+      auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, hs, b); };
+      if (head_dim == 64)
+        s.e4m3 ? go(pdy::paged_weigh_kernel<64, true>) : go(pdy::paged_weigh_kernel<64, false>);
+      else
+        s.e4m3 ? go(pdy::paged_weigh_kernel<128, true>) : go(pdy::paged_weigh_kernel<128, false>);
+    });
+    if (e != hipSuccess) return hip_fail(e, "paged_weigh_kernel launch");
+  }
+  return PDY_OK;
+}
+
+size_t attn_paged_evict_workspace_size(int32_t num_seqs, int32_t max_seqlen_k,
+                                       int32_t num_heads_kv, int32_t budget) {
+  g_err[0] = 0;
+  if (num_seqs < 1 || max_seqlen_k < 0 || num_heads_kv < 1 || budget < 1) return 0;
+  return 256;
+}
+
+pdy_status attn_paged_evict(void* k_pages, void* v_pages, float* scores, const int32_t* page_table,
+                            const int32_t* seqlens_k, const int32_t* new_table, int32_t num_seqs,
+                            int32_t num_pages, int32_t page_size, int32_t max_pages,
+                            int32_t new_max_pages, int32_t max_seqlen_k, int32_t num_heads_kv,
+                            int32_t head_dim, int32_t cache_e4m3, int32_t budget, int32_t recent,
+                            int32_t first, int32_t* kept, int32_t* new_lens, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  g_err[0] = 0;
+  PagedSizes s;
+  pdy_status st;
+  if ((st = check_pool(k_pages, v_pages, nullptr, nullptr, page_table, seqlens_k, num_seqs,
+                       num_pages, page_size, max_pages, max_seqlen_k, num_heads_kv, head_dim,
+                       cache_e4m3, false, &s)))
+    return st;
+  if (budget < 1) return fail(PDY_ERR_INVALID_ARG, "budget must be >= 1 (got %d)", budget);
+  if (recent < 0 || first < 0 || (int64_t)recent + first > budget)
+    return fail(PDY_ERR_INVALID_ARG,
+                "recent and first must be >= 0 and together at most the budget (got %d, %d, %d)",
+                recent, first, budget);
+  const int64_t most = std::min<int64_t>(budget, s.max_k);
+  if (new_max_pages < 0 || (int64_t)new_max_pages * page_size < most)
+    return fail(PDY_ERR_INVALID_ARG, "new_table has room for %d pages of %d keys, %d may stay",
+                new_max_pages, page_size, (int)most);
+  if (s.n * s.hkv * budget >= (int64_t)1 << 31)
+    return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
+  if (s.hkv > 65535 || s.n > 65535)
+    return fail(PDY_ERR_INVALID_ARG, "too many sequences or heads for one launch");
+  if (num_pages > 0 && (st = check_ptr(scores, "scores"))) return st;
+  if (new_max_pages > 0 && (st = check_ints(new_table, "new_table"))) return st;
+  if (new_table != nullptr && new_table == page_table)
+    return fail(PDY_ERR_INVALID_ARG, "new_table must name other pages than page_table");
+  if ((st = check_ints(kept, "kept")) || (st = check_ints(new_lens, "new_lens")) ||
+      (st = check_ptr(workspace, "workspace")))
+    return st;
+  if (workspace_bytes < 256)
+    return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, attn_paged_evict needs %zu",
+                workspace_bytes, (size_t)256);
+  pdy::PagedEvictArgs a;
+  a.c = cache_of(s, page_table, seqlens_k);
+  a.new_table = new_table;
+  a.new_pages = new_max_pages;
+  a.budget = budget;
+  a.recent = recent;
+  a.first = first;
+  a.scores = scores;
+  a.k = static_cast<uint8_t*>(k_pages);
+  a.v = static_cast<uint8_t*>(v_pages);
+  a.row_bytes = (int)s.row_bytes();
+  a.kept = kept;
+  a.new_len = new_lens;
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  hipError_t e = launch_timed(K_PAGED_SELECT, hs, [&] {
+    hipLaunchKernelGGL(pdy::paged_select_kernel, dim3((unsigned)(s.n * s.hkv)),
+                       dim3(pdy::kSelectThreads), 0, hs, a);
+  });
+  if (e != hipSuccess) return hip_fail(e, "paged_select_kernel launch");
+  const dim3 grid((unsigned)std::max<int64_t>(1, ceil_div(most, pdy::kGatherRows)),
+                  (unsigned)s.hkv, (unsigned)s.n);
+  e = launch_timed(K_PAGED_GATHER, hs, [&] {
+    hipLaunchKernelGGL(pdy::paged_gather_kernel, grid, dim3(256), 0, hs, a);
+  });
+  if (e != hipSuccess) return hip_fail(e, "paged_gather_kernel launch");
+  return PDY_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,697 @@
+// A paged key/value cache: new keys into their pages, attention of few rows a sequence
+// over the pages, the keys' sums of attention weight, and eviction by them.
+//
+// k and v are [num_pages][hkv][page][D], bf16 or e4m3 (value = byte * the head's scale);
+// key j of sequence i and head h is row j % page of page table[i][j / page].  A head's rows
+// of a page lie together, so that a run of 16 keys (pages are multiples of it) is one
+// piece of memory.  Such runs are numbered over the whole pool: run u starts at u * 16 * D
+// elements (scores: u * 16).
+//
+// Lengths and page numbers read from memory are clamped, so that no value in them makes a
+// kernel leave its tensors.
+#pragma once
+#include "common.hpp"
+
+namespace pdy {
+
+constexpr float kE4m3Max = 448.f;
+
+struct PagedCache {
+  const int32_t* table;  // [n][max_pages]
+  const int32_t* len;    // [n]
+  int n;
+  int num_pages;
+  int page;             // keys a page
+  int max_pages;        // of a sequence
+  int max_k;            // most keys of a sequence (at most max_pages * page)
+  int hkv;
+  int runs;             // page / 16
+  uint32_t runs_inv;    // 2^32 / runs, rounded down (runs > 1)
+};
+
+// Keys in use of sequence i.
+__device__ __forceinline__ int paged_len(const PagedCache& c, int i) {
+  return c.num_pages > 0 ? min(max(c.len[i], 0), c.max_k) : 0;
+}
+// x / runs by the reciprocal, off by at most one (x >= 0).
+__device__ __forceinline__ int paged_div(const PagedCache& c, int x) {
+  if (c.runs == 1) return x;  // uniform
+  const int t = (int)__umulhi((uint32_t)x, c.runs_inv);
+  return x - t * c.runs >= c.runs ? t + 1 : t;
+}
+// The run that holds keys 16 x .. 16 x + 15 of sequence i and head h (x in use); -1: its page
+// is none of the pool's.
+__device__ __forceinline__ int paged_run(const PagedCache& c, int i, int h, int x) {
+  const int p = paged_div(c, x);
+  const int id = c.table[(size_t)i * c.max_pages + p];
+  return (uint32_t)id < (uint32_t)c.num_pages ? (id * c.hkv + h) * c.runs + (x - p * c.runs) : -1;
+}
+
+// The sequence of packed token t: the last one that starts at t or before, of 64 evenly
+// spaced offsets, of the 64th part behind the one found, ...; n where t is behind the last.
+// (wave-uniform)
+__device__ __forceinline__ int paged_seq_of(const int32_t* cu, int n, int t) {
+  int lo = 0, span = n + 1;
+  while (true) {
+    const int step = (span + 63) >> 6, l = __lane_id();
+    const bool at = l * step < span && cu[lo + l * step] <= t;
+    const int k = max(0, __builtin_popcountll(__builtin_amdgcn_ballot_w64(at)) - 1);
+    lo += k * step;
+    span = min(step, span - k * step);
+    if (step == 1) break;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// ---------------------------------------------------------------------------
+// New keys and values into their pages.  Token t of a sequence with nq new tokens and nk
+// keys in use (the new ones among them) is its key nk - nq + t.  A wave per token, 8
+// elements a lane; e4m3 rounds x / scale once, to the nearest (beyond the largest number
+// to it).
+// ---------------------------------------------------------------------------
+struct PagedWriteArgs {
+  PagedCache c;
+  const uint16_t* in[2];  // k, v [tokens][hkv][D]
+  void* pages[2];
+  const float* scale[2];  // [hkv]; NULL: bf16
+  float* scores;          // NULL: none
+  const int32_t* cu;
+  int tokens;
+};
+
+// 8 bf16 of one 16-byte word as 8 e4m3, divided by s.
+__device__ __forceinline__ u32x2 paged_e4m3(const u32x4& x, float s) {
+  uint32_t out[2] = {0u, 0u};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float y[2] = {__uint_as_float(x[i] << 16) / s, __uint_as_float(x[i] & 0xffff0000u) / s};
+#pragma unroll
+    for (int j = 0; j < 2; ++j)  // (a NaN stays one)
+      if (y[j] == y[j]) y[j] = fminf(fmaxf(y[j], -kE4m3Max), kE4m3Max);
+    if (i & 1) out[i >> 1] = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], out[i >> 1], true);
+    else out[i >> 1] = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], out[i >> 1], false);
+  }
+  return u32x2{out[0], out[1]};
+}
+
+template <int D, bool F8>
+__global__ void __launch_bounds__(256) paged_write_kernel(PagedWriteArgs a) {
+  constexpr int LANES = D / 8;  // of a row
+  const int t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (t >= a.tokens) return;
+  const int i = paged_seq_of(a.cu, a.c.n, t);
+  if (i >= a.c.n) return;  // behind the last sequence
+  const int j = paged_len(a.c, i) - (a.cu[i + 1] - t);
+  if (j < 0 || j >= a.c.max_k) return;
+  for (int u = __lane_id(); u < a.c.hkv * LANES; u += 64) {
+    const int h = u / LANES, e = (u % LANES) * 8;
+    const int run = paged_run(a.c, i, h, j >> 4);
+    if (run < 0) continue;
+    const size_t from = ((size_t)t * a.c.hkv + h) * D + e, row = (size_t)run * 16 + (j & 15);
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(a.in[kv] + from);
+      if constexpr (F8)
+        *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.pages[kv]) + row * D + e) =
+            paged_e4m3(x, a.scale[kv][h]);
+      else
+        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.pages[kv]) + row * D + e) = x;
+    }
+    if (a.scores && e == 0) a.scores[row] = 0.f;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Attention of few rows a sequence over its pages.
+//   S_ij = scale <q_i, k_j>,  LSE_i = log sum_j exp(S_ij),  O_i = sum_j exp(S_ij - LSE_i) v_j
+// over the visible keys j (causal: the last query sees every key, the one before all but
+// the last, ...); a row that sees none gets O = 0, LSE = -inf.
+//
+// Rows are packed: the g heads of a group side by side, row R of a sequence and kv head hk
+// being head hk g + R % g of token R / g.  A workgroup has a
+// tile of 16 RB packed rows of a sequence and a kv head; its waves take steps of 32 keys in
+// turn, each on its own: S^T = K Q^T and O^T += V^T P^T on 16x16x32 matrix instructions (a
+// row per lane of 16, its keys over the four groups of lanes), K and V copied to the
+// wave's own LDS, so that no barrier stands in the loop.  At the end the waves' O, maxima
+// and sums are combined.
+//
+// P is rounded to bf16, as in the other attention kernels (O is off by 2.3e-3 of its norm,
+// 1.7e-3 of which its own rounding is); logits, sums, maxima and LSE are 32 bits.  e4m3
+// keys and values are widened to bf16, exactly, on their way to the matrix instructions;
+// the scales go into the logits' and the output's.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+// The largest (the sum) of the values that lanes l, l ^ 16, l ^ 32, l ^ 48 hold.
+__device__ __forceinline__ float quad_max(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// 8 e4m3 as 8 bf16.
+__device__ __forceinline__ bf16x8 widen8(const u32x2& x) {
+  bf16x8 out;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bf16x2 y = (i & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i >> 1], 1.f, true)
+                             : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i >> 1], 1.f, false);
+    out[2 * i] = y[0];
+    out[2 * i + 1] = y[1];
+  }
+  return out;
+}
+
+// LDS reads of the tiles: 16 bytes of K, to be waited for; V transposed (8 keys of a
+// column: 4 of a run and 4 of the next for 16 bits), waited for.
+template <int OFF>
+__device__ __forceinline__ void paged_read16(uint32_t addr, u32x4& x) {
+  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(x) : "v"(addr), "i"(OFF));
+}
+template <int RUN>
+__device__ __forceinline__ void paged_read_tr16(uint32_t addr, TrRegs& x) {
+  asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %2 offset:%3\n\t"
+               "s_waitcnt lgkmcnt(0)"
+               : "=&v"(x.lo), "=&v"(x.hi) : "v"(addr), "i"(RUN));
+}
+__device__ __forceinline__ void paged_read_tr8(uint32_t addr, u32x2& x) {
+  asm volatile("ds_read_b64_tr_b8 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x) : "v"(addr));
+}
+
+// A wave's tile of 32 keys (two runs) in LDS: rows of D elements as they are in memory, the
+// 16-byte chunks of row r exchanged by exclusive or, so that the reads of K (a chunk of 16
+// rows a quarter-wave) and the transposing reads of V (8 rows of 32 bytes, or 16 of 16,
+// a half-wave) meet no bank twice.
+template <int D, bool F8>
+struct PagedTile {
+  static constexpr int ROW = D * (F8 ? 1 : 2);  // bytes
+  static constexpr int CHUNKS = ROW / 16;
+  static constexpr int RUN = 16 * ROW;          // bytes of a run
+  static constexpr int COPIES = RUN / 1024;     // instructions that copy it
+  static constexpr int BYTES = 2 * RUN;
+  __device__ __forceinline__ static int swz_k(int r) {
+    return ROW == 256 ? r & 15 : ROW == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
+  }
+  __device__ __forceinline__ static int swz_v(int r) {
+    if constexpr (!F8) return ROW == 256 ? (2 * r) & 15 : 2 * ((r >> 1) & 3);
+    return ROW == 128 ? ((r >> 1) & 3) + 4 * ((r >> 4) & 1) : ((r >> 2) & 1) + 2 * ((r >> 4) & 1);
+  }
+};
+
+template <int D, bool F8, int RB, int NW>
+struct PagedFwdCfg {
+  using T = PagedTile<D, F8>;
+  static constexpr int NT = NW * 64;
+  static constexpr int ROWS = 16 * RB;
+  static constexpr int WAVE = 2 * T::BYTES;  // K and V
+  static constexpr int PITCH = D + 4;        // floats of a combined row
+  static constexpr int STAT = NW * ROWS * PITCH * 4;
+  static constexpr int END = STAT + NW * ROWS * 8;
+  static constexpr int LDS_BYTES = NW * WAVE > END ? NW * WAVE : END;
+  static_assert(LDS_BYTES <= 160 * 1024, "LDS");
+};
+
+struct PagedFwdArgs {
+  PagedCache c;
+  const uint16_t* q;
+  const void* k;
+  const void* v;
+  const float* k_scale;  // [hkv]; NULL: 1
+  const float* v_scale;
+  const int32_t* cu_q;
+  int tq, hq, g;
+  uint32_t g_inv;
+  int causal;
+  int max_tiles;  // row tiles of a sequence
+  float scale_log2;
+  uint16_t* o;
+  float* lse;
+};
+
+// One copy of 1 KB into LDS: lane l's 16 bytes at base + voff, zeros from `bytes` on.
+__device__ __forceinline__ void paged_copy(uint64_t base, int bytes, uint32_t voff, uint8_t* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto rs =
+      __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(base), 0, bytes, kBufferFlags);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)lds, 16,
+                                           voff, 0, 0, 0);
+#endif
+}
+
+template <int D, bool F8, int RB, int NW>
+__global__ void __launch_bounds__(NW * 64) paged_fwd_kernel(PagedFwdArgs a) {
+  using C = PagedFwdCfg<D, F8, RB, NW>;
+  using T = typename C::T;
+  constexpr int KS = D / 32, DB = D / 16;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t paged_smem[];
+  const PagedCache& c = a.c;
+  const int hk = blockIdx.x % (unsigned)c.hkv, entry = blockIdx.x / (unsigned)c.hkv;
+  const int seq = entry / a.max_tiles, tile = entry - seq * a.max_tiles;
+  const int q_lo = min(max(a.cu_q[seq], 0), a.tq);
+  const int nq = min(max(a.cu_q[seq + 1], q_lo), a.tq) - q_lo;
+  const int row_end = nq * a.g;  // packed rows, from the sequence's first on
+  const int row0 = tile * C::ROWS;
+  if (row0 >= row_end) return;
+  const int nk = paged_len(c, seq);
+
+  const int l = __lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i16 = l & 15, grp = l >> 4;
+  auto token = [&](int r) __attribute__((always_inline)) {
+    if (a.g == 1) return r;
+    const int t = (int)__umulhi((uint32_t)r, a.g_inv);
+    return r - t * a.g >= a.g ? t + 1 : t;
+  };
+  auto key_end = [&](int r) __attribute__((always_inline)) {
+    return a.causal ? max(0, min(nk, token(min(r, row_end - 1)) + nk - nq + 1)) : nk;
+  };
+  // (token, head) pair of a packed row, counted over the batch
+  auto pair_of = [&](int r) __attribute__((always_inline)) {
+    const int t = token(r);
+    return (size_t)(q_lo + t) * a.hq + hk * a.g + (r - t * a.g);
+  };
+  int end[RB];
+  bf16x8 qf[RB][KS];
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const int r = row0 + b * 16 + i16;
+    end[b] = key_end(r);
+    const bool ok = r < row_end;
+    const uint16_t* qp = a.q + pair_of(ok ? r : row0) * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      qf[b][ks] = load_bf16x8(qp + (F8 ? ((ks >> 1) * 4 + grp) * 16 + (ks & 1) * 8
+                                       : ks * 32 + grp * 8), ok);
+  }
+  const int all_end = __builtin_amdgcn_readfirstlane(key_end(row0));            // seen by every row
+  const int some_end = __builtin_amdgcn_readfirstlane(key_end(row0 + C::ROWS - 1));  // by some
+  const float scale2 = a.scale_log2 * (F8 ? a.k_scale[hk] : 1.f);
+
+  f32x4 oacc[RB][DB];
+  float m[RB], lsum[RB];
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    m[b] = -INFINITY;
+    lsum[b] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) oacc[b][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  uint8_t* const kt = paged_smem + w * C::WAVE;
+  uint8_t* const vt = kt + T::BYTES;
+  // lanes' places in a copy, and in the reads
+  uint32_t kv_off[2][T::COPIES][2];  // [k, v][copy][run]
+#pragma unroll
+  for (int i = 0; i < T::COPIES; ++i) {
+    const int at = i * 1024 + l * 16, r = at / T::ROW, slot = (at % T::ROW) / 16;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      kv_off[0][i][s] = r * T::ROW + (slot ^ T::swz_k(r + 16 * s)) * 16;
+      kv_off[1][i][s] = r * T::ROW + (slot ^ T::swz_v(r + 16 * s)) * 16;
+    }
+  }
+  const uint32_t ka = lds_addr(kt) + i16 * T::ROW + (grp ^ T::swz_k(i16)) * 16;
+  uint32_t va;
+  if constexpr (F8) {
+    const int e = i16 >> 1, r = e < 4 ? 4 * grp + e : 16 + 4 * grp + e - 4;
+    va = lds_addr(vt) + r * T::ROW + T::swz_v(r) * 16 + (i16 & 1) * 8;
+  } else {
+    const int r = 4 * grp + (i16 >> 2);
+    va = lds_addr(vt) + r * T::ROW + T::swz_v(r) * 16 + ((i16 & 3) >> 1) * 16 + (i16 & 1) * 8;
+  }
+
+  const int steps = (some_end + 31) >> 5;
+  for (int st = w; st < steps; st += NW) {
+    const int k0 = st * 32;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int x = st * 2 + s, valid = min(16, nk - x * 16);
+      const int run = valid > 0 ? max(0, __builtin_amdgcn_readfirstlane(paged_run(c, seq, hk, x))) : 0;
+      const size_t off = (size_t)run * T::RUN;
+      const int bytes = max(0, valid) * T::ROW;
+#pragma unroll
+      for (int i = 0; i < T::COPIES; ++i) {
+        paged_copy((uint64_t)a.k + off, bytes, kv_off[0][i][s], kt + s * T::RUN + i * 1024);
+        paged_copy((uint64_t)a.v + off, bytes, kv_off[1][i][s], vt + s * T::RUN + i * 1024);
+      }
+    }
+    wait_dma();
+
+    // S^T = K Q^T, a run of 16 keys at a time
+    f32x4 s[RB][2];
+    static_for<2>([&](auto R) {
+      constexpr int run = decltype(R)::value;
+      constexpr int N = F8 ? KS / 2 : KS;
+      u32x4 kr[N];
+      static_for<N>([&](auto I) {
+        constexpr int i = decltype(I)::value;
+        paged_read16<run * T::RUN>(ka ^ (i * 64), kr[i]);
+      });
+      static_for<N>([&](auto I) {
+        constexpr int i = decltype(I)::value;
+        row_wait<N - 1 - i>(kr[i]);
+      });
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        s[b][run] = f32x4{0.f, 0.f, 0.f, 0.f};
+        static_for<KS>([&](auto I) {
+          constexpr int ks = decltype(I)::value;
+          bf16x8 x;
+          if constexpr (F8) x = widen8(u32x2{kr[ks / 2][(ks & 1) * 2], kr[ks / 2][(ks & 1) * 2 + 1]});
+          else x = as_bf16x8(kr[ks]);
+          s[b][run] = mfma16(x, qf[b][ks], s[b][run]);
+        });
+      }
+    });
+
+    bf16x8 pf[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      if (k0 + 32 > all_end) {
+#pragma unroll
+        for (int run = 0; run < 2; ++run)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (k0 + run * 16 + grp * 4 + r >= end[b]) s[b][run][r] = -INFINITY;
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int run = 0; run < 2; ++run)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, s[b][run][r]);
+      top = quad_max(top) * scale2;
+      const bool grow = top > m[b] + kRescaleSlack;
+      if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+        const float alpha = grow ? fast_exp2(m[b] - top) : 1.f;
+        m[b] = grow ? top : m[b];
+        lsum[b] *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) oacc[b][db] *= alpha;
+      }
+      const float muse = m[b] == -INFINITY ? 0.f : m[b];
+#pragma unroll
+      for (int run = 0; run < 2; ++run)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = fast_exp2(__builtin_fmaf(s[b][run][r], scale2, -muse));
+          lsum[b] += p;
+          pf[b][run * 4 + r] = (__bf16)p;
+        }
+    }
+
+    // O^T += V^T P^T, 16 columns at a time
+    static_for<DB>([&](auto I) {
+      constexpr int db = decltype(I)::value;
+      bf16x8 x;
+      if constexpr (F8) {
+        u32x2 y;
+        paged_read_tr8(va ^ (db * 16), y);
+        x = widen8(y);
+      } else {
+        TrRegs y;
+        paged_read_tr16<T::RUN>(va ^ (db * 32), y);
+        x = y.operand();
+      }
+#pragma unroll
+      for (int b = 0; b < RB; ++b) oacc[b][db] = mfma16(x, pf[b], oacc[b][db]);
+    });
+  }
+
+  // combine the waves: O, offset and sum of every row through LDS
+  __syncthreads();
+  float* const slots = reinterpret_cast<float*>(paged_smem);
+  f32x2* const stat = reinterpret_cast<f32x2*>(paged_smem + C::STAT);
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const float tot = quad_sum(lsum[b]);
+    float* const mine = slots + ((size_t)w * C::ROWS + b * 16 + i16) * C::PITCH + grp * 4;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(mine + db * 16) = oacc[b][db];
+    if (grp == 0) stat[w * C::ROWS + b * 16 + i16] = f32x2{m[b], tot};
+  }
+  __syncthreads();
+  const float out_scale = F8 ? a.v_scale[hk] : 1.f;
+  for (int u = threadIdx.x; u < C::ROWS * (D / 8); u += C::NT) {
+    const int r = u / (D / 8), e = (u % (D / 8)) * 8;
+    if (row0 + r >= row_end) continue;
+    float mx = -INFINITY, tot = 0.f;
+#pragma unroll
+    for (int j = 0; j < NW; ++j) mx = fmaxf(mx, stat[j * C::ROWS + r][0]);
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NW; ++j) {
+      const f32x2 st = stat[j * C::ROWS + r];
+      // (a NaN sum makes the row's)
+      const float wt = st[1] > 0.f || st[1] != st[1] ? fast_exp2(st[0] - mx) : 0.f;
+      tot += wt * st[1];
+      const float* const src = slots + ((size_t)j * C::ROWS + r) * C::PITCH + e;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] += wt * src[k];
+    }
+    const float inv = tot > 0.f || tot != tot ? out_scale / tot : 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] *= inv;
+    const size_t pair = pair_of(row0 + r);
+    cross_put8(x, a.o + pair * D + e);
+    if (e == 0) {
+      const int t = token(row0 + r);
+      a.lse[(size_t)(hk * a.g + (row0 + r - t * a.g)) * a.tq + q_lo + t] =
+          tot > 0.f ? (mx + __builtin_log2f(tot)) * kLn2 : -INFINITY;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The keys' weights: scores_j += sum over the sequence's rows i (of all heads of the group)
+// of exp(S_ij - LSE_i), for the visible keys.  One wave sums a key's rows, in order, so
+// that results do not depend on the launch.  A wave takes runs of 16 keys; rows with LSE
+// = -inf (no key, or a NaN or +inf logit) add nothing.
+// ---------------------------------------------------------------------------
+struct PagedWeighArgs {
+  PagedCache c;
+  const uint16_t* q;
+  const void* k;
+  const float* k_scale;
+  const int32_t* cu_q;
+  const float* lse;
+  int tq, hq, g;
+  uint32_t g_inv;
+  int causal;
+  float scale_log2;
+  float* scores;
+};
+
+constexpr int kWeighRuns = 8;  // of a wave
+
+template <int D, bool F8>
+__global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
+  constexpr int KS = D / 32;
+  using T = PagedTile<D, F8>;
+  const PagedCache& c = a.c;
+  const int hk = blockIdx.y, seq = blockIdx.z;
+  const int q_lo = min(max(a.cu_q[seq], 0), a.tq);
+  const int nq = min(max(a.cu_q[seq + 1], q_lo), a.tq) - q_lo;
+  const int nk = paged_len(c, seq);
+  const int l = __lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i16 = l & 15, grp = l >> 4;
+  const int rows = nq * a.g;
+  const float scale2 = a.scale_log2 * (F8 ? a.k_scale[hk] : 1.f);
+  const int first = (blockIdx.x * 4 + w) * kWeighRuns;
+  if (rows == 0) return;
+  for (int x = first; x < first + kWeighRuns && x * 16 < nk; ++x) {
+    const int run = __builtin_amdgcn_readfirstlane(paged_run(c, seq, hk, x));
+    if (run < 0) continue;
+    const uint8_t* const kp = static_cast<const uint8_t*>(a.k) + (size_t)run * T::RUN + i16 * T::ROW;
+    bf16x8 kf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if constexpr (F8)
+        kf[ks] = widen8(*reinterpret_cast<const u32x2*>(kp + ks * 32 + grp * 8));
+      else
+        kf[ks] = load_bf16x8(reinterpret_cast<const uint16_t*>(kp) + ks * 32 + grp * 8, true);
+    }
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int r0 = 0; r0 < rows; r0 += 16) {
+      const int r = min(r0 + i16, rows - 1);
+      int t = r;
+      if (a.g > 1) {
+        t = (int)__umulhi((uint32_t)r, a.g_inv);
+        t = r - t * a.g >= a.g ? t + 1 : t;
+      }
+      const int h = hk * a.g + (r - t * a.g);
+      const uint16_t* const qp = a.q + ((size_t)(q_lo + t) * a.hq + h) * D + grp * 8;
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) s = mfma16(kf[ks], load_bf16x8(qp + ks * 32, true), s);
+      const float lse = a.lse[(size_t)h * a.tq + q_lo + t];
+      const int end = r0 + i16 < rows && lse > -INFINITY
+                          ? (a.causal ? min(nk, t + nk - nq + 1) : nk) - x * 16 - grp * 4 : 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e < end) sum[e] += fast_exp2(__builtin_fmaf(s[e], scale2, -lse * kLog2e));
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int off = 8; off > 0; off >>= 1) sum[e] += __shfl_xor(sum[e], off);
+    const float mine = i16 == 0 ? sum[0] : i16 == 1 ? sum[1] : i16 == 2 ? sum[2] : sum[3];
+    if (i16 < 4 && x * 16 + grp * 4 + i16 < nk)
+      a.scores[(size_t)run * 16 + grp * 4 + i16] += mine;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Eviction.  Of a head's L keys the first `first`, the last `recent` and, of those between,
+// the ones of the highest scores stay, `budget` together; equal scores: the earlier key.
+// Scores are ordered as numbers, a NaN below all.
+//
+// paged_select_kernel, a workgroup per sequence and head, finds the smallest score that
+// stays: its 32 bits from the highest on, 11 at a time, each by the counts of the keys that
+// share the bits found so far; then writes the numbers of the keys that stay, in order.
+// paged_gather_kernel copies them to their new places.
+// ---------------------------------------------------------------------------
+struct PagedEvictArgs {
+  PagedCache c;
+  const int32_t* new_table;  // [n][new_pages]
+  int new_pages;
+  int budget, recent, first;
+  float* scores;
+  uint8_t* k;
+  uint8_t* v;
+  int row_bytes;
+  int32_t* kept;  // [n][hkv][budget]
+  int32_t* new_len;
+};
+
+// Scores as unsigned numbers of the same order; a NaN is 0.
+__device__ __forceinline__ uint32_t paged_order(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return x != x ? 0u : b == 0x80000000u ? 0x80000000u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048;
+
+__global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvictArgs a) {
+  __shared__ uint32_t hist[kBins];
+  __shared__ uint32_t wave_sum_of[kSelectWaves], wave_tie[kSelectWaves], found[2];
+  const PagedCache& c = a.c;
+  const int hk = blockIdx.x % (unsigned)c.hkv, seq = blockIdx.x / (unsigned)c.hkv;
+  const int t = threadIdx.x, l = __lane_id(), w = t >> 6;
+  const int n = paged_len(c, seq);
+  int32_t* const kept = a.kept + ((size_t)seq * c.hkv + hk) * a.budget;
+  if (n <= a.budget) {
+    for (int j = t; j < a.budget; j += kSelectThreads) kept[j] = j < n ? j : -1;
+    return;
+  }
+  // (first + recent <= budget < n)
+  const int lo = a.first, hi = n - a.recent;
+  const int stay = a.budget - a.first - a.recent;  // of the keys lo .. hi
+  auto order = [&](int j) __attribute__((always_inline)) {
+    const int run = paged_run(c, seq, hk, j >> 4);
+    return run < 0 ? 0u : paged_order(a.scores[(size_t)run * 16 + (j & 15)]);
+  };
+  // the stay-th largest: bits 31..21, 20..10, 9..0; `need`: how many stay of those that
+  // share its bits
+  uint32_t bits = 0u, need = (uint32_t)stay;
+  if (stay > 0)
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      const uint32_t width = pass == 2 ? 10 : 11, bins = 1u << width;
+      for (int i = t; i < kBins; i += kSelectThreads) hist[i] = 0u;
+      __syncthreads();
+      for (int j = lo + t; j < hi; j += kSelectThreads) {
+        const uint32_t x = order(j);
+        if (pass == 0 || (x ^ bits) >> (shift + width) == 0u) atomicAdd(&hist[(x >> shift) & (bins - 1)], 1u);
+      }
+      __syncthreads();
+      // counts from the highest bin down: two bins a thread
+      const uint32_t b1 = bins - 1 - 2 * t, h1 = 2 * t < (int)bins ? hist[b1] : 0u,
+                     h0 = 2 * t < (int)bins ? hist[b1 - 1] : 0u;
+      const uint32_t incl = (uint32_t)wave_scan((int)(h1 + h0));
+      if (l == 63) wave_sum_of[w] = incl;
+      __syncthreads();
+      uint32_t above = incl - h1 - h0;
+      for (int i = 0; i < w; ++i) above += wave_sum_of[i];
+      if (above < need && need <= above + h1 + h0) {
+        const bool second = need > above + h1;
+        found[0] = second ? b1 - 1 : b1;
+        found[1] = need - above - (second ? h1 : 0u);
+      }
+      __syncthreads();
+      bits |= found[0] << shift;
+      need = found[1];
+      __syncthreads();
+    }
+  // each wave's keys in order: those above, and the first `need` equal ones
+  const int per = ((hi - lo + kSelectWaves - 1) / kSelectWaves + 63) & ~63;
+  const int from = min(hi, lo + w * per), to = min(hi, from + per);
+  uint32_t more = 0u, ties = 0u;
+  if (stay > 0)
+    for (int j0 = from; j0 < to; j0 += 64) {
+      const uint32_t x = j0 + l < to ? order(j0 + l) : 0u;
+      more += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j0 + l < to && x > bits));
+      ties += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j0 + l < to && x == bits));
+    }
+  if (l == 0) {
+    wave_sum_of[w] = more;
+    wave_tie[w] = ties;
+  }
+  __syncthreads();
+  uint32_t at = 0u, tie = 0u;
+  for (int i = 0; i < w; ++i) {
+    at += wave_sum_of[i];
+    tie += wave_tie[i];
+  }
+  at += min(tie, need);
+  if (stay > 0)
+    for (int j0 = from; j0 < to; j0 += 64) {
+      const int j = j0 + l;
+      const uint32_t x = j < to ? order(j) : 0u;
+      const uint64_t below = (1ull << l) - 1ull;
+      const uint64_t eq = __builtin_amdgcn_ballot_w64(j < to && x == bits);
+      const bool mine = j < to && (x > bits || (x == bits && tie + __builtin_popcountll(eq & below) < need));
+      const uint64_t in = __builtin_amdgcn_ballot_w64(mine);
+      if (mine) kept[a.first + at + __builtin_popcountll(in & below)] = j;
+      at += __builtin_popcountll(in);
+      tie += __builtin_popcountll(eq);
+    }
+  for (int j = t; j < a.first; j += kSelectThreads) kept[j] = j;
+  for (int j = t; j < a.recent; j += kSelectThreads) kept[a.budget - a.recent + j] = hi + j;
+}
+
+constexpr int kGatherRows = 64;  // of a workgroup
+
+__global__ void __launch_bounds__(256) paged_gather_kernel(PagedEvictArgs a) {
+  const PagedCache& c = a.c;
+  const int hk = blockIdx.y, seq = blockIdx.z;
+  const int n = min(paged_len(c, seq), a.budget);
+  if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) a.new_len[seq] = n;
+  const int32_t* const kept = a.kept + ((size_t)seq * c.hkv + hk) * a.budget;
+  const int lanes = a.row_bytes / 16, rows = 256 / lanes;
+  const int e = (threadIdx.x % lanes) * 16;
+  const int j0 = blockIdx.x * kGatherRows, j1 = min(n, j0 + kGatherRows);
+  for (int j = j0 + threadIdx.x / lanes; j < j1; j += rows) {
+    const int from = kept[j];
+    if (from < 0) continue;
+    const int run = paged_run(c, seq, hk, from >> 4);
+    const int p = paged_div(c, j >> 4);
+    const int id = a.new_table[(size_t)seq * a.new_pages + p];
+    if (run < 0 || (uint32_t)id >= (uint32_t)c.num_pages) continue;
+    const size_t src = (size_t)run * 16 + (from & 15);
+    const size_t dst = ((size_t)(id * c.hkv + hk) * c.runs + ((j >> 4) - p * c.runs)) * 16 + (j & 15);
+    const u32x4 x = *reinterpret_cast<const u32x4*>(a.k + src * a.row_bytes + e);
+    const u32x4 y = *reinterpret_cast<const u32x4*>(a.v + src * a.row_bytes + e);
+    const float z = a.scores[src];
+    *reinterpret_cast<u32x4*>(a.k + dst * a.row_bytes + e) = x;
+    *reinterpret_cast<u32x4*>(a.v + dst * a.row_bytes + e) = y;
+    if (e == 0) a.scores[dst] = z;
+  }
+}
+
+}  // namespace pdy

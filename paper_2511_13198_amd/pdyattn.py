@@ -29,6 +29,8 @@ SYMBOLS = ("attn_fwd_workspace_size", "attn_bwd_workspace_size", "attn_fwd", "at
            "attn_cross_fwd_workspace_size", "attn_cross_fwd", "attn_prefix_fwd_workspace_size",
            "attn_prefix_fwd", "attn_cross_bwd_workspace_size", "attn_cross_bwd",
            "attn_prefix_bwd_workspace_size", "attn_prefix_bwd", "attn_rotary_turns", "attn_rotary",
+           "attn_paged_write", "attn_paged_fwd_workspace_size", "attn_paged_fwd",
+           "attn_paged_evict_workspace_size", "attn_paged_evict",
            "attn_validate_cu_seqlens", "attn_bwd_noalloc", "pdy_launch_shapes",
            "pdy_chunk_launch_shapes", "pdy_cross_launch_shapes", "pdy_status_string", "pdy_last_error",
            "pdy_kernel_count", "pdy_kernel_name", "pdy_profile_start", "pdy_profile_stop")
@@ -100,6 +102,16 @@ def lib() -> ctypes.CDLL:
     L.attn_rotary_turns.restype = i32
     L.attn_rotary.argtypes = [vp] * 3 + [i32] * 6 + [vp] * 2 + [i32] * 4 + [vp] * 3
     L.attn_rotary.restype = i32
+    L.attn_paged_write.argtypes = [vp] * 7 + [i32] * 8 + [vp] * 4
+    L.attn_paged_write.restype = i32
+    L.attn_paged_fwd_workspace_size.argtypes = [i32] * 8
+    L.attn_paged_fwd_workspace_size.restype = sz
+    L.attn_paged_fwd.argtypes = [vp] * 8 + [i32] * 12 + [f32, vp, vp, vp, vp, sz, vp]
+    L.attn_paged_fwd.restype = i32
+    L.attn_paged_evict_workspace_size.argtypes = [i32] * 4
+    L.attn_paged_evict_workspace_size.restype = sz
+    L.attn_paged_evict.argtypes = [vp] * 6 + [i32] * 12 + [vp, vp, vp, sz, vp]
+    L.attn_paged_evict.restype = i32
     L.attn_validate_cu_seqlens.argtypes = [vp, i32, i32, ctypes.POINTER(i32), vp]
     L.attn_validate_cu_seqlens.restype = i32
     L.attn_bwd_noalloc.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
@@ -681,6 +693,169 @@ def attn_prefix_bwd(q, k, v, k_prefix, v_prefix, o, lse, dout, cu_seqlens_q, cu_
     return _cross_bwd(q, k, v, k_prefix, v_prefix, o, lse, dout, cu_seqlens_q, cu_seqlens_k,
                       max_seqlen_q, max_seqlen_k, causal, scale, seqlens_k,
                       (dq, dk, dv, dk_prefix, dv_prefix), grad_dtype, workspace)
+
+
+# ---------------------------------------------------------------------------
+# A paged key/value cache
+# ---------------------------------------------------------------------------
+def paged_fwd_workspace_size(total_q, num_seqs, max_seqlen_q, max_seqlen_k, hq, hkv, d,
+                             with_scores: bool = False) -> int:
+    return int(lib().attn_paged_fwd_workspace_size(total_q, num_seqs, max_seqlen_q, max_seqlen_k,
+                                                   hq, hkv, d, 1 if with_scores else 0))
+
+
+def paged_evict_workspace_size(num_seqs, max_seqlen_k, hkv, budget) -> int:
+    return int(lib().attn_paged_evict_workspace_size(num_seqs, max_seqlen_k, hkv, budget))
+
+
+def _paged_pool(k_pages, v_pages, page_table, seqlens_k, scores, scales=None):
+    """Checked pool and tables: (device, shape of the pages, 1 for e4m3, pointers of the
+    scores and of scales, (k_scale, v_scale), where the call takes them)."""
+    import torch
+    dev, dtype, shape = k_pages.device, k_pages.dtype, k_pages.shape
+    index, f32 = dev.index, torch.float32
+    if dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+        raise TypeError(f"k_pages must be torch.bfloat16 or torch.float8_e4m3fn, got {dtype}")
+    if not (_fits(k_pages, dtype, 4, index) and _fits(v_pages, dtype, 4, index) and
+            _fits(page_table, torch.int32, 2, index) and _fits(seqlens_k, torch.int32, 1, index)):
+        _refuse(dev, (k_pages, "k_pages", dtype, 4), (v_pages, "v_pages", dtype, 4),
+                (page_table, "page_table", torch.int32, 2),
+                (seqlens_k, "seqlens_k", torch.int32, 1))
+    if v_pages.shape != shape:
+        raise ValueError("v_pages must have k_pages' shape [pages, Hkv, page_size, d]")
+    n = seqlens_k.numel()
+    if n < 1 or page_table.shape[0] != n:
+        raise ValueError("page_table and seqlens_k must have num_seqs >= 1 rows each")
+    e4m3 = 1 if dtype is torch.float8_e4m3fn else 0
+    ks = vs = sc = 0
+    k_scale, v_scale = scales or (None, None)
+    if e4m3 and scales:
+        if k_scale is None or v_scale is None:
+            raise ValueError("an e4m3 cache needs k_scale and v_scale")
+        if not (_fits(k_scale, f32, 1, index) and _fits(v_scale, f32, 1, index)):
+            _refuse(dev, (k_scale, "k_scale", f32, 1), (v_scale, "v_scale", f32, 1))
+        if k_scale.numel() != shape[1] or v_scale.numel() != shape[1]:
+            raise ValueError("k_scale and v_scale must have one value a kv head")
+        ks, vs = k_scale.data_ptr(), v_scale.data_ptr()
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("k_scale and v_scale are of an e4m3 cache (a bf16 one has none)")
+    if scores is not None:
+        if not _fits(scores, f32, 3, index):
+            _refuse(dev, (scores, "scores", f32, 3))
+        if scores.shape != shape[:3]:
+            raise ValueError("scores must be [pages, Hkv, page_size]")
+        sc = scores.data_ptr()
+    return dev, shape, e4m3, sc, ks, vs
+
+
+def attn_paged_write(k, v, k_pages, v_pages, page_table, cu_seqlens, seqlens_k, k_scale=None,
+                     v_scale=None, scores=None):
+    """New keys and values k, v [T, Hkv, d] bf16 into k_pages, v_pages [pages, Hkv,
+    page_size, d], bf16 or torch.float8_e4m3fn (divided by k_scale, v_scale, fp32 [Hkv]):
+    the tokens cu_seqlens[i] .. cu_seqlens[i + 1] - 1 become the last of the seqlens_k[i]
+    keys (with them) of sequence i, whose pages page_table[i] names (int32 [N, max
+    pages]).  scores [pages, Hkv, page_size]: 0 for the new keys."""
+    import torch
+    dev, shape, e4m3, sc, ks, vs = _paged_pool(k_pages, v_pages, page_table, seqlens_k, scores,
+                                               (k_scale, v_scale))
+    index, (pages, hkv, page, d) = dev.index, shape
+    if not (_fits(k, torch.bfloat16, 3, index) and _fits(v, torch.bfloat16, 3, index) and
+            _fits(cu_seqlens, torch.int32, 1, index)):
+        _refuse(dev, (k, "k", torch.bfloat16, 3), (v, "v", torch.bfloat16, 3),
+                (cu_seqlens, "cu_seqlens", torch.int32, 1))
+    T, n = k.shape[0], seqlens_k.numel()
+    if k.shape != (T, hkv, d) or v.shape != k.shape:
+        raise ValueError("k and v must be [T, Hkv, d] with the pages' Hkv and d")
+    if cu_seqlens.numel() != n + 1:
+        raise ValueError("cu_seqlens must have num_seqs + 1 offsets")
+    _launch("attn_paged_write", dev, k.data_ptr(), v.data_ptr(), cu_seqlens.data_ptr(),
+            page_table.data_ptr(), seqlens_k.data_ptr(), ks, vs, n, T, pages, page,
+            page_table.shape[1], hkv, d, e4m3, k_pages.data_ptr(), v_pages.data_ptr(), sc)
+
+
+def attn_paged_fwd(q, k_pages, v_pages, page_table, cu_seqlens_q, seqlens_k,
+                   max_seqlen_q: Optional[int] = None, max_seqlen_k: Optional[int] = None,
+                   causal: bool = True, scale: Optional[float] = None, k_scale=None, v_scale=None,
+                   scores=None, out=None, lse=None, workspace=None):
+    """O [Tq, Hq, d] bf16 and LSE [Hq, Tq] fp32 of every sequence's queries over its
+    first seqlens_k[i] keys in the pages page_table[i] of k_pages, v_pages [pages, Hkv,
+    page_size, d] (bf16, or torch.float8_e4m3fn with k_scale, v_scale fp32 [Hkv]); q [Tq,
+    Hq, d] is cut by cu_seqlens_q.  max_seqlen_q, max_seqlen_k: upper bounds of the
+    lengths (None: max_seqlen_q read from the offsets, waiting for them, max_seqlen_k the
+    table's room).  causal aligns the ends: the last query sees every key.  scores fp32
+    [pages, Hkv, page_size]: each key's attention weight, summed over the sequence's rows
+    and its group's heads, is added.  Rows without a key get O = 0, LSE = -inf; rows of no
+    sequence are left."""
+    import torch
+    dev, shape, e4m3, sc, ks, vs = _paged_pool(k_pages, v_pages, page_table, seqlens_k, scores,
+                                               (k_scale, v_scale))
+    index, (pages, hkv, page, d) = dev.index, shape
+    if not (_fits(q, torch.bfloat16, 3, index) and _fits(cu_seqlens_q, torch.int32, 1, index)):
+        _refuse(dev, (q, "q", torch.bfloat16, 3), (cu_seqlens_q, "cu_seqlens_q", torch.int32, 1))
+    T, hq, dq = q.shape
+    n, width = page_table.shape
+    if dq != d:
+        raise ValueError("q must have the pages' head dimension")
+    if cu_seqlens_q.numel() != n + 1:
+        raise ValueError("cu_seqlens_q must have num_seqs + 1 offsets")
+    if max_seqlen_q is None:
+        max_seqlen_q = max(_longest(cu_seqlens_q, "cu_seqlens_q", T), min(1, T))
+    if max_seqlen_k is None:
+        max_seqlen_k = width * page
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty((hq, T), dtype=torch.float32, device=dev)
+    if workspace is None:
+        workspace = _ws(paged_fwd_workspace_size(T, n, max_seqlen_q, max_seqlen_k, hq, hkv, d,
+                                                 scores is not None), dev)
+    _check_outputs(dev, out, "out", lse, workspace, T, hq, d)
+    _launch("attn_paged_fwd", dev, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+            page_table.data_ptr(), cu_seqlens_q.data_ptr(), seqlens_k.data_ptr(), ks, vs, n, T,
+            pages, page, width, max_seqlen_q, max_seqlen_k, hq, hkv, d, e4m3, 1 if causal else 0,
+            1.0 / math.sqrt(d) if scale is None else scale, out.data_ptr(), lse.data_ptr(), sc,
+            workspace.data_ptr(), workspace.nbytes)
+    return out, lse
+
+
+def attn_paged_evict(k_pages, v_pages, scores, page_table, seqlens_k, new_table, budget: int,
+                     recent: int = 0, first: int = 0, max_seqlen_k: Optional[int] = None,
+                     kept=None, new_lens=None, workspace=None):
+    """Shortens every sequence to at most `budget` keys: each kv head keeps its first
+    `first` and last `recent` ones and, of those between, the ones of the highest scores
+    (equal ones: the earlier).  Keys, values and scores that stay are copied in their order
+    to the pages of new_table (int32 [N, max pages]), none of which the sequences use.
+    Returns kept int32 [N, Hkv, budget], the old number of each key (-1 behind the last),
+    and the new lengths int32 [N] (new_lens may be seqlens_k)."""
+    import torch
+    if scores is None:
+        raise ValueError("attn_paged_evict needs scores")
+    dev, shape, e4m3, sc, _, _ = _paged_pool(k_pages, v_pages, page_table, seqlens_k, scores)
+    i32, index, (pages, hkv, page, d) = torch.int32, dev.index, shape
+    n, width = page_table.shape
+    if not _fits(new_table, i32, 2, index):
+        _refuse(dev, (new_table, "new_table", i32, 2))
+    if new_table.shape[0] != n:
+        raise ValueError("new_table must have num_seqs rows")
+    if max_seqlen_k is None:
+        max_seqlen_k = width * page
+    if kept is None:
+        kept = torch.empty((n, hkv, budget), dtype=i32, device=dev)
+    if new_lens is None:
+        new_lens = torch.empty((n,), dtype=i32, device=dev)
+    if workspace is None:
+        workspace = _ws(paged_evict_workspace_size(n, max_seqlen_k, hkv, budget), dev)
+    if not (_fits(kept, i32, 3, index) and _fits(new_lens, i32, 1, index) and
+            workspace.is_contiguous() and workspace.get_device() == index):
+        _refuse(dev, (kept, "kept", i32, 3), (new_lens, "new_lens", i32, 1),
+                (workspace, "workspace", workspace.dtype, workspace.dim()))
+    if kept.shape != (n, hkv, budget) or new_lens.shape != (n,):
+        raise ValueError("kept must be [N, Hkv, budget], new_lens [N]")
+    _launch("attn_paged_evict", dev, k_pages.data_ptr(), v_pages.data_ptr(), sc,
+            page_table.data_ptr(), seqlens_k.data_ptr(), new_table.data_ptr(), n, pages, page,
+            width, new_table.shape[1], max_seqlen_k, hkv, d, e4m3, budget, recent, first,
+            kept.data_ptr(), new_lens.data_ptr(), workspace.data_ptr(), workspace.nbytes)
+    return kept, new_lens
 
 
 # ---------------------------------------------------------------------------
