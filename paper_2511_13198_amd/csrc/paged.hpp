@@ -210,7 +210,11 @@ struct PagedFwdCfg {
   using T = PagedTile<D, F8>;
   static constexpr int NT = NW * 64;
   static constexpr int ROWS = 16 * RB;
-  static constexpr int WAVE = 2 * T::BYTES;  // K and V
+  static constexpr int SLOTS = 16384 / (2 * T::BYTES);  // tiles of K and V: 16 KB a wave
+  static constexpr int WAVE = SLOTS * 2 * T::BYTES;
+  // waves a SIMD at least: 2 leave 256 registers, without a need for accumulation registers
+  // (and copies to and from them); 64 rows of 128 need more
+  static constexpr int WAVES = RB * D >= 512 ? 1 : 2;
   static constexpr int PITCH = D + 4;        // floats of a combined row
   static constexpr int STAT = NW * ROWS * PITCH * 4;
   static constexpr int END = STAT + NW * ROWS * 8;
@@ -246,7 +250,8 @@ __device__ __forceinline__ void paged_copy(uint64_t base, int bytes, uint32_t vo
 }
 
 template <int D, bool F8, int RB, int NW>
-__global__ void __launch_bounds__(NW * 64) paged_fwd_kernel(PagedFwdArgs a) {
+__global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
+    paged_fwd_kernel(PagedFwdArgs a) {
   using C = PagedFwdCfg<D, F8, RB, NW>;
   using T = typename C::T;
   constexpr int KS = D / 32, DB = D / 16;
@@ -303,10 +308,8 @@ __global__ void __launch_bounds__(NW * 64) paged_fwd_kernel(PagedFwdArgs a) {
     for (int db = 0; db < DB; ++db) oacc[b][db] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  uint8_t* const kt = paged_smem + w * C::WAVE;
-  uint8_t* const vt = kt + T::BYTES;
-  // lanes' places in a copy, and in the reads
-  uint32_t kv_off[2][T::COPIES][2];  // [k, v][copy][run]
+  uint8_t* const mine = paged_smem + w * C::WAVE;  // SLOTS times K, V
+  uint32_t kv_off[2][T::COPIES][2];  // this lane's bytes of a run: [k, v][copy][run]
 #pragma unroll
   for (int i = 0; i < T::COPIES; ++i) {
     const int at = i * 1024 + l * 16, r = at / T::ROW, slot = (at % T::ROW) / 16;
@@ -316,32 +319,54 @@ __global__ void __launch_bounds__(NW * 64) paged_fwd_kernel(PagedFwdArgs a) {
       kv_off[1][i][s] = r * T::ROW + (slot ^ T::swz_v(r + 16 * s)) * 16;
     }
   }
-  const uint32_t ka = lds_addr(kt) + i16 * T::ROW + (grp ^ T::swz_k(i16)) * 16;
+  const uint32_t ka = lds_addr(mine) + i16 * T::ROW + (grp ^ T::swz_k(i16)) * 16;
   uint32_t va;
   if constexpr (F8) {
     const int e = i16 >> 1, r = e < 4 ? 4 * grp + e : 16 + 4 * grp + e - 4;
-    va = lds_addr(vt) + r * T::ROW + T::swz_v(r) * 16 + (i16 & 1) * 8;
+    va = lds_addr(mine) + T::BYTES + r * T::ROW + T::swz_v(r) * 16 + (i16 & 1) * 8;
   } else {
     const int r = 4 * grp + (i16 >> 2);
-    va = lds_addr(vt) + r * T::ROW + T::swz_v(r) * 16 + ((i16 & 3) >> 1) * 16 + (i16 & 1) * 8;
+    va = lds_addr(mine) + T::BYTES + r * T::ROW + T::swz_v(r) * 16 + ((i16 & 3) >> 1) * 16 + (i16 & 1) * 8;
   }
 
-  const int steps = (some_end + 31) >> 5;
-  for (int st = w; st < steps; st += NW) {
-    const int k0 = st * 32;
+  // This wave's steps: step j is the 32 keys from (w + NW j) 32 on.  Lane 2 i + s knows
+  // where run s of step i (mod 32) is.
+  const int steps = max(0, ((some_end + 31) >> 5) - w + NW - 1) / NW;
+  int runs_of = 0;
+  auto find_runs = [&](int j) __attribute__((always_inline)) {
+    const int x = 2 * (w + NW * (j + (l >> 1))) + (l & 1);
+    runs_of = x * 16 < nk ? max(0, paged_run(c, seq, hk, x)) : 0;
+    wait_dma();
+  };
+  // copies of step j's K (kv = 0) or V; past the last step of an empty range, so that
+  // every step has as many copies
+  auto issue = [&](int kv, int j) __attribute__((always_inline)) {
+    uint8_t* const to = mine + ((j % C::SLOTS) * 2 + kv) * T::BYTES;
+    const uint64_t base = (uint64_t)(kv ? a.v : a.k);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const int x = st * 2 + s, valid = min(16, nk - x * 16);
-      const int run = valid > 0 ? max(0, __builtin_amdgcn_readfirstlane(paged_run(c, seq, hk, x))) : 0;
-      const size_t off = (size_t)run * T::RUN;
-      const int bytes = max(0, valid) * T::ROW;
+      const int run = __builtin_amdgcn_readlane(runs_of, ((j & 31) * 2) | s);
+      const int valid = j < steps ? min(16, nk - (w + NW * j) * 32 - s * 16) : 0;
+      const int bytes = __builtin_amdgcn_readfirstlane(max(0, valid) * T::ROW);
 #pragma unroll
-      for (int i = 0; i < T::COPIES; ++i) {
-        paged_copy((uint64_t)a.k + off, bytes, kv_off[0][i][s], kt + s * T::RUN + i * 1024);
-        paged_copy((uint64_t)a.v + off, bytes, kv_off[1][i][s], vt + s * T::RUN + i * 1024);
-      }
+      for (int i = 0; i < T::COPIES; ++i)
+        paged_copy(base + (uint64_t)run * T::RUN, bytes, kv_off[kv][i][s], to + s * T::RUN + i * 1024);
     }
-    wait_dma();
+  };
+  // copies in flight behind a step's K when its products begin, and behind its V
+  constexpr int FLIGHT = (2 * C::SLOTS - 1) * 2 * T::COPIES;
+  if (steps > 0) {
+    find_runs(0);
+#pragma unroll
+    for (int j = 0; j < C::SLOTS; ++j) {
+      issue(0, j);
+      issue(1, j);
+    }
+  }
+  for (int j = 0; j < steps; ++j) {
+    const int k0 = (w + NW * j) * 32;
+    const uint32_t slot = (j % C::SLOTS) * 2 * T::BYTES;
+    wait_dma_n<FLIGHT>();
 
     // S^T = K Q^T, a run of 16 keys at a time
     f32x4 s[RB][2];
@@ -351,7 +376,7 @@ __global__ void __launch_bounds__(NW * 64) paged_fwd_kernel(PagedFwdArgs a) {
       u32x4 kr[N];
       static_for<N>([&](auto I) {
         constexpr int i = decltype(I)::value;
-        paged_read16<run * T::RUN>(ka ^ (i * 64), kr[i]);
+        paged_read16<run * T::RUN>((ka ^ (i * 64)) + slot, kr[i]);
       });
       static_for<N>([&](auto I) {
         constexpr int i = decltype(I)::value;
@@ -369,6 +394,11 @@ __global__ void __launch_bounds__(NW * 64) paged_fwd_kernel(PagedFwdArgs a) {
         });
       }
     });
+
+    const int next = j + C::SLOTS;
+    if ((next & 31) == 0) find_runs(next);  // (the last use of the ones before was V's)
+    wave_lds_fence();
+    issue(0, next);
 
     bf16x8 pf[RB];
 #pragma unroll
@@ -406,33 +436,37 @@ __global__ void __launch_bounds__(NW * 64) paged_fwd_kernel(PagedFwdArgs a) {
     }
 
     // O^T += V^T P^T, 16 columns at a time
+    wait_dma_n<FLIGHT>();
     static_for<DB>([&](auto I) {
       constexpr int db = decltype(I)::value;
       bf16x8 x;
       if constexpr (F8) {
         u32x2 y;
-        paged_read_tr8(va ^ (db * 16), y);
+        paged_read_tr8((va ^ (db * 16)) + slot, y);
         x = widen8(y);
       } else {
         TrRegs y;
-        paged_read_tr16<T::RUN>(va ^ (db * 32), y);
+        paged_read_tr16<T::RUN>((va ^ (db * 32)) + slot, y);
         x = y.operand();
       }
 #pragma unroll
       for (int b = 0; b < RB; ++b) oacc[b][db] = mfma16(x, pf[b], oacc[b][db]);
     });
+    wave_lds_fence();
+    issue(1, next);
   }
 
   // combine the waves: O, offset and sum of every row through LDS
+  wait_dma();
   __syncthreads();
   float* const slots = reinterpret_cast<float*>(paged_smem);
   f32x2* const stat = reinterpret_cast<f32x2*>(paged_smem + C::STAT);
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     const float tot = quad_sum(lsum[b]);
-    float* const mine = slots + ((size_t)w * C::ROWS + b * 16 + i16) * C::PITCH + grp * 4;
+    float* const to = slots + ((size_t)w * C::ROWS + b * 16 + i16) * C::PITCH + grp * 4;
 #pragma unroll
-    for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(mine + db * 16) = oacc[b][db];
+    for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(to + db * 16) = oacc[b][db];
     if (grp == 0) stat[w * C::ROWS + b * 16 + i16] = f32x2{m[b], tot};
   }
   __syncthreads();
