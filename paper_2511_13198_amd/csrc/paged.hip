@@ -105,6 +105,40 @@ pdy_status check_rows(int32_t tq, int32_t n, int32_t max_q, int32_t hq, int32_t 
   return PDY_OK;
 }
 
+constexpr int64_t kCUs = 256;
+constexpr int kMaxParts = 256;
+constexpr int64_t kPartBytes = (int64_t)256 << 20;  // partial results at most
+
+// A launch's row tiles (16 << shape rows) and parts.
+struct PagedPlan {
+  int shape;
+  int max_tiles;
+  pdy::PagedCut cut;
+  int64_t wgs;  // a kv head
+  size_t part_o, part_lse, part_n;  // bytes of the workspace
+  size_t bytes() const { return std::max<size_t>(256, part_o + part_lse + part_n); }
+};
+
+PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, int64_t d) {
+  PagedPlan p;
+  const int64_t g = r.hq / hkv, rows = std::max<int64_t>(1, r.max_q * g);
+  p.shape = rows <= 16 ? 0 : rows <= 32 ? 1 : 2;
+  const int64_t tile = 16 << p.shape;
+  p.max_tiles = (int)ceil_div(rows, tile);
+  const int64_t items = std::min(r.tq * g / tile + n, n * p.max_tiles);
+  const int64_t slice = std::max<int64_t>(1, r.tq) * r.hq * (d + 1) * 4;
+  p.cut.least = 4;
+  p.cut.entries = (int)ceil_div(4 * kCUs, hkv);
+  p.cut.max_parts = (int)std::max<int64_t>(
+      1, std::min<int64_t>({kMaxParts, ceil_div(max_k, 32) / p.cut.least, kPartBytes / slice}));
+  const bool cut = p.cut.max_parts > 1;
+  p.wgs = cut ? items + p.cut.entries + 1 : n * p.max_tiles;
+  p.part_o = cut ? align256((size_t)p.cut.max_parts * r.tq * r.hq * d * 4) : 0;
+  p.part_lse = cut ? align256((size_t)p.cut.max_parts * r.tq * r.hq * 4) : 0;
+  p.part_n = cut ? align256((size_t)r.tq * r.hq * 4) : 0;
+  return p;
+}
+
 template <int D, bool F8, int RB, int NW>
 hipError_t launch_fwd(const pdy::PagedFwdArgs* a, dim3 grid, hipStream_t st) {
   using C = pdy::PagedFwdCfg<D, F8, RB, NW>;
@@ -194,7 +228,7 @@ size_t attn_paged_fwd_workspace_size(int32_t total_q, int32_t num_seqs, int32_t 
       (with_scores & ~1) ||
       check_rows(total_q, num_seqs, max_seqlen_q, num_heads_q, num_heads_kv, head_dim, &r) != PDY_OK)
     return 0;
-  return 256;
+  return plan_fwd(r, num_seqs, max_seqlen_k, num_heads_kv, head_dim).bytes();
 }
 
 pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_pages,
@@ -221,11 +255,11 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
       (st = check_ptr(workspace, "workspace")))
     return st;
   if (scores && (st = check_ptr(scores, "scores"))) return st;
-  if (workspace_bytes < 256)
+  const PagedPlan p = plan_fwd(r, s.n, s.max_k, s.hkv, s.d);
+  if (workspace_bytes < p.bytes())
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, attn_paged_fwd needs %zu",
-                workspace_bytes, (size_t)256);
-  const int64_t g = r.hq / s.hkv, rows = r.max_q * g;
-  const int shape = rows <= 16 ? 0 : rows <= 32 ? 1 : 2;
+                workspace_bytes, p.bytes());
+  const int64_t g = r.hq / s.hkv;
   pdy::PagedFwdArgs a;
   a.c = cache_of(s, page_table, seqlens_k);
   a.q = static_cast<const uint16_t*>(q);
@@ -239,19 +273,34 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
   a.g = (int)g;
   a.g_inv = (uint32_t)((1ull << 32) / g);
   a.causal = causal;
-  a.max_tiles = (int)ceil_div(rows, 16 << shape);
+  a.max_tiles = p.max_tiles;
+  a.cut = p.cut;
   a.scale_log2 = scale * pdy::kLog2e;
   a.o = static_cast<uint16_t*>(o);
   a.lse = lse;
-  const int64_t wgs = s.n * a.max_tiles * s.hkv;
+  uint8_t* const ws = static_cast<uint8_t*>(workspace);
+  a.part_o = reinterpret_cast<float*>(ws);
+  a.part_lse = reinterpret_cast<float*>(ws + p.part_o);
+  a.part_n = reinterpret_cast<int32_t*>(ws + p.part_o + p.part_lse);
+  const int64_t wgs = p.wgs * s.hkv;
   if (!fits_grid(wgs, 256)) return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
   hipError_t e = init_paged_kernels();
   if (e != hipSuccess) return hip_fail(e, "kernel attribute setup");
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
   e = launch_timed(K_PAGED_FWD, hs, [&] {
-    (void)kFwd[s.d == 128][s.e4m3][shape](&a, dim3((unsigned)wgs), hs);
+    (void)kFwd[s.d == 128][s.e4m3][p.shape](&a, dim3((unsigned)wgs), hs);
   });
   if (e != hipSuccess) return hip_fail(e, "paged_fwd_kernel launch");
+  if (p.cut.max_parts > 1) {
+    pdy::PagedMergeArgs m{a.part_o, a.part_lse, a.part_n, p.cut.max_parts, a.cu_q, a.c.n, a.tq,
+                          a.hq, a.o, a.lse};
+    const dim3 grid((unsigned)ceil_div(r.tq * r.hq, 4));
+    e = launch_timed(K_PAGED_MERGE, hs, [&] {
+      if (s.d == 64) hipLaunchKernelGGL(pdy::paged_merge_kernel<64>, grid, dim3(256), 0, hs, m);
+      else hipLaunchKernelGGL(pdy::paged_merge_kernel<128>, grid, dim3(256), 0, hs, m);
+    });
+    if (e != hipSuccess) return hip_fail(e, "paged_merge_kernel launch");
+  }
   if (scores) {
     pdy::PagedWeighArgs b{a.c, a.q, a.k, a.k_scale, a.cu_q, a.lse, a.tq, a.hq, a.g, a.g_inv,
                           a.causal, a.scale_log2, scores};

@@ -222,6 +222,99 @@ struct PagedFwdCfg {
   static_assert(LDS_BYTES <= 160 * 1024, "LDS");
 };
 
+// How a launch is cut.  An item is a row tile of a sequence and a kv head; its steps of 32
+// keys are cut into parts of at most C = max(least, steps of all items / entries), a
+// workgroup each: about `entries` parts a kv head, alike whatever the lengths, and up to
+// one an item more.  C follows from the lengths on the GPU, so that nothing waits for the
+// host: every workgroup computes it and its own place, with a lane per sequence, or a thread
+// where there are more.
+struct PagedCut {
+  int max_parts;  // of an item; 1: not cut
+  int least;      // fewest steps of a part
+  int entries;    // parts of a kv head
+};
+struct PagedPlace {
+  int seq, tile, part, nparts;
+};
+
+// Entry `entry` of a kv head's list; false past its end.  of(i, tiles, steps): row tiles of
+// sequence i, and steps of each.  (wave-uniform)
+template <int NT, class F>
+__device__ __forceinline__ bool paged_place(const PagedCut& c, int n, int entry, F&& of,
+                                            PagedPlace& out) {
+  __shared__ float sum_of[NT / 64];
+  __shared__ int entries_of[NT / 64], found[4];
+  const bool wide = n > 64;  // uniform
+  const int id = wide ? threadIdx.x : __lane_id(), stride = wide ? NT : 64;
+  const int w = threadIdx.x >> 6, l = __lane_id();
+  int tiles, steps;
+  float sum = 0.f;
+  for (int i = id; i < n; i += stride) {
+    of(i, tiles, steps);
+    sum += (float)tiles * (float)steps;
+  }
+  sum = wave_sum(sum);
+  if (wide) {
+    if (l == 0) sum_of[w] = sum;
+    __syncthreads();
+    sum = 0.f;
+    for (int i = 0; i < NT / 64; ++i) sum += sum_of[i];
+  }
+  const int cap = max(c.least, (int)fminf(sum / (float)c.entries + 1.f, 1e9f));
+  const float inv = 1.f / (float)cap;
+  // ceil(steps / cap) as a float product (any whole number near it does)
+  auto parts = [&]() __attribute__((always_inline)) {
+    return max(1, min(c.max_parts, (int)ceilf((float)steps * inv)));
+  };
+  int mine = 0;
+  for (int i = id; i < n; i += stride) {
+    of(i, tiles, steps);
+    mine += tiles * parts();
+  }
+  int before = wave_scan(mine) - mine;
+  if (wide) {
+    if (l == 63) entries_of[w] = before + mine;
+    if (threadIdx.x == 0) found[0] = -1;
+    __syncthreads();
+    for (int i = 0; i < w; ++i) before += entries_of[i];
+  }
+  const bool hit = entry >= before && entry < before + mine;
+  int seq = 0, rel = entry - before, np = 1;
+  if (hit)
+    for (int i = id; i < n; i += stride) {
+      of(i, tiles, steps);
+      np = parts();
+      seq = i;
+      if (rel < tiles * np) break;
+      rel -= tiles * np;
+    }
+  if (wide) {
+    if (hit) {
+      found[0] = seq;
+      found[1] = rel;
+      found[2] = np;
+    }
+    __syncthreads();
+    seq = found[0];
+    rel = found[1];
+    np = found[2];
+    if (seq < 0) return false;
+  } else {
+    const uint64_t any = __builtin_amdgcn_ballot_w64(hit);
+    if (!any) return false;
+    const int src = __builtin_ctzll(any);
+    seq = __builtin_amdgcn_readlane(seq, src);
+    rel = __builtin_amdgcn_readlane(rel, src);
+    np = __builtin_amdgcn_readlane(np, src);
+  }
+  out.seq = __builtin_amdgcn_readfirstlane(seq);
+  out.nparts = __builtin_amdgcn_readfirstlane(np);
+  rel = __builtin_amdgcn_readfirstlane(rel);
+  out.tile = rel / out.nparts;
+  out.part = rel - out.tile * out.nparts;
+  return true;
+}
+
 struct PagedFwdArgs {
   PagedCache c;
   const uint16_t* q;
@@ -234,9 +327,16 @@ struct PagedFwdArgs {
   uint32_t g_inv;
   int causal;
   int max_tiles;  // row tiles of a sequence
+  PagedCut cut;
   float scale_log2;
   uint16_t* o;
   float* lse;
+  // partial results (max_parts > 1): O (fp32, normalised by the part's own sums) and LSE of
+  // part p at part_o [p][tq * hq][D], part_lse [p][tq * hq] (NaN: a NaN or +inf logit), and
+  // how many parts a row has at part_n [tq * hq]
+  float* part_o;
+  float* part_lse;
+  int32_t* part_n;
 };
 
 // One copy of 1 KB into LDS: lane l's 16 bytes at base + voff, zeros from `bytes` on.
@@ -258,7 +358,23 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
   extern __shared__ __attribute__((aligned(1024))) uint8_t paged_smem[];
   const PagedCache& c = a.c;
   const int hk = blockIdx.x % (unsigned)c.hkv, entry = blockIdx.x / (unsigned)c.hkv;
-  const int seq = entry / a.max_tiles, tile = entry - seq * a.max_tiles;
+  PagedPlace at;
+  if (a.cut.max_parts == 1) {
+    at.seq = entry / a.max_tiles;
+    at.tile = entry - at.seq * a.max_tiles;
+    at.part = 0;
+    at.nparts = 1;
+  } else if (!paged_place<C::NT>(a.cut, c.n, entry,
+                                 [&](int i, int& tiles, int& steps) __attribute__((always_inline)) {
+                                   const int lo = min(max(a.cu_q[i], 0), a.tq);
+                                   const int rows = (min(max(a.cu_q[i + 1], lo), a.tq) - lo) * a.g;
+                                   tiles = min((rows + C::ROWS - 1) / C::ROWS, a.max_tiles);
+                                   steps = (paged_len(c, i) + 31) >> 5;
+                                 },
+                                 at)) {
+    return;
+  }
+  const int seq = at.seq, tile = at.tile;
   const int q_lo = min(max(a.cu_q[seq], 0), a.tq);
   const int nq = min(max(a.cu_q[seq + 1], q_lo), a.tq) - q_lo;
   const int row_end = nq * a.g;  // packed rows, from the sequence's first on
@@ -329,12 +445,15 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     va = lds_addr(mine) + T::BYTES + r * T::ROW + T::swz_v(r) * 16 + ((i16 & 3) >> 1) * 16 + (i16 & 1) * 8;
   }
 
-  // This wave's steps: step j is the 32 keys from (w + NW j) 32 on.  Lane 2 i + s knows
-  // where run s of step i (mod 32) is.
-  const int steps = max(0, ((some_end + 31) >> 5) - w + NW - 1) / NW;
+  // The part's steps, and this wave's: step j is the 32 keys from (first + NW j) 32 on.
+  // Lane 2 i + s knows where run s of step i (mod 32) is.
+  const int all_steps = (some_end + 31) >> 5;
+  const int first = (int)((int64_t)at.part * all_steps / at.nparts) + w;
+  const int last = (int)((int64_t)(at.part + 1) * all_steps / at.nparts);
+  const int steps = max(0, last - first + NW - 1) / NW;
   int runs_of = 0;
   auto find_runs = [&](int j) __attribute__((always_inline)) {
-    const int x = 2 * (w + NW * (j + (l >> 1))) + (l & 1);
+    const int x = 2 * (first + NW * (j + (l >> 1))) + (l & 1);
     runs_of = x * 16 < nk ? max(0, paged_run(c, seq, hk, x)) : 0;
     wait_dma();
   };
@@ -346,7 +465,7 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int run = __builtin_amdgcn_readlane(runs_of, ((j & 31) * 2) | s);
-      const int valid = j < steps ? min(16, nk - (w + NW * j) * 32 - s * 16) : 0;
+      const int valid = j < steps ? min(16, nk - (first + NW * j) * 32 - s * 16) : 0;
       const int bytes = __builtin_amdgcn_readfirstlane(max(0, valid) * T::ROW);
 #pragma unroll
       for (int i = 0; i < T::COPIES; ++i)
@@ -364,7 +483,7 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     }
   }
   for (int j = 0; j < steps; ++j) {
-    const int k0 = (w + NW * j) * 32;
+    const int k0 = (first + NW * j) * 32;
     const uint32_t slot = (j % C::SLOTS) * 2 * T::BYTES;
     wait_dma_n<FLIGHT>();
 
@@ -491,14 +610,97 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     const float inv = tot > 0.f || tot != tot ? out_scale / tot : 0.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[k] *= inv;
-    const size_t pair = pair_of(row0 + r);
-    cross_put8(x, a.o + pair * D + e);
-    if (e == 0) {
+    const size_t pair = pair_of(row0 + r), pairs = (size_t)a.tq * a.hq;
+    // (a part hands a NaN sum on as NaN)
+    const float lse = tot > 0.f ? (mx + __builtin_log2f(tot)) * kLn2
+                      : at.nparts > 1 ? tot - INFINITY : -INFINITY;
+    if (e == 0 && at.part == 0 && a.cut.max_parts > 1) a.part_n[pair] = at.nparts;
+    if (at.nparts > 1) {
+      cross_put8(x, a.part_o + (at.part * pairs + pair) * D + e);
+      if (e == 0) a.part_lse[at.part * pairs + pair] = lse;
+    } else {
+      cross_put8(x, a.o + pair * D + e);
       const int t = token(row0 + r);
-      a.lse[(size_t)(hk * a.g + (row0 + r - t * a.g)) * a.tq + q_lo + t] =
-          tot > 0.f ? (mx + __builtin_log2f(tot)) * kLn2 : -INFINITY;
+      if (e == 0) a.lse[(size_t)(hk * a.g + (row0 + r - t * a.g)) * a.tq + q_lo + t] = lse;
     }
   }
+}
+
+// Combine the partial results of the rows that have more than one:
+//   LSE = log sum_p exp(LSE_p),  O = sum_p exp(LSE_p - LSE) O_p;
+// a part with LSE = -inf weighs nothing, one with NaN makes the row O = NaN, LSE = -inf.  A
+// wave per (token, head) pair: a lane per part for the weights (64 at a time), then 512 / D
+// parts at a time, 8 elements a lane.
+struct PagedMergeArgs {
+  const float* part_o;
+  const float* part_lse;
+  const int32_t* part_n;
+  int max_parts;
+  const int32_t* cu_q;  // rows end at cu_q[n]
+  int n;
+  int tq, hq;
+  uint16_t* o;
+  float* lse;
+};
+
+template <int D>
+__global__ void __launch_bounds__(256) paged_merge_kernel(PagedMergeArgs a) {
+  constexpr int LANES = D / 8, GROUPS = 64 / LANES;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l = __lane_id();
+  const uint32_t pair = blockIdx.x * 4 + w;  // token * hq + head
+  const uint32_t pairs = (uint32_t)a.tq * a.hq;
+  if (pair >= pairs) return;
+  const int tok = (int)(pair / (uint32_t)a.hq), h = (int)(pair - (uint32_t)tok * a.hq);
+  const int parts = min(max(a.part_n[pair], 0), a.max_parts);
+  // rows behind the last sequence stay, and those written by their one part
+  if (tok >= a.cu_q[a.n] || parts <= 1) return;
+  const int c = (l % LANES) * 8, grp = l / LANES;
+  float mx = -INFINITY, tot = 0.f;
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  // (more than 64 parts: the sums so far are rescaled by each further 64)
+  for (int p0 = 0; p0 < parts; p0 += 64) {
+    const float x = p0 + l < parts ? a.part_lse[(size_t)(p0 + l) * pairs + pair] : -INFINITY;
+    float top = x;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+    top = fmaxf(top, mx);
+    const float keep = mx == -INFINITY ? 0.f : fast_exp2((mx - top) * kLog2e);
+    // (NaN where x is NaN: fmaxf passes it over)
+    const float wt = x == -INFINITY ? 0.f : fast_exp2((x - top) * kLog2e);
+    mx = top;
+    float sum = wt;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+    tot = tot * keep + sum;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= keep;
+    const int m = min(64, parts - p0);
+#pragma unroll 4
+    for (int j0 = 0; j0 < m; j0 += GROUPS) {
+      // (every lane takes part in the exchange; past the last part the weight is 0)
+      const float wj = __shfl(wt, j0 + grp);
+      const int pj = p0 + min(j0 + grp, m - 1);
+      const float* src = a.part_o + ((size_t)pj * pairs + pair) * D + c;
+      const f32x4 x0 = *reinterpret_cast<const f32x4*>(src);
+      const f32x4 x1 = *reinterpret_cast<const f32x4*>(src + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[e] += wj * x0[e];
+        acc[4 + e] += wj * x1[e];
+      }
+    }
+  }
+#pragma unroll
+  for (int off = LANES; off < 64; off <<= 1)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor(acc[e], off);
+  const float inv = tot > 0.f ? 1.f / tot : tot != tot ? NAN : 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] *= inv;
+  if (grp == 0) cross_put8(acc, a.o + (size_t)pair * D + c);
+  if (l == 0)
+    a.lse[(size_t)h * a.tq + tok] = tot > 0.f ? mx + __builtin_log2f(tot) * kLn2 : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
