@@ -36,8 +36,8 @@ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // ---------------------------------------------------------------------------
 enum KernelId { K_PLAN = 0, K_FWD, K_DKDV, K_DQ, K_SPLIT_MERGE, K_SPLIT_SUM, K_CROSS_LIST,
                 K_CROSS_FWD, K_CROSS_MERGE, K_CROSS_DQ, K_CROSS_DKDV, K_CROSS_SUM, K_ROTARY,
-                K_PAGED_WRITE, K_PAGED_FWD, K_PAGED_MERGE, K_PAGED_WEIGH, K_PAGED_SELECT,
-                K_PAGED_GATHER, K_COUNT };
+                K_PAGED_WRITE, K_PAGED_FWD, K_PAGED_MERGE, K_PAGED_JOIN, K_PAGED_WEIGH,
+                K_PAGED_SELECT, K_PAGED_GATHER, K_COUNT };
 const char* const kKernelNames[K_COUNT] = {"plan_kernel",     "fwd_kernel",
                                            "bwd_dkdv_kernel", "bwd_dq_kernel",
                                            "split_merge_kernel", "split_sum_kernel",
@@ -46,7 +46,7 @@ const char* const kKernelNames[K_COUNT] = {"plan_kernel",     "fwd_kernel",
                                            "cross_dkdv_kernel", "cross_sum_kernel",
                                            "rotary_kernel",     "paged_write_kernel",
                                            "paged_fwd_kernel",  "paged_merge_kernel",
-                                           "paged_weigh_kernel",
+                                           "paged_join_kernel", "paged_weigh_kernel",
                                            "paged_select_kernel", "paged_gather_kernel"};
 struct ProfRec {
   int kid;

@@ -109,17 +109,21 @@ constexpr int64_t kCUs = 256;
 constexpr int kMaxParts = 256;
 constexpr int64_t kPartBytes = (int64_t)256 << 20;  // partial results at most
 
+constexpr int64_t kLogitBytes = (int64_t)1 << 30;   // logits left for the weights at most
+
 // A launch's row tiles (16 << shape rows) and parts.
 struct PagedPlan {
   int shape;
   int max_tiles;
   pdy::PagedCut cut;
   int64_t wgs;  // a kv head
-  size_t part_o, part_lse, part_n;  // bytes of the workspace
-  size_t bytes() const { return std::max<size_t>(256, part_o + part_lse + part_n); }
+  int64_t logit_rows, logit_keys;   // (rows 0: no logits are left)
+  size_t part_o, part_lse, part_n, logits;  // bytes of the workspace
+  size_t bytes() const { return std::max<size_t>(256, part_o + part_lse + part_n + logits); }
 };
 
-PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, int64_t d) {
+PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, int64_t d,
+                   bool weigh) {
   PagedPlan p;
   const int64_t g = r.hq / hkv, rows = std::max<int64_t>(1, r.max_q * g);
   p.shape = rows <= 16 ? 0 : rows <= 32 ? 1 : 2;
@@ -136,29 +140,45 @@ PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, in
   p.part_o = cut ? align256((size_t)p.cut.max_parts * r.tq * r.hq * d * 4) : 0;
   p.part_lse = cut ? align256((size_t)p.cut.max_parts * r.tq * r.hq * 4) : 0;
   p.part_n = cut ? align256((size_t)r.tq * r.hq * 4) : 0;
+  p.logit_keys = ceil_div(std::max<int64_t>(max_k, 1), 32) * 32;
+  p.logit_rows = weigh && p.shape == 0 && n * hkv * rows * p.logit_keys * 4 <= kLogitBytes ? rows : 0;
+  p.logits = align256((size_t)(n * hkv * p.logit_rows * p.logit_keys * 4));
   return p;
 }
 
-template <int D, bool F8, int RB, int NW>
+template <int D, bool F8, int RB, int NW, bool LOGITS = false>
 hipError_t launch_fwd(const pdy::PagedFwdArgs* a, dim3 grid, hipStream_t st) {
   using C = pdy::PagedFwdCfg<D, F8, RB, NW>;
-  if (a == nullptr) return set_lds(pdy::paged_fwd_kernel<D, F8, RB, NW>, C::LDS_BYTES);
-  hipLaunchKernelGGL((pdy::paged_fwd_kernel<D, F8, RB, NW>), grid, dim3(C::NT), C::LDS_BYTES, st, *a);
+  if (a == nullptr) return set_lds(pdy::paged_fwd_kernel<D, F8, RB, NW, LOGITS>, C::LDS_BYTES);
+  hipLaunchKernelGGL((pdy::paged_fwd_kernel<D, F8, RB, NW, LOGITS>), grid, dim3(C::NT), C::LDS_BYTES,
+                     st, *a);
   return hipSuccess;
 }
 using LaunchFwd = hipError_t (*)(const pdy::PagedFwdArgs*, dim3, hipStream_t);
-// [d = 64, 128][bf16, e4m3][16, 32, 64 rows]
+// [d = 64, 128][bf16, e4m3][16, 32, 64 rows, 16 that leave their logits]
+constexpr int kShapes = 4;
 template <int D, bool F8>
-constexpr LaunchFwd kFwdOf[3] = {launch_fwd<D, F8, 1, 4>, launch_fwd<D, F8, 2, 4>,
-                                 launch_fwd<D, F8, 4, 4>};
+constexpr LaunchFwd kFwdOf[kShapes] = {launch_fwd<D, F8, 1, 4>, launch_fwd<D, F8, 2, 4>,
+                                       launch_fwd<D, F8, 4, 4>, launch_fwd<D, F8, 1, 4, true>};
 const LaunchFwd* const kFwd[2][2] = {{kFwdOf<64, false>, kFwdOf<64, true>},
                                      {kFwdOf<128, false>, kFwdOf<128, true>}};
+
+template <int D, bool F8, int RB>
+void launch_weigh(const pdy::PagedWeighArgs& a, dim3 grid, hipStream_t st) {
+  hipLaunchKernelGGL((pdy::paged_weigh_kernel<D, F8, RB>), grid, dim3(256), 0, st, a);
+}
+using LaunchWeigh = void (*)(const pdy::PagedWeighArgs&, dim3, hipStream_t);
+template <int D, bool F8>
+constexpr LaunchWeigh kWeighOf[3] = {launch_weigh<D, F8, 1>, launch_weigh<D, F8, 2>,
+                                     launch_weigh<D, F8, 4>};
+const LaunchWeigh* const kWeigh[2][2] = {{kWeighOf<64, false>, kWeighOf<64, true>},
+                                         {kWeighOf<128, false>, kWeighOf<128, true>}};
 
 hipError_t init_paged_kernels() {
   static hipError_t status = [] {
     for (const auto& d : kFwd)
       for (const LaunchFwd* f : d)
-        for (int i = 0; i < 3; ++i) {
+        for (int i = 0; i < kShapes; ++i) {
           const hipError_t e = f[i](nullptr, dim3(), nullptr);
           if (e != hipSuccess) return e;
         }
@@ -228,7 +248,7 @@ size_t attn_paged_fwd_workspace_size(int32_t total_q, int32_t num_seqs, int32_t 
       (with_scores & ~1) ||
       check_rows(total_q, num_seqs, max_seqlen_q, num_heads_q, num_heads_kv, head_dim, &r) != PDY_OK)
     return 0;
-  return plan_fwd(r, num_seqs, max_seqlen_k, num_heads_kv, head_dim).bytes();
+  return plan_fwd(r, num_seqs, max_seqlen_k, num_heads_kv, head_dim, with_scores).bytes();
 }
 
 pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_pages,
@@ -255,7 +275,7 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
       (st = check_ptr(workspace, "workspace")))
     return st;
   if (scores && (st = check_ptr(scores, "scores"))) return st;
-  const PagedPlan p = plan_fwd(r, s.n, s.max_k, s.hkv, s.d);
+  const PagedPlan p = plan_fwd(r, s.n, s.max_k, s.hkv, s.d, scores != nullptr);
   if (workspace_bytes < p.bytes())
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, attn_paged_fwd needs %zu",
                 workspace_bytes, p.bytes());
@@ -282,19 +302,38 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
   a.part_o = reinterpret_cast<float*>(ws);
   a.part_lse = reinterpret_cast<float*>(ws + p.part_o);
   a.part_n = reinterpret_cast<int32_t*>(ws + p.part_o + p.part_lse);
+  a.logits = reinterpret_cast<float*>(ws + p.part_o + p.part_lse + p.part_n);
+  a.logit_rows = (int)p.logit_rows;
+  a.logit_keys = (int)p.logit_keys;
   const int64_t wgs = p.wgs * s.hkv;
-  if (!fits_grid(wgs, 256)) return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
+  if (!fits_grid(wgs, 256) ||
+      (scores && (!fits_grid(s.n * s.hkv * ceil_div(s.max_k, 512), 256) || s.n > 65535 || s.hkv > 65535)))
+    return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
   hipError_t e = init_paged_kernels();
   if (e != hipSuccess) return hip_fail(e, "kernel attribute setup");
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
   e = launch_timed(K_PAGED_FWD, hs, [&] {
-    (void)kFwd[s.d == 128][s.e4m3][p.shape](&a, dim3((unsigned)wgs), hs);
+    (void)kFwd[s.d == 128][s.e4m3][p.logit_rows > 0 ? 3 : p.shape](&a, dim3((unsigned)wgs), hs);
   });
   if (e != hipSuccess) return hip_fail(e, "paged_fwd_kernel launch");
-  if (p.cut.max_parts > 1) {
-    pdy::PagedMergeArgs m{a.part_o, a.part_lse, a.part_n, p.cut.max_parts, a.cu_q, a.c.n, a.tq,
-                          a.hq, a.o, a.lse};
-    const dim3 grid((unsigned)ceil_div(r.tq * r.hq, 4));
+  const pdy::PagedMergeArgs m{a.part_o, a.part_lse, a.part_n, p.cut.max_parts, a.cu_q, a.c.n, a.tq,
+                              a.hq, a.o, a.lse};
+  const int64_t merge_blocks = p.cut.max_parts > 1 ? ceil_div(r.tq * r.hq, 4) : 0;
+  if (p.logit_rows > 0) {
+    const int64_t key_blocks = ceil_div(std::max<int64_t>(s.max_k, 1), pdy::kWeighKeys);
+    const pdy::PagedJoinArgs b{m, (int)merge_blocks, a.c, a.g, (int)key_blocks, a.logits,
+                               a.logit_rows, a.logit_keys, a.scale_log2, a.k_scale, scores};
+    const int64_t blocks = merge_blocks + s.n * s.hkv * key_blocks;
+    const dim3 grid((unsigned)blocks);
+    e = launch_timed(K_PAGED_JOIN, hs, [&] {
+      if (s.d == 64) hipLaunchKernelGGL(pdy::paged_join_kernel<64>, grid, dim3(256), 0, hs, b);
+      else hipLaunchKernelGGL(pdy::paged_join_kernel<128>, grid, dim3(256), 0, hs, b);
+    });
+    if (e != hipSuccess) return hip_fail(e, "paged_join_kernel launch");
+    return PDY_OK;
+  }
+  if (merge_blocks > 0) {
+    const dim3 grid((unsigned)merge_blocks);
     e = launch_timed(K_PAGED_MERGE, hs, [&] {
       if (s.d == 64) hipLaunchKernelGGL(pdy::paged_merge_kernel<64>, grid, dim3(256), 0, hs, m);
       else hipLaunchKernelGGL(pdy::paged_merge_kernel<128>, grid, dim3(256), 0, hs, m);
@@ -302,16 +341,12 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
     if (e != hipSuccess) return hip_fail(e, "paged_merge_kernel launch");
   }
   if (scores) {
-    pdy::PagedWeighArgs b{a.c, a.q, a.k, a.k_scale, a.cu_q, a.lse, a.tq, a.hq, a.g, a.g_inv,
-                          a.causal, a.scale_log2, scores};
+    const pdy::PagedWeighArgs b{a.c, a.q, a.k, a.k_scale, a.cu_q, a.lse, a.tq, a.hq, a.g, a.g_inv,
+                                a.causal, a.scale_log2, scores};
     const dim3 grid((unsigned)ceil_div(ceil_div(std::max<int64_t>(s.max_k, 1), 16),
                                        4 * pdy::kWeighRuns), (unsigned)s.hkv, (unsigned)s.n);
     e = launch_timed(K_PAGED_WEIGH, hs, [&] {
-      auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, hs, b); };
-      if (head_dim == 64)
-        s.e4m3 ? go(pdy::paged_weigh_kernel<64, true>) : go(pdy::paged_weigh_kernel<64, false>);
-      else
-        s.e4m3 ? go(pdy::paged_weigh_kernel<128, true>) : go(pdy::paged_weigh_kernel<128, false>);
+      kWeigh[s.d == 128][s.e4m3][p.shape](b, grid, hs);
     });
     if (e != hipSuccess) return hip_fail(e, "paged_weigh_kernel launch");
   }

@@ -337,6 +337,10 @@ struct PagedFwdArgs {
   float* part_o;
   float* part_lse;
   int32_t* part_n;
+  // logits <q_i, k_j> of row r of sequence i and kv head h at [(i hkv + h) rows + r][keys],
+  // -inf where not visible (LOGITS)
+  float* logits;
+  int logit_rows, logit_keys;
 };
 
 // One copy of 1 KB into LDS: lane l's 16 bytes at base + voff, zeros from `bytes` on.
@@ -349,7 +353,16 @@ __device__ __forceinline__ void paged_copy(uint64_t base, int bytes, uint32_t vo
 #endif
 }
 
-template <int D, bool F8, int RB, int NW>
+// 16 bytes to base + voff, nowhere from `bytes` on: one store, whatever the lanes.
+__device__ __forceinline__ void paged_store(uint64_t base, int bytes, uint32_t voff, f32x4 x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto rs =
+      __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(base), 0, bytes, kBufferFlags);
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), rs, voff, 0, 0);
+#endif
+}
+
+template <int D, bool F8, int RB, int NW, bool LOGITS = false>
 __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     paged_fwd_kernel(PagedFwdArgs a) {
   using C = PagedFwdCfg<D, F8, RB, NW>;
@@ -472,8 +485,22 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
         paged_copy(base + (uint64_t)run * T::RUN, bytes, kv_off[kv][i][s], to + s * T::RUN + i * 1024);
     }
   };
-  // copies in flight behind a step's K when its products begin, and behind its V
+  // copies in flight behind a step's K when its products begin, and behind its V; from
+  // step SLOTS on, the stores of the logits of as many steps too
   constexpr int FLIGHT = (2 * C::SLOTS - 1) * 2 * T::COPIES;
+  constexpr int STORES = LOGITS ? 2 * C::SLOTS : 0;
+  auto wait_step = [&](int j) __attribute__((always_inline)) {
+    if (LOGITS && j >= C::SLOTS) wait_dma_n<FLIGHT + STORES>();
+    else wait_dma_n<FLIGHT>();
+  };
+  // (rows that are none lie behind the end of the buffer)
+  uint32_t logit_off = 0;
+  uint64_t logit_at = 0;
+  if constexpr (LOGITS) {
+    static_assert(RB == 1, "one row a lane");
+    logit_off = i16 < row_end - row0 ? (uint32_t)(i16 * a.logit_keys + grp * 4) * 4 : 0x80000000u;
+    logit_at = (uint64_t)(a.logits + (size_t)(seq * c.hkv + hk) * a.logit_rows * a.logit_keys);
+  }
   if (steps > 0) {
     find_runs(0);
 #pragma unroll
@@ -485,7 +512,7 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
   for (int j = 0; j < steps; ++j) {
     const int k0 = (first + NW * j) * 32;
     const uint32_t slot = (j % C::SLOTS) * 2 * T::BYTES;
-    wait_dma_n<FLIGHT>();
+    wait_step(j);
 
     // S^T = K Q^T, a run of 16 keys at a time
     f32x4 s[RB][2];
@@ -529,6 +556,11 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
           for (int r = 0; r < 4; ++r)
             if (k0 + run * 16 + grp * 4 + r >= end[b]) s[b][run][r] = -INFINITY;
       }
+      if constexpr (LOGITS)
+#pragma unroll
+        for (int run = 0; run < 2; ++run)
+          paged_store(logit_at, a.logit_rows * a.logit_keys * 4,
+                      logit_off + (uint32_t)(k0 + run * 16) * 4, s[b][run]);
       float top = -INFINITY;
 #pragma unroll
       for (int run = 0; run < 2; ++run)
@@ -555,7 +587,7 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     }
 
     // O^T += V^T P^T, 16 columns at a time
-    wait_dma_n<FLIGHT>();
+    wait_step(j);
     static_for<DB>([&](auto I) {
       constexpr int db = decltype(I)::value;
       bf16x8 x;
@@ -644,11 +676,9 @@ struct PagedMergeArgs {
 };
 
 template <int D>
-__global__ void __launch_bounds__(256) paged_merge_kernel(PagedMergeArgs a) {
+__device__ __forceinline__ void paged_merge(const PagedMergeArgs& a, uint32_t pair) {
   constexpr int LANES = D / 8, GROUPS = 64 / LANES;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l = __lane_id();
-  const uint32_t pair = blockIdx.x * 4 + w;  // token * hq + head
   const uint32_t pairs = (uint32_t)a.tq * a.hq;
   if (pair >= pairs) return;
   const int tok = (int)(pair / (uint32_t)a.hq), h = (int)(pair - (uint32_t)tok * a.hq);
@@ -703,12 +733,100 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedMergeArgs a) {
     a.lse[(size_t)h * a.tq + tok] = tot > 0.f ? mx + __builtin_log2f(tot) * kLn2 : -INFINITY;
 }
 
+template <int D>
+__global__ void __launch_bounds__(256) paged_merge_kernel(PagedMergeArgs a) {
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  paged_merge<D>(a, blockIdx.x * 4 + w);  // token * hq + head
+}
+
 // ---------------------------------------------------------------------------
 // The keys' weights: scores_j += sum over the sequence's rows i (of all heads of the group)
-// of exp(S_ij - LSE_i), for the visible keys.  One wave sums a key's rows, in order, so
-// that results do not depend on the launch.  A wave takes runs of 16 keys; rows with LSE
-// = -inf (no key, or a NaN or +inf logit) add nothing.
+// of exp(S_ij - LSE_i), for the visible keys.  One lane sums a key's rows, in order, so that
+// results do not depend on the launch.  Rows with LSE = -inf (no key, or a NaN or +inf
+// logit) add nothing.
 // ---------------------------------------------------------------------------
+
+// From the logits that the attention kernel left (up to 16 rows a sequence and kv head), in
+// one launch with the joining of parts: a workgroup past those that join takes 1,024 keys
+// of a sequence and kv head, and joins the parts' LSE of its rows itself.
+struct PagedJoinArgs {
+  PagedMergeArgs m;
+  int merge_blocks;
+  PagedCache c;
+  int g, key_blocks;
+  const float* logits;
+  int logit_rows, logit_keys;
+  float scale_log2;
+  const float* k_scale;
+  float* scores;
+};
+
+constexpr int kWeighKeys = 1024;  // of a workgroup
+
+template <int D>
+__global__ void __launch_bounds__(256) paged_join_kernel(PagedJoinArgs a) {
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = __lane_id();
+  if ((int)blockIdx.x < a.merge_blocks) {
+    paged_merge<D>(a.m, blockIdx.x * 4 + w);
+    return;
+  }
+  __shared__ float lse2[16];  // base 2
+  const PagedCache& c = a.c;
+  const int block = blockIdx.x - a.merge_blocks;
+  const int item = block / a.key_blocks, seq = item / c.hkv, hk = item - seq * c.hkv;
+  const int nk = paged_len(c, seq), j0 = (block - item * a.key_blocks) * kWeighKeys;
+  const int q_lo = min(max(a.m.cu_q[seq], 0), a.m.tq);
+  const int nq = min(max(a.m.cu_q[seq + 1], q_lo), a.m.tq) - q_lo;
+  const int rows = min(nq * a.g, a.logit_rows);
+  if (j0 >= nk || rows == 0) return;
+  const size_t pairs = (size_t)a.m.tq * a.m.hq;
+  for (int r = w; r < rows; r += 4) {
+    const int t = q_lo + r / a.g, h = hk * a.g + r % a.g;
+    const size_t pair = (size_t)t * a.m.hq + h;
+    const int parts = a.m.max_parts > 1 ? min(max(a.m.part_n[pair], 0), a.m.max_parts) : 1;
+    float x = -INFINITY;
+    if (parts <= 1) {
+      x = a.m.lse[(size_t)h * a.m.tq + t] * kLog2e;
+    } else {
+      float top = -INFINITY, sum = 0.f;
+      for (int p = l; p < parts; p += 64) top = fmaxf(top, a.m.part_lse[p * pairs + pair]);
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+      for (int p = l; p < parts; p += 64) {
+        const float y = a.m.part_lse[p * pairs + pair];
+        sum += y == -INFINITY ? 0.f : fast_exp2((y - top) * kLog2e);
+      }
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+      if (sum > 0.f) x = top * kLog2e + __builtin_log2f(sum);  // (a NaN sum: nothing)
+    }
+    if (l == 0) lse2[r] = x;
+  }
+  __syncthreads();
+  const float scale2 = a.scale_log2 * (a.k_scale ? a.k_scale[hk] : 1.f);
+  const float* const from = a.logits + (size_t)item * a.logit_rows * a.logit_keys;
+  for (int j = j0 + threadIdx.x * 4; j < min(nk, j0 + kWeighKeys); j += 1024) {
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < rows; ++r) {
+      const float z = lse2[r];
+      const f32x4 x = *reinterpret_cast<const f32x4*>(from + (size_t)r * a.logit_keys + j);
+      if (z > -INFINITY)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += fast_exp2(__builtin_fmaf(x[e], scale2, -z));
+    }
+    const int run = paged_run(c, seq, hk, j >> 4);
+    if (run < 0) continue;
+    float* const to = a.scores + (size_t)run * 16 + (j & 15);
+    if (j + 4 <= nk) {
+      *reinterpret_cast<f32x4*>(to) += sum;
+    } else {
+      for (int e = 0; e < nk - j; ++e) to[e] += sum[e];
+    }
+  }
+}
+
+// From the keys again, where rows are many: a wave holds 16 RB rows, and takes runs of 16
+// keys, the next one loaded while one is worked on.
 struct PagedWeighArgs {
   PagedCache c;
   const uint16_t* q;
@@ -725,7 +843,7 @@ struct PagedWeighArgs {
 
 constexpr int kWeighRuns = 8;  // of a wave
 
-template <int D, bool F8>
+template <int D, bool F8, int RB>
 __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
   constexpr int KS = D / 32;
   using T = PagedTile<D, F8>;
@@ -739,22 +857,31 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
   const int rows = nq * a.g;
   const float scale2 = a.scale_log2 * (F8 ? a.k_scale[hk] : 1.f);
   const int first = (blockIdx.x * 4 + w) * kWeighRuns;
-  if (rows == 0) return;
-  for (int x = first; x < first + kWeighRuns && x * 16 < nk; ++x) {
-    const int run = __builtin_amdgcn_readfirstlane(paged_run(c, seq, hk, x));
-    if (run < 0) continue;
+  const int count = min(kWeighRuns, ((nk + 15) >> 4) - first);
+  if (count <= 0) return;
+  // lane i knows where run first + i is
+  int runs_of = -1;
+  if (l < count) runs_of = paged_run(c, seq, hk, first + l);
+  using Raw = std::conditional_t<F8, u32x2, u32x4>;
+  auto load = [&](int x, Raw (&k)[KS]) __attribute__((always_inline)) {
+    const int run = max(0, __builtin_amdgcn_readlane(runs_of, min(x, count - 1)));
     const uint8_t* const kp = static_cast<const uint8_t*>(a.k) + (size_t)run * T::RUN + i16 * T::ROW;
-    bf16x8 kf[KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      if constexpr (F8)
-        kf[ks] = widen8(*reinterpret_cast<const u32x2*>(kp + ks * 32 + grp * 8));
-      else
-        kf[ks] = load_bf16x8(reinterpret_cast<const uint16_t*>(kp) + ks * 32 + grp * 8, true);
-    }
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int r0 = 0; r0 < rows; r0 += 16) {
-      const int r = min(r0 + i16, rows - 1);
+    for (int ks = 0; ks < KS; ++ks)
+      k[ks] = *reinterpret_cast<const Raw*>(kp + (ks * 32 + grp * 8) * (F8 ? 1 : 2));
+  };
+  float sum[kWeighRuns][4];
+#pragma unroll
+  for (int x = 0; x < kWeighRuns; ++x)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[x][e] = 0.f;
+  for (int r0 = 0; r0 < rows; r0 += 16 * RB) {
+    bf16x8 qf[RB][KS];
+    float lse2[RB];
+    int end[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      const int r = min(r0 + b * 16 + i16, rows - 1);
       int t = r;
       if (a.g > 1) {
         t = (int)__umulhi((uint32_t)r, a.g_inv);
@@ -762,23 +889,49 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
       }
       const int h = hk * a.g + (r - t * a.g);
       const uint16_t* const qp = a.q + ((size_t)(q_lo + t) * a.hq + h) * D + grp * 8;
-      f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s = mfma16(kf[ks], load_bf16x8(qp + ks * 32, true), s);
+      for (int ks = 0; ks < KS; ++ks) qf[b][ks] = load_bf16x8(qp + ks * 32, true);
       const float lse = a.lse[(size_t)h * a.tq + q_lo + t];
-      const int end = r0 + i16 < rows && lse > -INFINITY
-                          ? (a.causal ? min(nk, t + nk - nq + 1) : nk) - x * 16 - grp * 4 : 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e < end) sum[e] += fast_exp2(__builtin_fmaf(s[e], scale2, -lse * kLog2e));
+      end[b] = r0 + b * 16 + i16 < rows && lse > -INFINITY
+                   ? (a.causal ? min(nk, t + nk - nq + 1) : nk) - grp * 4 : 0;
+      lse2[b] = lse * kLog2e;
     }
+    Raw kr[2][KS];
+    load(0, kr[0]);
+    static_for<kWeighRuns>([&](auto I) {
+      constexpr int x = decltype(I)::value, cur = x & 1;
+      if (x >= count) return;  // uniform
+      if constexpr (x + 1 < kWeighRuns) load(x + 1, kr[cur ^ 1]);
+      bf16x8 kf[KS];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if constexpr (F8) kf[ks] = widen8(kr[cur][ks]);
+        else kf[ks] = as_bf16x8(kr[cur][ks]);
+      }
+      const int j0 = (first + x) * 16;
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mfma16(kf[ks], qf[b][ks], s);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sum[x][e] += j0 + e < end[b] ? fast_exp2(__builtin_fmaf(s[e], scale2, -lse2[b])) : 0.f;
+      }
+    });
+  }
+  // over the 16 rows of a block: lane e of each 16 gets key e's sum
+#pragma unroll
+  for (int x = 0; x < kWeighRuns; ++x) {
+    if (x >= count) return;  // uniform
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int off = 8; off > 0; off >>= 1) sum[e] += __shfl_xor(sum[e], off);
-    const float mine = i16 == 0 ? sum[0] : i16 == 1 ? sum[1] : i16 == 2 ? sum[2] : sum[3];
-    if (i16 < 4 && x * 16 + grp * 4 + i16 < nk)
-      a.scores[(size_t)run * 16 + grp * 4 + i16] += mine;
+      for (int off = 8; off > 0; off >>= 1) sum[x][e] += __shfl_xor(sum[x][e], off);
+    const float own = i16 == 0 ? sum[x][0] : i16 == 1 ? sum[x][1] : i16 == 2 ? sum[x][2] : sum[x][3];
+    const int run = __builtin_amdgcn_readlane(runs_of, x);
+    if (run >= 0 && i16 < 4 && (first + x) * 16 + grp * 4 + i16 < nk)
+      a.scores[(size_t)run * 16 + grp * 4 + i16] += own;
   }
 }
 
