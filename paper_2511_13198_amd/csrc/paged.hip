@@ -131,7 +131,7 @@ PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, in
   p.max_tiles = (int)ceil_div(rows, tile);
   const int64_t items = std::min(r.tq * g / tile + n, n * p.max_tiles);
   const int64_t slice = std::max<int64_t>(1, r.tq) * r.hq * (d + 1) * 4;
-  p.cut.least = 4;
+  p.cut.least = 8;
   p.cut.entries = (int)ceil_div(4 * kCUs, hkv);
   p.cut.max_parts = (int)std::max<int64_t>(
       1, std::min<int64_t>({kMaxParts, ceil_div(max_k, 32) / p.cut.least, kPartBytes / slice}));
@@ -316,9 +316,10 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
     (void)kFwd[s.d == 128][s.e4m3][p.logit_rows > 0 ? 3 : p.shape](&a, dim3((unsigned)wgs), hs);
   });
   if (e != hipSuccess) return hip_fail(e, "paged_fwd_kernel launch");
+  const bool wide = r.tq * r.hq <= 2 * kCUs && p.cut.max_parts > 16;
   const pdy::PagedMergeArgs m{a.part_o, a.part_lse, a.part_n, p.cut.max_parts, a.cu_q, a.c.n, a.tq,
-                              a.hq, a.o, a.lse};
-  const int64_t merge_blocks = p.cut.max_parts > 1 ? ceil_div(r.tq * r.hq, 4) : 0;
+                              a.hq, a.o, a.lse, wide};
+  const int64_t merge_blocks = p.cut.max_parts == 1 ? 0 : wide ? r.tq * r.hq : ceil_div(r.tq * r.hq, 4);
   if (p.logit_rows > 0) {
     const int64_t key_blocks = ceil_div(std::max<int64_t>(s.max_k, 1), pdy::kWeighKeys);
     const pdy::PagedJoinArgs b{m, (int)merge_blocks, a.c, a.g, (int)key_blocks, a.logits,
@@ -407,19 +408,30 @@ pdy_status attn_paged_evict(void* k_pages, void* v_pages, float* scores, const i
   a.scores = scores;
   a.k = static_cast<uint8_t*>(k_pages);
   a.v = static_cast<uint8_t*>(v_pages);
-  a.row_bytes = (int)s.row_bytes();
   a.kept = kept;
   a.new_len = new_lens;
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = launch_timed(K_PAGED_SELECT, hs, [&] {
-    hipLaunchKernelGGL(pdy::paged_select_kernel, dim3((unsigned)(s.n * s.hkv)),
-                       dim3(pdy::kSelectThreads), 0, hs, a);
+    const dim3 grid((unsigned)(s.n * s.hkv));
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid, dim3(pdy::kSelectThreads), 0, hs, a);
+    };
+    // the smallest number of keys a thread that holds the longest sequence
+    if (s.max_k <= 4 * pdy::kSelectThreads) go(pdy::paged_select_kernel<4>);
+    else if (s.max_k <= 16 * pdy::kSelectThreads) go(pdy::paged_select_kernel<16>);
+    else if (s.max_k <= 32 * pdy::kSelectThreads) go(pdy::paged_select_kernel<32>);
+    else go(pdy::paged_select_kernel<0>);
   });
   if (e != hipSuccess) return hip_fail(e, "paged_select_kernel launch");
-  const dim3 grid((unsigned)std::max<int64_t>(1, ceil_div(most, pdy::kGatherRows)),
-                  (unsigned)s.hkv, (unsigned)s.n);
   e = launch_timed(K_PAGED_GATHER, hs, [&] {
-    hipLaunchKernelGGL(pdy::paged_gather_kernel, grid, dim3(256), 0, hs, a);
+    auto go = [&](auto kernel, int rows) {
+      const dim3 grid((unsigned)std::max<int64_t>(1, ceil_div(most, rows)), (unsigned)s.hkv,
+                      (unsigned)s.n);
+      hipLaunchKernelGGL(kernel, grid, dim3(256), 0, hs, a);
+    };
+    if (s.row_bytes() == 64) go(pdy::paged_gather_kernel<4>, pdy::kGatherRows<4>);
+    else if (s.row_bytes() == 128) go(pdy::paged_gather_kernel<8>, pdy::kGatherRows<8>);
+    else go(pdy::paged_gather_kernel<16>, pdy::kGatherRows<16>);
   });
   if (e != hipSuccess) return hip_fail(e, "paged_gather_kernel launch");
   return PDY_OK;

@@ -79,15 +79,21 @@ struct PagedWriteArgs {
   int tokens;
 };
 
-// 8 bf16 of one 16-byte word as 8 e4m3, divided by s.
-__device__ __forceinline__ u32x2 paged_e4m3(const u32x4& x, float s) {
+// 8 bf16 of one 16-byte word as 8 e4m3 of x / s; inv = 1 / s.  The quotient is x inv and a
+// correction by its remainder, which is as exact as the division (a quotient that a rounding
+// to e4m3 could tell from it is hit), in 3 instructions: of a prompt's tokens the division
+// in full took as long as their memory traffic.  512 stands for all that is larger.
+__device__ __forceinline__ u32x2 paged_e4m3(const u32x4& x, float s, float inv) {
   uint32_t out[2] = {0u, 0u};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float y[2] = {__uint_as_float(x[i] << 16) / s, __uint_as_float(x[i] & 0xffff0000u) / s};
+    float y[2] = {__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u)};
 #pragma unroll
-    for (int j = 0; j < 2; ++j)  // (a NaN stays one)
-      if (y[j] == y[j]) y[j] = fminf(fmaxf(y[j], -kE4m3Max), kE4m3Max);
+    for (int j = 0; j < 2; ++j) {
+      const float q = fminf(fmaxf(y[j] * inv, -512.f), 512.f);
+      const float z = copysignf(__builtin_fmaf(__builtin_fmaf(-q, s, y[j]), inv, q), q);  // (-0)
+      y[j] = z == z ? fminf(fmaxf(z, -kE4m3Max), kE4m3Max) : z;  // (a NaN stays one)
+    }
     if (i & 1) out[i >> 1] = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], out[i >> 1], true);
     else out[i >> 1] = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], out[i >> 1], false);
   }
@@ -97,27 +103,48 @@ __device__ __forceinline__ u32x2 paged_e4m3(const u32x4& x, float s) {
 template <int D, bool F8>
 __global__ void __launch_bounds__(256) paged_write_kernel(PagedWriteArgs a) {
   constexpr int LANES = D / 8;  // of a row
+  constexpr int AHEAD = 2;      // rounds of 64 lanes loaded at a time
   const int t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (t >= a.tokens) return;
-  const int i = paged_seq_of(a.cu, a.c.n, t);
-  if (i >= a.c.n) return;  // behind the last sequence
-  const int j = paged_len(a.c, i) - (a.cu[i + 1] - t);
-  if (j < 0 || j >= a.c.max_k) return;
-  for (int u = __lane_id(); u < a.c.hkv * LANES; u += 64) {
-    const int h = u / LANES, e = (u % LANES) * 8;
-    const int run = paged_run(a.c, i, h, j >> 4);
-    if (run < 0) continue;
-    const size_t from = ((size_t)t * a.c.hkv + h) * D + e, row = (size_t)run * 16 + (j & 15);
+  const int units = a.c.hkv * LANES, l = __lane_id();
+  const size_t from = (size_t)t * units * 8;
+  int i = -1, j = -1;
+  for (int u0 = 0; u0 < units; u0 += 64 * AHEAD) {
+    u32x4 x[AHEAD][2];
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(a.in[kv] + from);
-      if constexpr (F8)
-        *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.pages[kv]) + row * D + e) =
-            paged_e4m3(x, a.scale[kv][h]);
-      else
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.pages[kv]) + row * D + e) = x;
+    for (int r = 0; r < AHEAD; ++r) {
+      const int u = u0 + r * 64 + l;
+      if (u < units)
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv)
+          x[r][kv] = *reinterpret_cast<const u32x4*>(a.in[kv] + from + (size_t)u * 8);
     }
-    if (a.scores && e == 0) a.scores[row] = 0.f;
+    if (u0 == 0) {  // (behind the loads: neither waits for the other)
+      i = paged_seq_of(a.cu, a.c.n, t);
+      if (i >= a.c.n) return;  // behind the last sequence
+      j = paged_len(a.c, i) - (a.cu[i + 1] - t);
+      if (j < 0 || j >= a.c.max_k) return;
+    }
+#pragma unroll
+    for (int r = 0; r < AHEAD; ++r) {
+      const int u = u0 + r * 64 + l;
+      if (u >= units) continue;
+      const int h = u / LANES, e = (u % LANES) * 8;
+      const int run = paged_run(a.c, i, h, j >> 4);
+      if (run < 0) continue;
+      const size_t row = (size_t)run * 16 + (j & 15);
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        if constexpr (F8) {
+          const float s = a.scale[kv][h];
+          *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.pages[kv]) + row * D + e) =
+              paged_e4m3(x[r][kv], s, 1.f / s);
+        } else {
+          *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.pages[kv]) + row * D + e) = x[r][kv];
+        }
+      }
+      if (a.scores && e == 0) a.scores[row] = 0.f;
+    }
   }
 }
 
@@ -661,8 +688,8 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
 // Combine the partial results of the rows that have more than one:
 //   LSE = log sum_p exp(LSE_p),  O = sum_p exp(LSE_p - LSE) O_p;
 // a part with LSE = -inf weighs nothing, one with NaN makes the row O = NaN, LSE = -inf.  A
-// wave per (token, head) pair: a lane per part for the weights (64 at a time), then 512 / D
-// parts at a time, 8 elements a lane.
+// wave per (token, head) pair, or a workgroup where parts are many: a lane per part for the
+// weights (64 at a time), then 512 / D parts at a time, 8 elements a lane.
 struct PagedMergeArgs {
   const float* part_o;
   const float* part_lse;
@@ -673,15 +700,22 @@ struct PagedMergeArgs {
   int tq, hq;
   uint16_t* o;
   float* lse;
+  int wide;  // a workgroup a pair
 };
 
-template <int D>
+// One pair by W waves of a workgroup (1, or all 4, which take the parts in turn).
+template <int D, int W>
 __device__ __forceinline__ void paged_merge(const PagedMergeArgs& a, uint32_t pair) {
   constexpr int LANES = D / 8, GROUPS = 64 / LANES;
+  __shared__ float acc_of[W][D];
+  __shared__ float stat_of[W][2];
   const int l = __lane_id();
+  const int w = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t pairs = (uint32_t)a.tq * a.hq;
   if (pair >= pairs) return;
   const int tok = (int)(pair / (uint32_t)a.hq), h = (int)(pair - (uint32_t)tok * a.hq);
+  // (read before it is known how many there are)
+  const float x0 = w * 64 + l < a.max_parts ? a.part_lse[(size_t)(w * 64 + l) * pairs + pair] : 0.f;
   const int parts = min(max(a.part_n[pair], 0), a.max_parts);
   // rows behind the last sequence stay, and those written by their one part
   if (tok >= a.cu_q[a.n] || parts <= 1) return;
@@ -689,8 +723,9 @@ __device__ __forceinline__ void paged_merge(const PagedMergeArgs& a, uint32_t pa
   float mx = -INFINITY, tot = 0.f;
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   // (more than 64 parts: the sums so far are rescaled by each further 64)
-  for (int p0 = 0; p0 < parts; p0 += 64) {
-    const float x = p0 + l < parts ? a.part_lse[(size_t)(p0 + l) * pairs + pair] : -INFINITY;
+  for (int p0 = w * 64; p0 < parts; p0 += 64 * W) {
+    const float x = p0 + l >= parts ? -INFINITY
+                    : p0 == w * 64 ? x0 : a.part_lse[(size_t)(p0 + l) * pairs + pair];
     float top = x;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
@@ -725,6 +760,29 @@ __device__ __forceinline__ void paged_merge(const PagedMergeArgs& a, uint32_t pa
   for (int off = LANES; off < 64; off <<= 1)
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor(acc[e], off);
+  if constexpr (W > 1) {
+    if (grp == 0) cross_put8(acc, &acc_of[w][c]);
+    if (l == 0) {
+      stat_of[w][0] = mx;
+      stat_of[w][1] = tot;
+    }
+    __syncthreads();
+    if (w != 0) return;
+    mx = stat_of[0][0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) mx = fmaxf(mx, stat_of[i][0]);
+    tot = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float t = stat_of[i][1];
+      const float wt = t > 0.f || t != t ? fast_exp2((stat_of[i][0] - mx) * kLog2e) : 0.f;
+      tot += wt * t;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += wt * acc_of[i][c + e];
+    }
+  }
   const float inv = tot > 0.f ? 1.f / tot : tot != tot ? NAN : 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] *= inv;
@@ -736,7 +794,9 @@ __device__ __forceinline__ void paged_merge(const PagedMergeArgs& a, uint32_t pa
 template <int D>
 __global__ void __launch_bounds__(256) paged_merge_kernel(PagedMergeArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  paged_merge<D>(a, blockIdx.x * 4 + w);  // token * hq + head
+  // token * hq + head
+  if (a.wide) paged_merge<D, 4>(a, blockIdx.x);
+  else paged_merge<D, 1>(a, blockIdx.x * 4 + w);
 }
 
 // ---------------------------------------------------------------------------
@@ -761,13 +821,14 @@ struct PagedJoinArgs {
   float* scores;
 };
 
-constexpr int kWeighKeys = 1024;  // of a workgroup
+constexpr int kWeighKeys = 1024;  // of a workgroup, 4 a thread
 
 template <int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(PagedJoinArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = __lane_id();
   if ((int)blockIdx.x < a.merge_blocks) {
-    paged_merge<D>(a.m, blockIdx.x * 4 + w);
+    if (a.m.wide) paged_merge<D, 4>(a.m, blockIdx.x);
+    else paged_merge<D, 1>(a.m, blockIdx.x * 4 + w);
     return;
   }
   __shared__ float lse2[16];  // base 2
@@ -779,49 +840,65 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedJoinArgs a) {
   const int nq = min(max(a.m.cu_q[seq + 1], q_lo), a.m.tq) - q_lo;
   const int rows = min(nq * a.g, a.logit_rows);
   if (j0 >= nk || rows == 0) return;
+  const int j = j0 + threadIdx.x * 4;  // this thread's 4 keys
+  const float* const from = a.logits + (size_t)item * a.logit_rows * a.logit_keys + j;
+  constexpr int AHEAD = 4;
+  f32x4 x[AHEAD], old = {0.f, 0.f, 0.f, 0.f};
+  int run = -1;
+  if (j < nk) {  // (loaded while the rows' LSE are)
+#pragma unroll
+    for (int r = 0; r < AHEAD; ++r)
+      x[r] = *reinterpret_cast<const f32x4*>(from + (size_t)min(r, rows - 1) * a.logit_keys);
+    run = paged_run(c, seq, hk, j >> 4);
+  }
+  float* const to = a.scores + (size_t)max(run, 0) * 16 + (j & 15);
+  if (run >= 0) old = *reinterpret_cast<const f32x4*>(to);
   const size_t pairs = (size_t)a.m.tq * a.m.hq;
   for (int r = w; r < rows; r += 4) {
     const int t = q_lo + r / a.g, h = hk * a.g + r % a.g;
     const size_t pair = (size_t)t * a.m.hq + h;
+    const float y0 = l < a.m.max_parts && a.m.max_parts > 1 ? a.m.part_lse[l * pairs + pair] : 0.f;
     const int parts = a.m.max_parts > 1 ? min(max(a.m.part_n[pair], 0), a.m.max_parts) : 1;
-    float x = -INFINITY;
+    float z = -INFINITY;
     if (parts <= 1) {
-      x = a.m.lse[(size_t)h * a.m.tq + t] * kLog2e;
+      z = a.m.lse[(size_t)h * a.m.tq + t] * kLog2e;
     } else {
       float top = -INFINITY, sum = 0.f;
-      for (int p = l; p < parts; p += 64) top = fmaxf(top, a.m.part_lse[p * pairs + pair]);
+      for (int p = l; p < parts; p += 64) top = fmaxf(top, p == l ? y0 : a.m.part_lse[p * pairs + pair]);
 #pragma unroll
       for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
       for (int p = l; p < parts; p += 64) {
-        const float y = a.m.part_lse[p * pairs + pair];
+        const float y = p == l ? y0 : a.m.part_lse[p * pairs + pair];
         sum += y == -INFINITY ? 0.f : fast_exp2((y - top) * kLog2e);
       }
 #pragma unroll
       for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
-      if (sum > 0.f) x = top * kLog2e + __builtin_log2f(sum);  // (a NaN sum: nothing)
+      if (sum > 0.f) z = top * kLog2e + __builtin_log2f(sum);  // (a NaN sum: nothing)
     }
-    if (l == 0) lse2[r] = x;
+    if (l == 0) lse2[r] = z;
   }
   __syncthreads();
+  if (run < 0) return;
   const float scale2 = a.scale_log2 * (a.k_scale ? a.k_scale[hk] : 1.f);
-  const float* const from = a.logits + (size_t)item * a.logit_rows * a.logit_keys;
-  for (int j = j0 + threadIdx.x * 4; j < min(nk, j0 + kWeighKeys); j += 1024) {
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int r = 0; r < rows; ++r) {
-      const float z = lse2[r];
-      const f32x4 x = *reinterpret_cast<const f32x4*>(from + (size_t)r * a.logit_keys + j);
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int r0 = 0; r0 < rows; r0 += AHEAD) {
+#pragma unroll
+    for (int r = 0; r < AHEAD; ++r) {
+      const float z = r0 + r < rows ? lse2[r0 + r] : -INFINITY;
       if (z > -INFINITY)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += fast_exp2(__builtin_fmaf(x[e], scale2, -z));
+        for (int e = 0; e < 4; ++e) sum[e] += fast_exp2(__builtin_fmaf(x[r][e], scale2, -z));
     }
-    const int run = paged_run(c, seq, hk, j >> 4);
-    if (run < 0) continue;
-    float* const to = a.scores + (size_t)run * 16 + (j & 15);
-    if (j + 4 <= nk) {
-      *reinterpret_cast<f32x4*>(to) += sum;
-    } else {
-      for (int e = 0; e < nk - j; ++e) to[e] += sum[e];
-    }
+    if (r0 + AHEAD < rows)
+#pragma unroll
+      for (int r = 0; r < AHEAD; ++r)
+        x[r] = *reinterpret_cast<const f32x4*>(
+            from + (size_t)min(r0 + AHEAD + r, rows - 1) * a.logit_keys);
+  }
+  if (j + 4 <= nk) {
+    *reinterpret_cast<f32x4*>(to) = old + sum;
+  } else {
+    for (int e = 0; e < nk - j; ++e) to[e] = old[e] + sum[e];
   }
 }
 
@@ -953,7 +1030,6 @@ struct PagedEvictArgs {
   float* scores;
   uint8_t* k;
   uint8_t* v;
-  int row_bytes;
   int32_t* kept;  // [n][hkv][budget]
   int32_t* new_len;
 };
@@ -966,12 +1042,16 @@ __device__ __forceinline__ uint32_t paged_order(float x) {
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048;
 
+// PER: keys a thread holds in registers, of 64 consecutive ones a wave each; 0: every pass
+// reads them again.
+template <int PER>
 __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvictArgs a) {
   __shared__ uint32_t hist[kBins];
-  __shared__ uint32_t wave_sum_of[kSelectWaves], wave_tie[kSelectWaves], found[2];
+  __shared__ uint32_t wave_more[kSelectWaves], wave_tie[kSelectWaves], found[2];
   const PagedCache& c = a.c;
   const int hk = blockIdx.x % (unsigned)c.hkv, seq = blockIdx.x / (unsigned)c.hkv;
-  const int t = threadIdx.x, l = __lane_id(), w = t >> 6;
+  const int t = threadIdx.x, l = __lane_id();
+  const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int n = paged_len(c, seq);
   int32_t* const kept = a.kept + ((size_t)seq * c.hkv + hk) * a.budget;
   if (n <= a.budget) {
@@ -981,9 +1061,28 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvict
   // (first + recent <= budget < n)
   const int lo = a.first, hi = n - a.recent;
   const int stay = a.budget - a.first - a.recent;  // of the keys lo .. hi
+  // this wave's keys: from .. to, `per` rounds of 64
+  const int per = ((hi - lo + kSelectWaves - 1) / kSelectWaves + 63) >> 6;
+  const int from = min(hi, lo + w * per * 64), to = min(hi, from + per * 64);
   auto order = [&](int j) __attribute__((always_inline)) {
+    if (j >= to) return 0u;
     const int run = paged_run(c, seq, hk, j >> 4);
     return run < 0 ? 0u : paged_order(a.scores[(size_t)run * 16 + (j & 15)]);
+  };
+  uint32_t key[PER > 0 ? PER : 1];
+  if constexpr (PER > 0) {
+#pragma unroll
+    for (int u = 0; u < PER; ++u) key[u] = order(from + u * 64 + l);
+  }
+  auto each = [&](auto&& f) __attribute__((always_inline)) {
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int u = 0; u < PER; ++u)
+        if (u < per) f(from + u * 64 + l, key[u]);  // uniform
+    } else {
+#pragma unroll 4
+      for (int u = 0; u < per; ++u) f(from + u * 64 + l, order(from + u * 64 + l));
+    }
   };
   // the stay-th largest: bits 31..21, 20..10, 9..0; `need`: how many stay of those that
   // share its bits
@@ -992,21 +1091,21 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvict
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
       const uint32_t width = pass == 2 ? 10 : 11, bins = 1u << width;
-      for (int i = t; i < kBins; i += kSelectThreads) hist[i] = 0u;
+      hist[t] = hist[t + kSelectThreads] = 0u;
       __syncthreads();
-      for (int j = lo + t; j < hi; j += kSelectThreads) {
-        const uint32_t x = order(j);
-        if (pass == 0 || (x ^ bits) >> (shift + width) == 0u) atomicAdd(&hist[(x >> shift) & (bins - 1)], 1u);
-      }
+      each([&](int j, uint32_t x) __attribute__((always_inline)) {
+        if (j < to && (pass == 0 || (x ^ bits) >> (shift + width) == 0u))
+          atomicAdd(&hist[(x >> shift) & (bins - 1)], 1u);
+      });
       __syncthreads();
       // counts from the highest bin down: two bins a thread
       const uint32_t b1 = bins - 1 - 2 * t, h1 = 2 * t < (int)bins ? hist[b1] : 0u,
                      h0 = 2 * t < (int)bins ? hist[b1 - 1] : 0u;
       const uint32_t incl = (uint32_t)wave_scan((int)(h1 + h0));
-      if (l == 63) wave_sum_of[w] = incl;
+      if (l == 63) wave_more[w] = incl;
       __syncthreads();
       uint32_t above = incl - h1 - h0;
-      for (int i = 0; i < w; ++i) above += wave_sum_of[i];
+      for (int i = 0; i < w; ++i) above += wave_more[i];
       if (above < need && need <= above + h1 + h0) {
         const bool second = need > above + h1;
         found[0] = second ? b1 - 1 : b1;
@@ -1015,33 +1114,27 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvict
       __syncthreads();
       bits |= found[0] << shift;
       need = found[1];
-      __syncthreads();
     }
   // each wave's keys in order: those above, and the first `need` equal ones
-  const int per = ((hi - lo + kSelectWaves - 1) / kSelectWaves + 63) & ~63;
-  const int from = min(hi, lo + w * per), to = min(hi, from + per);
   uint32_t more = 0u, ties = 0u;
-  if (stay > 0)
-    for (int j0 = from; j0 < to; j0 += 64) {
-      const uint32_t x = j0 + l < to ? order(j0 + l) : 0u;
-      more += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j0 + l < to && x > bits));
-      ties += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j0 + l < to && x == bits));
-    }
+  each([&](int j, uint32_t x) __attribute__((always_inline)) {
+    more += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j < to && x > bits));
+    ties += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j < to && x == bits));
+  });
+  __syncthreads();  // (the last reads of wave_more)
   if (l == 0) {
-    wave_sum_of[w] = more;
+    wave_more[w] = more;
     wave_tie[w] = ties;
   }
   __syncthreads();
   uint32_t at = 0u, tie = 0u;
   for (int i = 0; i < w; ++i) {
-    at += wave_sum_of[i];
+    at += wave_more[i];
     tie += wave_tie[i];
   }
   at += min(tie, need);
   if (stay > 0)
-    for (int j0 = from; j0 < to; j0 += 64) {
-      const int j = j0 + l;
-      const uint32_t x = j < to ? order(j) : 0u;
+    each([&](int j, uint32_t x) __attribute__((always_inline)) {
       const uint64_t below = (1ull << l) - 1ull;
       const uint64_t eq = __builtin_amdgcn_ballot_w64(j < to && x == bits);
       const bool mine = j < to && (x > bits || (x == bits && tie + __builtin_popcountll(eq & below) < need));
@@ -1049,38 +1142,65 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvict
       if (mine) kept[a.first + at + __builtin_popcountll(in & below)] = j;
       at += __builtin_popcountll(in);
       tie += __builtin_popcountll(eq);
-    }
+    });
   for (int j = t; j < a.first; j += kSelectThreads) kept[j] = j;
   for (int j = t; j < a.recent; j += kSelectThreads) kept[a.budget - a.recent + j] = hi + j;
 }
 
-constexpr int kGatherRows = 64;  // of a workgroup
+// LANES lanes of 16 bytes a row; a workgroup finds the places of kGatherRows rows, then
+// every thread copies 4 rows' chunks of K and V, all loaded before the first is stored.
+template <int LANES>
+constexpr int kGatherRows = 4 * 256 / LANES;
 
+template <int LANES>
 __global__ void __launch_bounds__(256) paged_gather_kernel(PagedEvictArgs a) {
+  constexpr int ROWS = kGatherRows<LANES>;
+  __shared__ int64_t src_of[ROWS], dst_of[ROWS];  // -1: none
   const PagedCache& c = a.c;
   const int hk = blockIdx.y, seq = blockIdx.z;
   const int n = min(paged_len(c, seq), a.budget);
   if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) a.new_len[seq] = n;
-  const int32_t* const kept = a.kept + ((size_t)seq * c.hkv + hk) * a.budget;
-  const int lanes = a.row_bytes / 16, rows = 256 / lanes;
-  const int e = (threadIdx.x % lanes) * 16;
-  const int j0 = blockIdx.x * kGatherRows, j1 = min(n, j0 + kGatherRows);
-  for (int j = j0 + threadIdx.x / lanes; j < j1; j += rows) {
-    const int from = kept[j];
-    if (from < 0) continue;
-    const int run = paged_run(c, seq, hk, from >> 4);
-    const int p = paged_div(c, j >> 4);
-    const int id = a.new_table[(size_t)seq * a.new_pages + p];
-    if (run < 0 || (uint32_t)id >= (uint32_t)c.num_pages) continue;
-    const size_t src = (size_t)run * 16 + (from & 15);
-    const size_t dst = ((size_t)(id * c.hkv + hk) * c.runs + ((j >> 4) - p * c.runs)) * 16 + (j & 15);
-    const u32x4 x = *reinterpret_cast<const u32x4*>(a.k + src * a.row_bytes + e);
-    const u32x4 y = *reinterpret_cast<const u32x4*>(a.v + src * a.row_bytes + e);
-    const float z = a.scores[src];
-    *reinterpret_cast<u32x4*>(a.k + dst * a.row_bytes + e) = x;
-    *reinterpret_cast<u32x4*>(a.v + dst * a.row_bytes + e) = y;
-    if (e == 0) a.scores[dst] = z;
+  const int j0 = blockIdx.x * ROWS;
+  if (j0 >= n) return;
+  const int j = j0 + threadIdx.x;
+  if (threadIdx.x < ROWS) {
+    int64_t src = -1, dst = -1;
+    if (j < n) {
+      const int from = a.kept[((size_t)seq * c.hkv + hk) * a.budget + j];
+      const int p = paged_div(c, j >> 4);
+      const int id = a.new_table[(size_t)seq * a.new_pages + p];
+      const int run = from >= 0 ? paged_run(c, seq, hk, from >> 4) : -1;
+      if (run >= 0 && (uint32_t)id < (uint32_t)c.num_pages) {
+        src = (int64_t)run * 16 + (from & 15);
+        dst = ((int64_t)(id * c.hkv + hk) * c.runs + ((j >> 4) - p * c.runs)) * 16 + (j & 15);
+      }
+    }
+    src_of[threadIdx.x] = src;
+    dst_of[threadIdx.x] = dst;
   }
+  __syncthreads();
+  const int e = (threadIdx.x % LANES) * 16;
+  u32x4 x[4][2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t src = src_of[threadIdx.x / LANES + i * (256 / LANES)];
+    if (src >= 0) {
+      x[i][0] = *reinterpret_cast<const u32x4*>(a.k + src * (LANES * 16) + e);
+      x[i][1] = *reinterpret_cast<const u32x4*>(a.v + src * (LANES * 16) + e);
+    }
+  }
+  float score = 0.f;
+  const bool mine = threadIdx.x < ROWS && src_of[threadIdx.x] >= 0;
+  if (mine) score = a.scores[src_of[threadIdx.x]];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t dst = dst_of[threadIdx.x / LANES + i * (256 / LANES)];
+    if (dst >= 0) {
+      *reinterpret_cast<u32x4*>(a.k + dst * (LANES * 16) + e) = x[i][0];
+      *reinterpret_cast<u32x4*>(a.v + dst * (LANES * 16) + e) = x[i][1];
+    }
+  }
+  if (mine) a.scores[dst_of[threadIdx.x]] = score;
 }
 
 }  // namespace pdy
