@@ -416,10 +416,12 @@ pdy_status attn_paged_evict(void* k_pages, void* v_pages, float* scores, const i
     auto go = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, grid, dim3(pdy::kSelectThreads), 0, hs, a);
     };
-    // the smallest number of keys a thread that holds the longest sequence
-    if (s.max_k <= 4 * pdy::kSelectThreads) go(pdy::paged_select_kernel<4>);
-    else if (s.max_k <= 16 * pdy::kSelectThreads) go(pdy::paged_select_kernel<16>);
-    else if (s.max_k <= 32 * pdy::kSelectThreads) go(pdy::paged_select_kernel<32>);
+    // the smallest number of keys a thread that holds the longest sequence (and up to 3 in
+    // front of its first)
+    const int64_t quads = ceil_div(s.max_k + 3, 4 * pdy::kSelectThreads);
+    if (quads <= 1) go(pdy::paged_select_kernel<1>);
+    else if (quads <= 4) go(pdy::paged_select_kernel<4>);
+    else if (quads <= 8) go(pdy::paged_select_kernel<8>);
     else go(pdy::paged_select_kernel<0>);
   });
   if (e != hipSuccess) return hip_fail(e, "paged_select_kernel launch");

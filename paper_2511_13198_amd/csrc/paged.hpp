@@ -1034,17 +1034,16 @@ struct PagedEvictArgs {
   int32_t* new_len;
 };
 
-// Scores as unsigned numbers of the same order; a NaN is 0.
+// Scores as unsigned numbers of the same order, a NaN as 1; 0 is no key.
 __device__ __forceinline__ uint32_t paged_order(float x) {
   const uint32_t b = __float_as_uint(x);
-  return x != x ? 0u : b == 0x80000000u ? 0x80000000u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
+  return x != x ? 1u : b == 0x80000000u ? 0x80000000u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048;
 
-// PER: keys a thread holds in registers, of 64 consecutive ones a wave each; 0: every pass
-// reads them again.
-template <int PER>
+// QUADS: groups of 4 keys that a thread holds in registers; 0: every pass reads them again.
+template <int QUADS>
 __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvictArgs a) {
   __shared__ uint32_t hist[kBins];
   __shared__ uint32_t wave_more[kSelectWaves], wave_tie[kSelectWaves], found[2];
@@ -1061,27 +1060,38 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvict
   // (first + recent <= budget < n)
   const int lo = a.first, hi = n - a.recent;
   const int stay = a.budget - a.first - a.recent;  // of the keys lo .. hi
-  // this wave's keys: from .. to, `per` rounds of 64
-  const int per = ((hi - lo + kSelectWaves - 1) / kSelectWaves + 63) >> 6;
-  const int from = min(hi, lo + w * per * 64), to = min(hi, from + per * 64);
-  auto order = [&](int j) __attribute__((always_inline)) {
-    if (j >= to) return 0u;
-    const int run = paged_run(c, seq, hk, j >> 4);
-    return run < 0 ? 0u : paged_order(a.scores[(size_t)run * 16 + (j & 15)]);
+  // this wave's keys: `per` rounds of 256 from `from` on, 4 a lane
+  const int start = lo & ~3;
+  const int per = ((hi - start + kSelectWaves - 1) / kSelectWaves + 255) >> 8;
+  const int from = start + w * per * 256 + l * 4;
+  struct Quad {
+    uint32_t x[4];
   };
-  uint32_t key[PER > 0 ? PER : 1];
-  if constexpr (PER > 0) {
+  auto order = [&](int j) __attribute__((always_inline)) {
+    Quad q = {{0u, 0u, 0u, 0u}};
+    if (j < hi) {
+      const int run = paged_run(c, seq, hk, j >> 4);
+      const f32x4 y = run < 0 ? f32x4{NAN, NAN, NAN, NAN}
+                              : *reinterpret_cast<const f32x4*>(a.scores + (size_t)run * 16 + (j & 15));
 #pragma unroll
-    for (int u = 0; u < PER; ++u) key[u] = order(from + u * 64 + l);
+      for (int e = 0; e < 4; ++e) q.x[e] = j + e >= lo && j + e < hi ? paged_order(y[e]) : 0u;
+    }
+    return q;
+  };
+  Quad key[QUADS > 0 ? QUADS : 1];
+  if constexpr (QUADS > 0) {
+#pragma unroll
+    for (int u = 0; u < QUADS; ++u)
+      key[u] = u < per ? order(from + u * 256) : Quad{{0u, 0u, 0u, 0u}};
   }
   auto each = [&](auto&& f) __attribute__((always_inline)) {
-    if constexpr (PER > 0) {
+    if constexpr (QUADS > 0) {
 #pragma unroll
-      for (int u = 0; u < PER; ++u)
-        if (u < per) f(from + u * 64 + l, key[u]);  // uniform
+      for (int u = 0; u < QUADS; ++u)
+        if (u < per) f(from + u * 256, key[u]);  // uniform
     } else {
-#pragma unroll 4
-      for (int u = 0; u < per; ++u) f(from + u * 64 + l, order(from + u * 64 + l));
+#pragma unroll 2
+      for (int u = 0; u < per; ++u) f(from + u * 256, order(from + u * 256));
     }
   };
   // the stay-th largest: bits 31..21, 20..10, 9..0; `need`: how many stay of those that
@@ -1093,9 +1103,11 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvict
       const uint32_t width = pass == 2 ? 10 : 11, bins = 1u << width;
       hist[t] = hist[t + kSelectThreads] = 0u;
       __syncthreads();
-      each([&](int j, uint32_t x) __attribute__((always_inline)) {
-        if (j < to && (pass == 0 || (x ^ bits) >> (shift + width) == 0u))
-          atomicAdd(&hist[(x >> shift) & (bins - 1)], 1u);
+      each([&](int, const Quad& q) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (q.x[e] != 0u && (pass == 0 || (q.x[e] ^ bits) >> (shift + width) == 0u))
+            atomicAdd(&hist[(q.x[e] >> shift) & (bins - 1)], 1u);
       });
       __syncthreads();
       // counts from the highest bin down: two bins a thread
@@ -1117,9 +1129,12 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvict
     }
   // each wave's keys in order: those above, and the first `need` equal ones
   uint32_t more = 0u, ties = 0u;
-  each([&](int j, uint32_t x) __attribute__((always_inline)) {
-    more += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j < to && x > bits));
-    ties += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j < to && x == bits));
+  each([&](int, const Quad& q) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      more += __builtin_popcountll(__builtin_amdgcn_ballot_w64(q.x[e] > bits));
+      ties += __builtin_popcountll(__builtin_amdgcn_ballot_w64(q.x[e] == bits));
+    }
   });
   __syncthreads();  // (the last reads of wave_more)
   if (l == 0) {
@@ -1132,16 +1147,45 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvict
     at += wave_more[i];
     tie += wave_tie[i];
   }
-  at += min(tie, need);
+  at += a.first + min(tie, need);
+  // lanes below this one that a ballot has
+  auto below = [&](uint64_t m) __attribute__((always_inline)) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+  };
   if (stay > 0)
-    each([&](int j, uint32_t x) __attribute__((always_inline)) {
-      const uint64_t below = (1ull << l) - 1ull;
-      const uint64_t eq = __builtin_amdgcn_ballot_w64(j < to && x == bits);
-      const bool mine = j < to && (x > bits || (x == bits && tie + __builtin_popcountll(eq & below) < need));
-      const uint64_t in = __builtin_amdgcn_ballot_w64(mine);
-      if (mine) kept[a.first + at + __builtin_popcountll(in & below)] = j;
-      at += __builtin_popcountll(in);
-      tie += __builtin_popcountll(eq);
+    each([&](int j, const Quad& q) __attribute__((always_inline)) {
+      bool mine[4];
+      uint64_t eq[4], any = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        mine[e] = q.x[e] > bits;
+        eq[e] = __builtin_amdgcn_ballot_w64(q.x[e] == bits);
+        any |= eq[e];
+      }
+      if (any) {  // uniform
+        uint32_t before = tie;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) before += below(eq[e]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (q.x[e] == bits) {
+            mine[e] = before < need;
+            ++before;
+          }
+          tie += __builtin_popcountll(eq[e]);
+        }
+      }
+      uint32_t to = at;
+      uint64_t in[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        in[e] = __builtin_amdgcn_ballot_w64(mine[e]);
+        to += below(in[e]);
+        at += __builtin_popcountll(in[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (mine[e]) kept[to++] = j + e;
     });
   for (int j = t; j < a.first; j += kSelectThreads) kept[j] = j;
   for (int j = t; j < a.recent; j += kSelectThreads) kept[a.budget - a.recent + j] = hi + j;
