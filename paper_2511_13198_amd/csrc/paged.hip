@@ -115,6 +115,7 @@ constexpr int64_t kLogitBytes = (int64_t)1 << 30;   // logits left for the weigh
 struct PagedPlan {
   int shape;
   int max_tiles;
+  bool whole;  // an item a workgroup of 8 waves
   pdy::PagedCut cut;
   int64_t wgs;  // a kv head
   int64_t logit_rows, logit_keys;   // (rows 0: no logits are left)
@@ -135,6 +136,8 @@ PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, in
   p.cut.entries = (int)ceil_div(4 * kCUs, hkv);
   p.cut.max_parts = (int)std::max<int64_t>(
       1, std::min<int64_t>({kMaxParts, ceil_div(max_k, 32) / p.cut.least, kPartBytes / slice}));
+  p.whole = p.shape == 0 && max_k <= 2048 && n * hkv <= kCUs;
+  if (p.whole) p.cut.max_parts = 1;
   const bool cut = p.cut.max_parts > 1;
   p.wgs = cut ? items + p.cut.entries + 1 : n * p.max_tiles;
   p.part_o = cut ? align256((size_t)p.cut.max_parts * r.tq * r.hq * d * 4) : 0;
@@ -146,20 +149,23 @@ PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, in
   return p;
 }
 
-template <int D, bool F8, int RB, int NW, bool LOGITS = false>
+template <int D, bool F8, int RB, int NW, bool LOGITS = false, bool WHOLE = false>
 hipError_t launch_fwd(const pdy::PagedFwdArgs* a, dim3 grid, hipStream_t st) {
   using C = pdy::PagedFwdCfg<D, F8, RB, NW>;
-  if (a == nullptr) return set_lds(pdy::paged_fwd_kernel<D, F8, RB, NW, LOGITS>, C::LDS_BYTES);
-  hipLaunchKernelGGL((pdy::paged_fwd_kernel<D, F8, RB, NW, LOGITS>), grid, dim3(C::NT), C::LDS_BYTES,
+  if (a == nullptr) return set_lds(pdy::paged_fwd_kernel<D, F8, RB, NW, LOGITS, WHOLE>, C::LDS_BYTES);
+  hipLaunchKernelGGL((pdy::paged_fwd_kernel<D, F8, RB, NW, LOGITS, WHOLE>), grid, dim3(C::NT), C::LDS_BYTES,
                      st, *a);
   return hipSuccess;
 }
 using LaunchFwd = hipError_t (*)(const pdy::PagedFwdArgs*, dim3, hipStream_t);
-// [d = 64, 128][bf16, e4m3][16, 32, 64 rows, 16 that leave their logits]
-constexpr int kShapes = 4;
+// [d = 64, 128][bf16, e4m3][16, 32, 64 rows; 16: leaving their logits; whole items by 8
+// waves; both]
+constexpr int kShapes = 6;
 template <int D, bool F8>
 constexpr LaunchFwd kFwdOf[kShapes] = {launch_fwd<D, F8, 1, 4>, launch_fwd<D, F8, 2, 4>,
-                                       launch_fwd<D, F8, 4, 4>, launch_fwd<D, F8, 1, 4, true>};
+                                       launch_fwd<D, F8, 4, 4>, launch_fwd<D, F8, 1, 4, true>,
+                                       launch_fwd<D, F8, 1, 8, false, true>,
+                                       launch_fwd<D, F8, 1, 8, true, true>};
 const LaunchFwd* const kFwd[2][2] = {{kFwdOf<64, false>, kFwdOf<64, true>},
                                      {kFwdOf<128, false>, kFwdOf<128, true>}};
 
@@ -306,14 +312,14 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
   a.logit_rows = (int)p.logit_rows;
   a.logit_keys = (int)p.logit_keys;
   const int64_t wgs = p.wgs * s.hkv;
-  if (!fits_grid(wgs, 256) ||
+  if (!fits_grid(wgs, p.whole ? 512 : 256) ||
       (scores && (!fits_grid(s.n * s.hkv * ceil_div(s.max_k, 512), 256) || s.n > 65535 || s.hkv > 65535)))
     return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
   hipError_t e = init_paged_kernels();
   if (e != hipSuccess) return hip_fail(e, "kernel attribute setup");
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
   e = launch_timed(K_PAGED_FWD, hs, [&] {
-    (void)kFwd[s.d == 128][s.e4m3][p.logit_rows > 0 ? 3 : p.shape](&a, dim3((unsigned)wgs), hs);
+    (void)kFwd[s.d == 128][s.e4m3][p.whole ? (p.logit_rows > 0 ? 5 : 4) : p.logit_rows > 0 ? 3 : p.shape](&a, dim3((unsigned)wgs), hs);
   });
   if (e != hipSuccess) return hip_fail(e, "paged_fwd_kernel launch");
   const bool wide = r.tq * r.hq <= 2 * kCUs && p.cut.max_parts > 16;

@@ -196,20 +196,29 @@ __device__ __forceinline__ bf16x8 widen8(const u32x2& x) {
   return out;
 }
 
-// LDS reads of the tiles: 16 bytes of K, to be waited for; V transposed (8 keys of a
-// column: 4 of a run and 4 of the next for 16 bits), waited for.
+// LDS reads of the tiles, to be waited for: 16 bytes of K; 8 keys of a column of V (of 16
+// bits 4 of a run and 4 of the next).
 template <int OFF>
 __device__ __forceinline__ void paged_read16(uint32_t addr, u32x4& x) {
   asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(x) : "v"(addr), "i"(OFF));
 }
+// (early clobber: the second read needs the address after the first was issued)
 template <int RUN>
-__device__ __forceinline__ void paged_read_tr16(uint32_t addr, TrRegs& x) {
-  asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %2 offset:%3\n\t"
-               "s_waitcnt lgkmcnt(0)"
-               : "=&v"(x.lo), "=&v"(x.hi) : "v"(addr), "i"(RUN));
+__device__ __forceinline__ void paged_read_tr16(uint32_t addr, u32x2& x, u32x2& y) {
+  asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %2 offset:%3"
+               : "=&v"(x), "=&v"(y) : "v"(addr), "i"(RUN));
 }
 __device__ __forceinline__ void paged_read_tr8(uint32_t addr, u32x2& x) {
-  asm volatile("ds_read_b64_tr_b8 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x) : "v"(addr));
+  asm volatile("ds_read_b64_tr_b8 %0, %1" : "=v"(x) : "v"(addr));
+}
+// Waits until at most N LDS operations are outstanding; the registers are tied to it.
+template <int N>
+__device__ __forceinline__ void paged_wait(u32x2& x) {
+  asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(x) : "i"(N));
+}
+template <int N>
+__device__ __forceinline__ void paged_wait(u32x2& x, u32x2& y) {
+  asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(x), "+v"(y) : "i"(N));
 }
 
 // A wave's tile of 32 keys (two runs) in LDS: rows of D elements as they are in memory, the
@@ -260,24 +269,45 @@ struct PagedCut {
   int least;      // fewest steps of a part
   int entries;    // parts of a kv head
 };
+// A sequence as the kernels see it: its rows in q, and its keys.
+struct PagedSeq {
+  int q_lo, nq, nk;
+};
+__device__ __forceinline__ PagedSeq paged_seq(const PagedCache& c, const int32_t* cu_q, int tq,
+                                              int i) {
+  const int lo = cu_q[i], hi = cu_q[i + 1], len = c.len[i];
+  PagedSeq s;
+  s.q_lo = min(max(lo, 0), tq);
+  s.nq = min(max(hi, s.q_lo), tq) - s.q_lo;
+  s.nk = c.num_pages > 0 ? min(max(len, 0), c.max_k) : 0;
+  return s;
+}
+
 struct PagedPlace {
+  PagedSeq s;
   int seq, tile, part, nparts;
 };
 
-// Entry `entry` of a kv head's list; false past its end.  of(i, tiles, steps): row tiles of
-// sequence i, and steps of each.  (wave-uniform)
-template <int NT, class F>
-__device__ __forceinline__ bool paged_place(const PagedCut& c, int n, int entry, F&& of,
+// Entry `entry` of a kv head's list; false past its end.  get(i): sequence i; of(s, tiles,
+// steps): its row tiles, and steps of each.  (wave-uniform)
+template <int NT, class G, class F>
+__device__ __forceinline__ bool paged_place(const PagedCut& c, int n, int entry, G&& get, F&& of,
                                             PagedPlace& out) {
   __shared__ float sum_of[NT / 64];
-  __shared__ int entries_of[NT / 64], found[4];
+  __shared__ int entries_of[NT / 64], found[6];
   const bool wide = n > 64;  // uniform
   const int id = wide ? threadIdx.x : __lane_id(), stride = wide ? NT : 64;
   const int w = threadIdx.x >> 6, l = __lane_id();
-  int tiles, steps;
-  float sum = 0.f;
-  for (int i = id; i < n; i += stride) {
-    of(i, tiles, steps);
+  // (the first sequence of a lane is kept: more than one has a lane beyond 256 alone)
+  PagedSeq s0 = {0, 0, 0};
+  int tiles0 = 0, steps0 = 0, tiles, steps;
+  if (id < n) {
+    s0 = get(id);
+    of(s0, tiles0, steps0);
+  }
+  float sum = (float)tiles0 * (float)steps0;
+  for (int i = id + stride; i < n; i += stride) {
+    of(get(i), tiles, steps);
     sum += (float)tiles * (float)steps;
   }
   sum = wave_sum(sum);
@@ -290,13 +320,13 @@ __device__ __forceinline__ bool paged_place(const PagedCut& c, int n, int entry,
   const int cap = max(c.least, (int)fminf(sum / (float)c.entries + 1.f, 1e9f));
   const float inv = 1.f / (float)cap;
   // ceil(steps / cap) as a float product (any whole number near it does)
-  auto parts = [&]() __attribute__((always_inline)) {
+  auto parts = [&](int steps) __attribute__((always_inline)) {
     return max(1, min(c.max_parts, (int)ceilf((float)steps * inv)));
   };
-  int mine = 0;
-  for (int i = id; i < n; i += stride) {
-    of(i, tiles, steps);
-    mine += tiles * parts();
+  int np = parts(steps0), mine = tiles0 * np;
+  for (int i = id + stride; i < n; i += stride) {
+    of(get(i), tiles, steps);
+    mine += tiles * parts(steps);
   }
   int before = wave_scan(mine) - mine;
   if (wide) {
@@ -306,37 +336,50 @@ __device__ __forceinline__ bool paged_place(const PagedCut& c, int n, int entry,
     for (int i = 0; i < w; ++i) before += entries_of[i];
   }
   const bool hit = entry >= before && entry < before + mine;
-  int seq = 0, rel = entry - before, np = 1;
-  if (hit)
-    for (int i = id; i < n; i += stride) {
-      of(i, tiles, steps);
-      np = parts();
+  int seq = id, rel = entry - before;
+  if (hit && rel >= tiles0 * np) {
+    rel -= tiles0 * np;
+    for (int i = id + stride; i < n; i += stride) {
       seq = i;
+      s0 = get(i);
+      of(s0, tiles, steps);
+      np = parts(steps);
       if (rel < tiles * np) break;
       rel -= tiles * np;
     }
+  }
   if (wide) {
     if (hit) {
       found[0] = seq;
       found[1] = rel;
       found[2] = np;
+      found[3] = s0.q_lo;
+      found[4] = s0.nq;
+      found[5] = s0.nk;
     }
     __syncthreads();
     seq = found[0];
     rel = found[1];
     np = found[2];
+    s0 = PagedSeq{found[3], found[4], found[5]};
     if (seq < 0) return false;
   } else {
     const uint64_t any = __builtin_amdgcn_ballot_w64(hit);
     if (!any) return false;
     const int src = __builtin_ctzll(any);
-    seq = __builtin_amdgcn_readlane(seq, src);
-    rel = __builtin_amdgcn_readlane(rel, src);
-    np = __builtin_amdgcn_readlane(np, src);
+    auto lane = [&](int& x) __attribute__((always_inline)) { x = __builtin_amdgcn_readlane(x, src); };
+    lane(seq);
+    lane(rel);
+    lane(np);
+    lane(s0.q_lo);
+    lane(s0.nq);
+    lane(s0.nk);
   }
-  out.seq = __builtin_amdgcn_readfirstlane(seq);
-  out.nparts = __builtin_amdgcn_readfirstlane(np);
-  rel = __builtin_amdgcn_readfirstlane(rel);
+  auto uni = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
+  out.s = PagedSeq{uni(s0.q_lo), uni(s0.nq), uni(s0.nk)};
+  out.seq = uni(seq);
+  out.nparts = uni(np);
+  rel = uni(rel);
   out.tile = rel / out.nparts;
   out.part = rel - out.tile * out.nparts;
   return true;
@@ -389,7 +432,7 @@ __device__ __forceinline__ void paged_store(uint64_t base, int bytes, uint32_t v
 #endif
 }
 
-template <int D, bool F8, int RB, int NW, bool LOGITS = false>
+template <int D, bool F8, int RB, int NW, bool LOGITS, bool WHOLE>
 __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     paged_fwd_kernel(PagedFwdArgs a) {
   using C = PagedFwdCfg<D, F8, RB, NW>;
@@ -398,31 +441,36 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
   extern __shared__ __attribute__((aligned(1024))) uint8_t paged_smem[];
   const PagedCache& c = a.c;
   const int hk = blockIdx.x % (unsigned)c.hkv, entry = blockIdx.x / (unsigned)c.hkv;
+  const int l = __lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // Lane 2 i + s knows where run s of the wave's step i (mod 32) is: the 32 keys of its step
+  // j are those from (first + NW j) 32 on.  (A run past the last key in use may be any.)
+  int runs_of = 0;
+  auto find_runs = [&](int seq, int first, int j) __attribute__((always_inline)) {
+    const int x = 2 * (first + NW * (j + (l >> 1))) + (l & 1);
+    runs_of = x * 16 < c.max_k && c.num_pages > 0 ? max(0, paged_run(c, seq, hk, x)) : 0;
+  };
   PagedPlace at;
-  if (a.cut.max_parts == 1) {
-    at.seq = entry / a.max_tiles;
-    at.tile = entry - at.seq * a.max_tiles;
+  if (WHOLE || a.cut.max_parts == 1) {
+    at.seq = WHOLE ? entry : entry / a.max_tiles;
+    at.tile = entry - at.seq * (WHOLE ? 1 : a.max_tiles);
     at.part = 0;
     at.nparts = 1;
-  } else if (!paged_place<C::NT>(a.cut, c.n, entry,
-                                 [&](int i, int& tiles, int& steps) __attribute__((always_inline)) {
-                                   const int lo = min(max(a.cu_q[i], 0), a.tq);
-                                   const int rows = (min(max(a.cu_q[i + 1], lo), a.tq) - lo) * a.g;
-                                   tiles = min((rows + C::ROWS - 1) / C::ROWS, a.max_tiles);
-                                   steps = (paged_len(c, i) + 31) >> 5;
-                                 },
-                                 at)) {
+    if constexpr (WHOLE) find_runs(at.seq, w, 0);  // (without waiting for the lengths)
+    at.s = paged_seq(c, a.cu_q, a.tq, at.seq);
+  } else if (!paged_place<C::NT>(
+                 a.cut, c.n, entry,
+                 [&](int i) __attribute__((always_inline)) { return paged_seq(c, a.cu_q, a.tq, i); },
+                 [&](const PagedSeq& s, int& tiles, int& steps) __attribute__((always_inline)) {
+                   tiles = min((s.nq * a.g + C::ROWS - 1) / C::ROWS, a.max_tiles);
+                   steps = (s.nk + 31) >> 5;
+                 },
+                 at)) {
     return;
   }
-  const int seq = at.seq, tile = at.tile;
-  const int q_lo = min(max(a.cu_q[seq], 0), a.tq);
-  const int nq = min(max(a.cu_q[seq + 1], q_lo), a.tq) - q_lo;
+  const int seq = at.seq, tile = at.tile, q_lo = at.s.q_lo, nq = at.s.nq, nk = at.s.nk;
   const int row_end = nq * a.g;  // packed rows, from the sequence's first on
   const int row0 = tile * C::ROWS;
   if (row0 >= row_end) return;
-  const int nk = paged_len(c, seq);
-
-  const int l = __lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i16 = l & 15, grp = l >> 4;
   auto token = [&](int r) __attribute__((always_inline)) {
     if (a.g == 1) return r;
@@ -485,18 +533,11 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     va = lds_addr(mine) + T::BYTES + r * T::ROW + T::swz_v(r) * 16 + ((i16 & 3) >> 1) * 16 + (i16 & 1) * 8;
   }
 
-  // The part's steps, and this wave's: step j is the 32 keys from (first + NW j) 32 on.
-  // Lane 2 i + s knows where run s of step i (mod 32) is.
+  // the part's steps, and this wave's
   const int all_steps = (some_end + 31) >> 5;
-  const int first = (int)((int64_t)at.part * all_steps / at.nparts) + w;
-  const int last = (int)((int64_t)(at.part + 1) * all_steps / at.nparts);
+  const int first = (WHOLE ? 0 : (int)((int64_t)at.part * all_steps / at.nparts)) + w;
+  const int last = WHOLE ? all_steps : (int)((int64_t)(at.part + 1) * all_steps / at.nparts);
   const int steps = max(0, last - first + NW - 1) / NW;
-  int runs_of = 0;
-  auto find_runs = [&](int j) __attribute__((always_inline)) {
-    const int x = 2 * (first + NW * (j + (l >> 1))) + (l & 1);
-    runs_of = x * 16 < nk ? max(0, paged_run(c, seq, hk, x)) : 0;
-    wait_dma();
-  };
   // copies of step j's K (kv = 0) or V; past the last step of an empty range, so that
   // every step has as many copies
   auto issue = [&](int kv, int j) __attribute__((always_inline)) {
@@ -529,7 +570,8 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     logit_at = (uint64_t)(a.logits + (size_t)(seq * c.hkv + hk) * a.logit_rows * a.logit_keys);
   }
   if (steps > 0) {
-    find_runs(0);
+    if (!WHOLE) find_runs(seq, first, 0);
+    wait_dma();
 #pragma unroll
     for (int j = 0; j < C::SLOTS; ++j) {
       issue(0, j);
@@ -541,37 +583,50 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     const uint32_t slot = (j % C::SLOTS) * 2 * T::BYTES;
     wait_step(j);
 
-    // S^T = K Q^T, a run of 16 keys at a time
+    // S^T = K Q^T, two runs of 16 keys, all reads ahead of the products
     f32x4 s[RB][2];
-    static_for<2>([&](auto R) {
-      constexpr int run = decltype(R)::value;
-      constexpr int N = F8 ? KS / 2 : KS;
-      u32x4 kr[N];
-      static_for<N>([&](auto I) {
-        constexpr int i = decltype(I)::value;
-        paged_read16<run * T::RUN>((ka ^ (i * 64)) + slot, kr[i]);
-      });
-      static_for<N>([&](auto I) {
-        constexpr int i = decltype(I)::value;
-        row_wait<N - 1 - i>(kr[i]);
-      });
+    constexpr int N = F8 ? KS / 2 : KS;
+    u32x4 kr[N][2];
+    static_for<N>([&](auto I) {
+      constexpr int i = decltype(I)::value;
+      paged_read16<0>((ka ^ (i * 64)) + slot, kr[i][0]);
+      paged_read16<T::RUN>((ka ^ (i * 64)) + slot, kr[i][1]);
+    });
 #pragma unroll
-      for (int b = 0; b < RB; ++b) {
-        s[b][run] = f32x4{0.f, 0.f, 0.f, 0.f};
-        static_for<KS>([&](auto I) {
-          constexpr int ks = decltype(I)::value;
+    for (int b = 0; b < RB; ++b) s[b][0] = s[b][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    static_for<N>([&](auto I) {
+      constexpr int i = decltype(I)::value;
+      row_wait<2 * (N - 1 - i)>(kr[i][0], kr[i][1]);
+#pragma unroll
+      for (int h = 0; h < KS / N; ++h) {
+        const int ks = i * (KS / N) + h;
+#pragma unroll
+        for (int run = 0; run < 2; ++run) {
           bf16x8 x;
-          if constexpr (F8) x = widen8(u32x2{kr[ks / 2][(ks & 1) * 2], kr[ks / 2][(ks & 1) * 2 + 1]});
-          else x = as_bf16x8(kr[ks]);
-          s[b][run] = mfma16(x, qf[b][ks], s[b][run]);
-        });
+          if constexpr (F8) x = widen8(u32x2{kr[i][run][h * 2], kr[i][run][h * 2 + 1]});
+          else x = as_bf16x8(kr[i][run]);
+#pragma unroll
+          for (int b = 0; b < RB; ++b) s[b][run] = mfma16(x, qf[b][ks], s[b][run]);
+        }
       }
     });
-
     const int next = j + C::SLOTS;
-    if ((next & 31) == 0) find_runs(next);  // (the last use of the ones before was V's)
+    if ((next & 31) == 0) {  // (the last use of the ones before was V's)
+      find_runs(seq, first, next);
+      wait_dma();
+    }
     wave_lds_fence();
     issue(0, next);
+
+    // V's reads run beside the softmax
+    wait_step(j);
+    constexpr int VR = F8 ? 1 : 2;  // reads of 16 columns
+    u32x2 vr[DB][VR];
+    static_for<DB>([&](auto I) {
+      constexpr int db = decltype(I)::value;
+      if constexpr (F8) paged_read_tr8((va ^ (db * 16)) + slot, vr[db][0]);
+      else paged_read_tr16<T::RUN>((va ^ (db * 32)) + slot, vr[db][0], vr[db][VR - 1]);
+    });
 
     bf16x8 pf[RB];
 #pragma unroll
@@ -614,18 +669,15 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     }
 
     // O^T += V^T P^T, 16 columns at a time
-    wait_step(j);
     static_for<DB>([&](auto I) {
       constexpr int db = decltype(I)::value;
       bf16x8 x;
       if constexpr (F8) {
-        u32x2 y;
-        paged_read_tr8((va ^ (db * 16)) + slot, y);
-        x = widen8(y);
+        paged_wait<DB - 1 - db>(vr[db][0]);
+        x = widen8(vr[db][0]);
       } else {
-        TrRegs y;
-        paged_read_tr16<T::RUN>((va ^ (db * 32)) + slot, y);
-        x = y.operand();
+        paged_wait<2 * (DB - 1 - db)>(vr[db][0], vr[db][VR - 1]);
+        x = TrRegs{vr[db][0], vr[db][VR - 1]}.operand();
       }
 #pragma unroll
       for (int b = 0; b < RB; ++b) oacc[b][db] = mfma16(x, pf[b], oacc[b][db]);
@@ -672,9 +724,9 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     const size_t pair = pair_of(row0 + r), pairs = (size_t)a.tq * a.hq;
     // (a part hands a NaN sum on as NaN)
     const float lse = tot > 0.f ? (mx + __builtin_log2f(tot)) * kLn2
-                      : at.nparts > 1 ? tot - INFINITY : -INFINITY;
-    if (e == 0 && at.part == 0 && a.cut.max_parts > 1) a.part_n[pair] = at.nparts;
-    if (at.nparts > 1) {
+                      : !WHOLE && at.nparts > 1 ? tot - INFINITY : -INFINITY;
+    if (!WHOLE && e == 0 && at.part == 0 && a.cut.max_parts > 1) a.part_n[pair] = at.nparts;
+    if (!WHOLE && at.nparts > 1) {
       cross_put8(x, a.part_o + (at.part * pairs + pair) * D + e);
       if (e == 0) a.part_lse[at.part * pairs + pair] = lse;
     } else {

@@ -105,16 +105,84 @@ def test_binding_refuses_host_tensors_types_and_shapes():
         P.attn_paged_evict(kp, kp, None, table, lens, table, 5)
 
 
+def hazards_along_branches(body):
+    """isa.lds_wait_hazards along every path of one kernel: a read that is issued in front of
+    a branch may be waited for behind it.  Also the number of LDS reads."""
+    lines = [x.split(";", 1)[0].rstrip() for x in body.splitlines()]
+    lines = [x for x in lines if x.strip() and (re.match(r"^\.LBB\w+:", x) or not x.strip().startswith("."))]
+    at = {x[:-1]: i for i, x in enumerate(lines) if x.endswith(":")}
+    lgkm = [isa.WAIT.match(x) and isa.LGKM.search(x) for x in lines]
+    reads = [isa.LDS_READ.match(x) for x in lines]
+    dest = {i: isa._regs(m.group(2)) for i, m in enumerate(reads) if m}
+    used = [isa._regs(x[m.end():]) if m else isa._regs(x) for x, m in zip(lines, reads)]
+    state = [None] * (len(lines) + 1)  # of the reads in flight: later ones at least
+    state[0] = {}
+    todo, hazards = [0], set()
+    while todo:
+        i = todo.pop()
+        if i >= len(lines):
+            continue
+        x, now = lines[i].strip(), dict(state[i])
+        for r in now:
+            if dest[r] & (used[i] | dest.get(i, set())) and not lgkm[i]:
+                hazards.add((lines[r].strip(), x))
+        if lgkm[i]:
+            n = int(lgkm[i].group(1))
+            now = {r: k for r, k in now.items() if k < n}
+        if x.startswith("ds_"):  # (writes count as well, and end in order with the reads)
+            now = {r: k + 1 for r, k in now.items()}
+        if reads[i]:
+            now[i] = 0
+        to = re.match(r"s_c?branch\w*\s+(\S+)", x)
+        after = [at[to.group(1)]] if to else []
+        if not x.startswith(("s_branch", "s_endpgm")):
+            after.append(i + 1)
+        for j in after:
+            old = state[j]
+            new = dict(now) if old is None else dict(old)
+            for r, k in now.items():
+                new[r] = min(k, new.get(r, k))
+            if new != old:
+                state[j] = new
+                todo.append(j)
+    return sorted(hazards), len(dest)
+
+
 def test_lds_waits_and_no_scratch():
     asm = isa.device_asm(os.path.join(os.path.dirname(isa.SRC), "paged.hip"))
-    # (the reads of the other kernels are the compiler's own, and branch between)
-    asm_reads = re.findall(r"^_Z\w*paged_fwd_kernel\w*:.*?^\s*s_endpgm", asm, re.M | re.S)
-    assert len(asm_reads) >= 12
-    for body in asm_reads:
-        hazards, checked = isa.lds_wait_hazards(body)
-        assert checked >= 12 and not hazards, hazards[:20]
+    kernels = re.findall(r"^_Z\w+:.*?^\.Lfunc_end", asm, re.M | re.S)
+    checked = 0
+    for body in kernels:
+        hazards, reads = hazards_along_branches(body)
+        assert not hazards, (body.split(":")[0], hazards[:10])
+        checked += reads
+    assert checked >= 200 and len(kernels) >= 40
     sizes = re.findall(r"^\s*\.private_segment_fixed_size:\s*(\d+)", asm, re.M)
     assert len(sizes) >= 20 and not any(int(x) for x in sizes)
+
+
+def test_the_walk_follows_branches():
+    """A read whose wait stands behind a branch backwards is covered by it; a path around
+    the wait, and a use in front of it, are found."""
+    body = """_Z1kv:
+.LBB0_1:
+    s_waitcnt lgkmcnt({n})
+    v_mov_b32 v20, v5
+.LBB0_2:
+    {first}
+    ds_read_b128 v[4:7], v1
+    {between}
+    s_cbranch_scc1 .LBB0_1
+    s_endpgm
+"""
+    def found(n=0, first="v_mov_b32 v9, v8", between="v_mov_b32 v9, v8"):
+        return hazards_along_branches(body.format(n=n, first=first, between=between))[0]
+
+    assert not found()
+    assert any("v20" in x[1] for x in found(n=1))
+    assert found(between="v_mov_b32 v9, v6") and found(between="v_mov_b32 v4, v8")
+    assert found(between="s_cbranch_vccz .LBB0_2")
+    assert hazards_along_branches(body)[1] == 1
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
