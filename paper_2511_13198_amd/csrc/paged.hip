@@ -13,6 +13,8 @@ using namespace pdy_host;
 
 namespace {
 
+constexpr int64_t kCUs = 256;
+
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // The pool and its tables, checked.
@@ -105,7 +107,6 @@ pdy_status check_rows(int32_t tq, int32_t n, int32_t max_q, int32_t hq, int32_t 
   return PDY_OK;
 }
 
-constexpr int64_t kCUs = 256;
 constexpr int kMaxParts = 256;
 constexpr int64_t kPartBytes = (int64_t)256 << 20;  // partial results at most
 
@@ -115,7 +116,8 @@ constexpr int64_t kLogitBytes = (int64_t)1 << 30;   // logits left for the weigh
 struct PagedPlan {
   int shape;
   int max_tiles;
-  bool whole;  // an item a workgroup of 8 waves
+  bool whole;  // items are not cut
+  int waves;   // of a workgroup
   pdy::PagedCut cut;
   int64_t wgs;  // a kv head
   int64_t logit_rows, logit_keys;   // (rows 0: no logits are left)
@@ -123,8 +125,22 @@ struct PagedPlan {
   size_t bytes() const { return std::max<size_t>(256, part_o + part_lse + part_n + logits); }
 };
 
+// Sequences of so many keys at most stay whole: the launch that joins parts takes longer than
+// they save.  us cut / whole for a token of 32/8 heads, n sequences of equal lengths and of
+// 1 .. max (evenly over the logarithm), d = 128, bf16:
+//   n = 1: 1,024 8.9 / 8.7, 2,048 9.1 / 12.4;  n = 8: 2,048 18.2 / 15.8 and 9.6 / 8.7, 4,096
+//   34.6 / 45.7 and 10.5 / 12.7;  n = 32: 2,048 55.0 / 49.4 and 13.4 / 12.7, 4,096 99.1 / 96.4 and
+//   15.7 / 19.3;  n = 256: 1,024 (1 ..) 51.6 / 46.5, 2,048 73.6 / 74.9, 4,096 118 / 132
+// e4m3: n = 1: 1,024 9.0 / 8.3, 2,048 9.3 / 11.7;  n = 64: 2,048 56.7 / 51.9 and 17.4 / 16.7, 4,096
+// (1 ..) 22.6 / 26.7;  d = 64: n = 1: 2,048 8.6 / 9.0, 4,096 8.9 / 13.4;  n = 8 .. 32: 4,096 20.8 / 17.2
+// and 9.1 / 8.5, 54.7 / 50.1 and 13.5 / 13.0;  n = 64: 2,048 16.3 / 13.7 (1 ..), 4,096 20.5 / 21.5
+int64_t whole_keys(int64_t pairs, int64_t d) {
+  if (d == 64) return pairs >= 64 && pairs <= kCUs ? 4096 : 2048;
+  return pairs < 64 ? 1024 : 2048;
+}
+
 PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, int64_t d,
-                   bool weigh) {
+                   int64_t row_bytes, bool weigh) {
   PagedPlan p;
   const int64_t g = r.hq / hkv, rows = std::max<int64_t>(1, r.max_q * g);
   p.shape = rows <= 16 ? 0 : rows <= 32 ? 1 : 2;
@@ -136,8 +152,12 @@ PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, in
   p.cut.entries = (int)ceil_div(4 * kCUs, hkv);
   p.cut.max_parts = (int)std::max<int64_t>(
       1, std::min<int64_t>({kMaxParts, ceil_div(max_k, 32) / p.cut.least, kPartBytes / slice}));
-  p.whole = p.shape == 0 && max_k <= 2048 && n * hkv <= kCUs;
+  p.whole = max_k <= whole_keys(n * hkv, d);
   if (p.whole) p.cut.max_parts = 1;
+  // a workgroup a CU at most: 8 waves, where a step is short (us with 4 / 8 for a token of 8
+  // kv heads over 1,024 keys: bf16 of 128 8.7 / 8.7, e4m3 9.2 / 8.3, of 64 7.7 / 6.9; 64 tokens
+  // 49.8 / 51.6, 28.1 / 32.0, 26.7 / 29.4)
+  p.waves = p.shape == 0 && p.whole && n * hkv <= kCUs && row_bytes < 256 ? 8 : 4;
   const bool cut = p.cut.max_parts > 1;
   p.wgs = cut ? items + p.cut.entries + 1 : n * p.max_tiles;
   p.part_o = cut ? align256((size_t)p.cut.max_parts * r.tq * r.hq * d * 4) : 0;
@@ -158,13 +178,15 @@ hipError_t launch_fwd(const pdy::PagedFwdArgs* a, dim3 grid, hipStream_t st) {
   return hipSuccess;
 }
 using LaunchFwd = hipError_t (*)(const pdy::PagedFwdArgs*, dim3, hipStream_t);
-// [d = 64, 128][bf16, e4m3][16, 32, 64 rows; 16: leaving their logits; whole items by 8
-// waves; both]
-constexpr int kShapes = 6;
+// [d = 64, 128][bf16, e4m3][16, 32, 64 rows; 16: leaving their logits; whole items by 4 waves,
+// by 8; both leaving their logits]
+constexpr int kShapes = 8;
 template <int D, bool F8>
 constexpr LaunchFwd kFwdOf[kShapes] = {launch_fwd<D, F8, 1, 4>, launch_fwd<D, F8, 2, 4>,
                                        launch_fwd<D, F8, 4, 4>, launch_fwd<D, F8, 1, 4, true>,
+                                       launch_fwd<D, F8, 1, 4, false, true>,
                                        launch_fwd<D, F8, 1, 8, false, true>,
+                                       launch_fwd<D, F8, 1, 4, true, true>,
                                        launch_fwd<D, F8, 1, 8, true, true>};
 const LaunchFwd* const kFwd[2][2] = {{kFwdOf<64, false>, kFwdOf<64, true>},
                                      {kFwdOf<128, false>, kFwdOf<128, true>}};
@@ -232,8 +254,13 @@ pdy_status attn_paged_write(const void* k, const void* v, const int32_t* cu_seql
   a.scores = scores;
   a.cu = cu_seqlens;
   a.tokens = total_tokens;
+  // tokens of a workgroup: as many as leave 4 of these a CU
+  a.each_log2 = 0;
+  while (a.each_log2 < pdy::kWriteLog2 && total_tokens >> (a.each_log2 + 1) >= 4 * kCUs) ++a.each_log2;
+  const int64_t units = (int64_t)num_heads_kv * head_dim / 8;
+  a.units_inv = (uint32_t)((1ull << 32) / units);
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
-  const dim3 grid((unsigned)ceil_div(total_tokens, 4));
+  const dim3 grid((unsigned)ceil_div(total_tokens, 1 << a.each_log2));
   const hipError_t e = launch_timed(K_PAGED_WRITE, hs, [&] {
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, hs, a); };
     if (head_dim == 64)
@@ -254,7 +281,7 @@ size_t attn_paged_fwd_workspace_size(int32_t total_q, int32_t num_seqs, int32_t 
       (with_scores & ~1) ||
       check_rows(total_q, num_seqs, max_seqlen_q, num_heads_q, num_heads_kv, head_dim, &r) != PDY_OK)
     return 0;
-  return plan_fwd(r, num_seqs, max_seqlen_k, num_heads_kv, head_dim, with_scores).bytes();
+  return plan_fwd(r, num_seqs, max_seqlen_k, num_heads_kv, head_dim, 0, with_scores).bytes();
 }
 
 pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_pages,
@@ -281,7 +308,7 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
       (st = check_ptr(workspace, "workspace")))
     return st;
   if (scores && (st = check_ptr(scores, "scores"))) return st;
-  const PagedPlan p = plan_fwd(r, s.n, s.max_k, s.hkv, s.d, scores != nullptr);
+  const PagedPlan p = plan_fwd(r, s.n, s.max_k, s.hkv, s.d, s.row_bytes(), scores != nullptr);
   if (workspace_bytes < p.bytes())
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, attn_paged_fwd needs %zu",
                 workspace_bytes, p.bytes());
@@ -312,14 +339,17 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
   a.logit_rows = (int)p.logit_rows;
   a.logit_keys = (int)p.logit_keys;
   const int64_t wgs = p.wgs * s.hkv;
-  if (!fits_grid(wgs, p.whole ? 512 : 256) ||
+  if (!fits_grid(wgs, 64 * p.waves) ||
       (scores && (!fits_grid(s.n * s.hkv * ceil_div(s.max_k, 512), 256) || s.n > 65535 || s.hkv > 65535)))
     return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
   hipError_t e = init_paged_kernels();
   if (e != hipSuccess) return hip_fail(e, "kernel attribute setup");
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  int kernel = p.shape;
+  if (p.shape == 0 && p.whole) kernel = (p.logit_rows > 0 ? 6 : 4) + (p.waves == 8);
+  else if (p.logit_rows > 0) kernel = 3;
   e = launch_timed(K_PAGED_FWD, hs, [&] {
-    (void)kFwd[s.d == 128][s.e4m3][p.whole ? (p.logit_rows > 0 ? 5 : 4) : p.logit_rows > 0 ? 3 : p.shape](&a, dim3((unsigned)wgs), hs);
+    (void)kFwd[s.d == 128][s.e4m3][kernel](&a, dim3((unsigned)wgs), hs);
   });
   if (e != hipSuccess) return hip_fail(e, "paged_fwd_kernel launch");
   const bool wide = r.tq * r.hq <= 2 * kCUs && p.cut.max_parts > 16;

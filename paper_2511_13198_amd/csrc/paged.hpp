@@ -65,8 +65,8 @@ __device__ __forceinline__ int paged_seq_of(const int32_t* cu, int n, int t) {
 
 // ---------------------------------------------------------------------------
 // New keys and values into their pages.  Token t of a sequence with nq new tokens and nk
-// keys in use (the new ones among them) is its key nk - nq + t.  A wave per token, 8
-// elements a lane; e4m3 rounds x / scale once, to the nearest (beyond the largest number
+// keys in use (the new ones among them) is its key nk - nq + t.  A workgroup takes 2^each_log2
+// tokens, 8 elements a thread: it loads them, finds the tokens' places, and stores.  e4m3 rounds x / scale once, to the nearest (beyond the largest number
 // to it).
 // ---------------------------------------------------------------------------
 struct PagedWriteArgs {
@@ -77,7 +77,10 @@ struct PagedWriteArgs {
   float* scores;          // NULL: none
   const int32_t* cu;
   int tokens;
+  int each_log2;
+  uint32_t units_inv;  // 2^32 / (hkv D / 8), rounded down
 };
+constexpr int kWriteLog2 = 4;
 
 // 8 bf16 of one 16-byte word as 8 e4m3 of x / s; inv = 1 / s.  The quotient is x inv and a
 // correction by its remainder, which is as exact as the division (a quotient that a rounding
@@ -103,36 +106,55 @@ __device__ __forceinline__ u32x2 paged_e4m3(const u32x4& x, float s, float inv) 
 template <int D, bool F8>
 __global__ void __launch_bounds__(256) paged_write_kernel(PagedWriteArgs a) {
   constexpr int LANES = D / 8;  // of a row
-  constexpr int AHEAD = 2;      // rounds of 64 lanes loaded at a time
-  const int t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (t >= a.tokens) return;
-  const int units = a.c.hkv * LANES, l = __lane_id();
-  const size_t from = (size_t)t * units * 8;
-  int i = -1, j = -1;
-  for (int u0 = 0; u0 < units; u0 += 64 * AHEAD) {
+  constexpr int AHEAD = 4;      // rounds of 256 threads loaded at a time
+  __shared__ int64_t row_of[1 << kWriteLog2];  // row of kv head 0 in the pool; -1: none
+  const PagedCache& c = a.c;
+  const int t0 = blockIdx.x << a.each_log2, count = min(1 << a.each_log2, a.tokens - t0);
+  const int units = c.hkv * LANES, total = count * units;
+  const size_t from = (size_t)t0 * units * 8;
+  for (int u0 = 0; u0 < total; u0 += 256 * AHEAD) {
     u32x4 x[AHEAD][2];
 #pragma unroll
     for (int r = 0; r < AHEAD; ++r) {
-      const int u = u0 + r * 64 + l;
-      if (u < units)
+      const int u = u0 + r * 256 + threadIdx.x;
+      if (u < total)
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv)
           x[r][kv] = *reinterpret_cast<const u32x4*>(a.in[kv] + from + (size_t)u * 8);
     }
     if (u0 == 0) {  // (behind the loads: neither waits for the other)
-      i = paged_seq_of(a.cu, a.c.n, t);
-      if (i >= a.c.n) return;  // behind the last sequence
-      j = paged_len(a.c, i) - (a.cu[i + 1] - t);
-      if (j < 0 || j >= a.c.max_k) return;
+      if (threadIdx.x < 64) {
+        int i = paged_seq_of(a.cu, c.n, t0);
+        const int t = t0 + threadIdx.x;
+        if ((int)threadIdx.x < count) {
+          if (i < c.n && a.cu[i + 1] <= t) {  // of a later sequence: by bisection
+            int hi = c.n;  // cu[i] <= t, and t < cu[hi + 1] or hi = n
+            while (i < hi) {
+              const int mid = (i + hi + 1) >> 1;
+              if (a.cu[mid] <= t) i = mid;
+              else hi = mid - 1;
+            }
+          }
+          int64_t row = -1;
+          if (i < c.n) {
+            const int j = paged_len(c, i) - (a.cu[i + 1] - t);
+            const int run = j >= 0 && j < c.max_k ? paged_run(c, i, 0, j >> 4) : -1;
+            if (run >= 0) row = (int64_t)run * 16 + (j & 15);
+          }
+          row_of[threadIdx.x] = row;
+        }
+      }
+      __syncthreads();
     }
 #pragma unroll
     for (int r = 0; r < AHEAD; ++r) {
-      const int u = u0 + r * 64 + l;
-      if (u >= units) continue;
-      const int h = u / LANES, e = (u % LANES) * 8;
-      const int run = paged_run(a.c, i, h, j >> 4);
-      if (run < 0) continue;
-      const size_t row = (size_t)run * 16 + (j & 15);
+      const int u = u0 + r * 256 + threadIdx.x;
+      if (u >= total) continue;
+      int k = (int)__umulhi((uint32_t)u, a.units_inv);  // u / units, off by at most one
+      if (u - k * units >= units) ++k;
+      const int h = (u - k * units) / LANES, e = (u % LANES) * 8;
+      if (row_of[k] < 0) continue;
+      const size_t row = (size_t)row_of[k] + (size_t)h * c.page;
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         if constexpr (F8) {

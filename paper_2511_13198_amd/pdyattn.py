@@ -712,21 +712,25 @@ def _paged_pool(k_pages, v_pages, page_table, seqlens_k, scores, scales=None):
     """Checked pool and tables: (device, shape of the pages, 1 for e4m3, pointers of the
     scores and of scales, (k_scale, v_scale), where the call takes them)."""
     import torch
-    dev, dtype, shape = k_pages.device, k_pages.dtype, k_pages.shape
-    index, f32 = dev.index, torch.float32
-    if dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+    dev, dtype, shape, i32 = k_pages.device, k_pages.dtype, k_pages.shape, torch.int32
+    index = dev.index
+    e4m3 = 1 if dtype is torch.float8_e4m3fn else 0
+    if not e4m3 and dtype is not torch.bfloat16:
         raise TypeError(f"k_pages must be torch.bfloat16 or torch.float8_e4m3fn, got {dtype}")
-    if not (_fits(k_pages, dtype, 4, index) and _fits(v_pages, dtype, 4, index) and
-            _fits(page_table, torch.int32, 2, index) and _fits(seqlens_k, torch.int32, 1, index)):
+    if not (len(shape) == 4 and v_pages.dtype is dtype and page_table.dtype is i32 and
+            seqlens_k.dtype is i32 and page_table.dim() == 2 and seqlens_k.dim() == 1 and
+            k_pages.is_contiguous() and v_pages.is_contiguous() and page_table.is_contiguous() and
+            seqlens_k.is_contiguous() and k_pages.get_device() == index and
+            v_pages.get_device() == index and page_table.get_device() == index and
+            seqlens_k.get_device() == index):
         _refuse(dev, (k_pages, "k_pages", dtype, 4), (v_pages, "v_pages", dtype, 4),
-                (page_table, "page_table", torch.int32, 2),
-                (seqlens_k, "seqlens_k", torch.int32, 1))
+                (page_table, "page_table", i32, 2), (seqlens_k, "seqlens_k", i32, 1))
     if v_pages.shape != shape:
         raise ValueError("v_pages must have k_pages' shape [pages, Hkv, page_size, d]")
     n = seqlens_k.numel()
     if n < 1 or page_table.shape[0] != n:
         raise ValueError("page_table and seqlens_k must have num_seqs >= 1 rows each")
-    e4m3 = 1 if dtype is torch.float8_e4m3fn else 0
+    f32 = torch.float32
     ks = vs = sc = 0
     k_scale, v_scale = scales or (None, None)
     if e4m3 and scales:
