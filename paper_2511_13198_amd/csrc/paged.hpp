@@ -120,7 +120,8 @@ __global__ void __launch_bounds__(256) paged_write_kernel(PagedWriteArgs a) {
       if (u < total)
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv)
-          x[r][kv] = *reinterpret_cast<const u32x4*>(a.in[kv] + from + (size_t)u * 8);
+          x[r][kv] = __builtin_nontemporal_load(
+              reinterpret_cast<const u32x4*>(a.in[kv] + from + (size_t)u * 8));
     }
     if (u0 == 0) {  // (behind the loads: neither waits for the other)
       if (threadIdx.x < 64) {
@@ -159,10 +160,12 @@ __global__ void __launch_bounds__(256) paged_write_kernel(PagedWriteArgs a) {
       for (int kv = 0; kv < 2; ++kv) {
         if constexpr (F8) {
           const float s = a.scale[kv][h];
-          *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.pages[kv]) + row * D + e) =
-              paged_e4m3(x[r][kv], s, 1.f / s);
+          __builtin_nontemporal_store(
+              paged_e4m3(x[r][kv], s, 1.f / s),
+              reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.pages[kv]) + row * D + e));
         } else {
-          *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.pages[kv]) + row * D + e) = x[r][kv];
+          __builtin_nontemporal_store(
+              x[r][kv], reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.pages[kv]) + row * D + e));
         }
       }
       if (a.scores && e == 0) a.scores[row] = 0.f;
@@ -308,7 +311,15 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedCache& c, const int32_t
 struct PagedPlace {
   PagedSeq s;
   int seq, tile, part, nparts;
+  float steps;  // of all items
 };
+
+// Steps of 32 keys of all sequences, by every wave on its own.
+__device__ __forceinline__ float paged_all_steps(const PagedCache& c) {
+  float sum = 0.f;
+  for (int i = __lane_id(); i < c.n; i += 64) sum += (float)((paged_len(c, i) + 31) >> 5);
+  return wave_sum(sum);
+}
 
 // Entry `entry` of a kv head's list; false past its end.  get(i): sequence i; of(s, tiles,
 // steps): its row tiles, and steps of each.  (wave-uniform)
@@ -399,6 +410,7 @@ __device__ __forceinline__ bool paged_place(const PagedCut& c, int n, int entry,
   }
   auto uni = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
   out.s = PagedSeq{uni(s0.q_lo), uni(s0.nq), uni(s0.nk)};
+  out.steps = sum;
   out.seq = uni(seq);
   out.nparts = uni(np);
   rel = uni(rel);
@@ -420,6 +432,9 @@ struct PagedFwdArgs {
   int causal;
   int max_tiles;  // row tiles of a sequence
   PagedCut cut;
+  // steps of 32 keys of a kv head beyond which K and V do not fit the last-level cache, and
+  // are read past it; -1: they are read through it without a look
+  int stream_steps;
   float scale_log2;
   uint16_t* o;
   float* lse;
@@ -435,13 +450,15 @@ struct PagedFwdArgs {
   int logit_rows, logit_keys;
 };
 
-// One copy of 1 KB into LDS: lane l's 16 bytes at base + voff, zeros from `bytes` on.
+// One copy of 1 KB into LDS: lane l's 16 bytes at base + voff, zeros from `bytes` on; STREAM:
+// past the caches (non-temporal).
+template <bool STREAM>
 __device__ __forceinline__ void paged_copy(uint64_t base, int bytes, uint32_t voff, uint8_t* lds) {
 #if defined(__HIP_DEVICE_COMPILE__)
   const auto rs =
       __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(base), 0, bytes, kBufferFlags);
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)lds, 16,
-                                           voff, 0, 0, 0);
+                                           voff, 0, 0, STREAM ? 2 : 0);
 #endif
 }
 
@@ -479,6 +496,7 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     at.nparts = 1;
     if constexpr (WHOLE) find_runs(at.seq, w, 0);  // (without waiting for the lengths)
     at.s = paged_seq(c, a.cu_q, a.tq, at.seq);
+    at.steps = a.stream_steps >= 0 ? paged_all_steps(c) : 0.f;
   } else if (!paged_place<C::NT>(
                  a.cut, c.n, entry,
                  [&](int i) __attribute__((always_inline)) { return paged_seq(c, a.cu_q, a.tq, i); },
@@ -562,7 +580,7 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
   const int steps = max(0, last - first + NW - 1) / NW;
   // copies of step j's K (kv = 0) or V; past the last step of an empty range, so that
   // every step has as many copies
-  auto issue = [&](int kv, int j) __attribute__((always_inline)) {
+  auto issue = [&](auto Stream, int kv, int j) __attribute__((always_inline)) {
     uint8_t* const to = mine + ((j % C::SLOTS) * 2 + kv) * T::BYTES;
     const uint64_t base = (uint64_t)(kv ? a.v : a.k);
 #pragma unroll
@@ -570,9 +588,11 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
       const int run = __builtin_amdgcn_readlane(runs_of, ((j & 31) * 2) | s);
       const int valid = j < steps ? min(16, nk - (first + NW * j) * 32 - s * 16) : 0;
       const int bytes = __builtin_amdgcn_readfirstlane(max(0, valid) * T::ROW);
+      const uint64_t from = base + (uint64_t)run * T::RUN;
+      uint8_t* const dst = to + s * T::RUN;
 #pragma unroll
       for (int i = 0; i < T::COPIES; ++i)
-        paged_copy(base + (uint64_t)run * T::RUN, bytes, kv_off[kv][i][s], to + s * T::RUN + i * 1024);
+        paged_copy<decltype(Stream)::value>(from, bytes, kv_off[kv][i][s], dst + i * 1024);
     }
   };
   // copies in flight behind a step's K when its products begin, and behind its V; from
@@ -591,122 +611,125 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     logit_off = i16 < row_end - row0 ? (uint32_t)(i16 * a.logit_keys + grp * 4) * 4 : 0x80000000u;
     logit_at = (uint64_t)(a.logits + (size_t)(seq * c.hkv + hk) * a.logit_rows * a.logit_keys);
   }
-  if (steps > 0) {
+  auto all_of = [&](auto Stream) __attribute__((always_inline)) {
+    if (steps <= 0) return;
     if (!WHOLE) find_runs(seq, first, 0);
     wait_dma();
 #pragma unroll
     for (int j = 0; j < C::SLOTS; ++j) {
-      issue(0, j);
-      issue(1, j);
+      issue(Stream, 0, j);
+      issue(Stream, 1, j);
     }
-  }
-  for (int j = 0; j < steps; ++j) {
-    const int k0 = (first + NW * j) * 32;
-    const uint32_t slot = (j % C::SLOTS) * 2 * T::BYTES;
-    wait_step(j);
+    for (int j = 0; j < steps; ++j) {
+      const int k0 = (first + NW * j) * 32;
+      const uint32_t slot = (j % C::SLOTS) * 2 * T::BYTES;
+      wait_step(j);
 
-    // S^T = K Q^T, two runs of 16 keys, all reads ahead of the products
-    f32x4 s[RB][2];
-    constexpr int N = F8 ? KS / 2 : KS;
-    u32x4 kr[N][2];
-    static_for<N>([&](auto I) {
-      constexpr int i = decltype(I)::value;
-      paged_read16<0>((ka ^ (i * 64)) + slot, kr[i][0]);
-      paged_read16<T::RUN>((ka ^ (i * 64)) + slot, kr[i][1]);
-    });
+      // S^T = K Q^T, two runs of 16 keys, all reads ahead of the products
+      f32x4 s[RB][2];
+      constexpr int N = F8 ? KS / 2 : KS;
+      u32x4 kr[N][2];
+      static_for<N>([&](auto I) {
+        constexpr int i = decltype(I)::value;
+        paged_read16<0>((ka ^ (i * 64)) + slot, kr[i][0]);
+        paged_read16<T::RUN>((ka ^ (i * 64)) + slot, kr[i][1]);
+      });
 #pragma unroll
-    for (int b = 0; b < RB; ++b) s[b][0] = s[b][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-    static_for<N>([&](auto I) {
-      constexpr int i = decltype(I)::value;
-      row_wait<2 * (N - 1 - i)>(kr[i][0], kr[i][1]);
+      for (int b = 0; b < RB; ++b) s[b][0] = s[b][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      static_for<N>([&](auto I) {
+        constexpr int i = decltype(I)::value;
+        row_wait<2 * (N - 1 - i)>(kr[i][0], kr[i][1]);
 #pragma unroll
-      for (int h = 0; h < KS / N; ++h) {
-        const int ks = i * (KS / N) + h;
+        for (int h = 0; h < KS / N; ++h) {
+          const int ks = i * (KS / N) + h;
 #pragma unroll
-        for (int run = 0; run < 2; ++run) {
-          bf16x8 x;
-          if constexpr (F8) x = widen8(u32x2{kr[i][run][h * 2], kr[i][run][h * 2 + 1]});
-          else x = as_bf16x8(kr[i][run]);
+          for (int run = 0; run < 2; ++run) {
+            bf16x8 x;
+            if constexpr (F8) x = widen8(u32x2{kr[i][run][h * 2], kr[i][run][h * 2 + 1]});
+            else x = as_bf16x8(kr[i][run]);
 #pragma unroll
-          for (int b = 0; b < RB; ++b) s[b][run] = mfma16(x, qf[b][ks], s[b][run]);
+            for (int b = 0; b < RB; ++b) s[b][run] = mfma16(x, qf[b][ks], s[b][run]);
+          }
         }
+      });
+      const int next = j + C::SLOTS;
+      if ((next & 31) == 0) {  // (the last use of the ones before was V's)
+        find_runs(seq, first, next);
+        wait_dma();
       }
-    });
-    const int next = j + C::SLOTS;
-    if ((next & 31) == 0) {  // (the last use of the ones before was V's)
-      find_runs(seq, first, next);
-      wait_dma();
-    }
-    wave_lds_fence();
-    issue(0, next);
+      wave_lds_fence();
+      issue(Stream, 0, next);
 
-    // V's reads run beside the softmax
-    wait_step(j);
-    constexpr int VR = F8 ? 1 : 2;  // reads of 16 columns
-    u32x2 vr[DB][VR];
-    static_for<DB>([&](auto I) {
-      constexpr int db = decltype(I)::value;
-      if constexpr (F8) paged_read_tr8((va ^ (db * 16)) + slot, vr[db][0]);
-      else paged_read_tr16<T::RUN>((va ^ (db * 32)) + slot, vr[db][0], vr[db][VR - 1]);
-    });
+      // V's reads run beside the softmax
+      wait_step(j);
+      constexpr int VR = F8 ? 1 : 2;  // reads of 16 columns
+      u32x2 vr[DB][VR];
+      static_for<DB>([&](auto I) {
+        constexpr int db = decltype(I)::value;
+        if constexpr (F8) paged_read_tr8((va ^ (db * 16)) + slot, vr[db][0]);
+        else paged_read_tr16<T::RUN>((va ^ (db * 32)) + slot, vr[db][0], vr[db][VR - 1]);
+      });
 
-    bf16x8 pf[RB];
+      bf16x8 pf[RB];
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      if (k0 + 32 > all_end) {
+      for (int b = 0; b < RB; ++b) {
+        if (k0 + 32 > all_end) {
+#pragma unroll
+          for (int run = 0; run < 2; ++run)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (k0 + run * 16 + grp * 4 + r >= end[b]) s[b][run][r] = -INFINITY;
+        }
+        if constexpr (LOGITS)
+#pragma unroll
+          for (int run = 0; run < 2; ++run)
+            paged_store(logit_at, a.logit_rows * a.logit_keys * 4,
+                        logit_off + (uint32_t)(k0 + run * 16) * 4, s[b][run]);
+        float top = -INFINITY;
 #pragma unroll
         for (int run = 0; run < 2; ++run)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (k0 + run * 16 + grp * 4 + r >= end[b]) s[b][run][r] = -INFINITY;
-      }
-      if constexpr (LOGITS)
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[b][run][r]);
+        top = quad_max(top) * scale2;
+        const bool grow = top > m[b] + kRescaleSlack;
+        if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+          const float alpha = grow ? fast_exp2(m[b] - top) : 1.f;
+          m[b] = grow ? top : m[b];
+          lsum[b] *= alpha;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) oacc[b][db] *= alpha;
+        }
+        const float muse = m[b] == -INFINITY ? 0.f : m[b];
 #pragma unroll
         for (int run = 0; run < 2; ++run)
-          paged_store(logit_at, a.logit_rows * a.logit_keys * 4,
-                      logit_off + (uint32_t)(k0 + run * 16) * 4, s[b][run]);
-      float top = -INFINITY;
 #pragma unroll
-      for (int run = 0; run < 2; ++run)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) top = fmaxf(top, s[b][run][r]);
-      top = quad_max(top) * scale2;
-      const bool grow = top > m[b] + kRescaleSlack;
-      if (__builtin_amdgcn_ballot_w64(grow) != 0) {
-        const float alpha = grow ? fast_exp2(m[b] - top) : 1.f;
-        m[b] = grow ? top : m[b];
-        lsum[b] *= alpha;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) oacc[b][db] *= alpha;
+          for (int r = 0; r < 4; ++r) {
+            const float p = fast_exp2(__builtin_fmaf(s[b][run][r], scale2, -muse));
+            lsum[b] += p;
+            pf[b][run * 4 + r] = (__bf16)p;
+          }
       }
-      const float muse = m[b] == -INFINITY ? 0.f : m[b];
-#pragma unroll
-      for (int run = 0; run < 2; ++run)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float p = fast_exp2(__builtin_fmaf(s[b][run][r], scale2, -muse));
-          lsum[b] += p;
-          pf[b][run * 4 + r] = (__bf16)p;
-        }
-    }
 
-    // O^T += V^T P^T, 16 columns at a time
-    static_for<DB>([&](auto I) {
-      constexpr int db = decltype(I)::value;
-      bf16x8 x;
-      if constexpr (F8) {
-        paged_wait<DB - 1 - db>(vr[db][0]);
-        x = widen8(vr[db][0]);
-      } else {
-        paged_wait<2 * (DB - 1 - db)>(vr[db][0], vr[db][VR - 1]);
-        x = TrRegs{vr[db][0], vr[db][VR - 1]}.operand();
-      }
+      // O^T += V^T P^T, 16 columns at a time
+      static_for<DB>([&](auto I) {
+        constexpr int db = decltype(I)::value;
+        bf16x8 x;
+        if constexpr (F8) {
+          paged_wait<DB - 1 - db>(vr[db][0]);
+          x = widen8(vr[db][0]);
+        } else {
+          paged_wait<2 * (DB - 1 - db)>(vr[db][0], vr[db][VR - 1]);
+          x = TrRegs{vr[db][0], vr[db][VR - 1]}.operand();
+        }
 #pragma unroll
-      for (int b = 0; b < RB; ++b) oacc[b][db] = mfma16(x, pf[b], oacc[b][db]);
-    });
-    wave_lds_fence();
-    issue(1, next);
-  }
+        for (int b = 0; b < RB; ++b) oacc[b][db] = mfma16(x, pf[b], oacc[b][db]);
+      });
+      wave_lds_fence();
+      issue(Stream, 1, next);
+    }
+  };
+  if (a.stream_steps >= 0 && at.steps > (float)a.stream_steps) all_of(std::true_type{});
+  else all_of(std::false_type{});
 
   // combine the waves: O, offset and sum of every row through LDS
   wait_dma();
@@ -1303,8 +1326,10 @@ __global__ void __launch_bounds__(256) paged_gather_kernel(PagedEvictArgs a) {
   for (int i = 0; i < 4; ++i) {
     const int64_t src = src_of[threadIdx.x / LANES + i * (256 / LANES)];
     if (src >= 0) {
-      x[i][0] = *reinterpret_cast<const u32x4*>(a.k + src * (LANES * 16) + e);
-      x[i][1] = *reinterpret_cast<const u32x4*>(a.v + src * (LANES * 16) + e);
+      x[i][0] = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x4*>(a.k + src * (LANES * 16) + e));
+      x[i][1] = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x4*>(a.v + src * (LANES * 16) + e));
     }
   }
   float score = 0.f;
@@ -1314,8 +1339,10 @@ __global__ void __launch_bounds__(256) paged_gather_kernel(PagedEvictArgs a) {
   for (int i = 0; i < 4; ++i) {
     const int64_t dst = dst_of[threadIdx.x / LANES + i * (256 / LANES)];
     if (dst >= 0) {
-      *reinterpret_cast<u32x4*>(a.k + dst * (LANES * 16) + e) = x[i][0];
-      *reinterpret_cast<u32x4*>(a.v + dst * (LANES * 16) + e) = x[i][1];
+      __builtin_nontemporal_store(x[i][0],
+                                  reinterpret_cast<u32x4*>(a.k + dst * (LANES * 16) + e));
+      __builtin_nontemporal_store(x[i][1],
+                                  reinterpret_cast<u32x4*>(a.v + dst * (LANES * 16) + e));
     }
   }
   if (mine) a.scores[dst_of[threadIdx.x]] = score;
