@@ -904,8 +904,10 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedMergeArgs a) {
 // ---------------------------------------------------------------------------
 
 // From the logits that the attention kernel left (up to 16 rows a sequence and kv head), in
-// one launch with the joining of parts: a workgroup past those that join takes 1,024 keys
-// of a sequence and kv head, and joins the parts' LSE of its rows itself.
+// one launch with the joining of parts: a workgroup past those that join takes 4,096 keys
+// of a sequence and kv head, and joins the parts' LSE of its rows itself.  (Workgroups start
+// at about 440 a microsecond: with 1,024 keys each, the 4,608 of 64 sequences of up to 8,192 keys
+// and 8 kv heads had all started after 10.5 us, of 14.)
 struct PagedJoinArgs {
   PagedMergeArgs m;
   int merge_blocks;
@@ -918,7 +920,7 @@ struct PagedJoinArgs {
   float* scores;
 };
 
-constexpr int kWeighKeys = 1024;  // of a workgroup, 4 a thread
+constexpr int kWeighKeys = 4096;  // of a workgroup, 4 a thread at a time
 
 template <int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(PagedJoinArgs a) {
@@ -937,19 +939,27 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedJoinArgs a) {
   const int nq = min(max(a.m.cu_q[seq + 1], q_lo), a.m.tq) - q_lo;
   const int rows = min(nq * a.g, a.logit_rows);
   if (j0 >= nk || rows == 0) return;
-  const int j = j0 + threadIdx.x * 4;  // this thread's 4 keys
-  const float* const from = a.logits + (size_t)item * a.logit_rows * a.logit_keys + j;
-  constexpr int AHEAD = 4;
-  f32x4 x[AHEAD], old = {0.f, 0.f, 0.f, 0.f};
-  int run = -1;
-  if (j < nk) {  // (loaded while the rows' LSE are)
+  constexpr int AHEAD = 4;  // rows
+  struct Keys {  // 4 of this thread
+    int j, run;
+    f32x4 x[AHEAD], old;
+  };
+  const float* const item_logits = a.logits + (size_t)item * a.logit_rows * a.logit_keys;
+  auto load = [&](int i, Keys& k) __attribute__((always_inline)) {
+    k.j = j0 + i * 1024 + threadIdx.x * 4;
+    k.run = -1;
+    if (k.j < nk) {
 #pragma unroll
-    for (int r = 0; r < AHEAD; ++r)
-      x[r] = *reinterpret_cast<const f32x4*>(from + (size_t)min(r, rows - 1) * a.logit_keys);
-    run = paged_run(c, seq, hk, j >> 4);
-  }
-  float* const to = a.scores + (size_t)max(run, 0) * 16 + (j & 15);
-  if (run >= 0) old = *reinterpret_cast<const f32x4*>(to);
+      for (int r = 0; r < AHEAD; ++r)
+        k.x[r] = *reinterpret_cast<const f32x4*>(
+            item_logits + (size_t)min(r, rows - 1) * a.logit_keys + k.j);
+      k.run = paged_run(c, seq, hk, k.j >> 4);
+    }
+    if (k.run >= 0)
+      k.old = *reinterpret_cast<const f32x4*>(a.scores + (size_t)k.run * 16 + (k.j & 15));
+  };
+  Keys keys[2];
+  load(0, keys[0]);  // (while the rows' LSE are joined)
   const size_t pairs = (size_t)a.m.tq * a.m.hq;
   for (int r = w; r < rows; r += 4) {
     const int t = q_lo + r / a.g, h = hk * a.g + r % a.g;
@@ -975,28 +985,35 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedJoinArgs a) {
     if (l == 0) lse2[r] = z;
   }
   __syncthreads();
-  if (run < 0) return;
   const float scale2 = a.scale_log2 * (a.k_scale ? a.k_scale[hk] : 1.f);
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int r0 = 0; r0 < rows; r0 += AHEAD) {
+  static_for<kWeighKeys / 1024>([&](auto I) {
+    constexpr int i = decltype(I)::value;
+    if (j0 + i * 1024 >= nk) return;  // uniform
+    if constexpr ((i + 1) * 1024 < kWeighKeys) load(i + 1, keys[(i + 1) & 1]);
+    Keys& k = keys[i & 1];
+    if (k.run < 0) return;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int r0 = 0; r0 < rows; r0 += AHEAD) {
 #pragma unroll
-    for (int r = 0; r < AHEAD; ++r) {
-      const float z = r0 + r < rows ? lse2[r0 + r] : -INFINITY;
-      if (z > -INFINITY)
+      for (int r = 0; r < AHEAD; ++r) {
+        const float z = r0 + r < rows ? lse2[r0 + r] : -INFINITY;
+        if (z > -INFINITY)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += fast_exp2(__builtin_fmaf(x[r][e], scale2, -z));
+          for (int e = 0; e < 4; ++e) sum[e] += fast_exp2(__builtin_fmaf(k.x[r][e], scale2, -z));
+      }
+      if (r0 + AHEAD < rows)
+#pragma unroll
+        for (int r = 0; r < AHEAD; ++r)
+          k.x[r] = *reinterpret_cast<const f32x4*>(
+              item_logits + (size_t)min(r0 + AHEAD + r, rows - 1) * a.logit_keys + k.j);
     }
-    if (r0 + AHEAD < rows)
-#pragma unroll
-      for (int r = 0; r < AHEAD; ++r)
-        x[r] = *reinterpret_cast<const f32x4*>(
-            from + (size_t)min(r0 + AHEAD + r, rows - 1) * a.logit_keys);
-  }
-  if (j + 4 <= nk) {
-    *reinterpret_cast<f32x4*>(to) = old + sum;
-  } else {
-    for (int e = 0; e < nk - j; ++e) to[e] = old[e] + sum[e];
-  }
+    float* const to = a.scores + (size_t)k.run * 16 + (k.j & 15);
+    if (k.j + 4 <= nk) {
+      *reinterpret_cast<f32x4*>(to) = k.old + sum;
+    } else {
+      for (int e = 0; e < nk - k.j; ++e) to[e] = k.old[e] + sum[e];
+    }
+  });
 }
 
 // From the keys again, where rows are many: a wave holds 16 RB rows, and takes runs of 16
@@ -1042,7 +1059,8 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
     const uint8_t* const kp = static_cast<const uint8_t*>(a.k) + (size_t)run * T::RUN + i16 * T::ROW;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
-      k[ks] = *reinterpret_cast<const Raw*>(kp + (ks * 32 + grp * 8) * (F8 ? 1 : 2));
+      k[ks] = __builtin_nontemporal_load(
+          reinterpret_cast<const Raw*>(kp + (ks * 32 + grp * 8) * (F8 ? 1 : 2)));
   };
   float sum[kWeighRuns][4];
 #pragma unroll
@@ -1070,12 +1088,14 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
                    ? (a.causal ? min(nk, t + nk - nq + 1) : nk) - grp * 4 : 0;
       lse2[b] = lse * kLog2e;
     }
-    Raw kr[2][KS];
-    load(0, kr[0]);
+    constexpr int AHEAD = 4;  // runs in flight
+    Raw kr[AHEAD][KS];
+#pragma unroll
+    for (int x = 0; x < AHEAD - 1; ++x) load(x, kr[x]);
     static_for<kWeighRuns>([&](auto I) {
-      constexpr int x = decltype(I)::value, cur = x & 1;
+      constexpr int x = decltype(I)::value, cur = x % AHEAD;
       if (x >= count) return;  // uniform
-      if constexpr (x + 1 < kWeighRuns) load(x + 1, kr[cur ^ 1]);
+      if constexpr (x + AHEAD - 1 < kWeighRuns) load(x + AHEAD - 1, kr[(x + AHEAD - 1) % AHEAD]);
       bf16x8 kf[KS];
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
