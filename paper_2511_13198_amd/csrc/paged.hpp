@@ -1017,7 +1017,8 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedJoinArgs a) {
 }
 
 // From the keys again, where rows are many: a wave holds 16 RB rows, and takes runs of 16
-// keys, the next one loaded while one is worked on.
+// keys, some loaded while one is worked on.  S = Q K^T here, a key per lane of 16, so that a
+// key's rows are in its four lanes' registers, and the sum over them is joined once.
 struct PagedWeighArgs {
   PagedCache c;
   const uint16_t* q;
@@ -1032,7 +1033,7 @@ struct PagedWeighArgs {
   float* scores;
 };
 
-constexpr int kWeighRuns = 8;  // of a wave
+constexpr int kWeighRuns = 16;  // of a wave
 
 template <int D, bool F8, int RB>
 __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
@@ -1062,31 +1063,38 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
       k[ks] = __builtin_nontemporal_load(
           reinterpret_cast<const Raw*>(kp + (ks * 32 + grp * 8) * (F8 ? 1 : 2)));
   };
-  float sum[kWeighRuns][4];
+  float sum[kWeighRuns];
 #pragma unroll
-  for (int x = 0; x < kWeighRuns; ++x)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sum[x][e] = 0.f;
+  for (int x = 0; x < kWeighRuns; ++x) sum[x] = 0.f;
   for (int r0 = 0; r0 < rows; r0 += 16 * RB) {
     bf16x8 qf[RB][KS];
-    float lse2[RB];
-    int end[RB];
+    float lse2[RB][4];
+    int end[RB][4], all_end = 0x7fffffff;  // of the lane's rows, and seen by all of them
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-      const int r = min(r0 + b * 16 + i16, rows - 1);
-      int t = r;
-      if (a.g > 1) {
-        t = (int)__umulhi((uint32_t)r, a.g_inv);
-        t = r - t * a.g >= a.g ? t + 1 : t;
-      }
-      const int h = hk * a.g + (r - t * a.g);
+      auto place = [&](int r, int& t, int& h) __attribute__((always_inline)) {
+        t = r;
+        if (a.g > 1) {
+          t = (int)__umulhi((uint32_t)r, a.g_inv);
+          t = r - t * a.g >= a.g ? t + 1 : t;
+        }
+        h = hk * a.g + (r - t * a.g);
+      };
+      int t, h;
+      place(min(r0 + b * 16 + i16, rows - 1), t, h);
       const uint16_t* const qp = a.q + ((size_t)(q_lo + t) * a.hq + h) * D + grp * 8;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) qf[b][ks] = load_bf16x8(qp + ks * 32, true);
-      const float lse = a.lse[(size_t)h * a.tq + q_lo + t];
-      end[b] = r0 + b * 16 + i16 < rows && lse > -INFINITY
-                   ? (a.causal ? min(nk, t + nk - nq + 1) : nk) - grp * 4 : 0;
-      lse2[b] = lse * kLog2e;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = r0 + b * 16 + grp * 4 + e;
+        place(min(r, rows - 1), t, h);
+        const float lse = a.lse[(size_t)h * a.tq + q_lo + t];
+        const bool ok = r < rows && lse > -INFINITY;
+        end[b][e] = ok ? (a.causal ? min(nk, t + nk - nq + 1) : nk) : 0;
+        lse2[b][e] = ok ? lse * kLog2e : 0.f;
+        all_end = min(all_end, end[b][e]);
+      }
     }
     constexpr int AHEAD = 4;  // runs in flight
     Raw kr[AHEAD][KS];
@@ -1102,30 +1110,27 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
         if constexpr (F8) kf[ks] = widen8(kr[cur][ks]);
         else kf[ks] = as_bf16x8(kr[cur][ks]);
       }
-      const int j0 = (first + x) * 16;
+      const int j = (first + x) * 16 + i16;
+      const bool masked = __builtin_amdgcn_ballot_w64((first + x + 1) * 16 > all_end) != 0;
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = mfma16(kf[ks], qf[b][ks], s);
+        for (int ks = 0; ks < KS; ++ks) s = mfma16(qf[b][ks], kf[ks], s);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          sum[x][e] += j0 + e < end[b] ? fast_exp2(__builtin_fmaf(s[e], scale2, -lse2[b])) : 0.f;
+        for (int e = 0; e < 4; ++e) {
+          const float p = fast_exp2(__builtin_fmaf(s[e], scale2, -lse2[b][e]));
+          sum[x] += !masked || j < end[b][e] ? p : 0.f;
+        }
       }
     });
   }
-  // over the 16 rows of a block: lane e of each 16 gets key e's sum
 #pragma unroll
   for (int x = 0; x < kWeighRuns; ++x) {
     if (x >= count) return;  // uniform
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int off = 8; off > 0; off >>= 1) sum[x][e] += __shfl_xor(sum[x][e], off);
-    const float own = i16 == 0 ? sum[x][0] : i16 == 1 ? sum[x][1] : i16 == 2 ? sum[x][2] : sum[x][3];
+    const float all = quad_sum(sum[x]);
     const int run = __builtin_amdgcn_readlane(runs_of, x);
-    if (run >= 0 && i16 < 4 && (first + x) * 16 + grp * 4 + i16 < nk)
-      a.scores[(size_t)run * 16 + grp * 4 + i16] += own;
+    if (run >= 0 && grp == 0 && (first + x) * 16 + i16 < nk) a.scores[(size_t)run * 16 + i16] += all;
   }
 }
 
