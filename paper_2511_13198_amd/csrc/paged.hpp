@@ -595,12 +595,14 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
         paged_copy<decltype(Stream)::value>(from, bytes, kv_off[kv][i][s], dst + i * 1024);
     }
   };
-  // copies in flight behind a step's K when its products begin, and behind its V; from
-  // step SLOTS on, the stores of the logits of as many steps too
+  // What is in flight behind a step's K when its products begin, and behind its V when these
+  // are read: (2 SLOTS - 1) tiles' copies, and the stores of logits since the step's K were
+  // issued (in front of those of their step) or its V (behind them); before step SLOTS
+  // these are fewer, and not counted.
   constexpr int FLIGHT = (2 * C::SLOTS - 1) * 2 * T::COPIES;
-  constexpr int STORES = LOGITS ? 2 * C::SLOTS : 0;
-  auto wait_step = [&](int j) __attribute__((always_inline)) {
-    if (LOGITS && j >= C::SLOTS) wait_dma_n<FLIGHT + STORES>();
+  auto wait_step = [&](auto V, int j) __attribute__((always_inline)) {
+    constexpr int stores = LOGITS ? 2 * (decltype(V)::value ? C::SLOTS - 1 : C::SLOTS) : 0;
+    if (stores > 0 && j >= C::SLOTS) wait_dma_n<FLIGHT + stores>();
     else wait_dma_n<FLIGHT>();
   };
   // (rows that are none lie behind the end of the buffer)
@@ -623,7 +625,7 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     for (int j = 0; j < steps; ++j) {
       const int k0 = (first + NW * j) * 32;
       const uint32_t slot = (j % C::SLOTS) * 2 * T::BYTES;
-      wait_step(j);
+      wait_step(std::false_type{}, j);
 
       // S^T = K Q^T, two runs of 16 keys, all reads ahead of the products
       f32x4 s[RB][2];
@@ -661,7 +663,7 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
       issue(Stream, 0, next);
 
       // V's reads run beside the softmax
-      wait_step(j);
+      wait_step(std::true_type{}, j);
       constexpr int VR = F8 ? 1 : 2;  // reads of 16 columns
       u32x2 vr[DB][VR];
       static_for<DB>([&](auto I) {
@@ -1033,7 +1035,7 @@ struct PagedWeighArgs {
   float* scores;
 };
 
-constexpr int kWeighRuns = 16;  // of a wave
+constexpr int kWeighRuns = 8;  // of a wave
 
 template <int D, bool F8, int RB>
 __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
@@ -1063,10 +1065,17 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
       k[ks] = __builtin_nontemporal_load(
           reinterpret_cast<const Raw*>(kp + (ks * 32 + grp * 8) * (F8 ? 1 : 2)));
   };
-  float sum[kWeighRuns];
+  float sum[kWeighRuns], old[kWeighRuns];  // (lanes of a key: the same)
 #pragma unroll
-  for (int x = 0; x < kWeighRuns; ++x) sum[x] = 0.f;
+  for (int x = 0; x < kWeighRuns; ++x) {
+    sum[x] = 0.f;
+    old[x] = a.scores[(size_t)max(0, __builtin_amdgcn_readlane(runs_of, x)) * 16 + i16];
+  }
   for (int r0 = 0; r0 < rows; r0 += 16 * RB) {
+    constexpr int AHEAD = 4;  // runs in flight
+    Raw kr[AHEAD][KS];
+#pragma unroll
+    for (int x = 0; x < AHEAD - 1; ++x) load(x, kr[x]);
     bf16x8 qf[RB][KS];
     float lse2[RB][4];
     int end[RB][4], all_end = 0x7fffffff;  // of the lane's rows, and seen by all of them
@@ -1096,13 +1105,9 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
         all_end = min(all_end, end[b][e]);
       }
     }
-    constexpr int AHEAD = 4;  // runs in flight
-    Raw kr[AHEAD][KS];
-#pragma unroll
-    for (int x = 0; x < AHEAD - 1; ++x) load(x, kr[x]);
     static_for<kWeighRuns>([&](auto I) {
+      // (runs past the last are the last again, and masked: no branch parts the loads)
       constexpr int x = decltype(I)::value, cur = x % AHEAD;
-      if (x >= count) return;  // uniform
       if constexpr (x + AHEAD - 1 < kWeighRuns) load(x + AHEAD - 1, kr[(x + AHEAD - 1) % AHEAD]);
       bf16x8 kf[KS];
 #pragma unroll
@@ -1127,10 +1132,10 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
   }
 #pragma unroll
   for (int x = 0; x < kWeighRuns; ++x) {
-    if (x >= count) return;  // uniform
     const float all = quad_sum(sum[x]);
     const int run = __builtin_amdgcn_readlane(runs_of, x);
-    if (run >= 0 && grp == 0 && (first + x) * 16 + i16 < nk) a.scores[(size_t)run * 16 + i16] += all;
+    if (run >= 0 && grp == 0 && (first + x) * 16 + i16 < nk)
+      a.scores[(size_t)run * 16 + i16] = old[x] + all;
   }
 }
 

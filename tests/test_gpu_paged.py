@@ -69,6 +69,40 @@ def test_attention_and_weights(case, e4m3):
     assert pg.same_bits(c.scores[~live], before[~live])
 
 
+@pytest.mark.parametrize("e4m3,d", [(False, 64), (False, 128), (True, 64), (True, 128)])
+@pytest.mark.parametrize("n,most", [(40, 9000), (6, 1000), (300, 1000)])
+def test_attention_is_the_same_again_and_beside_the_weights(n, most, e4m3, d):
+    """Bit for bit, while the memory is busy: in parts, whole, by 4 and 8 waves."""
+    lens = [(977 * i) % most + 1 for i in range(n)]
+    c = pg.Cache([1], 8, d, 16, e4m3, "cuda")
+    used = [-(-x // 16) for x in lens]
+    g = torch.Generator(device="cuda").manual_seed(3)
+    shape = (sum(used), 8, 16, d)
+    for name in ("k", "v"):
+        x = torch.randn(shape, generator=g, device="cuda")
+        setattr(c, name, (x * 50).clamp(-448, 448).to(pg.E4M3) if e4m3 else x.to(torch.bfloat16))
+    order = torch.randperm(sum(used), generator=g, device="cuda").int()
+    c.table = torch.zeros((n, max(used)), dtype=torch.int32, device="cuda")
+    at = 0
+    for i, x in enumerate(used):
+        c.table[i, :x] = order[at:at + x]
+        at += x
+    c.lens, c.len = lens, torch.tensor(lens, dtype=torch.int32, device="cuda")
+    c.scores = torch.zeros(shape[:3], device="cuda")
+    q, cuq = pg.queries([1] * n, 32, d, "cuda")
+    first = run(c, q, cuq, [1] * n, True)
+    runs = [run(c, q, cuq, [1] * n, True, scores=c.scores if i % 2 else None) for i in range(30)]
+    for o, lse in runs:
+        assert torch.equal(o, first[0]) and torch.equal(lse, first[1])
+    again = torch.zeros_like(c.scores)
+    for _ in range(15):
+        run(c, q, cuq, [1] * n, True, scores=again)
+    assert torch.equal(again, c.scores)
+    # a row's weights are 1 together
+    total = 15.0 * 32 * n
+    assert abs(float(again.double().sum()) - total) < 1e-4 * total
+
+
 WRITE = [
     ([1], [1], 1, 64, 16), ([1, 1, 1], [700, 16, 17], 8, 128, 16), ([3, 0, 5, 1], [3, 9, 900, 48], 3, 64, 48),
     ([300, 1, 77], [1000, 1, 77], 4, 128, 80), ([9, 2], [4, 2], 2, 128, 32),  # tokens in front of key 0
