@@ -113,7 +113,7 @@ pdy_status check_rows(int32_t tq, int32_t n, int32_t max_q, int32_t hq, int32_t 
 // to 2,048 of 2 heads, 75 MB, three such caches in turn 22 / 34.
 constexpr int64_t kCachedBytes = (int64_t)128 << 20;
 constexpr int kMaxParts = 256;
-constexpr int64_t kPartBytes = (int64_t)256 << 20;  // partial results at most
+constexpr int64_t kPartBytes = (int64_t)64 << 20;   // partial results at most
 
 constexpr int64_t kLogitBytes = (int64_t)1 << 30;   // logits left for the weights at most
 
@@ -163,7 +163,8 @@ PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, in
   if (p.shape == 2 && d == 128) entries = 8 * items * hkv <= 5 * kCUs ? kCUs - items * hkv : kCUs;
   p.cut.entries = (int)ceil_div(entries, hkv);
   p.cut.max_parts = (int)std::max<int64_t>(
-      1, std::min<int64_t>({kMaxParts, ceil_div(max_k, 32) / p.cut.least, kPartBytes / slice}));
+      1, std::min<int64_t>({kMaxParts, p.cut.entries + 1, ceil_div(max_k, 32) / p.cut.least,
+                            kPartBytes / slice}));
   p.whole = max_k <= whole_keys(n * hkv, d);
   if (p.whole) p.cut.max_parts = 1;
   // a workgroup a CU at most: 8 waves, where a step is short (us with 4 / 8 for a token of 8

@@ -314,11 +314,13 @@ struct PagedPlace {
   float steps;  // of all items
 };
 
-// Steps of 32 keys of all sequences, by every wave on its own.
+// Steps of 32 keys of all sequences, by every wave on its own (of more than 1,024 sequences
+// by the first).
 __device__ __forceinline__ float paged_all_steps(const PagedCache& c) {
+  const int n = min(c.n, 1024);
   float sum = 0.f;
-  for (int i = __lane_id(); i < c.n; i += 64) sum += (float)((paged_len(c, i) + 31) >> 5);
-  return wave_sum(sum);
+  for (int i = __lane_id(); i < n; i += 64) sum += (float)((paged_len(c, i) + 31) >> 5);
+  return wave_sum(sum) * ((float)c.n / (float)n);
 }
 
 // Entry `entry` of a kv head's list; false past its end.  get(i): sequence i; of(s, tiles,

@@ -744,7 +744,7 @@ def _paged_pool(k_pages, v_pages, page_table, seqlens_k, scores, scales=None):
     elif k_scale is not None or v_scale is not None:
         raise ValueError("k_scale and v_scale are of an e4m3 cache (a bf16 one has none)")
     if scores is not None:
-        if not _fits(scores, f32, 3, index):
+        if not (scores.dtype is f32 and scores.is_contiguous() and scores.get_device() == index):
             _refuse(dev, (scores, "scores", f32, 3))
         if scores.shape != shape[:3]:
             raise ValueError("scores must be [pages, Hkv, page_size]")
@@ -762,19 +762,21 @@ def attn_paged_write(k, v, k_pages, v_pages, page_table, cu_seqlens, seqlens_k, 
     import torch
     dev, shape, e4m3, sc, ks, vs = _paged_pool(k_pages, v_pages, page_table, seqlens_k, scores,
                                                (k_scale, v_scale))
-    index, (pages, hkv, page, d) = dev.index, shape
-    if not (_fits(k, torch.bfloat16, 3, index) and _fits(v, torch.bfloat16, 3, index) and
-            _fits(cu_seqlens, torch.int32, 1, index)):
-        _refuse(dev, (k, "k", torch.bfloat16, 3), (v, "v", torch.bfloat16, 3),
-                (cu_seqlens, "cu_seqlens", torch.int32, 1))
-    T, n = k.shape[0], seqlens_k.numel()
-    if k.shape != (T, hkv, d) or v.shape != k.shape:
+    index, (pages, hkv, page, d), bf16, i32 = dev.index, shape, torch.bfloat16, torch.int32
+    if not (k.dtype is bf16 and v.dtype is bf16 and cu_seqlens.dtype is i32 and
+            k.is_contiguous() and v.is_contiguous() and cu_seqlens.is_contiguous() and
+            k.get_device() == index and v.get_device() == index and
+            cu_seqlens.get_device() == index):
+        _refuse(dev, (k, "k", bf16, 3), (v, "v", bf16, 3), (cu_seqlens, "cu_seqlens", i32, 1))
+    rows = k.shape
+    T, (n, width) = rows[0], page_table.shape
+    if rows != (T, hkv, d) or v.shape != rows:
         raise ValueError("k and v must be [T, Hkv, d] with the pages' Hkv and d")
-    if cu_seqlens.numel() != n + 1:
+    if cu_seqlens.shape != (n + 1,):
         raise ValueError("cu_seqlens must have num_seqs + 1 offsets")
     _launch("attn_paged_write", dev, k.data_ptr(), v.data_ptr(), cu_seqlens.data_ptr(),
-            page_table.data_ptr(), seqlens_k.data_ptr(), ks, vs, n, T, pages, page,
-            page_table.shape[1], hkv, d, e4m3, k_pages.data_ptr(), v_pages.data_ptr(), sc)
+            page_table.data_ptr(), seqlens_k.data_ptr(), ks, vs, n, T, pages, page, width, hkv, d,
+            e4m3, k_pages.data_ptr(), v_pages.data_ptr(), sc)
 
 
 def attn_paged_fwd(q, k_pages, v_pages, page_table, cu_seqlens_q, seqlens_k,
