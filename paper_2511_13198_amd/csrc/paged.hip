@@ -82,6 +82,12 @@ pdy::PagedCache cache_of(const PagedSizes& s, const int32_t* table, const int32_
                          (int)s.max_k, (int)s.hkv, (int)runs, (uint32_t)((1ull << 32) / runs)};
 }
 
+// K of a head that an eviction keeps, up to which (and a workgroup a CU) one launch selects
+// and copies: us of two launches / one, 8 kv heads, d = 128, bf16: 300 keys to 100 of 1 sequence
+// 10.2 / 9.0, of 4 10.9 / 9.3, of 16 13.2 / 10.7, of 64 22.2 / 22.8; 1,000 to 250 10.4 / 10.4, 11.8 / 11.5,
+// 14.7 / 15.3; to 500 10.6 / 13.5, 13.2 / 16.8, 20.3 / 22.8.
+constexpr int64_t kFusedBytes = 48 << 10;
+
 // Whether a grid's threads can be counted in 32 bits, as a launch's are.
 bool fits_grid(int64_t wgs, int threads) { return wgs * threads < (int64_t)1 << 32; }
 
@@ -463,29 +469,43 @@ pdy_status attn_paged_evict(void* k_pages, void* v_pages, float* scores, const i
   a.kept = kept;
   a.new_len = new_lens;
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  // the smallest number of keys a thread that holds the longest sequence (and up to 3 in front
+  // of its first)
+  const int64_t quads = ceil_div(s.max_k + 3, 4 * pdy::kSelectThreads);
+  const int per = quads <= 1 ? 0 : quads <= 4 ? 1 : quads <= 8 ? 2 : 3;
+  // Few rows are copied by the workgroups that selected them, not in a launch of its own.
+  // (Where the new lengths are written over the old, these are read until the end.)
+  const int64_t gap = reinterpret_cast<const char*>(new_lens) - reinterpret_cast<const char*>(seqlens_k);
+  const bool fused = per <= 1 && most * s.row_bytes() <= kFusedBytes && s.n * s.hkv <= kCUs &&
+                     (gap >= 4 * s.n || -gap >= 4 * s.n);
+  const int lanes = s.row_bytes() == 64 ? 0 : s.row_bytes() == 128 ? 1 : 2;
   hipError_t e = launch_timed(K_PAGED_SELECT, hs, [&] {
-    const dim3 grid((unsigned)(s.n * s.hkv));
-    auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, grid, dim3(pdy::kSelectThreads), 0, hs, a);
-    };
-    // the smallest number of keys a thread that holds the longest sequence (and up to 3 in
-    // front of its first)
-    const int64_t quads = ceil_div(s.max_k + 3, 4 * pdy::kSelectThreads);
-    if (quads <= 1) go(pdy::paged_select_kernel<1>);
-    else if (quads <= 4) go(pdy::paged_select_kernel<4>);
-    else if (quads <= 8) go(pdy::paged_select_kernel<8>);
-    else go(pdy::paged_select_kernel<0>);
+    const dim3 grid((unsigned)(s.n * s.hkv)), block(pdy::kSelectThreads);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, hs, a); };
+    if (fused && per == 0)
+      lanes == 0   ? go(pdy::paged_select_kernel<1, 4>)
+      : lanes == 1 ? go(pdy::paged_select_kernel<1, 8>)
+                   : go(pdy::paged_select_kernel<1, 16>);
+    else if (fused)
+      lanes == 0   ? go(pdy::paged_select_kernel<4, 4>)
+      : lanes == 1 ? go(pdy::paged_select_kernel<4, 8>)
+                   : go(pdy::paged_select_kernel<4, 16>);
+    else if (per == 0) go(pdy::paged_select_kernel<1, 0>);
+    else if (per == 1) go(pdy::paged_select_kernel<4, 0>);
+    else if (per == 2) go(pdy::paged_select_kernel<8, 0>);
+    else go(pdy::paged_select_kernel<0, 0>);
   });
   if (e != hipSuccess) return hip_fail(e, "paged_select_kernel launch");
+  if (fused) return PDY_OK;
   e = launch_timed(K_PAGED_GATHER, hs, [&] {
     auto go = [&](auto kernel, int rows) {
       const dim3 grid((unsigned)std::max<int64_t>(1, ceil_div(most, rows)), (unsigned)s.hkv,
                       (unsigned)s.n);
       hipLaunchKernelGGL(kernel, grid, dim3(256), 0, hs, a);
     };
-    if (s.row_bytes() == 64) go(pdy::paged_gather_kernel<4>, pdy::kGatherRows<4>);
-    else if (s.row_bytes() == 128) go(pdy::paged_gather_kernel<8>, pdy::kGatherRows<8>);
-    else go(pdy::paged_gather_kernel<16>, pdy::kGatherRows<16>);
+    if (lanes == 0) go(pdy::paged_gather_kernel<4>, pdy::kGatherRows<4, 256>);
+    else if (lanes == 1) go(pdy::paged_gather_kernel<8>, pdy::kGatherRows<8, 256>);
+    else go(pdy::paged_gather_kernel<16>, pdy::kGatherRows<16, 256>);
   });
   if (e != hipSuccess) return hip_fail(e, "paged_gather_kernel launch");
   return PDY_OK;

@@ -1171,13 +1171,69 @@ __device__ __forceinline__ uint32_t paged_order(float x) {
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048;
 
+// Rows j0 .. of sequence and head to their new places, by THREADS threads, LANES lanes of 16
+// bytes a row: the workgroup finds the places of 4 THREADS / LANES rows, then every thread
+// copies 4 rows' chunks of K and V, all loaded before the first is stored.
+template <int LANES, int THREADS>
+constexpr int kGatherRows = 4 * THREADS / LANES;
+
+template <int LANES, int THREADS>
+__device__ __forceinline__ void paged_gather(const PagedEvictArgs& a, int seq, int hk, int j0, int n) {
+  constexpr int ROWS = kGatherRows<LANES, THREADS>, STEP = THREADS / LANES;
+  static_assert(ROWS <= THREADS, "a thread a row");
+  __shared__ int64_t src_of[ROWS], dst_of[ROWS];  // -1: none
+  const PagedCache& c = a.c;
+  const int t = threadIdx.x, j = j0 + t;
+  if (t < ROWS) {
+    int64_t src = -1, dst = -1;
+    if (j < n) {
+      const int from = a.kept[((size_t)seq * c.hkv + hk) * a.budget + j];
+      const int p = paged_div(c, j >> 4);
+      const int id = a.new_table[(size_t)seq * a.new_pages + p];
+      const int run = from >= 0 ? paged_run(c, seq, hk, from >> 4) : -1;
+      if (run >= 0 && (uint32_t)id < (uint32_t)c.num_pages) {
+        src = (int64_t)run * 16 + (from & 15);
+        dst = ((int64_t)(id * c.hkv + hk) * c.runs + ((j >> 4) - p * c.runs)) * 16 + (j & 15);
+      }
+    }
+    src_of[t] = src;
+    dst_of[t] = dst;
+  }
+  __syncthreads();
+  const int e = (t % LANES) * 16;
+  u32x4 x[4][2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t src = src_of[t / LANES + i * STEP];
+    if (src >= 0) {
+      x[i][0] = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x4*>(a.k + src * (LANES * 16) + e));
+      x[i][1] = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x4*>(a.v + src * (LANES * 16) + e));
+    }
+  }
+  float score = 0.f;
+  const bool mine = t < ROWS && src_of[t] >= 0;
+  if (mine) score = a.scores[src_of[t]];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t dst = dst_of[t / LANES + i * STEP];
+    if (dst >= 0) {
+      __builtin_nontemporal_store(x[i][0],
+                                  reinterpret_cast<u32x4*>(a.k + dst * (LANES * 16) + e));
+      __builtin_nontemporal_store(x[i][1],
+                                  reinterpret_cast<u32x4*>(a.v + dst * (LANES * 16) + e));
+    }
+  }
+  if (mine) a.scores[dst_of[t]] = score;
+}
+
 // QUADS: groups of 4 keys that a thread holds in registers; 0: every pass reads them again.
 template <int QUADS>
-__global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvictArgs a) {
+__device__ __forceinline__ void paged_select(const PagedEvictArgs& a, int seq, int hk) {
   __shared__ uint32_t hist[kBins];
   __shared__ uint32_t wave_more[kSelectWaves], wave_tie[kSelectWaves], found[2];
   const PagedCache& c = a.c;
-  const int hk = blockIdx.x % (unsigned)c.hkv, seq = blockIdx.x / (unsigned)c.hkv;
   const int t = threadIdx.x, l = __lane_id();
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int n = paged_len(c, seq);
@@ -1320,64 +1376,28 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvict
   for (int j = t; j < a.recent; j += kSelectThreads) kept[a.budget - a.recent + j] = hi + j;
 }
 
-// LANES lanes of 16 bytes a row; a workgroup finds the places of kGatherRows rows, then
-// every thread copies 4 rows' chunks of K and V, all loaded before the first is stored.
-template <int LANES>
-constexpr int kGatherRows = 4 * 256 / LANES;
+// A workgroup a sequence and head.  LANES > 0: it copies the rows as well.
+template <int QUADS, int LANES>
+__global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(PagedEvictArgs a) {
+  const int hk = blockIdx.x % (unsigned)a.c.hkv, seq = blockIdx.x / (unsigned)a.c.hkv;
+  paged_select<QUADS>(a, seq, hk);
+  if constexpr (LANES > 0) {
+    const int n = min(paged_len(a.c, seq), a.budget);
+    for (int j0 = 0; j0 < n; j0 += kGatherRows<LANES, kSelectThreads>) {
+      __syncthreads();  // (kept, and the places of the rows before, are read)
+      paged_gather<LANES, kSelectThreads>(a, seq, hk, j0, n);
+    }
+    if (hk == 0 && threadIdx.x == 0) a.new_len[seq] = n;
+  }
+}
 
 template <int LANES>
 __global__ void __launch_bounds__(256) paged_gather_kernel(PagedEvictArgs a) {
-  constexpr int ROWS = kGatherRows<LANES>;
-  __shared__ int64_t src_of[ROWS], dst_of[ROWS];  // -1: none
-  const PagedCache& c = a.c;
   const int hk = blockIdx.y, seq = blockIdx.z;
-  const int n = min(paged_len(c, seq), a.budget);
+  const int n = min(paged_len(a.c, seq), a.budget);
   if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) a.new_len[seq] = n;
-  const int j0 = blockIdx.x * ROWS;
-  if (j0 >= n) return;
-  const int j = j0 + threadIdx.x;
-  if (threadIdx.x < ROWS) {
-    int64_t src = -1, dst = -1;
-    if (j < n) {
-      const int from = a.kept[((size_t)seq * c.hkv + hk) * a.budget + j];
-      const int p = paged_div(c, j >> 4);
-      const int id = a.new_table[(size_t)seq * a.new_pages + p];
-      const int run = from >= 0 ? paged_run(c, seq, hk, from >> 4) : -1;
-      if (run >= 0 && (uint32_t)id < (uint32_t)c.num_pages) {
-        src = (int64_t)run * 16 + (from & 15);
-        dst = ((int64_t)(id * c.hkv + hk) * c.runs + ((j >> 4) - p * c.runs)) * 16 + (j & 15);
-      }
-    }
-    src_of[threadIdx.x] = src;
-    dst_of[threadIdx.x] = dst;
-  }
-  __syncthreads();
-  const int e = (threadIdx.x % LANES) * 16;
-  u32x4 x[4][2];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t src = src_of[threadIdx.x / LANES + i * (256 / LANES)];
-    if (src >= 0) {
-      x[i][0] = __builtin_nontemporal_load(
-          reinterpret_cast<const u32x4*>(a.k + src * (LANES * 16) + e));
-      x[i][1] = __builtin_nontemporal_load(
-          reinterpret_cast<const u32x4*>(a.v + src * (LANES * 16) + e));
-    }
-  }
-  float score = 0.f;
-  const bool mine = threadIdx.x < ROWS && src_of[threadIdx.x] >= 0;
-  if (mine) score = a.scores[src_of[threadIdx.x]];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t dst = dst_of[threadIdx.x / LANES + i * (256 / LANES)];
-    if (dst >= 0) {
-      __builtin_nontemporal_store(x[i][0],
-                                  reinterpret_cast<u32x4*>(a.k + dst * (LANES * 16) + e));
-      __builtin_nontemporal_store(x[i][1],
-                                  reinterpret_cast<u32x4*>(a.v + dst * (LANES * 16) + e));
-    }
-  }
-  if (mine) a.scores[dst_of[threadIdx.x]] = score;
+  const int j0 = blockIdx.x * kGatherRows<LANES, 256>;
+  if (j0 < n) paged_gather<LANES, 256>(a, seq, hk, j0, n);
 }
 
 }  // namespace pdy
