@@ -424,6 +424,14 @@ pdy_status pdy_cross_launch_shapes(int32_t prefix_len, int32_t total_q, int32_t 
                                    int32_t num_heads_q, int32_t num_heads_kv, int32_t head_dim,
                                    int32_t causal, int32_t* shapes);
 
+/* The same for attn_paged_fwd: {waves per workgroup, packed rows (queries times heads of a
+ * group) per tile, parts per tile's keys at most, 1 where the weights come from the logits
+ * that the attention leaves, not from the keys again}: 4 values. */
+pdy_status pdy_paged_launch_shapes(int32_t total_q, int32_t num_seqs, int32_t max_seqlen_q,
+                                   int32_t max_seqlen_k, int32_t num_heads_q,
+                                   int32_t num_heads_kv, int32_t head_dim, int32_t cache_e4m3,
+                                   int32_t with_scores, int32_t* shapes);
+
 /* Static text for a status code. */
 const char* pdy_status_string(int32_t status);
 

@@ -511,4 +511,28 @@ pdy_status attn_paged_evict(void* k_pages, void* v_pages, float* scores, const i
   return PDY_OK;
 }
 
+pdy_status pdy_paged_launch_shapes(int32_t total_q, int32_t num_seqs, int32_t max_seqlen_q,
+                                   int32_t max_seqlen_k, int32_t num_heads_q,
+                                   int32_t num_heads_kv, int32_t head_dim, int32_t cache_e4m3,
+                                   int32_t with_scores, int32_t* shapes) {
+  g_err[0] = 0;
+  PagedRows r;
+  pdy_status st;
+  if ((st = check_heads(num_seqs, num_heads_kv, head_dim)) ||
+      (st = check_rows(total_q, num_seqs, max_seqlen_q, num_heads_q, num_heads_kv, head_dim, &r)))
+    return st;
+  if (max_seqlen_k < 0)
+    return fail(PDY_ERR_INVALID_ARG, "max_seqlen_k must be >= 0 (got %d)", max_seqlen_k);
+  if ((cache_e4m3 & ~1) || (with_scores & ~1))
+    return fail(PDY_ERR_INVALID_ARG, "cache_e4m3 and with_scores must be 0 or 1");
+  if (shapes == nullptr) return fail(PDY_ERR_INVALID_ARG, "shapes is NULL");
+  const PagedPlan p = plan_fwd(r, num_seqs, max_seqlen_k, num_heads_kv, head_dim,
+                               head_dim * (cache_e4m3 ? 1 : 2), with_scores);
+  shapes[0] = p.waves;
+  shapes[1] = 16 << p.shape;
+  shapes[2] = p.cut.max_parts;
+  shapes[3] = p.logit_rows > 0;
+  return PDY_OK;
+}
+
 }  // extern "C"

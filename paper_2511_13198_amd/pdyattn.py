@@ -32,7 +32,8 @@ SYMBOLS = ("attn_fwd_workspace_size", "attn_bwd_workspace_size", "attn_fwd", "at
            "attn_paged_write", "attn_paged_fwd_workspace_size", "attn_paged_fwd",
            "attn_paged_evict_workspace_size", "attn_paged_evict",
            "attn_validate_cu_seqlens", "attn_bwd_noalloc", "pdy_launch_shapes",
-           "pdy_chunk_launch_shapes", "pdy_cross_launch_shapes", "pdy_status_string", "pdy_last_error",
+           "pdy_chunk_launch_shapes", "pdy_cross_launch_shapes", "pdy_paged_launch_shapes",
+           "pdy_status_string", "pdy_last_error",
            "pdy_kernel_count", "pdy_kernel_name", "pdy_profile_start", "pdy_profile_stop")
 
 
@@ -123,6 +124,8 @@ def lib() -> ctypes.CDLL:
     L.pdy_chunk_launch_shapes.restype = i32
     L.pdy_cross_launch_shapes.argtypes = [i32] * 10 + [ctypes.POINTER(i32)]
     L.pdy_cross_launch_shapes.restype = i32
+    L.pdy_paged_launch_shapes.argtypes = [i32] * 9 + [ctypes.POINTER(i32)]
+    L.pdy_paged_launch_shapes.restype = i32
     L.pdy_status_string.argtypes = [i32]
     L.pdy_status_string.restype = ctypes.c_char_p
     L.pdy_last_error.argtypes = []
@@ -706,6 +709,17 @@ def paged_fwd_workspace_size(total_q, num_seqs, max_seqlen_q, max_seqlen_k, hq, 
 
 def paged_evict_workspace_size(num_seqs, max_seqlen_k, hkv, budget) -> int:
     return int(lib().attn_paged_evict_workspace_size(num_seqs, max_seqlen_k, hkv, budget))
+
+
+def paged_launch_shapes(total_q, num_seqs, max_seqlen_q, max_seqlen_k, hq, hkv, d,
+                        e4m3: bool = False, with_scores: bool = False) -> dict:
+    """How attn_paged_fwd is launched: waves of a workgroup, rows of a tile, parts at most
+    of its keys, and whether weights come from logits that the attention leaves."""
+    out = (ctypes.c_int32 * 4)()
+    _check(lib().pdy_paged_launch_shapes(total_q, num_seqs, max_seqlen_q, max_seqlen_k, hq, hkv, d,
+                                         1 if e4m3 else 0, 1 if with_scores else 0, out),
+           "pdy_paged_launch_shapes")
+    return {"waves": out[0], "rows": out[1], "parts": out[2], "logits": bool(out[3])}
 
 
 def _paged_pool(k_pages, v_pages, page_table, seqlens_k, scores, scales=None):

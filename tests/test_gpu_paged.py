@@ -30,6 +30,13 @@ ATTEND = [
     ([1] * 130, [(37 * i) % 211 for i in range(130)], 4, 2, 64, 16, True),
     ([(i % 3) for i in range(300)], [(53 * i) % 90 + 3 for i in range(300)], 2, 1, 128, 32, True),
     ([1], [66000], 4, 2, 64, 64, True),
+    ([6, 2, 8], [3000, 100, 5000], 8, 2, 128, 16, True),   # 32 rows, in parts
+    ([30, 17], [6000, 2100], 3, 3, 64, 32, True),
+    ([12, 40], [7000, 333], 8, 2, 128, 48, True),          # 64 rows and more, in parts
+    ([64, 3], [5000, 9000], 1, 1, 64, 128, False),
+    ([1] * 40, [(103 * i) % 1500 for i in range(40)], 16, 8, 128, 16, True),  # whole, 4 waves
+    ([2, 1], [900, 700], 16, 2, 64, 16, True),             # 16 rows
+    ([8, 3], [900, 500], 8, 2, 128, 16, True),             # 32 rows, whole
 ]
 
 
@@ -41,6 +48,13 @@ def run(c, q, cuq, lq, causal, scale=None, scores=None, out=None, **kw):
     return P.attn_paged_fwd(q, c.k, c.v, c.table, cuq, c.len, max(lq), max(max(c.lens), 1),
                             causal=causal, scale=scale, **c.scales(), scores=scores, out=out,
                             lse=lse, **kw)
+
+
+def shapes_of(case, e4m3, scores):
+    """The launch of a case's call, as below."""
+    lq, lk, hq, hkv, d, page, causal = ATTEND[case]
+    return P.paged_launch_shapes(sum(lq) + 2, len(lq), max(lq), max(max(lk), 1), hq, hkv, d, e4m3,
+                                 scores)
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
@@ -103,6 +117,26 @@ def test_attention_is_the_same_again_and_beside_the_weights(n, most, e4m3, d):
     assert abs(float(again.double().sum()) - total) < 1e-4 * total
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_weights_of_few_rows_from_the_keys(e4m3):
+    """A bound of the lengths for which no logits are left: from the keys, as of many rows."""
+    lens, lq, wide = [700, 33, 2100], [1, 0, 3], 1 << 20
+    c = pg.Cache(lens, 2, 64, 16, e4m3, "cuda", seed=8)
+    table = torch.full((3, wide), -7, dtype=torch.int32, device="cuda")
+    table[:, :c.table.shape[1]] = c.table
+    c.table = table
+    q, cuq = pg.queries(lq, 8, 64, "cuda")
+    assert not P.paged_launch_shapes(4, 3, 3, 16 * wide, 8, 2, 64, e4m3, True)["logits"]
+    before = c.scores.clone()
+    o, lse = P.attn_paged_fwd(q, c.k, c.v, c.table, cuq, c.len, 3, **c.scales(), scores=c.scores)
+    want = pg.attention(c, q, lq, True, 0.125)
+    cu.check("o", o, want["o"])
+    cu.check("lse", lse, want["lse"])
+    live = c.live.cuda()[:, None].expand_as(before)
+    cu.check("scores", c.scores[live].double() - before[live].double(),
+             [x[live] for x in want["scores"]])
+
+
 WRITE = [
     ([1], [1], 1, 64, 16), ([1, 1, 1], [700, 16, 17], 8, 128, 16), ([3, 0, 5, 1], [3, 9, 900, 48], 3, 64, 48),
     ([300, 1, 77], [1000, 1, 77], 4, 128, 80), ([9, 2], [4, 2], 2, 128, 32),  # tokens in front of key 0
@@ -134,6 +168,7 @@ EVICT = [
     ([3000, 2048, 2049], 4, 128, 48, 2048, 64, 4), ([17, 40], 2, 64, 32, 1, 0, 0),
     ([17, 40], 2, 64, 32, 1, 1, 0), ([500, 300], 2, 128, 80, 32, 16, 16),  # nothing by score
     ([20000, 7], 2, 64, 128, 4097, 0, 1), ([70000], 1, 64, 256, 100, 3, 0),
+    ([9000, 300], 2, 64, 32, 120, 7, 2), ([9000, 300, 12000], 1, 128, 16, 2000, 0, 3),
 ]
 
 

@@ -10,6 +10,7 @@ import torch
 from paper_2511_13198_amd import pdyattn as P
 from tests import cross_util as cu
 from tests import paged_util as pg
+from tests import test_gpu_paged as gpu
 from tests import test_isa_lds_waits as isa
 
 FAKE = 0x10000  # aligned, never dereferenced: every call below fails validation first
@@ -86,6 +87,41 @@ def test_nothing_to_do_and_sizes():
         assert size(5, 2, 6, 300, 8, 2, 128, scores) == 0 == size(5, 2, 3, 300, 8, 3, 128, scores)
     assert P.paged_evict_workspace_size(2, 300, 2, 100) >= 256
     assert P.paged_evict_workspace_size(2, 300, 2, 0) == 0
+
+
+def test_shapes_of_launches_and_what_the_gpu_cases_cover():
+    """The rules' two sides, and that the GPU tests' cases reach every kernel."""
+    def shape(n, q, k, hq, hkv, d, e4m3=False, scores=False):
+        return tuple(P.paged_launch_shapes(n * q, n, q, k, hq, hkv, d, e4m3, scores).values())
+
+    # the smallest tile that holds a sequence's rows; few keys whole, more waves where a step
+    # is short and a CU has one workgroup at most
+    assert shape(4, 1, 1024, 8, 8, 128) == (4, 16, 1, False)
+    assert shape(4, 1, 1025, 8, 8, 128)[2] > 1 and shape(8, 1, 2048, 8, 8, 128)[2] == 1
+    assert shape(4, 1, 1024, 8, 8, 128, True) == (8, 16, 1, False) == shape(4, 1, 2048, 8, 8, 64)
+    assert shape(33, 1, 1024, 8, 8, 128, True)[0] == 4 == shape(4, 1, 4000, 8, 8, 64)[0]
+    assert [shape(2, q, 500, 4, 4, 64)[1] for q in (16, 17, 32, 33, 500)] == [16, 32, 32, 64, 64]
+    # up to 16 rows leave their logits, while these fit
+    assert shape(4, 4, 5000, 16, 4, 64, scores=True)[3] and not shape(4, 5, 5000, 16, 4, 64, scores=True)[3]
+    assert not shape(4, 1, 1 << 24, 16, 4, 64, scores=True)[3]
+    for bad in (dict(max_seqlen_q=6), dict(max_seqlen_k=-1), dict(hkv=3), dict(d=96)):
+        with pytest.raises(P.PdyError):
+            P.paged_launch_shapes(**dict(dict(total_q=5, num_seqs=2, max_seqlen_q=3, max_seqlen_k=9,
+                                              hq=4, hkv=2, d=64), **bad))
+    seen = set()
+    for case, (_, _, _, _, d, _, _) in enumerate(gpu.ATTEND):
+        for e4m3 in (False, True):
+            for scores in (False, True):
+                s = gpu.shapes_of(case, e4m3, scores)
+                whole = "parts" if s["parts"] > 1 else "whole"
+                seen |= {(d, e4m3, s["rows"], whole, s["waves"], scores and s["logits"])}
+    want = {(d, e4m3, rows, how, 4, False) for d in (64, 128) for e4m3 in (False, True)
+            for rows in (16, 32, 64) for how in ("parts", "whole")}
+    want |= {(d, e4m3, 16, how, 4, True) for d in (64, 128) for e4m3 in (False, True)
+             for how in ("parts", "whole")}
+    want |= {(d, e4m3, 16, "whole", 8, logits) for logits in (False, True)
+             for d, e4m3 in ((64, False), (64, True), (128, True))}
+    assert not want - seen, sorted(map(str, want - seen))
 
 
 def test_binding_refuses_host_tensors_types_and_shapes():
