@@ -106,7 +106,7 @@ __device__ __forceinline__ u32x2 paged_e4m3(const u32x4& x, float s, float inv) 
 template <int D, bool F8>
 __global__ void __launch_bounds__(256) paged_write_kernel(PagedWriteArgs a) {
   constexpr int LANES = D / 8;  // of a row
-  constexpr int AHEAD = 4;      // rounds of 256 threads loaded at a time
+  constexpr int AHEAD = 2;      // rounds of 256 threads loaded at a time
   __shared__ int64_t row_of[1 << kWriteLog2];  // row of kv head 0 in the pool; -1: none
   const PagedCache& c = a.c;
   const int t0 = blockIdx.x << a.each_log2, count = min(1 << a.each_log2, a.tokens - t0);
@@ -804,7 +804,7 @@ struct PagedMergeArgs {
   int wide;  // a workgroup a pair
 };
 
-// One pair by W waves of a workgroup (1, or all 4, which take the parts in turn).
+// One pair by W waves of a workgroup (1, or all 4, a share of the parts each).
 template <int D, int W>
 __device__ __forceinline__ void paged_merge(const PagedMergeArgs& a, uint32_t pair) {
   constexpr int LANES = D / 8, GROUPS = 64 / LANES;
@@ -815,18 +815,19 @@ __device__ __forceinline__ void paged_merge(const PagedMergeArgs& a, uint32_t pa
   const uint32_t pairs = (uint32_t)a.tq * a.hq;
   if (pair >= pairs) return;
   const int tok = (int)(pair / (uint32_t)a.hq), h = (int)(pair - (uint32_t)tok * a.hq);
-  // (read before it is known how many there are)
-  const float x0 = w * 64 + l < a.max_parts ? a.part_lse[(size_t)(w * 64 + l) * pairs + pair] : 0.f;
+  // (one wave: read before it is known how many there are)
+  const float x0 = W == 1 && l < a.max_parts ? a.part_lse[(size_t)l * pairs + pair] : 0.f;
   const int parts = min(max(a.part_n[pair], 0), a.max_parts);
   // rows behind the last sequence stay, and those written by their one part
   if (tok >= a.cu_q[a.n] || parts <= 1) return;
   const int c = (l % LANES) * 8, grp = l / LANES;
   float mx = -INFINITY, tot = 0.f;
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const int share = (parts + W - 1) / W, last = min(parts, (w + 1) * share);  // this wave's
   // (more than 64 parts: the sums so far are rescaled by each further 64)
-  for (int p0 = w * 64; p0 < parts; p0 += 64 * W) {
-    const float x = p0 + l >= parts ? -INFINITY
-                    : p0 == w * 64 ? x0 : a.part_lse[(size_t)(p0 + l) * pairs + pair];
+  for (int p0 = w * share; p0 < last; p0 += 64) {
+    const float x = p0 + l >= last ? -INFINITY
+                    : W == 1 && p0 == 0 ? x0 : a.part_lse[(size_t)(p0 + l) * pairs + pair];
     float top = x;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
@@ -841,7 +842,7 @@ __device__ __forceinline__ void paged_merge(const PagedMergeArgs& a, uint32_t pa
     tot = tot * keep + sum;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] *= keep;
-    const int m = min(64, parts - p0);
+    const int m = min(64, last - p0);
 #pragma unroll 4
     for (int j0 = 0; j0 < m; j0 += GROUPS) {
       // (every lane takes part in the exchange; past the last part the weight is 0)
