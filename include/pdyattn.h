@@ -312,7 +312,7 @@ pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
  *   - Tables and lengths are trusted, but clamped to the tensors: wrong ones give wrong
  *     results, no stray access (keys in no page of the pool are not written).
  *   - Slots that hold no key in use may hold anything, NaN among it.
- *   - num_pages * Hkv * page_size / 16 and max_pages * page_size are below 2^31.
+ *   - num_pages * Hkv * page_size / 16 is below 2^31, max_pages * page_size below 2^30.
  * Other rules as above. */
 
 /* New keys and values into their pages: token t of the nq = cu_seqlens[i+1] -

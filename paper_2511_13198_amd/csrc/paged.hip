@@ -52,9 +52,10 @@ pdy_status check_pool(const void* k, const void* v, const float* k_scale, const 
   if (num_pages < 0 || max_pages < 0)
     return fail(PDY_ERR_INVALID_ARG, "num_pages and max_pages must be >= 0 (got %d, %d)",
                 num_pages, max_pages);
-  // runs of 16 keys are counted in 32 bits, over the pool and over a sequence
+  // runs of 16 keys are counted in 32 bits over the pool, keys over a sequence (and a little
+  // past its end)
   if ((int64_t)num_pages * hkv * (page / 16) >= (int64_t)1 << 31 ||
-      (int64_t)max_pages * page >= (int64_t)1 << 31)
+      (int64_t)max_pages * page >= (int64_t)1 << 30)
     return fail(PDY_ERR_INVALID_ARG, "too many pages (num_pages=%d, max_pages=%d)", num_pages,
                 max_pages);
   if (max_k < 0 || max_k > (int64_t)max_pages * page)
@@ -442,7 +443,7 @@ pdy_status attn_paged_evict(void* k_pages, void* v_pages, float* scores, const i
   if (new_max_pages < 0 || (int64_t)new_max_pages * page_size < most)
     return fail(PDY_ERR_INVALID_ARG, "new_table has room for %d pages of %d keys, %d may stay",
                 new_max_pages, page_size, (int)most);
-  if (s.n * s.hkv * budget >= (int64_t)1 << 31)
+  if (s.n * s.hkv * budget >= (int64_t)1 << 31 || !fits_grid(s.n * s.hkv, pdy::kSelectThreads))
     return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
   if (s.hkv > 65535 || s.n > 65535)
     return fail(PDY_ERR_INVALID_ARG, "too many sequences or heads for one launch");

@@ -35,7 +35,10 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIBRARY_KERNELS = ("plan_kernel", "fwd_kernel", "bwd_dkdv_kernel", "bwd_dq_kernel",
                    "split_merge_kernel", "split_sum_kernel", "cross_list_kernel",
                    "cross_fwd_kernel", "cross_merge_kernel", "cross_dq_kernel",
-                   "cross_dkdv_kernel", "cross_sum_kernel", "rotary_kernel")
+                   "cross_dkdv_kernel", "cross_sum_kernel", "rotary_kernel",
+                   "paged_write_kernel", "paged_fwd_kernel", "paged_merge_kernel",
+                   "paged_join_kernel", "paged_weigh_kernel", "paged_select_kernel",
+                   "paged_gather_kernel")
 
 
 def code_text(src: str) -> str:

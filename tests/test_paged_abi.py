@@ -42,7 +42,7 @@ BAD = [
     (dict(n=0), "num_seqs"), (dict(hkv=0), "head counts"), (dict(page=0), "page_size"),
     (dict(page=24), "page_size"), (dict(page=-16), "page_size"), (dict(pages=-1), "num_pages"),
     (dict(width=-1), "max_pages"), (dict(pages=1 << 30), "too many pages"),
-    (dict(width=1 << 27, page=16), "too many pages"), (dict(e4m3=2), "cache_e4m3"),
+    (dict(width=1 << 26, page=16), "too many pages"), (dict(e4m3=2), "cache_e4m3"),
     (dict(len=0), "seqlens_k"), (dict(len=FAKE + 2), "seqlens_k"), (dict(table=0), "page_table"),
     (dict(kp=0), "k_pages"), (dict(vp=FAKE + 8), "v_pages"), (dict(scores=FAKE + 4), "scores"),
     (dict(hkv=1 << 15), "too many heads"),
@@ -64,7 +64,8 @@ OWN = {
         (dict(recent=97), "recent"), (dict(nwidth=3), "new_table"), (dict(new=0), "new_table"),
         (dict(new=FAKE), "other pages"), (dict(scores=0), "scores"), (dict(kept=0), "kept"),
         (dict(lens=FAKE + 2), "new_lens"), (dict(ws=0), "workspace"), (dict(mk=321), "max_seqlen_k"),
-        (dict(budget=1 << 30, nwidth=1 << 26), "too large")],
+        (dict(budget=1 << 30, nwidth=1 << 26), "too large"), (dict(n=1 << 22), "too large"),
+        (dict(n=70000), "too many")],
 }
 
 
