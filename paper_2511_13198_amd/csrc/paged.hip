@@ -350,6 +350,10 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
   // (tiles of one sequence share its keys through the caches)
   const int64_t fit = kCachedBytes / (s.hkv * 64 * s.row_bytes());
   a.stream_steps = p.max_tiles == 1 && s.n * ceil_div(s.max_k, 32) > fit ? (int)fit : -1;
+  // (weights from the keys read K again: us past the caches / through them with V past, for 32
+  // tokens of 16 heads, d = 64, over 4,000-16,384 keys of 6 sequences (K 100 MB) 73 / 67, of 16 (250
+  // MB) 164 / 150, of 24 (390 MB) 244 / 232)
+  a.keep_k = scores != nullptr;
   a.cut = p.cut;
   a.scale_log2 = scale * pdy::kLog2e;
   a.o = static_cast<uint16_t*>(o);

@@ -437,6 +437,7 @@ struct PagedFwdArgs {
   // steps of 32 keys of a kv head beyond which K and V do not fit the last-level cache, and
   // are read past it; -1: they are read through it without a look
   int stream_steps;
+  int keep_k;  // (more than 16 rows) K through the caches all the same
   float scale_log2;
   uint16_t* o;
   float* lse;
@@ -582,7 +583,8 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
   const int steps = max(0, last - first + NW - 1) / NW;
   // copies of step j's K (kv = 0) or V; past the last step of an empty range, so that
   // every step has as many copies
-  auto issue = [&](auto Stream, int kv, int j) __attribute__((always_inline)) {
+  auto issue = [&](auto Stream, auto Kv, int j) __attribute__((always_inline)) {
+    constexpr int kv = decltype(Kv)::value;
     uint8_t* const to = mine + ((j % C::SLOTS) * 2 + kv) * T::BYTES;
     const uint64_t base = (uint64_t)(kv ? a.v : a.k);
 #pragma unroll
@@ -594,7 +596,8 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
       uint8_t* const dst = to + s * T::RUN;
 #pragma unroll
       for (int i = 0; i < T::COPIES; ++i)
-        paged_copy<decltype(Stream)::value>(from, bytes, kv_off[kv][i][s], dst + i * 1024);
+        paged_copy<((decltype(Stream)::value >> kv) & 1) != 0>(from, bytes, kv_off[kv][i][s],
+                                                                dst + i * 1024);
     }
   };
   // What is in flight behind a step's K when its products begin, and behind its V when these
@@ -615,14 +618,16 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     logit_off = i16 < row_end - row0 ? (uint32_t)(i16 * a.logit_keys + grp * 4) * 4 : 0x80000000u;
     logit_at = (uint64_t)(a.logits + (size_t)(seq * c.hkv + hk) * a.logit_rows * a.logit_keys);
   }
+  constexpr std::integral_constant<int, 0> K;
+  constexpr std::integral_constant<int, 1> V;
   auto all_of = [&](auto Stream) __attribute__((always_inline)) {
     if (steps <= 0) return;
     if (!WHOLE) find_runs(seq, first, 0);
     wait_dma();
 #pragma unroll
     for (int j = 0; j < C::SLOTS; ++j) {
-      issue(Stream, 0, j);
-      issue(Stream, 1, j);
+      issue(Stream, K, j);
+      issue(Stream, V, j);
     }
     for (int j = 0; j < steps; ++j) {
       const int k0 = (first + NW * j) * 32;
@@ -662,7 +667,7 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
         wait_dma();
       }
       wave_lds_fence();
-      issue(Stream, 0, next);
+      issue(Stream, K, next);
 
       // V's reads run beside the softmax
       wait_step(std::true_type{}, j);
@@ -729,11 +734,13 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
         for (int b = 0; b < RB; ++b) oacc[b][db] = mfma16(x, pf[b], oacc[b][db]);
       });
       wave_lds_fence();
-      issue(Stream, 1, next);
+      issue(Stream, V, next);
     }
   };
-  if (a.stream_steps >= 0 && at.steps > (float)a.stream_steps) all_of(std::true_type{});
-  else all_of(std::false_type{});
+  const bool stream = a.stream_steps >= 0 && at.steps > (float)a.stream_steps;
+  if (RB > 1 && stream && a.keep_k) all_of(std::integral_constant<int, 2>{});
+  else if (stream) all_of(std::integral_constant<int, 3>{});
+  else all_of(std::integral_constant<int, 0>{});
 
   // combine the waves: O, offset and sum of every row through LDS
   wait_dma();

@@ -37,6 +37,9 @@ ATTEND = [
     ([1] * 40, [(103 * i) % 1500 for i in range(40)], 16, 8, 128, 16, True),  # whole, 4 waves
     ([2, 1], [900, 700], 16, 2, 64, 16, True),             # 16 rows
     ([8, 3], [900, 500], 8, 2, 128, 16, True),             # 32 rows, whole
+    # past the caches (more keys than these hold), 32 and 64 rows
+    ([30, 32, 20, 1], [16000, 9100, 12345, 3], 16, 16, 64, 64, True),
+    ([16, 9], [40000, 28000], 32, 8, 128, 128, True),
 ]
 
 
