@@ -302,13 +302,14 @@ pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
  * A pool of num_pages pages of page_size keys (a multiple of 16):
  *   k_pages, v_pages [num_pages, Hkv, page_size, d], bf16, or with cache_e4m3 = 1 8-bit
  *   floats (e4m3, largest 448): a value is its byte's times k_scale (v_scale) of the head,
- *   fp32 device arrays [Hkv] (NULL with bf16);
+ *   fp32 device arrays [Hkv] (NULL with bf16), positive, finite and with a finite reciprocal;
  *   scores fp32 [num_pages, Hkv, page_size]: a running weight of every key, where kept.
  * page_table: int32 device array [num_seqs, max_pages]; key j of sequence i is key
  * j % page_size of page page_table[i][j / page_size].  seqlens_k: int32 device array
  * [num_seqs], the keys in use.  Entries behind the last page in use are not read.
  *   - Pages may be shared by sequences (a common beginning) in calls that only read them;
- *     what a call writes (new keys, scores, kept keys) is in pages of one sequence.
+ *     what a call writes (new keys, scores, kept keys) is in pages of one sequence, each once
+ *     in its table.
  *   - Tables and lengths are trusted, but clamped to the tensors: wrong ones give wrong
  *     results, no stray access (keys in no page of the pool are not written).
  *   - Slots that hold no key in use may hold anything, NaN among it.
@@ -338,7 +339,10 @@ pdy_status attn_paged_write(const void* k, const void* v, const int32_t* cu_seql
  *   rows and the heads of its group of exp(S - lse), with logits S and lse as above; rows
  *   with lse = -inf add nothing.
  * Probabilities (before the product with v) are rounded to bf16; logits, sums, weights and
- * lse are 32 bits.  with_scores: whether scores will be given. */
+ * lse are 32 bits.  with_scores: whether scores will be given.  The workspace is for a call
+ * of just these sizes, the bound max_seqlen_k among them: at most about 70 MB, and with
+ * scores up to 1 GiB of logits more (4 bytes a query head, query and key, where a sequence
+ * has up to 16 queries times heads of a group; more logits than that are computed twice). */
 size_t attn_paged_fwd_workspace_size(int32_t total_q, int32_t num_seqs, int32_t max_seqlen_q,
                                      int32_t max_seqlen_k, int32_t num_heads_q,
                                      int32_t num_heads_kv, int32_t head_dim,

@@ -65,13 +65,15 @@ pdy_status check_pool(const void* k, const void* v, const float* k_scale, const 
   if (e4m3 & ~1) return fail(PDY_ERR_INVALID_ARG, "cache_e4m3 must be 0 or 1");
   if ((st = check_ints(len, "seqlens_k")) != PDY_OK) return st;
   if (max_pages > 0 && (st = check_ints(table, "page_table"))) return st;
-  if (num_pages > 0 && ((st = check_ptr(k, "k_pages")) || (st = check_ptr(v, "v_pages")))) return st;
+  if (num_pages > 0 && ((st = check_ptr(k, "k_pages")) || (st = check_ptr(v, "v_pages"))))
+    return st;
   if (scales && e4m3) {
     if ((st = check_ints(reinterpret_cast<const int32_t*>(k_scale), "k_scale")) ||
         (st = check_ints(reinterpret_cast<const int32_t*>(v_scale), "v_scale")))
       return st;
   } else if (scales && (k_scale || v_scale)) {
-    return fail(PDY_ERR_INVALID_ARG, "k_scale and v_scale are of an e4m3 cache (a bf16 one has none)");
+    return fail(PDY_ERR_INVALID_ARG,
+                "k_scale and v_scale are of an e4m3 cache (a bf16 one has none)");
   }
   *out = PagedSizes{n, num_pages, page, max_pages, max_k, hkv, d, e4m3 != 0};
   return PDY_OK;
@@ -84,9 +86,9 @@ pdy::PagedCache cache_of(const PagedSizes& s, const int32_t* table, const int32_
 }
 
 // K of a head that an eviction keeps, up to which (and a workgroup a CU) one launch selects
-// and copies: us of two launches / one, 8 kv heads, d = 128, bf16: 300 keys to 100 of 1 sequence
-// 10.2 / 9.0, of 4 10.9 / 9.3, of 16 13.2 / 10.7, of 64 22.2 / 22.8; 1,000 to 250 10.4 / 10.4, 11.8 / 11.5,
-// 14.7 / 15.3; to 500 10.6 / 13.5, 13.2 / 16.8, 20.3 / 22.8.
+// and copies: us of two launches / one, 8 kv heads, d = 128, bf16: 300 keys to 100 of 1
+// sequence 10.2 / 9.0, of 4 10.9 / 9.3, of 16 13.2 / 10.7, of 64 22.2 / 22.8; 1,000 to 250
+// 10.4 / 10.4, 11.8 / 11.5, 14.7 / 15.3; to 500 10.6 / 13.5, 13.2 / 16.8, 20.3 / 22.8.
 constexpr int64_t kFusedBytes = 48 << 10;
 
 // Whether a grid's threads can be counted in 32 bits, as a launch's are.
@@ -116,8 +118,8 @@ pdy_status check_rows(int32_t tq, int32_t n, int32_t max_q, int32_t hq, int32_t 
 
 // Keys and values of more bytes do not stay in the 256 MB last-level cache until they are
 // read again, and are faster read past it.  us through / past it: 64 sequences over 256-16,384
-// keys of 8 heads, 888 MB 167 / 149, e4m3 444 MB 91 / 80; 17 over 900-9,000, 278 MB 61 / 56; 256 over up
-// to 2,048 of 2 heads, 75 MB, three such caches in turn 22 / 34.
+// keys of 8 heads, 888 MB 167 / 149, e4m3 444 MB 91 / 80; 17 over 900-9,000, 278 MB 61 / 56; 256
+// over up to 2,048 of 2 heads, 75 MB, three such caches in turn 22 / 34.
 constexpr int64_t kCachedBytes = (int64_t)128 << 20;
 constexpr int kMaxParts = 256;
 constexpr int64_t kPartBytes = (int64_t)64 << 20;   // partial results at most
@@ -143,9 +145,10 @@ struct PagedPlan {
 //   n = 1: 1,024 8.9 / 8.7, 2,048 9.1 / 12.4;  n = 8: 2,048 18.2 / 15.8 and 9.6 / 8.7, 4,096
 //   34.6 / 45.7 and 10.5 / 12.7;  n = 32: 2,048 55.0 / 49.4 and 13.4 / 12.7, 4,096 99.1 / 96.4 and
 //   15.7 / 19.3;  n = 256: 1,024 (1 ..) 51.6 / 46.5, 2,048 73.6 / 74.9, 4,096 118 / 132
-// e4m3: n = 1: 1,024 9.0 / 8.3, 2,048 9.3 / 11.7;  n = 64: 2,048 56.7 / 51.9 and 17.4 / 16.7, 4,096
-// (1 ..) 22.6 / 26.7;  d = 64: n = 1: 2,048 8.6 / 9.0, 4,096 8.9 / 13.4;  n = 8 .. 32: 4,096 20.8 / 17.2
-// and 9.1 / 8.5, 54.7 / 50.1 and 13.5 / 13.0;  n = 64: 2,048 16.3 / 13.7 (1 ..), 4,096 20.5 / 21.5
+// e4m3: n = 1: 1,024 9.0 / 8.3, 2,048 9.3 / 11.7;  n = 64: 2,048 56.7 / 51.9 and 17.4 / 16.7,
+//   4,096 (1 ..) 22.6 / 26.7
+// d = 64: n = 1: 2,048 8.6 / 9.0, 4,096 8.9 / 13.4;  n = 8 .. 32: 4,096 20.8 / 17.2 and 9.1 / 8.5,
+//   54.7 / 50.1 and 13.5 / 13.0;  n = 64: 2,048 16.3 / 13.7 (1 ..), 4,096 20.5 / 21.5
 int64_t whole_keys(int64_t pairs, int64_t d) {
   if (d == 64) return pairs >= 64 && pairs <= kCUs ? 4096 : 2048;
   return pairs < 64 ? 1024 : 2048;
@@ -163,9 +166,9 @@ PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, in
   p.cut.least = 8;
   // Two rounds of two workgroups a CU, which even out lengths that the host does not know.  Of
   // 64 rows of 128 a CU holds one, and one round with the items' last parts is the fastest: us
-  // with 4 / 2 / 1 parts a CU, and with 1 less the items, for 16 tokens of each of 12 sequences over
-  // 1,000-8,000 keys, 32/8 heads 77 / 61 / 54 / 42, e4m3 68 / 52 / 48 / 37, of one over 50,000 81 / 61 / 48 /
-  // 47; 12 of 40 over 500-4,000 (320 items) 93 / 76 / 67.
+  // with 4 / 2 / 1 parts a CU, and with 1 less the items, for 16 tokens of each of 12 sequences
+  // over 1,000-8,000 keys, 32/8 heads 77 / 61 / 54 / 42, e4m3 68 / 52 / 48 / 37, of one over
+  // 50,000 81 / 61 / 48 / 47; 12 of 40 over 500-4,000 (320 items) 93 / 76 / 67.
   int64_t entries = 4 * kCUs;
   if (p.shape == 2 && d == 128) entries = 8 * items * hkv <= 5 * kCUs ? kCUs - items * hkv : kCUs;
   p.cut.entries = (int)ceil_div(entries, hkv);
@@ -184,7 +187,8 @@ PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, in
   p.part_lse = cut ? align256((size_t)p.cut.max_parts * r.tq * r.hq * 4) : 0;
   p.part_n = cut ? align256((size_t)r.tq * r.hq * 4) : 0;
   p.logit_keys = ceil_div(std::max<int64_t>(max_k, 1), 32) * 32;
-  p.logit_rows = weigh && p.shape == 0 && n * hkv * rows * p.logit_keys * 4 <= kLogitBytes ? rows : 0;
+  const bool leave = weigh && p.shape == 0 && n * hkv * rows * p.logit_keys * 4 <= kLogitBytes;
+  p.logit_rows = leave ? rows : 0;
   p.logits = align256((size_t)(n * hkv * p.logit_rows * p.logit_keys * 4));
   return p;
 }
@@ -192,9 +196,9 @@ PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, in
 template <int D, bool F8, int RB, int NW, bool LOGITS = false, bool WHOLE = false>
 hipError_t launch_fwd(const pdy::PagedFwdArgs* a, dim3 grid, hipStream_t st) {
   using C = pdy::PagedFwdCfg<D, F8, RB, NW>;
-  if (a == nullptr) return set_lds(pdy::paged_fwd_kernel<D, F8, RB, NW, LOGITS, WHOLE>, C::LDS_BYTES);
-  hipLaunchKernelGGL((pdy::paged_fwd_kernel<D, F8, RB, NW, LOGITS, WHOLE>), grid, dim3(C::NT), C::LDS_BYTES,
-                     st, *a);
+  constexpr auto kernel = pdy::paged_fwd_kernel<D, F8, RB, NW, LOGITS, WHOLE>;
+  if (a == nullptr) return set_lds(kernel, C::LDS_BYTES);
+  hipLaunchKernelGGL(kernel, grid, dim3(C::NT), C::LDS_BYTES, st, *a);
   return hipSuccess;
 }
 using LaunchFwd = hipError_t (*)(const pdy::PagedFwdArgs*, dim3, hipStream_t);
@@ -276,7 +280,8 @@ pdy_status attn_paged_write(const void* k, const void* v, const int32_t* cu_seql
   a.tokens = total_tokens;
   // tokens of a workgroup: as many as leave 4 of these a CU
   a.each_log2 = 0;
-  while (a.each_log2 < pdy::kWriteLog2 && total_tokens >> (a.each_log2 + 1) >= 4 * kCUs) ++a.each_log2;
+  while (a.each_log2 < pdy::kWriteLog2 && total_tokens >> (a.each_log2 + 1) >= 4 * kCUs)
+    ++a.each_log2;
   const int64_t units = (int64_t)num_heads_kv * head_dim / 8;
   a.units_inv = (uint32_t)((1ull << 32) / units);
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
@@ -299,7 +304,8 @@ size_t attn_paged_fwd_workspace_size(int32_t total_q, int32_t num_seqs, int32_t 
   PagedRows r;
   if (check_heads(num_seqs, num_heads_kv, head_dim) != PDY_OK || max_seqlen_k < 0 ||
       (with_scores & ~1) ||
-      check_rows(total_q, num_seqs, max_seqlen_q, num_heads_q, num_heads_kv, head_dim, &r) != PDY_OK)
+      check_rows(total_q, num_seqs, max_seqlen_q, num_heads_q, num_heads_kv, head_dim, &r) !=
+          PDY_OK)
     return 0;
   return plan_fwd(r, num_seqs, max_seqlen_k, num_heads_kv, head_dim, 0, with_scores).bytes();
 }
@@ -351,8 +357,8 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
   const int64_t fit = kCachedBytes / (s.hkv * 64 * s.row_bytes());
   a.stream_steps = p.max_tiles == 1 && s.n * ceil_div(s.max_k, 32) > fit ? (int)fit : -1;
   // (weights from the keys read K again: us past the caches / through them with V past, for 32
-  // tokens of 16 heads, d = 64, over 4,000-16,384 keys of 6 sequences (K 100 MB) 73 / 67, of 16 (250
-  // MB) 164 / 150, of 24 (390 MB) 244 / 232)
+  // tokens of 16 heads, d = 64, over 4,000-16,384 keys of 6 sequences (K 100 MB) 72 / 67, of 16
+  // (250 MB) 164 / 150, of 24 (390 MB) 244 / 232)
   a.keep_k = scores != nullptr;
   a.cut = p.cut;
   a.scale_log2 = scale * pdy::kLog2e;
@@ -366,8 +372,9 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
   a.logit_rows = (int)p.logit_rows;
   a.logit_keys = (int)p.logit_keys;
   const int64_t wgs = p.wgs * s.hkv;
-  if (!fits_grid(wgs, 64 * p.waves) ||
-      (scores && (!fits_grid(s.n * s.hkv * ceil_div(s.max_k, 512), 256) || s.n > 65535 || s.hkv > 65535)))
+  const bool weighs = fits_grid(s.n * s.hkv * ceil_div(s.max_k, 512), 256) && s.n <= 65535 &&
+                      s.hkv <= 65535;
+  if (!fits_grid(wgs, 64 * p.waves) || (scores && !weighs))
     return fail(PDY_ERR_INVALID_ARG, "problem too large for one launch");
   hipError_t e = init_paged_kernels();
   if (e != hipSuccess) return hip_fail(e, "kernel attribute setup");
@@ -379,10 +386,13 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
     (void)kFwd[s.d == 128][s.e4m3][kernel](&a, dim3((unsigned)wgs), hs);
   });
   if (e != hipSuccess) return hip_fail(e, "paged_fwd_kernel launch");
+  // a workgroup a (token, head) pair where few have many parts: us with a wave / a workgroup
+  // for 32 pairs of 128 parts 17.5 / 6.6
   const bool wide = r.tq * r.hq <= 2 * kCUs && p.cut.max_parts > 16;
   const pdy::PagedMergeArgs m{a.part_o, a.part_lse, a.part_n, p.cut.max_parts, a.cu_q, a.c.n, a.tq,
                               a.hq, a.o, a.lse, wide};
-  const int64_t merge_blocks = p.cut.max_parts == 1 ? 0 : wide ? r.tq * r.hq : ceil_div(r.tq * r.hq, 4);
+  const int64_t merge_blocks =
+      p.cut.max_parts == 1 ? 0 : wide ? r.tq * r.hq : ceil_div(r.tq * r.hq, 4);
   if (p.logit_rows > 0) {
     const int64_t key_blocks = ceil_div(std::max<int64_t>(s.max_k, 1), pdy::kWeighKeys);
     const pdy::PagedJoinArgs b{m, (int)merge_blocks, a.c, a.g, (int)key_blocks, a.logits,
@@ -480,7 +490,8 @@ pdy_status attn_paged_evict(void* k_pages, void* v_pages, float* scores, const i
   const int per = quads <= 1 ? 0 : quads <= 4 ? 1 : quads <= 8 ? 2 : 3;
   // Few rows are copied by the workgroups that selected them, not in a launch of its own.
   // (Where the new lengths are written over the old, these are read until the end.)
-  const int64_t gap = reinterpret_cast<const char*>(new_lens) - reinterpret_cast<const char*>(seqlens_k);
+  const int64_t gap =
+      reinterpret_cast<const char*>(new_lens) - reinterpret_cast<const char*>(seqlens_k);
   const bool fused = per <= 1 && most * s.row_bytes() <= kFusedBytes && s.n * s.hkv <= kCUs &&
                      (gap >= 4 * s.n || -gap >= 4 * s.n);
   const int lanes = s.row_bytes() == 64 ? 0 : s.row_bytes() == 128 ? 1 : 2;

@@ -66,8 +66,12 @@ __device__ __forceinline__ int paged_seq_of(const int32_t* cu, int n, int t) {
 // ---------------------------------------------------------------------------
 // New keys and values into their pages.  Token t of a sequence with nq new tokens and nk
 // keys in use (the new ones among them) is its key nk - nq + t.  A workgroup takes 2^each_log2
-// tokens, 8 elements a thread: it loads them, finds the tokens' places, and stores.  e4m3 rounds x / scale once, to the nearest (beyond the largest number
-// to it).
+// tokens, 8 elements a thread: it loads them, finds the tokens' places, and stores.  e4m3
+// rounds x / scale once, to the nearest (beyond the largest number to it).
+//
+// Bound by memory, one token a sequence by the launch (3.3 us on the GPU).  All is read and
+// written once, so past the caches: 8 prompts of 1,024-8,192 tokens to e4m3, 154 MB, 39.3 us
+// through them, 35.4 past them, and 33.3 with two rounds' loads in flight (4.6 TB/s).
 // ---------------------------------------------------------------------------
 struct PagedWriteArgs {
   PagedCache c;
@@ -84,8 +88,9 @@ constexpr int kWriteLog2 = 4;
 
 // 8 bf16 of one 16-byte word as 8 e4m3 of x / s; inv = 1 / s.  The quotient is x inv and a
 // correction by its remainder, which is as exact as the division (a quotient that a rounding
-// to e4m3 could tell from it is hit), in 3 instructions: of a prompt's tokens the division
-// in full took as long as their memory traffic.  512 stands for all that is larger.
+// to e4m3 could tell from it is hit), in 3 instructions where the division takes 10 and more.
+// (Beside the traffic of prompts either is hidden: 38.0 and 39.2 us.)  512 stands for all that
+// is larger.
 __device__ __forceinline__ u32x2 paged_e4m3(const u32x4& x, float s, float inv) {
   uint32_t out[2] = {0u, 0u};
 #pragma unroll
@@ -165,7 +170,8 @@ __global__ void __launch_bounds__(256) paged_write_kernel(PagedWriteArgs a) {
               reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.pages[kv]) + row * D + e));
         } else {
           __builtin_nontemporal_store(
-              x[r][kv], reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.pages[kv]) + row * D + e));
+              x[r][kv],
+              reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.pages[kv]) + row * D + e));
         }
       }
       if (a.scores && e == 0) a.scores[row] = 0.f;
@@ -180,12 +186,20 @@ __global__ void __launch_bounds__(256) paged_write_kernel(PagedWriteArgs a) {
 // the last, ...); a row that sees none gets O = 0, LSE = -inf.
 //
 // Rows are packed: the g heads of a group side by side, row R of a sequence and kv head hk
-// being head hk g + R % g of token R / g.  A workgroup has a
-// tile of 16 RB packed rows of a sequence and a kv head; its waves take steps of 32 keys in
-// turn, each on its own: S^T = K Q^T and O^T += V^T P^T on 16x16x32 matrix instructions (a
-// row per lane of 16, its keys over the four groups of lanes), K and V copied to the
-// wave's own LDS, so that no barrier stands in the loop.  At the end the waves' O, maxima
-// and sums are combined.
+// being head hk g + R % g of token R / g, so that a key is read once for its group.  A
+// workgroup has a tile of 16 RB packed rows of a sequence and a kv head; its waves take steps
+// of 32 keys in turn, each on its own: S^T = K Q^T and O^T += V^T P^T on 16x16x32 matrix
+// instructions (a row per lane of 16, its keys over the four groups of lanes), K and V copied
+// to the wave's own LDS, so that no barrier stands in the loop.  At the end the waves' O,
+// maxima and sums are combined.
+//
+// Bound by the bytes of K and V (d flops a byte and row of a group at most): what counts is
+// that copies never pause.  A wave's 16 KB of LDS hold K and V of one step (d = 128, bf16) to
+// four; K of a later step is issued as soon as the registers have the K in its place, V
+// likewise, and waits are for a count of copies, so that a tile and more is always in flight:
+// with each step waiting for its own copies a token for each of 64 sequences over 256-16,384
+// keys of 8 heads (888 MB) took 410 us, so 266, with the keys in parts 166, past the caches 148
+// (6.0 TB/s; a kernel that only reads reaches 6.3); e4m3 318, 152, 92, 79.  32 KB: no gain.
 //
 // P is rounded to bf16, as in the other attention kernels (O is off by 2.3e-3 of its norm,
 // 1.7e-3 of which its own rounding is); logits, sums, maxima and LSE are 32 bits.  e4m3
@@ -402,7 +416,9 @@ __device__ __forceinline__ bool paged_place(const PagedCut& c, int n, int entry,
     const uint64_t any = __builtin_amdgcn_ballot_w64(hit);
     if (!any) return false;
     const int src = __builtin_ctzll(any);
-    auto lane = [&](int& x) __attribute__((always_inline)) { x = __builtin_amdgcn_readlane(x, src); };
+    auto lane = [&](int& x) __attribute__((always_inline)) {
+      x = __builtin_amdgcn_readlane(x, src);
+    };
     lane(seq);
     lane(rel);
     lane(np);
@@ -502,7 +518,9 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     at.steps = a.stream_steps >= 0 ? paged_all_steps(c) : 0.f;
   } else if (!paged_place<C::NT>(
                  a.cut, c.n, entry,
-                 [&](int i) __attribute__((always_inline)) { return paged_seq(c, a.cu_q, a.tq, i); },
+                 [&](int i) __attribute__((always_inline)) {
+                   return paged_seq(c, a.cu_q, a.tq, i);
+                 },
                  [&](const PagedSeq& s, int& tiles, int& steps) __attribute__((always_inline)) {
                    tiles = min((s.nq * a.g + C::ROWS - 1) / C::ROWS, a.max_tiles);
                    steps = (s.nk + 31) >> 5;
@@ -573,7 +591,8 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
     va = lds_addr(mine) + T::BYTES + r * T::ROW + T::swz_v(r) * 16 + (i16 & 1) * 8;
   } else {
     const int r = 4 * grp + (i16 >> 2);
-    va = lds_addr(mine) + T::BYTES + r * T::ROW + T::swz_v(r) * 16 + ((i16 & 3) >> 1) * 16 + (i16 & 1) * 8;
+    va = lds_addr(mine) + T::BYTES + r * T::ROW + T::swz_v(r) * 16 + ((i16 & 3) >> 1) * 16 +
+         (i16 & 1) * 8;
   }
 
   // the part's steps, and this wave's
@@ -797,7 +816,8 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
 //   LSE = log sum_p exp(LSE_p),  O = sum_p exp(LSE_p - LSE) O_p;
 // a part with LSE = -inf weighs nothing, one with NaN makes the row O = NaN, LSE = -inf.  A
 // wave per (token, head) pair, or a workgroup where parts are many: a lane per part for the
-// weights (64 at a time), then 512 / D parts at a time, 8 elements a lane.
+// weights (64 at a time), then 512 / D parts at a time, 8 elements a lane.  Bound by the
+// launch and two rounds of loads: 5 us, 32 rows of 128 parts 6.6 (a wave each: 17.5).
 struct PagedMergeArgs {
   const float* part_o;
   const float* part_lse;
@@ -918,8 +938,10 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedMergeArgs a) {
 // From the logits that the attention kernel left (up to 16 rows a sequence and kv head), in
 // one launch with the joining of parts: a workgroup past those that join takes 4,096 keys
 // of a sequence and kv head, and joins the parts' LSE of its rows itself.  (Workgroups start
-// at about 440 a microsecond: with 1,024 keys each, the 4,608 of 64 sequences of up to 8,192 keys
-// and 8 kv heads had all started after 10.5 us, of 14.)
+// at about 440 a microsecond: with 1,024 keys each, the 4,608 of 64 sequences of up to 8,192
+// keys and 8 kv heads had all started after 10.5 us, of 14.)  The logits cost 4 bytes a row
+// and key written and read, the keys again 2 D: a token of those sequences, 32/8 heads, 306 us
+// from the keys, 140 so (the attention 128, without logits 110; this kernel 13).
 struct PagedJoinArgs {
   PagedMergeArgs m;
   int merge_blocks;
@@ -983,7 +1005,8 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedJoinArgs a) {
       z = a.m.lse[(size_t)h * a.m.tq + t] * kLog2e;
     } else {
       float top = -INFINITY, sum = 0.f;
-      for (int p = l; p < parts; p += 64) top = fmaxf(top, p == l ? y0 : a.m.part_lse[p * pairs + pair]);
+      for (int p = l; p < parts; p += 64)
+        top = fmaxf(top, p == l ? y0 : a.m.part_lse[p * pairs + pair]);
 #pragma unroll
       for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
       for (int p = l; p < parts; p += 64) {
@@ -1030,7 +1053,9 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedJoinArgs a) {
 
 // From the keys again, where rows are many: a wave holds 16 RB rows, and takes runs of 16
 // keys, some loaded while one is worked on.  S = Q K^T here, a key per lane of 16, so that a
-// key's rows are in its four lanes' registers, and the sum over them is joined once.
+// key's rows are in its four lanes' registers, and the sum over them is joined once.  Bound
+// by K's bytes, where the attention left them in the last-level cache: 32 tokens of 6
+// sequences over 4,000-16,384 keys of 16 heads, d = 64 (K 100 MB), 21 us, from memory 26.
 struct PagedWeighArgs {
   PagedCache c;
   const uint16_t* q;
@@ -1069,7 +1094,8 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
   using Raw = std::conditional_t<F8, u32x2, u32x4>;
   auto load = [&](int x, Raw (&k)[KS]) __attribute__((always_inline)) {
     const int run = max(0, __builtin_amdgcn_readlane(runs_of, min(x, count - 1)));
-    const uint8_t* const kp = static_cast<const uint8_t*>(a.k) + (size_t)run * T::RUN + i16 * T::ROW;
+    const uint8_t* const kp =
+        static_cast<const uint8_t*>(a.k) + (size_t)run * T::RUN + i16 * T::ROW;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
       k[ks] = __builtin_nontemporal_load(
@@ -1157,7 +1183,11 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
 // paged_select_kernel, a workgroup per sequence and head, finds the smallest score that
 // stays: its 32 bits from the highest on, 11 at a time, each by the counts of the keys that
 // share the bits found so far; then writes the numbers of the keys that stay, in order.
-// paged_gather_kernel copies them to their new places.
+// Scores are read once, into registers.  Over 32,768 keys a workgroup is bound by its own
+// instructions (18 us: loads 5, counts of the first bits 4, two further passes 3 each, the
+// numbers 4); those of 4 sequences and 8 heads leave most CUs idle.
+// paged_gather_kernel copies them to their new places, bound by memory: 64 sequences of 2,304
+// keys to 2,048, 8 heads, d = 128, 1.07 GB, 207 us (5.2 TB/s; through the caches 217).
 // ---------------------------------------------------------------------------
 struct PagedEvictArgs {
   PagedCache c;
@@ -1186,7 +1216,8 @@ template <int LANES, int THREADS>
 constexpr int kGatherRows = 4 * THREADS / LANES;
 
 template <int LANES, int THREADS>
-__device__ __forceinline__ void paged_gather(const PagedEvictArgs& a, int seq, int hk, int j0, int n) {
+__device__ __forceinline__ void paged_gather(const PagedEvictArgs& a, int seq, int hk, int j0,
+                                             int n) {
   constexpr int ROWS = kGatherRows<LANES, THREADS>, STEP = THREADS / LANES;
   static_assert(ROWS <= THREADS, "a thread a row");
   __shared__ int64_t src_of[ROWS], dst_of[ROWS];  // -1: none
@@ -1264,8 +1295,9 @@ __device__ __forceinline__ void paged_select(const PagedEvictArgs& a, int seq, i
     Quad q = {{0u, 0u, 0u, 0u}};
     if (j < hi) {
       const int run = paged_run(c, seq, hk, j >> 4);
-      const f32x4 y = run < 0 ? f32x4{NAN, NAN, NAN, NAN}
-                              : *reinterpret_cast<const f32x4*>(a.scores + (size_t)run * 16 + (j & 15));
+      const f32x4* const at =
+          reinterpret_cast<const f32x4*>(a.scores + (size_t)max(run, 0) * 16 + (j & 15));
+      const f32x4 y = run < 0 ? f32x4{NAN, NAN, NAN, NAN} : *at;
 #pragma unroll
       for (int e = 0; e < 4; ++e) q.x[e] = j + e >= lo && j + e < hi ? paged_order(y[e]) : 0u;
     }
@@ -1343,7 +1375,8 @@ __device__ __forceinline__ void paged_select(const PagedEvictArgs& a, int seq, i
   at += a.first + min(tie, need);
   // lanes below this one that a ballot has
   auto below = [&](uint64_t m) __attribute__((always_inline)) {
-    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32),
+                                     __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
   };
   if (stay > 0)
     each([&](int j, const Quad& q) __attribute__((always_inline)) {
