@@ -1319,20 +1319,29 @@ __device__ __forceinline__ void paged_select(const PagedEvictArgs& a, int seq, i
       for (int u = 0; u < per; ++u) f(from + u * 256, order(from + u * 256));
     }
   };
+  // the sum over the waves in front of this one
+  auto in_front = [&](const uint32_t* of) __attribute__((always_inline)) {
+    const int x = wave_scan(l < w ? (int)of[l] : 0);
+    return (uint32_t)__builtin_amdgcn_readlane(x, 63);
+  };
   // the stay-th largest: bits 31..21, 20..10, 9..0; `need`: how many stay of those that
   // share its bits
   uint32_t bits = 0u, need = (uint32_t)stay;
   if (stay > 0)
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-      const uint32_t width = pass == 2 ? 10 : 11, bins = 1u << width;
+    static_for<3>([&](auto Pass) __attribute__((always_inline)) {
+      constexpr int pass = decltype(Pass)::value;
+      constexpr int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
+      constexpr uint32_t bins = 1u << width;
       hist[t] = hist[t + kSelectThreads] = 0u;
       __syncthreads();
       each([&](int, const Quad& q) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (q.x[e] != 0u && (pass == 0 || (q.x[e] ^ bits) >> (shift + width) == 0u))
-            atomicAdd(&hist[(q.x[e] >> shift) & (bins - 1)], 1u);
+        {
+          // (what is no key counts as the smallest, and `stay` are keys)
+          const uint32_t x = pass == 0 ? q.x[e] : q.x[e] - bits;
+          if (pass == 0 ? x != 0u : x >> shift < bins) atomicAdd(&hist[x >> shift], 1u);
+        }
       });
       __syncthreads();
       // counts from the highest bin down: two bins a thread
@@ -1341,8 +1350,7 @@ __device__ __forceinline__ void paged_select(const PagedEvictArgs& a, int seq, i
       const uint32_t incl = (uint32_t)wave_scan((int)(h1 + h0));
       if (l == 63) wave_more[w] = incl;
       __syncthreads();
-      uint32_t above = incl - h1 - h0;
-      for (int i = 0; i < w; ++i) above += wave_more[i];
+      const uint32_t above = incl - h1 - h0 + in_front(wave_more);
       if (above < need && need <= above + h1 + h0) {
         const bool second = need > above + h1;
         found[0] = second ? b1 - 1 : b1;
@@ -1351,7 +1359,7 @@ __device__ __forceinline__ void paged_select(const PagedEvictArgs& a, int seq, i
       __syncthreads();
       bits |= found[0] << shift;
       need = found[1];
-    }
+    });
   // each wave's keys in order: those above, and the first `need` equal ones
   uint32_t more = 0u, ties = 0u;
   each([&](int, const Quad& q) __attribute__((always_inline)) {
@@ -1367,12 +1375,7 @@ __device__ __forceinline__ void paged_select(const PagedEvictArgs& a, int seq, i
     wave_tie[w] = ties;
   }
   __syncthreads();
-  uint32_t at = 0u, tie = 0u;
-  for (int i = 0; i < w; ++i) {
-    at += wave_more[i];
-    tie += wave_tie[i];
-  }
-  at += a.first + min(tie, need);
+  uint32_t tie = in_front(wave_tie), at = in_front(wave_more) + a.first + min(tie, need);
   // lanes below this one that a ballot has
   auto below = [&](uint64_t m) __attribute__((always_inline)) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32),
