@@ -484,9 +484,9 @@ pdy_status attn_paged_evict(void* k_pages, void* v_pages, float* scores, const i
   a.kept = kept;
   a.new_len = new_lens;
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
-  // the smallest number of keys a thread that holds the longest sequence (and up to 3 in front
-  // of its first)
-  const int64_t quads = ceil_div(s.max_k + 3, 4 * pdy::kSelectThreads);
+  // the smallest number of keys a thread that holds those of the longest sequence that may go
+  // (and up to 15 in front of them)
+  const int64_t quads = ceil_div(s.max_k - recent - (first & ~15), 4 * pdy::kSelectThreads);
   const int per = quads <= 1 ? 0 : quads <= 4 ? 1 : quads <= 8 ? 2 : 3;
   // Few rows are copied by the workgroups that selected them, not in a launch of its own.
   // (Where the new lengths are written over the old, these are read until the end.)

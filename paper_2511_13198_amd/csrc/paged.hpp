@@ -1183,9 +1183,10 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
 // paged_select_kernel, a workgroup per sequence and head, finds the smallest score that
 // stays: its 32 bits from the highest on, 11 at a time, each by the counts of the keys that
 // share the bits found so far; then writes the numbers of the keys that stay, in order.
-// Scores are read once, into registers.  Over 32,768 keys a workgroup is bound by its own
-// instructions (18 us: loads 5, counts of the first bits 4, two further passes 3 each, the
-// numbers 4); those of 4 sequences and 8 heads leave most CUs idle.
+// Scores are read once, into registers.  Over up to 32,768 keys a workgroup is bound by its own
+// instructions, while those of 4 sequences and 8 heads leave most CUs idle: 18 us with the sums
+// over waves in a loop and a page looked up for every 4 keys, 14 with them in one scan, passes
+// with constant shifts and a page's place found once for its run.
 // paged_gather_kernel copies them to their new places, bound by memory: 64 sequences of 2,304
 // keys to 2,048, 8 heads, d = 128, 1.07 GB, 207 us (5.2 TB/s; through the caches 217).
 // ---------------------------------------------------------------------------
@@ -1285,16 +1286,15 @@ __device__ __forceinline__ void paged_select(const PagedEvictArgs& a, int seq, i
   const int lo = a.first, hi = n - a.recent;
   const int stay = a.budget - a.first - a.recent;  // of the keys lo .. hi
   // this wave's keys: `per` rounds of 256 from `from` on, 4 a lane
-  const int start = lo & ~3;
+  const int start = lo & ~15;
   const int per = ((hi - start + kSelectWaves - 1) / kSelectWaves + 255) >> 8;
   const int from = start + w * per * 256 + l * 4;
   struct Quad {
     uint32_t x[4];
   };
-  auto order = [&](int j) __attribute__((always_inline)) {
+  auto order = [&](int j, int run) __attribute__((always_inline)) {
     Quad q = {{0u, 0u, 0u, 0u}};
     if (j < hi) {
-      const int run = paged_run(c, seq, hk, j >> 4);
       const f32x4* const at =
           reinterpret_cast<const f32x4*>(a.scores + (size_t)max(run, 0) * 16 + (j & 15));
       const f32x4 y = run < 0 ? f32x4{NAN, NAN, NAN, NAN} : *at;
@@ -1305,9 +1305,17 @@ __device__ __forceinline__ void paged_select(const PagedEvictArgs& a, int seq, i
   };
   Quad key[QUADS > 0 ? QUADS : 1];
   if constexpr (QUADS > 0) {
+    // lane i knows where run i of every 64 of them is
+    constexpr int BATCHES = (QUADS + 3) / 4;
+    int runs_of[BATCHES];
 #pragma unroll
-    for (int u = 0; u < QUADS; ++u)
-      key[u] = u < per ? order(from + u * 256) : Quad{{0u, 0u, 0u, 0u}};
+    for (int b = 0; b < BATCHES; ++b)
+      runs_of[b] = paged_run(c, seq, hk, min(((from - l * 4) >> 4) + b * 64 + l, (hi - 1) >> 4));
+#pragma unroll
+    for (int u = 0; u < QUADS; ++u) {
+      const int run = __shfl(runs_of[u / 4], u % 4 * 16 + (l >> 2));
+      key[u] = u < per ? order(from + u * 256, run) : Quad{{0u, 0u, 0u, 0u}};
+    }
   }
   auto each = [&](auto&& f) __attribute__((always_inline)) {
     if constexpr (QUADS > 0) {
@@ -1316,7 +1324,10 @@ __device__ __forceinline__ void paged_select(const PagedEvictArgs& a, int seq, i
         if (u < per) f(from + u * 256, key[u]);  // uniform
     } else {
 #pragma unroll 2
-      for (int u = 0; u < per; ++u) f(from + u * 256, order(from + u * 256));
+      for (int u = 0; u < per; ++u) {
+        const int j = from + u * 256;
+        f(j, order(j, j < hi ? paged_run(c, seq, hk, j >> 4) : -1));
+      }
     }
   };
   // the sum over the waves in front of this one

@@ -172,6 +172,9 @@ EVICT = [
     ([17, 40], 2, 64, 32, 1, 1, 0), ([500, 300], 2, 128, 80, 32, 16, 16),  # nothing by score
     ([20000, 7], 2, 64, 128, 4097, 0, 1), ([70000], 1, 64, 256, 100, 3, 0),
     ([9000, 300], 2, 64, 32, 120, 7, 2), ([9000, 300, 12000], 1, 128, 16, 2000, 0, 3),
+    # as many keys that may go as a kernel's threads hold, and one more
+    ([4112], 1, 64, 16, 400, 16, 0), ([4128], 2, 64, 16, 400, 15, 16),
+    ([32800, 32784], 1, 64, 16, 100, 16, 19), ([32800, 32784], 1, 64, 16, 100, 15, 19),
 ]
 
 
