@@ -1055,7 +1055,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedJoinArgs a) {
 // keys, some loaded while one is worked on.  S = Q K^T here, a key per lane of 16, so that a
 // key's rows are in its four lanes' registers, and the sum over them is joined once.  Bound
 // by K's bytes, where the attention left them in the last-level cache: 32 tokens of 6
-// sequences over 4,000-16,384 keys of 16 heads, d = 64 (K 100 MB), 21 us, from memory 26.
+// sequences over 4,000-16,384 keys of 16 heads, d = 64 (K 100 MB), 23 us, from memory 27.
 struct PagedWeighArgs {
   PagedCache c;
   const uint16_t* q;
