@@ -802,10 +802,10 @@ def attn_paged_fwd(q, k_pages, v_pages, page_table, cu_seqlens_q, seqlens_k,
     page_size, d] (bf16, or torch.float8_e4m3fn with k_scale, v_scale fp32 [Hkv]); q [Tq,
     Hq, d] is cut by cu_seqlens_q.  max_seqlen_q, max_seqlen_k: upper bounds of the
     lengths (None: max_seqlen_q read from the offsets, waiting for them, max_seqlen_k the
-    table's room).  causal aligns the ends: the last query sees every key.  scores fp32
-    [pages, Hkv, page_size]: each key's attention weight, summed over the sequence's rows
-    and its group's heads, is added.  Rows without a key get O = 0, LSE = -inf; rows of no
-    sequence are left."""
+    table's room; with scores the workspace grows with it, up to 1 GiB).  causal aligns
+    the ends: the last query sees every key.  scores fp32 [pages, Hkv, page_size]: each
+    key's attention weight, summed over the sequence's rows and its group's heads, is
+    added.  Rows without a key get O = 0, LSE = -inf; rows of no sequence are left."""
     import torch
     dev, shape, e4m3, sc, ks, vs = _paged_pool(k_pages, v_pages, page_table, seqlens_k, scores,
                                                (k_scale, v_scale))
