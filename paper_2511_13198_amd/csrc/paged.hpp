@@ -222,6 +222,12 @@ __device__ __forceinline__ float quad_sum(float x) {
   r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// The logits' factor, the head's scale in it.  Never 0 or infinite, where the product rounds to
+// that: a masked logit (-inf) times 0, and a logit of 0 times infinity, would be NaN.
+__device__ __forceinline__ float paged_scale(float scale_log2, const float* k_scale, int hk) {
+  const float x = k_scale ? scale_log2 * k_scale[hk] : scale_log2;
+  return x == 0.f ? __uint_as_float(1u) : fminf(x, 3.4028235e38f);
+}
 // 8 e4m3 as 8 bf16.
 __device__ __forceinline__ bf16x8 widen8(const u32x2& x) {
   bf16x8 out;
@@ -561,7 +567,7 @@ __global__ void __launch_bounds__(NW * 64, (PagedFwdCfg<D, F8, RB, NW>::WAVES))
   }
   const int all_end = __builtin_amdgcn_readfirstlane(key_end(row0));            // seen by every row
   const int some_end = __builtin_amdgcn_readfirstlane(key_end(row0 + C::ROWS - 1));  // by some
-  const float scale2 = a.scale_log2 * (F8 ? a.k_scale[hk] : 1.f);
+  const float scale2 = paged_scale(a.scale_log2, F8 ? a.k_scale : nullptr, hk);
 
   f32x4 oacc[RB][DB];
   float m[RB], lsum[RB];
@@ -1020,7 +1026,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedJoinArgs a) {
     if (l == 0) lse2[r] = z;
   }
   __syncthreads();
-  const float scale2 = a.scale_log2 * (a.k_scale ? a.k_scale[hk] : 1.f);
+  const float scale2 = paged_scale(a.scale_log2, a.k_scale, hk);
   static_for<kWeighKeys / 1024>([&](auto I) {
     constexpr int i = decltype(I)::value;
     if (j0 + i * 1024 >= nk) return;  // uniform
@@ -1084,7 +1090,7 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
   const int l = __lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i16 = l & 15, grp = l >> 4;
   const int rows = nq * a.g;
-  const float scale2 = a.scale_log2 * (F8 ? a.k_scale[hk] : 1.f);
+  const float scale2 = paged_scale(a.scale_log2, F8 ? a.k_scale : nullptr, hk);
   const int first = (blockIdx.x * 4 + w) * kWeighRuns;
   const int count = min(kWeighRuns, ((nk + 15) >> 4) - first);
   if (count <= 0) return;
