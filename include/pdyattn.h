@@ -302,7 +302,7 @@ pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
  * A pool of num_pages pages of page_size keys (a multiple of 16):
  *   k_pages, v_pages [num_pages, Hkv, page_size, d], bf16, or with cache_e4m3 = 1 8-bit
  *   floats (e4m3, largest 448): a value is its byte's times k_scale (v_scale) of the head,
- *   fp32 device arrays [Hkv] (NULL with bf16), positive, finite and with a finite reciprocal;
+ *   fp32 device arrays [Hkv] (NULL with bf16), positive and finite;
  *   scores fp32 [num_pages, Hkv, page_size]: a running weight of every key, where kept.
  * page_table: int32 device array [num_seqs, max_pages]; key j of sequence i is key
  * j % page_size of page page_table[i][j / page_size].  seqlens_k: int32 device array

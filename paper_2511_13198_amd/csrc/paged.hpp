@@ -86,16 +86,18 @@ struct PagedWriteArgs {
 };
 constexpr int kWriteLog2 = 4;
 
-// 8 bf16 of one 16-byte word as 8 e4m3 of x / s; inv = 1 / s.  The quotient is x inv and a
-// correction by its remainder, which is as exact as the division (a quotient that a rounding
-// to e4m3 could tell from it is hit), in 3 instructions where the division takes 10 and more.
-// (Beside the traffic of prompts either is hidden: 38.0 and 39.2 us.)  512 stands for all that
-// is larger.
-__device__ __forceinline__ u32x2 paged_e4m3(const u32x4& x, float s, float inv) {
+// 8 bf16 of one 16-byte word as 8 e4m3 of x / s.  The quotient is x inv and a correction by
+// its remainder, which is as exact as the division (a quotient that a rounding to e4m3 could
+// tell from it is hit), in 3 instructions where the division takes 10 and more.  (Beside the
+// traffic of prompts either is hidden: 38.0 and 39.2 us.)  512 stands for all that is larger.
+// A remainder under 2^-126 would lose bits, so a scale below 2^-64 is taken 2^64 times, and x
+// with it.
+__device__ __forceinline__ u32x2 paged_e4m3(const u32x4& x, float scale) {
+  const float up = scale < 0x1p-64f ? 0x1p64f : 1.f, s = scale * up, inv = 1.f / s;
   uint32_t out[2] = {0u, 0u};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float y[2] = {__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u)};
+    float y[2] = {__uint_as_float(x[i] << 16) * up, __uint_as_float(x[i] & 0xffff0000u) * up};
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const float q = fminf(fmaxf(y[j] * inv, -512.f), 512.f);
@@ -164,9 +166,8 @@ __global__ void __launch_bounds__(256) paged_write_kernel(PagedWriteArgs a) {
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         if constexpr (F8) {
-          const float s = a.scale[kv][h];
           __builtin_nontemporal_store(
-              paged_e4m3(x[r][kv], s, 1.f / s),
+              paged_e4m3(x[r][kv], a.scale[kv][h]),
               reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.pages[kv]) + row * D + e));
         } else {
           __builtin_nontemporal_store(

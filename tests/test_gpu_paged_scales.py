@@ -31,3 +31,34 @@ def test_products_of_scales_beyond_the_range(scale, ks, lq, lens):
     live = c.live.cuda()[:, None].expand_as(before)
     cu.check("scores", c.scores[live].double() - before[live].double(),
              [x[live] for x in want["scores"]])
+
+
+@pytest.mark.parametrize("top", [-126, -123, -100, -63, 0, 100, 126])
+def test_writes_by_scales_of_any_size(top):
+    """8-bit values are the 32-bit quotients x / scale rounded to the nearest, for scales
+    down to the smallest and up to the largest numbers, and quotients next to a border."""
+    hkv, d = 512, 64
+    g = torch.Generator().manual_seed(top + 200)
+    c = pg.Cache([1], hkv, d, 16, True, seed=1)
+    new, want = [], []
+    for pool in (c.k, c.v):
+        x = (2.0 ** top * (1 + torch.rand(hkv, generator=g, dtype=torch.float64))).to(torch.bfloat16)
+        # x / s is next to the middle of two 8-bit numbers, on either side
+        middle = (2 * torch.randint(8, 16, (hkv,), generator=g) + 1) / 16.0
+        s = (x.double() / middle / 2.0 ** (max(top, 0) // 20)).float()
+        s = (s.view(torch.int32) + torch.randint(-1, 2, (hkv,), generator=g).int()).view(torch.float32)
+        e = torch.arange(d) % 8 - 4
+        x = (x[:, None].double() * 2.0 ** e).to(torch.bfloat16) * (1 - 2 * (e % 2)).to(torch.bfloat16)
+        x[:, 0], x[:, 1], x[:, 2] = math.inf, -0.0, -math.inf
+        new.append((x[None], s))
+        y = (x.float() / s[:, None]).clamp(-448, 448).to(pg.E4M3)
+        out = pool.clone()
+        p, at = c.rows[0][0]
+        out.view(torch.uint8)[p, :, at] = y.view(torch.uint8)
+        want.append(out)
+    (k, ks), (v, vs) = new
+    kp, vp = c.k.cuda(), c.v.cuda()
+    P.attn_paged_write(k.cuda().contiguous(), v.cuda().contiguous(), kp, vp, c.table.cuda(),
+                       cu.offsets([1], "cuda"), c.len.cuda(), ks.cuda(), vs.cuda())
+    for x, y in zip((kp, vp), want):
+        assert pg.same_bits(x.cpu(), y)
