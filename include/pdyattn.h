@@ -320,7 +320,8 @@ pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
  * cu_seqlens[i] tokens of sequence i becomes its key seqlens_k[i] - nq + t (seqlens_k
  * counts the new ones; tokens that would lie in front of key 0 are dropped).
  *   k, v bf16 [total_tokens, Hkv, d]; tokens from cu_seqlens[num_seqs] on are no
- *   sequence's.  e4m3: x / scale, up to 448, rounded once to the nearest (ties to even).
+ *   sequence's.  e4m3: the 32-bit quotient x / scale, up to 448, rounded to the nearest
+ *   (ties to even).
  *   scores (or NULL): 0 for the new keys.
  * total_tokens is below 2^26 - 4.  Needs no workspace. */
 pdy_status attn_paged_write(const void* k, const void* v, const int32_t* cu_seqlens,

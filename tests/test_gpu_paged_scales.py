@@ -62,3 +62,16 @@ def test_writes_by_scales_of_any_size(top):
                        cu.offsets([1], "cuda"), c.len.cuda(), ks.cuda(), vs.cuda())
     for x, y in zip((kp, vp), want):
         assert pg.same_bits(x.cpu(), y)
+
+
+def test_a_quotient_that_meets_a_border_in_32_bits():
+    """1 / 0.04: the scale's 32 bits are a little less than 0.04, the exact quotient a little
+    over 25; in 32 bits it is 25, the middle of 24 and 26, and goes to the even one, 24."""
+    c = pg.Cache([1], 2, 64, 16, True, "cuda", seed=1)
+    s = torch.full((2,), 0.04, device="cuda")
+    k = torch.ones((1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    assert 1.0 / float(s[0].double()) > 25
+    P.attn_paged_write(k, -k, c.k, c.v, c.table, cu.offsets([1], "cuda"), c.len, s, s)
+    p, at = c.rows[0][0]
+    for x, want in ((c.k, 24.0), (c.v, -24.0)):
+        assert bool((x.view(torch.uint8)[p, :, at].view(pg.E4M3).float() == want).all())
