@@ -187,7 +187,7 @@ PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, in
   p.part_lse = cut ? align256((size_t)p.cut.max_parts * r.tq * r.hq * 4) : 0;
   p.part_n = cut ? align256((size_t)r.tq * r.hq * 4) : 0;
   p.logit_keys = ceil_div(std::max<int64_t>(max_k, 1), 32) * 32;
-  const bool leave = weigh && p.shape == 0 && n * hkv * rows * p.logit_keys * 4 <= kLogitBytes;
+  const bool leave = weigh && p.shape == 0 && n * hkv * rows <= kLogitBytes / 4 / p.logit_keys;
   p.logit_rows = leave ? rows : 0;
   p.logits = align256((size_t)(n * hkv * p.logit_rows * p.logit_keys * 4));
   return p;

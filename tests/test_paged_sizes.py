@@ -1,0 +1,14 @@
+"""Sizes and tensors at the edges of what the paged cache's calls take, without a GPU."""
+from paper_2511_13198_amd import pdyattn as P
+from tests.test_paged_abi import FAKE, call
+
+
+def test_workspaces_of_the_largest_sizes():
+    """The logits' bytes of the largest sizes pass 64 bits: more than may be left, so none."""
+    size = P.paged_fwd_workspace_size
+    most = (1 << 30) - 16
+    for n in ((1 << 31) - 33, (1 << 27) + 1, 1 << 28, (1 << 30) + 5):
+        assert size(16, n, 16, most, 1, 1, 64, True) == size(16, n, 16, most, 1, 1, 64, False)
+        assert not P.paged_launch_shapes(16, n, 16, most, 1, 1, 64, with_scores=True)["logits"]
+    for scores in (False, True):
+        assert size(1 << 20, 1 << 20, 1, most, 256, 256, 64, scores) < (2 << 30)
