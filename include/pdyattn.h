@@ -364,7 +364,8 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
  * pages of new_table, int32 device array [num_seqs, new_max_pages], which must be none that
  * the sequences use.  (Keys keep what they were rotated by.)
  *   kept int32 [num_seqs, Hkv, budget] (out): the old number of each key, -1 behind the
- *   last.  new_lens int32 [num_seqs] (out): min(seqlens_k, budget); may be seqlens_k.
+ *   last.  new_lens int32 [num_seqs] (out): min(seqlens_k, budget); may be seqlens_k (all
+ *   of it, not a part).
  * first + recent <= budget <= new_max_pages * page_size (or max_seqlen_k is). */
 size_t attn_paged_evict_workspace_size(int32_t num_seqs, int32_t max_seqlen_k,
                                        int32_t num_heads_kv, int32_t budget);

@@ -468,6 +468,11 @@ pdy_status attn_paged_evict(void* k_pages, void* v_pages, float* scores, const i
   if ((st = check_ints(kept, "kept")) || (st = check_ints(new_lens, "new_lens")) ||
       (st = check_ptr(workspace, "workspace")))
     return st;
+  // (in bytes: some workgroups read a length when others have written the new ones)
+  const int64_t gap = (int64_t)(reinterpret_cast<uintptr_t>(new_lens) -
+                                reinterpret_cast<uintptr_t>(seqlens_k));
+  if (gap != 0 && gap < 4 * s.n && -gap < 4 * s.n)
+    return fail(PDY_ERR_INVALID_ARG, "new_lens overlaps seqlens_k without being it");
   if (workspace_bytes < 256)
     return fail(PDY_ERR_WORKSPACE, "workspace has %zu bytes, attn_paged_evict needs %zu",
                 workspace_bytes, (size_t)256);
@@ -490,10 +495,8 @@ pdy_status attn_paged_evict(void* k_pages, void* v_pages, float* scores, const i
   const int per = quads <= 1 ? 0 : quads <= 4 ? 1 : quads <= 8 ? 2 : 3;
   // Few rows are copied by the workgroups that selected them, not in a launch of its own.
   // (Where the new lengths are written over the old, these are read until the end.)
-  const int64_t gap =
-      reinterpret_cast<const char*>(new_lens) - reinterpret_cast<const char*>(seqlens_k);
   const bool fused = per <= 1 && most * s.row_bytes() <= kFusedBytes && s.n * s.hkv <= kCUs &&
-                     (gap >= 4 * s.n || -gap >= 4 * s.n);
+                     gap != 0;
   const int lanes = s.row_bytes() == 64 ? 0 : s.row_bytes() == 128 ? 1 : 2;
   hipError_t e = launch_timed(K_PAGED_SELECT, hs, [&] {
     const dim3 grid((unsigned)(s.n * s.hkv)), block(pdy::kSelectThreads);

@@ -12,3 +12,13 @@ def test_workspaces_of_the_largest_sizes():
         assert not P.paged_launch_shapes(16, n, 16, most, 1, 1, 64, with_scores=True)["logits"]
     for scores in (False, True):
         assert size(1 << 20, 1 << 20, 1, most, 256, 256, 64, scores) < (2 << 30)
+
+
+def test_an_evictions_new_lengths_beside_the_old():
+    """All of the old lengths, or none of them: a part would be read after it was written."""
+    for off in (-4, 4):
+        assert call("evict", len=FAKE + 64, lens=FAKE + 64 + off) == P.PDY_ERR_INVALID_ARG
+        assert "new_lens" in P.last_error()
+    # (in place, in front of and behind: refused for the next reason)
+    for off in (-8, 0, 8):
+        assert call("evict", len=FAKE + 64, lens=FAKE + 64 + off, wsb=0) == P.PDY_ERR_WORKSPACE
