@@ -306,10 +306,12 @@ pdy_status attn_rotary(const void* q, const void* k, const int32_t* positions,
  *   scores fp32 [num_pages, Hkv, page_size]: a running weight of every key, where kept.
  * page_table: int32 device array [num_seqs, max_pages]; key j of sequence i is key
  * j % page_size of page page_table[i][j / page_size].  seqlens_k: int32 device array
- * [num_seqs], the keys in use.  Entries behind the last page in use are not read.
+ * [num_seqs], the keys in use.  Entries behind the last page in use are not used, whatever
+ * they hold.
  *   - Pages may be shared by sequences (a common beginning) in calls that only read them;
- *     what a call writes (new keys, scores, kept keys) is in pages of one sequence, each once
- *     in its table.
+ *     what a call writes (new keys, scores -- those that attn_paged_fwd adds to, too: sums
+ *     of sequences that share a page would be lost --, kept keys) is in pages of one
+ *     sequence, each once in its table.
  *   - Tables and lengths are trusted, but clamped to the tensors: wrong ones give wrong
  *     results, no stray access (keys in no page of the pool are not written).
  *   - Slots that hold no key in use may hold anything, NaN among it.
@@ -340,7 +342,9 @@ pdy_status attn_paged_write(const void* k, const void* v, const int32_t* cu_seql
  *   rows and the heads of its group of exp(S - lse), with logits S and lse as above; rows
  *   with lse = -inf add nothing.
  * Probabilities (before the product with v) are rounded to bf16; logits, sums, weights and
- * lse are 32 bits.  with_scores: whether scores will be given.  The workspace is for a call
+ * lse are 32 bits.  The same call gives the same bits; launches of other sizes differ in
+ * rounding.  With scores num_seqs is at most 65,535, and num_seqs * Hkv * (max_seqlen_k /
+ * 512, rounded up) below 2^24.  with_scores: whether scores will be given.  The workspace is for a call
  * of just these sizes, the bound max_seqlen_k among them: at most about 70 MB, and with
  * scores up to 1 GiB of logits more (4 bytes a query head, query and key, where a sequence
  * has up to 16 queries times heads of a group; more logits than that are computed twice). */
@@ -366,7 +370,9 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
  *   kept int32 [num_seqs, Hkv, budget] (out): the old number of each key, -1 behind the
  *   last.  new_lens int32 [num_seqs] (out): min(seqlens_k, budget); may be seqlens_k (all
  *   of it, not a part).
- * first + recent <= budget <= new_max_pages * page_size (or max_seqlen_k is). */
+ * first + recent <= budget <= new_max_pages * page_size (or max_seqlen_k is); num_seqs is at
+ * most 65,535, num_seqs * Hkv below 2^22 and num_seqs * Hkv * budget below 2^31.  The
+ * workspace, 256 bytes, is asked for and checked as other calls' is; nothing is held there. */
 size_t attn_paged_evict_workspace_size(int32_t num_seqs, int32_t max_seqlen_k,
                                        int32_t num_heads_kv, int32_t budget);
 pdy_status attn_paged_evict(void* k_pages, void* v_pages, float* scores, const int32_t* page_table,

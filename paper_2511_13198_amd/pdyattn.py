@@ -805,7 +805,9 @@ def attn_paged_fwd(q, k_pages, v_pages, page_table, cu_seqlens_q, seqlens_k,
     table's room; with scores the workspace grows with it, up to 1 GiB).  causal aligns
     the ends: the last query sees every key.  scores fp32 [pages, Hkv, page_size]: each
     key's attention weight, summed over the sequence's rows and its group's heads, is
-    added.  Rows without a key get O = 0, LSE = -inf; rows of no sequence are left."""
+    added (at most 65,535 sequences then, and no page in use may be shared by two: sums
+    would be lost).  Rows without a key get O = 0, LSE = -inf; rows of no sequence are
+    left."""
     import torch
     dev, shape, e4m3, sc, ks, vs = _paged_pool(k_pages, v_pages, page_table, seqlens_k, scores,
                                                (k_scale, v_scale))
@@ -844,8 +846,8 @@ def attn_paged_evict(k_pages, v_pages, scores, page_table, seqlens_k, new_table,
     """Shortens every sequence to at most `budget` keys: each kv head keeps its first
     `first` and last `recent` ones and, of those between, the ones of the highest scores
     (equal ones: the earlier).  Keys, values and scores that stay are copied in their order
-    to the pages of new_table (int32 [N, max pages]), none of which the sequences use.
-    Returns kept int32 [N, Hkv, budget], the old number of each key (-1 behind the last),
+    to the pages of new_table (int32 [N, max pages]), none of which the sequences use;
+    it is the table of the calls after this one.  At most 65,535 sequences.  Returns kept int32 [N, Hkv, budget], the old number of each key (-1 behind the last),
     and the new lengths int32 [N] (new_lens may be seqlens_k)."""
     import torch
     if scores is None:

@@ -22,3 +22,12 @@ def test_an_evictions_new_lengths_beside_the_old():
     # (in place, in front of and behind: refused for the next reason)
     for off in (-8, 0, 8):
         assert call("evict", len=FAKE + 64, lens=FAKE + 64 + off, wsb=0) == P.PDY_ERR_WORKSPACE
+
+
+def test_refused_numbers_of_sequences():
+    """As the header has them: 65,535 sequences with scores and of evictions, and the grids."""
+    for kw in (dict(n=65536), dict(n=65535, mk=512 * 129, width=4200)):
+        assert call("fwd", **kw) == P.PDY_ERR_INVALID_ARG and "too large" in P.last_error()
+    assert call("evict", n=65536) == P.PDY_ERR_INVALID_ARG and "too many" in P.last_error()
+    for kw in (dict(n=65535, hkv=65), dict(n=65535, hkv=3, budget=1 << 14, nwidth=1 << 9)):
+        assert call("evict", **kw) == P.PDY_ERR_INVALID_ARG and "too large" in P.last_error()
