@@ -167,8 +167,9 @@ PagedPlan plan_fwd(const PagedRows& r, int64_t n, int64_t max_k, int64_t hkv, in
   // Two rounds of two workgroups a CU, which even out lengths that the host does not know.  Of
   // 64 rows of 128 a CU holds one, and one round with the items' last parts is the fastest: us
   // with 4 / 2 / 1 parts a CU, and with 1 less the items, for 16 tokens of each of 12 sequences
-  // over 1,000-8,000 keys, 32/8 heads 77 / 61 / 54 / 42, e4m3 68 / 52 / 48 / 37, of one over
-  // 50,000 81 / 61 / 48 / 47; 12 of 40 over 500-4,000 (320 items) 93 / 76 / 67.
+  // over 1,000-8,000 keys, 32/8 heads 77 / 61 / 54 / 42 (their bytes take 25), e4m3 68 / 52 /
+  // 48 / 37 (13), of one over 50,000 81 / 61 / 48 / 47; 12 tokens of each of 40 sequences over
+  // 500-4,000 (320 items) 93 / 76 / 67 (51).
   int64_t entries = 4 * kCUs;
   if (p.shape == 2 && d == 128) entries = 8 * items * hkv <= 5 * kCUs ? kCUs - items * hkv : kCUs;
   p.cut.entries = (int)ceil_div(entries, hkv);
@@ -427,6 +428,7 @@ pdy_status attn_paged_fwd(const void* q, const void* k_pages, const void* v_page
   return PDY_OK;
 }
 
+// (As of every call that may come to need scratch memory; no kernel takes it now.)
 size_t attn_paged_evict_workspace_size(int32_t num_seqs, int32_t max_seqlen_k,
                                        int32_t num_heads_kv, int32_t budget) {
   g_err[0] = 0;

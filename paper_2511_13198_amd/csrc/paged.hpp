@@ -295,7 +295,7 @@ struct PagedFwdCfg {
   static constexpr int SLOTS = 16384 / (2 * T::BYTES);  // tiles of K and V: 16 KB a wave
   static constexpr int WAVE = SLOTS * 2 * T::BYTES;
   // waves a SIMD at least: 2 leave 256 registers, without a need for accumulation registers
-  // (and copies to and from them); 64 rows of 128 need more
+  // (and copies to and from them); 64 rows of 128 need more (478, e4m3 459: one wave a SIMD)
   static constexpr int WAVES = RB * D >= 512 ? 1 : 2;
   static constexpr int PITCH = D + 4;        // floats of a combined row
   static constexpr int STAT = NW * ROWS * PITCH * 4;
@@ -937,9 +937,11 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedMergeArgs a) {
 
 // ---------------------------------------------------------------------------
 // The keys' weights: scores_j += sum over the sequence's rows i (of all heads of the group)
-// of exp(S_ij - LSE_i), for the visible keys.  One lane sums a key's rows, in order, so that
-// results do not depend on the launch.  Rows with LSE = -inf (no key, or a NaN or +inf
-// logit) add nothing.
+// of exp(S_ij - LSE_i), for the visible keys.  A key's rows are summed in a fixed order, by one
+// lane from the logits, by four from the keys, whose sums are joined, and added once, without
+// atomics: the same call gives the same bits.  (LSE differs in rounding with the parts that a
+// launch is cut into, and the weights with it.)  Rows with LSE = -inf (no key, or a NaN or
+// +inf logit) add nothing.
 // ---------------------------------------------------------------------------
 
 // From the logits that the attention kernel left (up to 16 rows a sequence and kv head), in
@@ -1190,10 +1192,11 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
 // paged_select_kernel, a workgroup per sequence and head, finds the smallest score that
 // stays: its 32 bits from the highest on, 11 at a time, each by the counts of the keys that
 // share the bits found so far; then writes the numbers of the keys that stay, in order.
-// Scores are read once, into registers.  Over up to 32,768 keys a workgroup is bound by its own
-// instructions, while those of 4 sequences and 8 heads leave most CUs idle: 18 us with the sums
-// over waves in a loop and a page looked up for every 4 keys, 14 with them in one scan, passes
-// with constant shifts and a page's place found once for its run.
+// Scores are read once, into registers.  Over up to 32,768 keys the time is that of one
+// workgroup's steps one after the other, while those of 4 sequences and 8 heads leave most CUs
+// idle: 18 us with the sums over waves in a loop and a page looked up for every 4 keys, 14 with
+// them in one scan, passes with constant shifts and a page's place found once for its run.  Its
+// waves wait (for LDS, barriers and the scores) 57 % of that, and issue VALU work in 12 %.
 // paged_gather_kernel copies them to their new places, bound by memory: 64 sequences of 2,304
 // keys to 2,048, 8 heads, d = 128, 1.07 GB, 207 us (5.2 TB/s; through the caches 217).
 // ---------------------------------------------------------------------------
