@@ -1196,7 +1196,7 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(PagedWeighArgs a) {
 // workgroup's steps one after the other, while those of 4 sequences and 8 heads leave most CUs
 // idle: 18 us with the sums over waves in a loop and a page looked up for every 4 keys, 14 with
 // them in one scan, passes with constant shifts and a page's place found once for its run.  Its
-// waves wait (for LDS, barriers and the scores) 57 % of that, and issue VALU work in 12 %.
+// waves wait (for LDS, barriers and the scores) 58 % of that, and issue VALU work in 12 %.
 // paged_gather_kernel copies them to their new places, bound by memory: 64 sequences of 2,304
 // keys to 2,048, 8 heads, d = 128, 1.07 GB, 207 us (5.2 TB/s; through the caches 217).
 // ---------------------------------------------------------------------------
