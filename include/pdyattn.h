@@ -344,10 +344,11 @@ pdy_status attn_paged_write(const void* k, const void* v, const int32_t* cu_seql
  * Probabilities (before the product with v) are rounded to bf16; logits, sums, weights and
  * lse are 32 bits.  The same call gives the same bits; launches of other sizes differ in
  * rounding.  With scores num_seqs is at most 65,535, and num_seqs * Hkv * (max_seqlen_k /
- * 512, rounded up) below 2^24.  with_scores: whether scores will be given.  The workspace is for a call
- * of just these sizes, the bound max_seqlen_k among them: at most about 70 MB, and with
- * scores up to 1 GiB of logits more (4 bytes a query head, query and key, where a sequence
- * has up to 16 queries times heads of a group; more logits than that are computed twice). */
+ * 512, rounded up) below 2^24.  with_scores: whether scores will be given.  The workspace
+ * is for a call of just these sizes, the bound max_seqlen_k among them: at most about 70 MB,
+ * and with scores up to 1 GiB of logits more (4 bytes a query head, query and key, where a
+ * sequence has up to 16 queries times heads of a group; more logits than that are computed
+ * twice). */
 size_t attn_paged_fwd_workspace_size(int32_t total_q, int32_t num_seqs, int32_t max_seqlen_q,
                                      int32_t max_seqlen_k, int32_t num_heads_q,
                                      int32_t num_heads_kv, int32_t head_dim,
